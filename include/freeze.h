@@ -54,6 +54,9 @@ enum {
 };
 
 enum { FREEZE_F32 = 0, FREEZE_BF16 = 1 }; /* element type of the entries handed to freeze_cache_build */
+/* Codes of freeze_quantise_rows (8 bits: sign, 4 exponent, 3 mantissa bits; largest finite value 448, no infinity),
+ * accepted by freeze_quantised_build and freeze_quantised_project only. */
+enum { FREEZE_E4M3 = 2 };
 
 /* Largest k and largest re-scoring width accepted by the look-ups.  The bf16 matrix-core pass
  * keeps FREEZE_MAX_RESCORE candidates per query at most for the exact fp32 re-scoring. */
@@ -315,6 +318,104 @@ int freeze_compact_misses(const uint8_t *hit, const int32_t *sel_in, int64_t cou
  */
 int freeze_gather_rows(const float *x, int64_t d, const int32_t *sel, const int32_t *count,
                        int64_t max_count, float *out, void *stream);
+
+/*
+ * Dense layer in 8 bits: what no layer of caches freezes goes on to the model's own output layer, and the
+ * layer in front of a look-up (freeze_project) may be wide; few rows through such a layer take the time of reading
+ * its weights, half as many bytes here as in bf16.
+ *
+ * Quantised rows: a row of d values is cut into blocks of 128 (the last one may be shorter).  A block is held as codes
+ * and an exponent E, the smallest integer >= -126 with max|x| <= 448 * 2^E; its codes are x * 2^-E rounded to nearest even
+ * (FREEZE_E4M3).  Every factor is a power of two, so that a code is one rounding of the value.
+ *   codes   [rows, freeze_quantised_code_stride(d)] bytes, zero behind d;
+ *   scales  [rows, freeze_quantised_scale_stride(d)] bytes E + 127, 1 behind the last block.
+ * Strides: d rounded up to 128, the number of blocks rounded up to 4; 0 on invalid d.  1 <= d <= 2^22.
+ *
+ * freeze_quantise_rows: x [rows, d] fp32 or bf16, row_stride elements from row to row (>= d); codes 16-byte, scales 4-byte
+ * aligned; neither may lie over x.  rows == 0 is a no-op.
+ */
+int64_t freeze_quantised_code_stride(int64_t d);
+int64_t freeze_quantised_scale_stride(int64_t d);
+int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, int64_t row_stride,
+                         uint8_t *codes, uint8_t *scales, void *stream);
+
+/*
+ * Dense layer with quantised weights: y = W x + bias, optionally through ReLU, W and x as quantised rows.  It occupies
+ * one of the context's slots (look-ups and freeze_project on that slot fail with FREEZE_ENOTBUILT, and
+ * freeze_quantised_project does on every other slot).
+ *   weights  [m, d] row-major, fp32 or bf16, quantised by the call (weight_scales NULL); or FREEZE_E4M3: codes and
+ *            weight_scales as of freeze_quantise_rows (codes behind d are not looked at).
+ *   bias     [m] fp32, or NULL for none.
+ *   storage  >= freeze_quantised_storage_bytes() bytes, 256-byte aligned; everything is copied into it; it must outlive
+ *            the calls of freeze_quantised_project on the slot.
+ *   x        [b, d] fp32 or bf16, x_stride elements from row to row, quantised by the call (x_scales NULL); or
+ *            FREEZE_E4M3: codes and x_scales as of freeze_quantise_rows (16 and 4 bytes aligned, their own strides, zeros behind d; x_stride
+ *            is not looked at).
+ *   out      [b, m] out_dtype, out_stride elements from row to row (>= m); elements between rows are left as they
+ *            are.  It may lie over an x that the call quantises, not over given codes or scales (FREEZE_EINVAL).
+ *            FREEZE_F32: products are exact and summed in fp32.  FREEZE_BF16: larger batches go through the 8-bit matrix
+ *            instructions, which cut the products of eight neighbouring elements off 13 bits below the largest of them
+ *            before they are summed in fp32: less than the rounding of the output, but not what the fp32 output rounds to.
+ *   workspace  freeze_quantised_workspace_bytes() bytes, 256-byte aligned; scratch only.
+ * 1 <= m < 2^31 - 512, 0 <= b <= 2^30; b == 0 is a no-op.
+ */
+size_t freeze_quantised_storage_bytes(int64_t m, int64_t d);
+int freeze_quantised_build(freeze_ctx *ctx, int slot, const void *weights, int weights_dtype,
+                           const uint8_t *weight_scales, int64_t m, int64_t d, const float *bias,
+                           void *storage, size_t storage_bytes, void *stream);
+size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t b, int x_dtype);
+int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dtype, const uint8_t *x_scales,
+                             int64_t b, int64_t x_stride, int relu, void *out, int out_dtype, int64_t out_stride,
+                             void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The next tokens of a generating model's requests (beam search): a group of `beams` rows belongs to one request; a row
+ * holds the output layer's values for every token of the vocabulary and has a score so far.  A continuation (row j, token v)
+ * is worth
+ *     scores[j] + logits[j, v] - log sum_u exp logits[j, u]
+ * and the k best continuations of each group are returned, best first; equal ones: lower row, then lower token.
+ *   logits    [groups * beams, vocab] fp32 or bf16, row_stride elements from row to row.  -inf: the token is forbidden
+ *             (any number of them, whole rows too).  Other values must be finite.
+ *   scores    [groups * beams] fp32; -inf: an empty row, whose logits are not looked at.
+ *   finished  [groups * beams] uint8 or NULL: a row that has ended goes on with end_token at its score and nothing else,
+ *             its logits are not looked at.  end_token in [0, vocab); -1 where finished is NULL and no token ends a row.
+ *   out_scores [groups, k] fp32, out_tokens [groups, k] int32;
+ *   out_parents [groups, k] int32: the row (0 .. groups * beams - 1) that is continued, as freeze_gather_rows
+ *             and freeze_reorder_states take it;
+ *   out_finished [groups, k] uint8 or NULL: token == end_token.
+ *   A group with fewer than k continuations: its last places get score -inf, token end_token (0 for -1), parent its first row.
+ *   workspace  freeze_beam_workspace_bytes() bytes, 256-byte aligned; scratch only.
+ * 1 <= beams <= 64, 1 <= k <= FREEZE_MAX_K, 1 <= vocab < 2^31 - 512, groups * beams <= 2^20; groups == 0 is a no-op.  Totals are formed in
+ * fp64 from fp32 exponentials and rounded once; within a row, the values themselves decide.  No output may lie over an input.
+ */
+#define FREEZE_MAX_BEAMS 64
+size_t freeze_beam_workspace_bytes(int64_t groups, int beams, int64_t vocab, int k);
+int freeze_beam_select(const void *logits, int logits_dtype, int64_t groups, int beams, int64_t vocab,
+                       int64_t row_stride, const float *scores, const uint8_t *finished, int32_t end_token, int k,
+                       float *out_scores, int32_t *out_tokens, int32_t *out_parents, uint8_t *out_finished,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Batch reconstruction of a model's states (freeze_gather_rows for tensors of any type that hold more than a row's
+ * values side by side, several in one call): dst row r = src row parents[r], for every state, r < rows.
+ *   states   host array [num_states] of freeze_state.  A row of a state is `outer` x `pieces` runs of piece_bytes bytes:
+ *            run (o, p) of row r starts o * outer_stride + r * row_stride + p * piece_stride bytes behind src (or
+ *            dst).  Keys and values of attention, [layers, rows, heads, places, width], the first `used` places filled: outer =
+ *            layers, pieces = heads, piece_bytes = used * width * element size; what lies behind the runs is left as it is.
+ *   parents  [rows] int32 (device); a row whose parent is outside [0, src_rows) is left as it was.
+ * No dst may share a byte of its whole extent (first to last run) with any src or another dst: FREEZE_EINVAL.
+ * 0 <= num_states <= 1024, strides >= 0, piece_bytes >= 0, at most 2^31 - 1 runs a state; rows == 0 is a no-op.
+ */
+typedef struct freeze_state {
+    const void *src;
+    void *dst;
+    int64_t outer, outer_stride;
+    int64_t row_stride;
+    int64_t pieces, piece_stride;
+    int64_t piece_bytes;
+} freeze_state;
+int freeze_reorder_states(const freeze_state *states, int num_states, const int32_t *parents, int64_t rows,
+                          int64_t src_rows, void *stream);
 
 /*
  * Counters of how the look-ups of this context were confirmed (measurement aid): while a device

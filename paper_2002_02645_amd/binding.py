@@ -18,9 +18,16 @@ LIB_PATH = os.path.join(_PKG, "_lib", "libfreeze_hip.so")
 FREEZE_OK, FREEZE_EINVAL, FREEZE_ELAYER, FREEZE_ENOTBUILT, FREEZE_EWORKSPACE, FREEZE_EHIP = 0, -1, -2, -3, -4, -5
 FREEZE_ESCRATCH = -6
 FREEZE_STATIC_SCRATCH_BYTES = 32 << 20
-FREEZE_F32, FREEZE_BF16 = 0, 1
+FREEZE_F32, FREEZE_BF16, FREEZE_E4M3 = 0, 1, 2
 
 _lib = None
+
+
+class FreezeState(ctypes.Structure):
+    """freeze_state of the C ABI."""
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("outer", ctypes.c_int64), ("outer_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64), ("pieces", ctypes.c_int64), ("piece_stride", ctypes.c_int64),
+                ("piece_bytes", ctypes.c_int64)]
 
 
 class FreezeError(RuntimeError):
@@ -84,6 +91,25 @@ def lib():
     L.freeze_project.argtypes = [p, i32, p, i64, i32, p, p, sz, p]
     L.freeze_gather_rows.restype = i32
     L.freeze_gather_rows.argtypes = [p, i64, p, p, i64, p, p]
+    for name in ("freeze_quantised_code_stride", "freeze_quantised_scale_stride"):
+        getattr(L, name).restype = i64
+        getattr(L, name).argtypes = [i64]
+    L.freeze_quantise_rows.restype = i32
+    L.freeze_quantise_rows.argtypes = [p, i32, i64, i64, i64, p, p, p]
+    L.freeze_quantised_storage_bytes.restype = sz
+    L.freeze_quantised_storage_bytes.argtypes = [i64, i64]
+    L.freeze_quantised_build.restype = i32
+    L.freeze_quantised_build.argtypes = [p, i32, p, i32, p, i64, i64, p, p, sz, p]
+    L.freeze_quantised_workspace_bytes.restype = sz
+    L.freeze_quantised_workspace_bytes.argtypes = [p, i32, i64, i32]
+    L.freeze_quantised_project.restype = i32
+    L.freeze_quantised_project.argtypes = [p, i32, p, i32, p, i64, i64, i32, p, i32, i64, p, sz, p]
+    L.freeze_beam_workspace_bytes.restype = sz
+    L.freeze_beam_workspace_bytes.argtypes = [i64, i32, i64, i32]
+    L.freeze_beam_select.restype = i32
+    L.freeze_beam_select.argtypes = [p, i32, i64, i32, i64, i64, p, p, ctypes.c_int32, i32, p, p, p, p, p, sz, p]
+    L.freeze_reorder_states.restype = i32
+    L.freeze_reorder_states.argtypes = [p, i32, p, i64, i64, p]
     L.freeze_compute_thresholds.restype = i32
     L.freeze_compute_thresholds.argtypes = [p, i32, p, p, i64, i32, i32, p, p, p, sz, p]
     L.freeze_lookup_stats_attach.restype = i32
@@ -317,6 +343,142 @@ def freeze_gather_rows(x: torch.Tensor, sel: torch.Tensor, count: Optional[torch
                                     _stream(stream)), "freeze_gather_rows")
 
 
+def freeze_quantised_code_stride(d: int) -> int:
+    return int(lib().freeze_quantised_code_stride(d))
+
+
+def freeze_quantised_scale_stride(d: int) -> int:
+    return int(lib().freeze_quantised_scale_stride(d))
+
+
+def _here(*tensors: Optional[torch.Tensor]) -> None:
+    """The library's kernels run on the current device."""
+    dev = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or (t.is_cuda and t.device.index == dev), "tensors of the current device are needed"
+
+
+def _rows_of(t: torch.Tensor) -> int:
+    """Elements from row to row of a two-dimensional tensor whose rows are dense."""
+    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _values_dtype(t: torch.Tensor) -> int:
+    return {torch.float32: FREEZE_F32, torch.bfloat16: FREEZE_BF16, torch.float8_e4m3fn: FREEZE_E4M3}[t.dtype]
+
+
+def freeze_quantise_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """codes [rows, freeze_quantised_code_stride(d)] float8_e4m3fn, scales [rows, freeze_quantised_scale_stride(d)] uint8."""
+    _here(x, codes, scales)
+    rows, d = x.shape
+    assert x.dtype in (torch.float32, torch.bfloat16)
+    assert codes.dtype == torch.float8_e4m3fn and codes.is_contiguous() and codes.shape == (rows, freeze_quantised_code_stride(d))
+    assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (rows, freeze_quantised_scale_stride(d))
+    _check(lib().freeze_quantise_rows(_ptr(x), _values_dtype(x), rows, d, _rows_of(x), _ptr(codes), _ptr(scales), _stream(stream)),
+           "freeze_quantise_rows")
+
+
+def freeze_quantised_storage_bytes(m: int, d: int) -> int:
+    return int(lib().freeze_quantised_storage_bytes(m, d))
+
+
+def freeze_quantised_build(ctx, slot: int, weights: torch.Tensor, scales: Optional[torch.Tensor], d: int, bias: Optional[torch.Tensor],
+                           storage: torch.Tensor, stream=None) -> None:
+    """weights [m, d] fp32 / bf16 (scales None), or codes [m, freeze_quantised_code_stride(d)] with their scales."""
+    _here(weights, scales, bias, storage)
+    m = weights.shape[0]
+    assert weights.is_contiguous() and weights.dim() == 2
+    assert bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == m)
+    if scales is None:
+        assert weights.shape[1] == d
+    else:
+        assert weights.dtype == torch.float8_e4m3fn and weights.shape[1] == freeze_quantised_code_stride(d)
+        assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (m, freeze_quantised_scale_stride(d))
+    _check(lib().freeze_quantised_build(ctx, slot, _ptr(weights), _values_dtype(weights), _ptr(scales), m, d, _ptr(bias), _ptr(storage),
+                                        storage.numel() * storage.element_size(), _stream(stream)), "freeze_quantised_build")
+
+
+def freeze_quantised_workspace_bytes(ctx, slot: int, b: int, x_dtype: int) -> int:
+    return int(lib().freeze_quantised_workspace_bytes(ctx, slot, b, x_dtype))
+
+
+def freeze_quantised_project(ctx, slot: int, x: torch.Tensor, scales: Optional[torch.Tensor], d: int, relu: bool, out: torch.Tensor,
+                             workspace: torch.Tensor, stream=None) -> None:
+    """x [b, d] fp32 / bf16 (scales None), or codes with their scales; out [b, m] fp32 or bf16.  d, m: the built layer's."""
+    _here(x, scales, out, workspace)
+    b = x.shape[0]
+    assert out.dtype in (torch.float32, torch.bfloat16) and out.shape[0] == b
+    if scales is None:
+        assert x.shape[1] == d
+        stride = _rows_of(x)
+    else:
+        assert x.dtype == torch.float8_e4m3fn and x.is_contiguous() and x.shape[1] == freeze_quantised_code_stride(d)
+        assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (b, freeze_quantised_scale_stride(d))
+        stride = 0
+    _check(lib().freeze_quantised_project(ctx, slot, _ptr(x), _values_dtype(x), _ptr(scales), b, stride, int(relu), _ptr(out),
+                                          _values_dtype(out), _rows_of(out), _ptr(workspace),
+                                          workspace.numel() * workspace.element_size(), _stream(stream)), "freeze_quantised_project")
+
+
+def freeze_beam_workspace_bytes(groups: int, beams: int, vocab: int, k: int) -> int:
+    return int(lib().freeze_beam_workspace_bytes(groups, beams, vocab, k))
+
+
+def freeze_beam_select(logits: torch.Tensor, scores: torch.Tensor, finished: Optional[torch.Tensor], beams: int, end_token: int, k: int,
+                       out_scores: torch.Tensor, out_tokens: torch.Tensor, out_parents: torch.Tensor,
+                       out_finished: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
+    _here(logits, scores, finished, out_scores, out_tokens, out_parents, out_finished, workspace)
+    rows, vocab = logits.shape
+    assert logits.dtype in (torch.float32, torch.bfloat16) and rows % beams == 0
+    assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
+    assert finished is None or (finished.dtype in (torch.uint8, torch.bool) and finished.is_contiguous() and finished.numel() == rows)
+    groups = rows // beams
+    for t, dt in ((out_scores, torch.float32), (out_tokens, torch.int32), (out_parents, torch.int32), (out_finished, torch.uint8)):
+        assert t is None or (t.dtype == dt and t.is_contiguous() and t.numel() == groups * k)
+    _check(lib().freeze_beam_select(_ptr(logits), _values_dtype(logits), groups, beams, vocab, _rows_of(logits), _ptr(scores),
+                                    _ptr(finished), end_token, k, _ptr(out_scores), _ptr(out_tokens), _ptr(out_parents),
+                                    _ptr(out_finished), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                    _stream(stream)), "freeze_beam_select")
+
+
+def state_of(src: torch.Tensor, dst: torch.Tensor, used: Optional[int] = None, row_dim: int = 0) -> FreezeState:
+    """The freeze_state of two tensors of one shape, type and layout [outer..., rows, pieces..., places, width] (row_dim: the place of
+    the rows; after it at most three dimensions, before it at most one).  used: how many places are taken along; None: all."""
+    assert src.shape == dst.shape and src.dtype == dst.dtype and src.stride() == dst.stride(), "src and dst of one layout are needed"
+    assert 0 <= row_dim <= 1 and src.dim() - row_dim <= 4 and src.dim() > row_dim
+    size = src.element_size()
+    shape, stride = list(src.shape), list(src.stride())
+    outer, outer_stride = (shape[0], stride[0]) if row_dim else (1, 0)
+    row_stride = stride[row_dim]
+    inner, istr = shape[row_dim + 1:], stride[row_dim + 1:]
+    if used is not None:
+        assert len(inner) >= 2 and 0 <= used <= inner[-2]
+        inner[-2] = used
+    pieces, piece_stride, run = 1, 0, size
+    if inner:
+        assert istr[-1] == 1 or inner[-1] <= 1, "the last dimension has to be dense"
+        run *= inner[-1]
+    if len(inner) >= 2:
+        if istr[-2] * size == run or inner[-2] <= 1:
+            run *= inner[-2]
+            if len(inner) == 3:
+                pieces, piece_stride = inner[0], istr[0]
+        else:
+            assert len(inner) == 2 or inner[0] == 1, "places that do not follow each other, in several pieces"
+            pieces, piece_stride = inner[-2], istr[-2]
+    return FreezeState(src.data_ptr(), dst.data_ptr(), outer, outer_stride * size, row_stride * size, pieces, piece_stride * size, run)
+
+
+def freeze_reorder_states(states: Sequence[FreezeState], parents: torch.Tensor, src_rows: int, stream=None) -> None:
+    """states as of state_of; row r of every dst becomes row parents[r] of its src."""
+    _here(parents)
+    assert parents.dtype == torch.int32 and parents.is_contiguous()
+    arr = (FreezeState * len(states))(*states)
+    _check(lib().freeze_reorder_states(ctypes.cast(arr, ctypes.c_void_p), len(states), _ptr(parents), parents.numel(), src_rows,
+                                       _stream(stream)), "freeze_reorder_states")
+
+
 def freeze_compact_misses(hit: torch.Tensor, sel_in: Optional[torch.Tensor], sel_out: torch.Tensor,
                           out_count: torch.Tensor, stream=None) -> None:
     assert hit.is_cuda and hit.dtype == torch.uint8
@@ -520,3 +682,62 @@ class FreezeCache:
             raise FreezeError(FREEZE_EINVAL, "freeze_project_workspace_bytes")
         freeze_project(self.ctx, slot, x, relu, out, self._workspace(nbytes))
         return out
+
+    def quantise_rows(self, x: torch.Tensor):
+        """Rows in 8 bits: codes [rows, d rounded up to 128] float8_e4m3fn and a scale byte for each block of 128 values."""
+        rows, d = x.shape
+        codes = torch.empty((rows, freeze_quantised_code_stride(d)), dtype=torch.float8_e4m3fn, device=self.device)
+        scales = torch.empty((rows, freeze_quantised_scale_stride(d)), dtype=torch.uint8, device=self.device)
+        freeze_quantise_rows(x, codes, scales)
+        return codes, scales
+
+    def build_quantised(self, slot: int, weights: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                        scales: Optional[torch.Tensor] = None, d: Optional[int] = None):
+        """A dense layer y = W x + bias in 8 bits (a model's output layer, or the layer in front of a look-up); occupies one slot.
+        weights: fp32 / bf16, quantised here, or codes with their scales (d: the values of a row, where fewer than the codes)."""
+        m = weights.shape[0]
+        d = weights.shape[1] if d is None else d
+        nbytes = freeze_quantised_storage_bytes(m, d)
+        if nbytes == 0:
+            raise FreezeError(FREEZE_EINVAL, "freeze_quantised_storage_bytes")
+        st = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+        freeze_quantised_build(self.ctx, slot, weights, scales, d, bias, st)
+        self.storage[slot] = st
+        self.meta[slot] = (m, d, 0)
+
+    def quantised_project(self, slot: int, x: torch.Tensor, scales: Optional[torch.Tensor] = None, relu: bool = False,
+                          out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """x: fp32 / bf16 rows, or codes with their scales."""
+        m, d, _ = self.meta[slot]
+        if out is None:
+            out = torch.empty((x.shape[0], m), dtype=out_dtype, device=self.device)
+        assert out.shape == (x.shape[0], m)
+        nbytes = freeze_quantised_workspace_bytes(self.ctx, slot, x.shape[0], _values_dtype(x))
+        if nbytes == 0:
+            raise FreezeError(FREEZE_EINVAL, "freeze_quantised_workspace_bytes")
+        freeze_quantised_project(self.ctx, slot, x, scales, d, relu, out, self._workspace(nbytes))
+        return out
+
+    def beam_select(self, logits: torch.Tensor, scores: torch.Tensor, beams: int, k: int, finished: Optional[torch.Tensor] = None,
+                    end_token: int = -1) -> dict:
+        """The k best continuations of every group of `beams` rows: score, token, parent (row), finished; each [groups, k]."""
+        groups = logits.shape[0] // beams
+        out = dict(score=torch.empty((groups, k), dtype=torch.float32, device=self.device),
+                   token=torch.empty((groups, k), dtype=torch.int32, device=self.device),
+                   parent=torch.empty((groups, k), dtype=torch.int32, device=self.device),
+                   finished=torch.empty((groups, k), dtype=torch.uint8, device=self.device))
+        nbytes = freeze_beam_workspace_bytes(groups, beams, logits.shape[1], k)
+        if nbytes == 0:
+            raise FreezeError(FREEZE_EINVAL, "freeze_beam_workspace_bytes")
+        freeze_beam_select(logits, scores, finished, beams, end_token, k, out["score"], out["token"], out["parent"], out["finished"],
+                           self._workspace(nbytes))
+        return out
+
+    def reorder_states(self, src, dst, parents: torch.Tensor, used: Optional[int] = None, row_dim: int = 0) -> None:
+        """Row r of every dst becomes row parents[r] of its src (tensors or lists of tensors; see state_of)."""
+        src, dst = ([t] if isinstance(t, torch.Tensor) else list(t) for t in (src, dst))
+        assert len(src) == len(dst) and all(t.shape[row_dim] == src[0].shape[row_dim] for t in src)
+        assert all(parents.numel() <= t.shape[row_dim] for t in dst)
+        _here(*src, *dst)
+        freeze_reorder_states([state_of(s, d, used, row_dim) for s, d in zip(src, dst)], parents,
+                              src[0].shape[row_dim] if src else 0)

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "freeze_internal.h"
+#include "quantised.h"
 
 using namespace fz;
 
@@ -723,6 +724,22 @@ bool kmeans_layout(const freeze_ctx *ctx, int64_t n, int64_t d, int64_t kc, Kmea
     return true;
 }
 
+constexpr int64_t kQuantMaxStride = (int64_t)1 << 32;   // elements from row to row: 2^30 rows stay within 64 bits of bytes
+inline bool aligned(const void *p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+inline bool share_bytes(const void *a, size_t na, const void *b, size_t nb)
+{
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + nb && y < x + na;
+}
+
+const LayerCache *get_quantised(const freeze_ctx *ctx, int slot, int *err)
+{
+    *err = !ctx ? FREEZE_EINVAL : (slot < 0 || slot >= (int)ctx->layers.size() ? FREEZE_ELAYER : FREEZE_OK);
+    if (*err != FREEZE_OK) return nullptr;
+    if (!ctx->layers[slot].codes) *err = FREEZE_ENOTBUILT;
+    return *err == FREEZE_OK ? &ctx->layers[slot] : nullptr;
+}
+
 const LayerCache *get_projection(const freeze_ctx *ctx, int slot, int *err)
 {
     if (!ctx) {
@@ -873,6 +890,7 @@ int cache_build_impl(freeze_ctx *ctx, int layer, const void *entries, int entrie
     L.fraction = nullptr;
     L.bias = nullptr;
     L.mu = centre ? mu : nullptr;
+    L.codes = nullptr;
     L.built = true;
     return FREEZE_OK;
 }
@@ -1254,6 +1272,115 @@ int freeze_project(freeze_ctx *ctx, int slot, const float *x, int64_t b, int rel
     if (launch_dist_topr(pl, da, s) != hipSuccess) return FREEZE_EHIP;
     if (!direct && launch_copy_rows_f32(tmp, P->n_pad, out, b, P->n, s) != hipSuccess) return FREEZE_EHIP;
     return FREEZE_OK;
+}
+
+int64_t freeze_quantised_code_stride(int64_t d) { return d < 1 || d > kQuantMaxD ? 0 : quant_code_stride(d); }
+
+int64_t freeze_quantised_scale_stride(int64_t d) { return d < 1 || d > kQuantMaxD ? 0 : quant_scale_stride(d); }
+
+int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, int64_t row_stride, uint8_t *codes, uint8_t *scales,
+                         void *stream)
+{
+    if (rows < 0 || rows > (int64_t)1 << 30 || d < 1 || d > kQuantMaxD || row_stride < d || row_stride > kQuantMaxStride) return FREEZE_EINVAL;
+    if (x_dtype != FREEZE_F32 && x_dtype != FREEZE_BF16) return FREEZE_EINVAL;
+    if (rows == 0) return FREEZE_OK;
+    const int size = x_dtype == FREEZE_F32 ? 4 : 2;
+    if (!x || !codes || !scales || !aligned(x, size) || !aligned(codes, 16) || !aligned(scales, 4)) return FREEZE_EINVAL;
+    const size_t xb = (size_t)((rows - 1) * row_stride + d) * size;
+    const size_t cb = (size_t)(rows * quant_code_stride(d)), sb = (size_t)(rows * quant_scale_stride(d));
+    if (share_bytes(x, xb, codes, cb) || share_bytes(x, xb, scales, sb) || share_bytes(codes, cb, scales, sb)) return FREEZE_EINVAL;
+    return launch_quantise_rows(x, x_dtype, rows, d, row_stride, codes, scales, static_cast<hipStream_t>(stream)) == hipSuccess ? FREEZE_OK
+                                                                                                                              : FREEZE_EHIP;
+}
+
+size_t freeze_quantised_storage_bytes(int64_t m, int64_t d)
+{
+    if (m < 1 || m >= (int64_t)2147483647 - 512 || d < 1 || d > kQuantMaxD) return 0;
+    return align_up((size_t)(m * quant_code_stride(d))) + align_up((size_t)(m * quant_scale_stride(d))) + align_up((size_t)m * 4);
+}
+
+int freeze_quantised_build(freeze_ctx *ctx, int slot, const void *weights, int weights_dtype, const uint8_t *weight_scales, int64_t m,
+                           int64_t d, const float *bias, void *storage, size_t storage_bytes, void *stream)
+{
+    if (!ctx || !weights || !storage) return FREEZE_EINVAL;
+    if (slot < 0 || slot >= (int)ctx->layers.size()) return FREEZE_ELAYER;
+    const size_t bytes = freeze_quantised_storage_bytes(m, d);
+    const bool given = weights_dtype == FREEZE_E4M3;
+    if (bytes == 0 || (!given && weights_dtype != FREEZE_F32 && weights_dtype != FREEZE_BF16) || given != (weight_scales != nullptr))
+        return FREEZE_EINVAL;
+    if (!aligned(weights, given ? 16 : (weights_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(weight_scales, 4) || !aligned(bias, 4)) return FREEZE_EINVAL;
+    if (storage_bytes < bytes || !aligned(storage, kAlign)) return FREEZE_EWORKSPACE;
+    Carver st(storage);
+    uint8_t *codes = st.take<uint8_t>((size_t)(m * quant_code_stride(d))), *scales = st.take<uint8_t>((size_t)(m * quant_scale_stride(d)));
+    float *q_bias = bias ? st.take<float>((size_t)m) : nullptr;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    LayerCache &L = ctx->layers[slot];
+    L = LayerCache();
+    const hipError_t e = given ? launch_copy_codes(static_cast<const uint8_t *>(weights), weight_scales, m, d, codes, scales, s)
+                               : launch_quantise_rows(weights, weights_dtype, m, d, d, codes, scales, s);
+    if (e != hipSuccess || (bias && launch_copy_rows_f32(bias, 1, q_bias, m, 1, s) != hipSuccess)) return FREEZE_EHIP;
+    L.n = m;
+    L.d = d;
+    L.codes = codes;
+    L.scales = scales;
+    L.q_bias = q_bias;
+    return FREEZE_OK;
+}
+
+size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t b, int x_dtype)
+{
+    int err;
+    const LayerCache *P = get_quantised(ctx, slot, &err);
+    if (!P || b < 0 || b > (int64_t)1 << 30 || x_dtype < FREEZE_F32 || x_dtype > FREEZE_E4M3) return 0;
+    if (b < 1) b = 1;
+    size_t bytes = kAlign;
+    if (x_dtype != FREEZE_E4M3) bytes += align_up((size_t)(b * quant_code_stride(P->d))) + align_up((size_t)(b * quant_scale_stride(P->d)));
+    return bytes;
+}
+
+int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dtype, const uint8_t *x_scales, int64_t b, int64_t x_stride,
+                             int relu, void *out, int out_dtype, int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int err;
+    const LayerCache *P = get_quantised(ctx, slot, &err);
+    if (!P) return err;
+    const bool given = x_dtype == FREEZE_E4M3;
+    if (b < 0 || b > (int64_t)1 << 30 || (!given && x_dtype != FREEZE_F32 && x_dtype != FREEZE_BF16) ||
+        (out_dtype != FREEZE_F32 && out_dtype != FREEZE_BF16) || out_stride < P->n || out_stride > kQuantMaxStride ||
+        (!given && (x_stride < P->d || x_stride > kQuantMaxStride)))
+        return FREEZE_EINVAL;
+    if (b == 0) return FREEZE_OK;
+    const int out_size = out_dtype == FREEZE_F32 ? 4 : 2;
+    if (!x || !out || !workspace || given != (x_scales != nullptr) || !aligned(out, out_size) ||
+        !aligned(x, given ? 16 : (x_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(x_scales, 4))
+        return FREEZE_EINVAL;
+    const size_t cb = (size_t)(b * quant_code_stride(P->d)), sb = (size_t)(b * quant_scale_stride(P->d));
+    const size_t ob = (size_t)((b - 1) * out_stride + P->n) * out_size;
+    if (given && (share_bytes(out, ob, x, cb) || share_bytes(out, ob, x_scales, sb))) return FREEZE_EINVAL;
+    if (workspace_bytes < freeze_quantised_workspace_bytes(ctx, slot, b, x_dtype) || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    Carver ws(workspace);
+    QuantProduct q{};
+    q.x = static_cast<const uint8_t *>(x);
+    q.xs = x_scales;
+    if (!given) {
+        uint8_t *codes = ws.take<uint8_t>(cb), *scales = ws.take<uint8_t>(sb);
+        if (launch_quantise_rows(x, x_dtype, b, P->d, x_stride, codes, scales, s) != hipSuccess) return FREEZE_EHIP;
+        q.x = codes;
+        q.xs = scales;
+    }
+    q.w = P->codes;
+    q.ws = P->scales;
+    q.bias = P->q_bias;
+    q.out = out;
+    q.out_stride = out_stride;
+    q.b = b;
+    q.m = P->n;
+    q.d_pad = quant_code_stride(P->d);
+    q.sd = quant_scale_stride(P->d);
+    q.out_bf16 = out_dtype == FREEZE_BF16;
+    q.relu = relu != 0;
+    return launch_quant_product(q, s) == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
 }
 
 int freeze_compact_misses(const uint8_t *hit, const int32_t *sel_in, int64_t count, int32_t *sel_out,

@@ -99,6 +99,10 @@ struct LayerCache {
     const float *bias = nullptr;      // [n_pad] its bias, zero padded (else null); not a cache: look-ups reject it
     // the matrix-core copy c_bf (and norm) is taken relative to this vector, and so must the queries' bf16
     const float *mu = nullptr;        // [d_pad] copy be: the cache's mean, or all zeros (decided on the device); null: none
+    // dense layer with quantised weights (n outputs of d values; `built` is false: neither a cache nor a projection):
+    const uint8_t *codes = nullptr;   // [n, codes of a row], null for everything else
+    const uint8_t *scales = nullptr;  // [n, scale bytes of a row]
+    const float *q_bias = nullptr;    // [n] or null
 };
 
 // Number of splits of the cache tiles for `live_mt` live query tiles.  Units (query tile, split)
