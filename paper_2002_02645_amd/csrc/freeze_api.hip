@@ -740,6 +740,17 @@ const LayerCache *get_quantised(const freeze_ctx *ctx, int slot, int *err)
     return *err == FREEZE_OK ? &ctx->layers[slot] : nullptr;
 }
 
+// the sums of cut tiles, for either type of the outputs
+size_t quant_part_bytes(const freeze_ctx *ctx, const LayerCache &P, int64_t b)
+{
+    size_t most = 0;
+    for (int half = 0; half < 2; ++half) {
+        const size_t part = plan_quant_product(b, P.n, quant_code_stride(P.d), half != 0, ctx->num_cus).part;
+        most = part > most ? part : most;
+    }
+    return align_up(most * 4);
+}
+
 const LayerCache *get_projection(const freeze_ctx *ctx, int slot, int *err)
 {
     if (!ctx) {
@@ -1333,7 +1344,7 @@ size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t
     const LayerCache *P = get_quantised(ctx, slot, &err);
     if (!P || b < 0 || b > (int64_t)1 << 30 || x_dtype < FREEZE_F32 || x_dtype > FREEZE_E4M3) return 0;
     if (b < 1) b = 1;
-    size_t bytes = kAlign;
+    size_t bytes = kAlign + quant_part_bytes(ctx, *P, b);
     if (x_dtype != FREEZE_E4M3) bytes += align_up((size_t)(b * quant_code_stride(P->d))) + align_up((size_t)(b * quant_scale_stride(P->d)));
     return bytes;
 }
@@ -1380,7 +1391,9 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
     q.sd = quant_scale_stride(P->d);
     q.out_bf16 = out_dtype == FREEZE_BF16;
     q.relu = relu != 0;
-    return launch_quant_product(q, s) == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
+    const QuantPlan pl = plan_quant_product(b, P->n, q.d_pad, q.out_bf16, ctx->num_cus);
+    q.part = pl.part ? ws.take<float>(pl.part) : nullptr;
+    return launch_quant_product(pl, q, s) == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
 }
 
 int freeze_compact_misses(const uint8_t *hit, const int32_t *sel_in, int64_t count, int32_t *sel_out,

@@ -55,6 +55,20 @@ __device__ __forceinline__ void load16_global_to_lds_nt(uint64_t sbase, uint32_t
     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds_byte_addr), "v"(voff), "s"(sbase)
                  : "memory", "m0");
 }
+// the same with 4 bytes a lane
+__device__ __forceinline__ void load4_global_to_lds(uint64_t sbase, uint32_t voff, uint32_t lds_byte_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte_addr), "v"(voff), "s"(sbase)
+                 : "memory", "m0");
+}
+// Rows of 128 bytes in LDS: chunk c (16 bytes) of a row lies at c ^ row128_swizzle(row).  A fragment read takes one chunk of each
+// of 16 rows for every two groups of lanes, chunks 2g or 2g + 1 for group g = lane >> 4, and the 16 lanes a cycle serves (rows 0-3
+// and 12-15 of one group with rows 4-11 of the next) meet 16 different positions.
+__device__ __forceinline__ int row128_swizzle(int row)
+{
+    const int u = (row >> 1) & 7;
+    return u ^ (((u + 2) & 4) >> 1);
+}
 __device__ __forceinline__ uint64_t uniform_u64(uint64_t x)
 {
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);

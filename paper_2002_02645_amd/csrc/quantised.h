@@ -25,7 +25,21 @@ struct QuantProduct {
     int64_t out_stride;
     int64_t b, m, d_pad, sd;
     int out_bf16, relu;
+    int vec;                 // four outputs of a row from a multiple of four on are one aligned store
+    float *part;             // plan's floats of scratch (none: null)
+    // the plan's
+    int64_t len;             // k-steps of a workgroup's range of the flattened (tile, k-step) space
+    int nk, x_tiles, w_tiles, slots, xcd_share;
 };
-hipError_t launch_quant_product(const QuantProduct &p, hipStream_t s);
+// How a product is cut.
+struct QuantPlan {
+    int variant;        // of quant_gemm_kernel
+    int bm, bn;         // rows of x, rows of w of a tile
+    int x_tiles, w_tiles, nk, slots, wgs;
+    int64_t len;
+    size_t part;        // floats of the sums of cut tiles
+};
+QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16, int num_cus);
+hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t s);
 
 }  // namespace fz

@@ -1,14 +1,9 @@
-// Rows held in 8 bits (e4m3 codes, a power of two for each block of 128 values) and the dense layer on them
-// (gfx950 / CDNA4).
-//
-//     y[r, c] = act(bias[c] + sum_B 2^(Ex[r, B] + Ew[c, B]) sum_{i in B} x8[r, i] w8[c, i])
+// Rows held in 8 bits (gfx950 / CDNA4): e4m3 codes and a power of two for each block of 128 values.
 #include "../../include/freeze.h"
 #include "quantised.h"
 
 namespace fz {
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
@@ -111,53 +106,6 @@ __global__ __launch_bounds__(256) void copy_codes_kernel(const uint8_t *codes, c
     }
 }
 
-// the four code bytes of a word, times 2^(exponent of s): two words of bf16 pairs (exact)
-__device__ __forceinline__ void widen(uint32_t codes, float s, uint32_t &lo, uint32_t &hi)
-{
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, s, false));
-    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, s, true));
-}
-
-// A wave forms 16 x 16 outputs straight from memory.
-__global__ __launch_bounds__(256) void quant_product_kernel(QuantProduct p)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t c0 = ((int64_t)blockIdx.x * 4 + wave) * 16, r0 = (int64_t)blockIdx.y * 16;
-    if (c0 >= p.m) return;
-    const int64_t wr = c0 + (lane & 15) < p.m ? c0 + (lane & 15) : p.m - 1, xr = r0 + (lane & 15) < p.b ? r0 + (lane & 15) : p.b - 1;
-    const uint8_t *w = p.w + wr * p.d_pad + (lane >> 4) * 32, *x = p.x + xr * p.d_pad + (lane >> 4) * 32;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t k = 0; k < p.d_pad; k += kQuantBlock) {
-        const float sw = __uint_as_float((uint32_t)p.ws[wr * p.sd + k / kQuantBlock] << 23);
-        const float sx = __uint_as_float((uint32_t)p.xs[xr * p.sd + k / kQuantBlock] << 23);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const u32x4 a = *reinterpret_cast<const u32x4 *>(w + k + h * 16), b = *reinterpret_cast<const u32x4 *>(x + k + h * 16);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                uint32_t aw[4], bw[4];
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    widen(a[2 * q + e], sw, aw[2 * e], aw[2 * e + 1]);
-                    widen(b[2 * q + e], sx, bw[2 * e], bw[2 * e + 1]);
-                }
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{aw[0], aw[1], aw[2], aw[3]}),
-                                                              __builtin_bit_cast(bf16x8, u32x4{bw[0], bw[1], bw[2], bw[3]}), acc, 0, 0, 0);
-            }
-        }
-    }
-    const int64_t row = r0 + (lane & 15), col = c0 + (lane >> 4) * 4;
-    if (row >= p.b) return;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (col + e >= p.m) break;
-        float v = acc[e] + (p.bias ? p.bias[col + e] : 0.f);
-        if (p.relu) v = __builtin_fmaxf(v, 0.f);
-        if (p.out_bf16) static_cast<uint16_t *>(p.out)[row * p.out_stride + col + e] = bf16_rne(v);
-        else static_cast<float *>(p.out)[row * p.out_stride + col + e] = v;
-    }
-}
-
 unsigned blocks_for(int64_t threads)
 {
     const int64_t n = (threads + 255) / 256;
@@ -191,22 +139,6 @@ hipError_t launch_copy_codes(const uint8_t *codes, const uint8_t *scales, int64_
     hipLaunchKernelGGL(copy_codes_kernel, dim3(blocks_for(rows * (d_pad / 16))), dim3(256), 0, s, codes, scales, rows, d, d_pad, sd,
                        out_codes, out_scales);
     return hipGetLastError();
-}
-
-hipError_t launch_quant_product(const QuantProduct &p, hipStream_t s)
-{
-    // rows in slices that a grid's second axis holds
-    constexpr int64_t kSlice = 65535 * 16;
-    for (int64_t r = 0; r < p.b; r += kSlice) {
-        QuantProduct q = p;
-        q.b = p.b - r < kSlice ? p.b - r : kSlice;
-        q.x = p.x + r * p.d_pad;
-        q.xs = p.xs + r * p.sd;
-        q.out = static_cast<uint8_t *>(p.out) + r * p.out_stride * (p.out_bf16 ? 2 : 4);
-        hipLaunchKernelGGL(quant_product_kernel, dim3((unsigned)((p.m + 63) / 64), (unsigned)((q.b + 15) / 16)), dim3(256), 0, s, q);
-        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    }
-    return hipSuccess;
 }
 
 }  // namespace fz

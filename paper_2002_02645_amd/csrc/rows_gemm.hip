@@ -53,14 +53,6 @@ typedef __attribute__((address_space(3))) void *lds_void_ptr;
 
 namespace {
 
-
-// LDS-direct 4-byte load: as load16_global_to_lds, 4 bytes per lane
-__device__ __forceinline__ void load4_global_to_lds(uint64_t sbase, uint32_t voff, uint32_t lds_byte_addr)
-{
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_byte_addr), "v"(voff), "s"(sbase)
-                 : "memory", "m0");
-}
-
 struct RowsGemmArgs {
     const float *x;               // [n, d]
     const uint16_t *hi, *lo;      // prepared rows, tiled (tiles of kTileN rows, d_pad elements); lo: split ones only
@@ -95,12 +87,6 @@ __device__ __forceinline__ void store_projected(const RowsGemmArgs &p, int64_t r
         for (int e = 0; e < 4; ++e)
             if (col + e < p.m) dst[e] = v[e];
     }
-}
-
-__device__ __forceinline__ int a_swizzle(int row)
-{
-    const int u = (row >> 1) & 7;
-    return u ^ (((u + 2) & 4) >> 1);
 }
 
 // VEC: rows start on 16-byte boundaries (d a multiple of 4)
@@ -158,14 +144,14 @@ __global__ __launch_bounds__(512) void rows_gemm_kernel(RowsGemmArgs p)
     if (g_begin >= g_end) return;   // uniform
 
     // fp32 rows: lane's place in a load instruction.  The LDS image of a row is its eight 16-byte chunks, chunk c at
-    // position c ^ a_swizzle(row): a fragment read takes one chunk of each of 16 rows for every two lanes groups, and the
+    // position c ^ row128_swizzle(row): a fragment read takes one chunk of each of 16 rows for every two lanes groups, and the
     // 16 lanes a cycle serves (rows 0-3 and 12-15 of one group with rows 4-11 of the next) meet 16 different positions.
     const uint32_t d4 = (uint32_t)p.d * 4;
     const uint32_t a_row = VEC ? w * WR + (lane >> 3) : w * WR + (lane >> 5);   // + i * (8 or 2)
     const uint32_t a_row_off = a_row * d4;
     // fragment addresses, in 16-byte units
     const int rA = wm * 16 * RB + (lane & 15);          // + 16 i: leaves the swizzle as it is
-    const int swA = a_swizzle(rA);
+    const int swA = row128_swizzle(rA);
     const int rdA0 = rA * 8 + ((2 * (lane >> 4)) ^ swA), rdA1 = rA * 8 + ((2 * (lane >> 4) + 1) ^ swA);
     const int rB = wn * TNB * 16 + (lane & 15);
     const int rdB = rB * 4 + ((lane >> 4) ^ tiled_chunk_swizzle(rB));
@@ -196,14 +182,14 @@ __global__ __launch_bounds__(512) void rows_gemm_kernel(RowsGemmArgs p)
         auto issue_a = [&](int stage, int kt, int i) {
             const uint32_t ko = (uint32_t)kt * 128;
             if constexpr (VEC) {
-                const uint32_t c = (lane & 7) ^ a_swizzle(w * WR + i * 8 + (lane >> 3));
+                const uint32_t c = (lane & 7) ^ row128_swizzle(w * WR + i * 8 + (lane >> 3));
                 const uint32_t at = ko + c * 16;
                 const uint64_t base = gA + (uint64_t)(i * 8) * d4;
                 const uint32_t off = a_row_off + (at < d4 ? at : 0u), to = smem_base + stage * kAStage + w * (WR * 128) + i * 1024;
                 if constexpr (SPLIT) load16_global_to_lds_nt(base, off, to);
                 else load16_global_to_lds(base, off, to);   // (the group's other workgroups ask for it too: 3,000 x 8,192 -> 700 81 us, 72 so)
             } else {
-                const uint32_t at = ko + (((lane & 31) ^ (a_swizzle(w * WR + i * 2) << 2)) << 2);
+                const uint32_t at = ko + (((lane & 31) ^ (row128_swizzle(w * WR + i * 2) << 2)) << 2);
                 load4_global_to_lds(gA + (uint64_t)(i * 2) * d4, a_row_off + (at < d4 ? at : 0u), smem_base + stage * kAStage + w * (WR * 128) + i * 256);
             }
         };
