@@ -349,10 +349,10 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
  *   storage  >= freeze_quantised_storage_bytes() bytes, 256-byte aligned; everything is copied into it; it must outlive
  *            the calls of freeze_quantised_project on the slot.
  *   x        [b, d] fp32 or bf16, x_stride elements from row to row, quantised by the call (x_scales NULL); or
- *            FREEZE_E4M3: codes and x_scales as of freeze_quantise_rows (16 and 4 bytes aligned, their own strides, zeros behind d; x_stride
- *            is not looked at).
+ *            FREEZE_E4M3: codes and x_scales as of freeze_quantise_rows (16 and 4 bytes aligned, their own strides; codes behind d
+ *            and x_stride are not looked at).
  *   out      [b, m] out_dtype, out_stride elements from row to row (>= m); elements between rows are left as they
- *            are.  It may lie over an x that the call quantises, not over given codes or scales (FREEZE_EINVAL).
+ *            are.  It may lie over x.
  *            FREEZE_F32: products are exact and summed in fp32.  FREEZE_BF16: larger batches go through the 8-bit matrix
  *            instructions, which cut the products of eight neighbouring elements off 13 bits below the largest of them
  *            before they are summed in fp32: less than the rounding of the output, but not what the fp32 output rounds to.

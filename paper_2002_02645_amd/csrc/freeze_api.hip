@@ -740,15 +740,16 @@ const LayerCache *get_quantised(const freeze_ctx *ctx, int slot, int *err)
     return *err == FREEZE_OK ? &ctx->layers[slot] : nullptr;
 }
 
-// the sums of cut tiles, for either type of the outputs
-size_t quant_part_bytes(const freeze_ctx *ctx, const LayerCache &P, int64_t b)
+QuantRows take_rows(Carver &c, int64_t rows, int64_t d, int tile)
 {
-    size_t most = 0;
-    for (int half = 0; half < 2; ++half) {
-        const size_t part = plan_quant_product(b, P.n, quant_code_stride(P.d), half != 0, ctx->num_cus).part;
-        most = part > most ? part : most;
-    }
-    return align_up(most * 4);
+    const int64_t n = quant_tiled_rows(rows, tile);
+    QuantRows q{};
+    q.d_pad = quant_code_stride(d);
+    q.sd = quant_scale_stride(d);
+    q.tile = tile;
+    q.codes = c.take<uint8_t>((size_t)(n * q.d_pad));
+    q.scales = c.take<uint8_t>((size_t)(n * q.sd));
+    return q;
 }
 
 const LayerCache *get_projection(const freeze_ctx *ctx, int slot, int *err)
@@ -1300,14 +1301,15 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
     const size_t xb = (size_t)((rows - 1) * row_stride + d) * size;
     const size_t cb = (size_t)(rows * quant_code_stride(d)), sb = (size_t)(rows * quant_scale_stride(d));
     if (share_bytes(x, xb, codes, cb) || share_bytes(x, xb, scales, sb) || share_bytes(codes, cb, scales, sb)) return FREEZE_EINVAL;
-    return launch_quantise_rows(x, x_dtype, rows, d, row_stride, codes, scales, static_cast<hipStream_t>(stream)) == hipSuccess ? FREEZE_OK
-                                                                                                                              : FREEZE_EHIP;
+    const QuantRows out{codes, scales, quant_code_stride(d), quant_scale_stride(d), 0};
+    return launch_quantise_rows(x, x_dtype, rows, d, row_stride, out, static_cast<hipStream_t>(stream)) == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
 }
 
 size_t freeze_quantised_storage_bytes(int64_t m, int64_t d)
 {
     if (m < 1 || m >= (int64_t)2147483647 - 512 || d < 1 || d > kQuantMaxD) return 0;
-    return align_up((size_t)(m * quant_code_stride(d))) + align_up((size_t)(m * quant_scale_stride(d))) + align_up((size_t)m * 4);
+    const int64_t rows = quant_tiled_rows(m, kQuantTile);
+    return align_up((size_t)(rows * quant_code_stride(d))) + align_up((size_t)(rows * quant_scale_stride(d))) + align_up((size_t)m * 4);
 }
 
 int freeze_quantised_build(freeze_ctx *ctx, int slot, const void *weights, int weights_dtype, const uint8_t *weight_scales, int64_t m,
@@ -1322,18 +1324,18 @@ int freeze_quantised_build(freeze_ctx *ctx, int slot, const void *weights, int w
     if (!aligned(weights, given ? 16 : (weights_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(weight_scales, 4) || !aligned(bias, 4)) return FREEZE_EINVAL;
     if (storage_bytes < bytes || !aligned(storage, kAlign)) return FREEZE_EWORKSPACE;
     Carver st(storage);
-    uint8_t *codes = st.take<uint8_t>((size_t)(m * quant_code_stride(d))), *scales = st.take<uint8_t>((size_t)(m * quant_scale_stride(d)));
+    const QuantRows w = take_rows(st, m, d, kQuantTile);
     float *q_bias = bias ? st.take<float>((size_t)m) : nullptr;
     hipStream_t s = static_cast<hipStream_t>(stream);
     LayerCache &L = ctx->layers[slot];
     L = LayerCache();
-    const hipError_t e = given ? launch_copy_codes(static_cast<const uint8_t *>(weights), weight_scales, m, d, codes, scales, s)
-                               : launch_quantise_rows(weights, weights_dtype, m, d, d, codes, scales, s);
+    const hipError_t e = given ? launch_tile_codes(static_cast<const uint8_t *>(weights), weight_scales, m, d, w, s)
+                               : launch_quantise_rows(weights, weights_dtype, m, d, d, w, s);
     if (e != hipSuccess || (bias && launch_copy_rows_f32(bias, 1, q_bias, m, 1, s) != hipSuccess)) return FREEZE_EHIP;
     L.n = m;
     L.d = d;
-    L.codes = codes;
-    L.scales = scales;
+    L.codes = w.codes;
+    L.scales = w.scales;
     L.q_bias = q_bias;
     return FREEZE_OK;
 }
@@ -1344,9 +1346,15 @@ size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t
     const LayerCache *P = get_quantised(ctx, slot, &err);
     if (!P || b < 0 || b > (int64_t)1 << 30 || x_dtype < FREEZE_F32 || x_dtype > FREEZE_E4M3) return 0;
     if (b < 1) b = 1;
-    size_t bytes = kAlign + quant_part_bytes(ctx, *P, b);
-    if (x_dtype != FREEZE_E4M3) bytes += align_up((size_t)(b * quant_code_stride(P->d))) + align_up((size_t)(b * quant_scale_stride(P->d)));
-    return bytes;
+    // the largest of what the two types of outputs take
+    size_t most = 0;
+    for (int half = 0; half < 2; ++half) {
+        const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), half != 0, ctx->num_cus);
+        const int64_t rows = quant_tiled_rows(b, pl.bm);
+        const size_t bytes = align_up((size_t)(rows * quant_code_stride(P->d))) + align_up((size_t)(rows * quant_scale_stride(P->d))) + align_up(pl.part * 4);
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 
 int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dtype, const uint8_t *x_scales, int64_t b, int64_t x_stride,
@@ -1365,21 +1373,17 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
     if (!x || !out || !workspace || given != (x_scales != nullptr) || !aligned(out, out_size) ||
         !aligned(x, given ? 16 : (x_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(x_scales, 4))
         return FREEZE_EINVAL;
-    const size_t cb = (size_t)(b * quant_code_stride(P->d)), sb = (size_t)(b * quant_scale_stride(P->d));
-    const size_t ob = (size_t)((b - 1) * out_stride + P->n) * out_size;
-    if (given && (share_bytes(out, ob, x, cb) || share_bytes(out, ob, x_scales, sb))) return FREEZE_EINVAL;
     if (workspace_bytes < freeze_quantised_workspace_bytes(ctx, slot, b, x_dtype) || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), out_dtype == FREEZE_BF16, ctx->num_cus);
     Carver ws(workspace);
+    const QuantRows rows = take_rows(ws, b, P->d, pl.bm);
+    const hipError_t e = given ? launch_tile_codes(static_cast<const uint8_t *>(x), x_scales, b, P->d, rows, s)
+                               : launch_quantise_rows(x, x_dtype, b, P->d, x_stride, rows, s);
+    if (e != hipSuccess) return FREEZE_EHIP;
     QuantProduct q{};
-    q.x = static_cast<const uint8_t *>(x);
-    q.xs = x_scales;
-    if (!given) {
-        uint8_t *codes = ws.take<uint8_t>(cb), *scales = ws.take<uint8_t>(sb);
-        if (launch_quantise_rows(x, x_dtype, b, P->d, x_stride, codes, scales, s) != hipSuccess) return FREEZE_EHIP;
-        q.x = codes;
-        q.xs = scales;
-    }
+    q.x = rows.codes;
+    q.xs = rows.scales;
     q.w = P->codes;
     q.ws = P->scales;
     q.bias = P->q_bias;
@@ -1391,7 +1395,6 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
     q.sd = quant_scale_stride(P->d);
     q.out_bf16 = out_dtype == FREEZE_BF16;
     q.relu = relu != 0;
-    const QuantPlan pl = plan_quant_product(b, P->n, q.d_pad, q.out_bf16, ctx->num_cus);
     q.part = pl.part ? ws.take<float>(pl.part) : nullptr;
     return launch_quant_product(pl, q, s) == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
 }

@@ -64,7 +64,7 @@ __device__ __forceinline__ void load4_global_to_lds(uint64_t sbase, uint32_t vof
 // Rows of 128 bytes in LDS: chunk c (16 bytes) of a row lies at c ^ row128_swizzle(row).  A fragment read takes one chunk of each
 // of 16 rows for every two groups of lanes, chunks 2g or 2g + 1 for group g = lane >> 4, and the 16 lanes a cycle serves (rows 0-3
 // and 12-15 of one group with rows 4-11 of the next) meet 16 different positions.
-__device__ __forceinline__ int row128_swizzle(int row)
+__host__ __device__ __forceinline__ int row128_swizzle(int row)
 {
     const int u = (row >> 1) & 7;
     return u ^ (((u + 2) & 4) >> 1);

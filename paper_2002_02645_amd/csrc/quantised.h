@@ -10,16 +10,38 @@ constexpr int64_t kQuantMaxD = 1 << 22;      // a tile of 256 rows spans 32-bit 
 inline int64_t quant_code_stride(int64_t d) { return (d + kQuantBlock - 1) / kQuantBlock * kQuantBlock; }
 inline int64_t quant_scale_stride(int64_t d) { return ((d + kQuantBlock - 1) / kQuantBlock + 3) / 4 * 4; }
 
+// Quantised rows as the product reads them: tiles of `tile` rows (kQuantTile, or fewer for a small batch), in a tile k-step by k-step
+// (128 codes), so that a stage of the product is one run of memory; of a row's 128 bytes, chunk c (16 bytes) lies at
+// c ^ row128_swizzle(row), as in LDS.  The scale bytes of four k-steps lie together, 4 bytes a row.  Rows behind the last one are
+// whatever they were: they meet outputs that are not stored.
+constexpr int kQuantTile = 256;
+inline int64_t quant_tiled_rows(int64_t rows, int64_t tile) { return (rows + tile - 1) / tile * tile; }
+struct QuantRows {
+    uint8_t *codes, *scales;
+    int64_t d_pad, sd;      // bytes of a row
+    int tile;               // rows of a tile; 0: row after row (the layout of freeze_quantise_rows)
+    __host__ __device__ int64_t code_at(int64_t r, int64_t chunk) const   // chunk: 16 codes
+    {
+        if (tile == 0) return r * d_pad + chunk * 16;
+        const int64_t t = r >> __builtin_ctz(tile), in = r - t * tile;   // (a power of two)
+        return t * tile * d_pad + ((chunk >> 3) * tile + in) * 128 + (((int)chunk & 7) ^ row128_swizzle((int)in)) * 16;
+    }
+    __host__ __device__ int64_t scale_at(int64_t r, int64_t block) const
+    {
+        if (tile == 0) return r * sd + block;
+        const int64_t t = r >> __builtin_ctz(tile), in = r - t * tile;
+        return t * tile * sd + ((block >> 2) * tile + in) * 4 + (block & 3);
+    }
+};
+
 // x [rows, d] (dtype: FREEZE_F32 or FREEZE_BF16) -> codes, scales
-hipError_t launch_quantise_rows(const void *x, int dtype, int64_t rows, int64_t d, int64_t row_stride, uint8_t *codes,
-                                uint8_t *scales, hipStream_t s);
-// codes and scales as given -> the same with zeros behind d
-hipError_t launch_copy_codes(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, uint8_t *out_codes, uint8_t *out_scales,
-                             hipStream_t s);
+hipError_t launch_quantise_rows(const void *x, int dtype, int64_t rows, int64_t d, int64_t row_stride, const QuantRows &out, hipStream_t s);
+// codes and scales row after row -> out, zeros behind d
+hipError_t launch_tile_codes(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, const QuantRows &out, hipStream_t s);
 
 struct QuantProduct {
-    const uint8_t *x, *xs;   // [b, d_pad], [b, sd]
-    const uint8_t *w, *ws;   // [m, d_pad], [m, sd]
+    const uint8_t *x, *xs;   // b rows in tiles of the plan's bm
+    const uint8_t *w, *ws;   // m rows in tiles of kQuantTile
     const float *bias;       // [m] or null
     void *out;               // [b, m], rows out_stride elements apart
     int64_t out_stride;

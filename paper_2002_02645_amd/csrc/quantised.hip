@@ -20,10 +20,9 @@ __device__ __forceinline__ int block_exponent(uint32_t amax_bits)
 
 // Eight values a thread, sixteen threads a block of 128.  VEC: rows start on 16-byte boundaries (bases and strides).
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void quantise_rows_kernel(const T *x, int64_t rows, int64_t d, int64_t row_stride, int64_t d_pad,
-                                                            int64_t sd, uint8_t *codes, uint8_t *scales)
+__global__ __launch_bounds__(256) void quantise_rows_kernel(const T *x, int64_t rows, int64_t d, int64_t row_stride, QuantRows out)
 {
-    const int64_t per_row = d_pad / 8, total = rows * per_row;   // a multiple of 16: a block's threads go on together
+    const int64_t per_row = out.d_pad / 8, total = rows * per_row;   // a multiple of 16: a block's threads go on together
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
         const int64_t r = t / per_row, c = (t - r * per_row) * 8;
         const T *src = x + r * row_stride + c;
@@ -72,23 +71,22 @@ __global__ __launch_bounds__(256) void quantise_rows_kernel(const T *x, int64_t 
         w0 = __builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inv, v[3] * inv, w0, true);
         w1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[4] * inv, v[5] * inv, w1, false);
         w1 = __builtin_amdgcn_cvt_pk_fp8_f32(v[6] * inv, v[7] * inv, w1, true);
-        *reinterpret_cast<u32x2 *>(codes + r * d_pad + c) = u32x2{(uint32_t)w0, (uint32_t)w1};
+        *reinterpret_cast<u32x2 *>(out.codes + out.code_at(r, c >> 4) + (c & 8)) = u32x2{(uint32_t)w0, (uint32_t)w1};
         if ((c & 127) == 0) {
             const int64_t b = c >> 7;
-            scales[r * sd + b] = (uint8_t)(ex + 127);
-            if (c + 128 == d_pad)
-                for (int64_t q = b + 1; q < sd; ++q) scales[r * sd + q] = 1;
+            out.scales[out.scale_at(r, b)] = (uint8_t)(ex + 127);
+            if (c + 128 == out.d_pad)
+                for (int64_t q = b + 1; q < out.sd; ++q) out.scales[out.scale_at(r, q)] = 1;
         }
     }
 }
 
-__global__ __launch_bounds__(256) void copy_codes_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, int64_t d_pad,
-                                                         int64_t sd, uint8_t *out_codes, uint8_t *out_scales)
+__global__ __launch_bounds__(256) void tile_codes_kernel(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, QuantRows out)
 {
-    const int64_t per_row = d_pad / 16, total = rows * per_row;
+    const int64_t per_row = out.d_pad / 16, total = rows * per_row;
     for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < total; t += (int64_t)gridDim.x * 256) {
-        const int64_t r = t / per_row, c = (t - r * per_row) * 16;
-        u32x4 v = *reinterpret_cast<const u32x4 *>(codes + r * d_pad + c);
+        const int64_t r = t / per_row, chunk = t - r * per_row, c = chunk * 16;
+        u32x4 v = *reinterpret_cast<const u32x4 *>(codes + r * out.d_pad + c);
         if (c + 16 > d) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -96,12 +94,12 @@ __global__ __launch_bounds__(256) void copy_codes_kernel(const uint8_t *codes, c
                 v[e] = left >= 4 ? v[e] : (left <= 0 ? 0u : v[e] & ((1u << (8 * (int)left)) - 1u));
             }
         }
-        *reinterpret_cast<u32x4 *>(out_codes + r * d_pad + c) = v;
+        *reinterpret_cast<u32x4 *>(out.codes + out.code_at(r, chunk)) = v;
         if ((c & 127) == 0) {
             const int64_t b = c >> 7;
-            out_scales[r * sd + b] = scales[r * sd + b];
-            if (c + 128 == d_pad)
-                for (int64_t q = b + 1; q < sd; ++q) out_scales[r * sd + q] = 1;
+            out.scales[out.scale_at(r, b)] = scales[r * out.sd + b];
+            if (c + 128 == out.d_pad)
+                for (int64_t q = b + 1; q < out.sd; ++q) out.scales[out.scale_at(r, q)] = 1;
         }
     }
 }
@@ -114,30 +112,25 @@ unsigned blocks_for(int64_t threads)
 
 }  // namespace
 
-hipError_t launch_quantise_rows(const void *x, int dtype, int64_t rows, int64_t d, int64_t row_stride, uint8_t *codes,
-                                uint8_t *scales, hipStream_t s)
+hipError_t launch_quantise_rows(const void *x, int dtype, int64_t rows, int64_t d, int64_t row_stride, const QuantRows &out, hipStream_t s)
 {
     if (rows <= 0) return hipSuccess;
-    const int64_t d_pad = quant_code_stride(d), sd = quant_scale_stride(d);
-    const dim3 grid(blocks_for(rows * (d_pad / 8))), block(256);
+    const dim3 grid(blocks_for(rows * (out.d_pad / 8))), block(256);
     const int64_t size = dtype == FREEZE_F32 ? 4 : 2;
     const bool vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && row_stride * size % 16 == 0;
     if (dtype == FREEZE_F32) {
         auto k = vec ? quantise_rows_kernel<float, true> : quantise_rows_kernel<float, false>;
-        hipLaunchKernelGGL(k, grid, block, 0, s, static_cast<const float *>(x), rows, d, row_stride, d_pad, sd, codes, scales);
+        hipLaunchKernelGGL(k, grid, block, 0, s, static_cast<const float *>(x), rows, d, row_stride, out);
     } else {
         auto k = vec ? quantise_rows_kernel<uint16_t, true> : quantise_rows_kernel<uint16_t, false>;
-        hipLaunchKernelGGL(k, grid, block, 0, s, static_cast<const uint16_t *>(x), rows, d, row_stride, d_pad, sd, codes, scales);
+        hipLaunchKernelGGL(k, grid, block, 0, s, static_cast<const uint16_t *>(x), rows, d, row_stride, out);
     }
     return hipGetLastError();
 }
 
-hipError_t launch_copy_codes(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, uint8_t *out_codes, uint8_t *out_scales,
-                             hipStream_t s)
+hipError_t launch_tile_codes(const uint8_t *codes, const uint8_t *scales, int64_t rows, int64_t d, const QuantRows &out, hipStream_t s)
 {
-    const int64_t d_pad = quant_code_stride(d), sd = quant_scale_stride(d);
-    hipLaunchKernelGGL(copy_codes_kernel, dim3(blocks_for(rows * (d_pad / 16))), dim3(256), 0, s, codes, scales, rows, d, d_pad, sd,
-                       out_codes, out_scales);
+    hipLaunchKernelGGL(tile_codes_kernel, dim3(blocks_for(rows * (out.d_pad / 16))), dim3(256), 0, s, codes, scales, rows, d, out);
     return hipGetLastError();
 }
 

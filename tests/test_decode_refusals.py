@@ -28,7 +28,7 @@ def test_strides_and_sizes(ctx):
         assert binding.freeze_quantised_code_stride(d) == 0 and binding.freeze_quantised_scale_stride(d) == 0
         assert binding.freeze_quantised_storage_bytes(5, d) == 0
     up = lambda x: (x + 255) // 256 * 256
-    assert binding.freeze_quantised_storage_bytes(1000, 129) == up(256000) + up(4000) + up(4000)
+    assert binding.freeze_quantised_storage_bytes(1000, 129) == 1024 * 256 + 1024 * 4 + up(4000)   # rows in tiles of 256
     assert binding.freeze_quantised_storage_bytes(0, 8) == 0 and binding.freeze_quantised_storage_bytes(2147483647, 8) == 0
     assert L.freeze_quantised_workspace_bytes(ctx, 0, 4, 0) == 0     # nothing built
 

@@ -225,14 +225,15 @@ def test_output_over_its_input():
         want = fc.quantised_project(0, x)
         fc.quantised_project(0, x, out=x)
         assert torch.equal(x, want)
-        # given codes are read to the end: an output over them is refused
+        # the same over given codes and scales
         buf = torch.zeros(1 << 16, dtype=torch.uint8, device="cuda")
-        codes = buf[:50 * 256].view(50, 256).view(torch.float8_e4m3fn)
-        scales = torch.full((50, 4), 127, dtype=torch.uint8, device="cuda")
-        for at in (0, 50 * 256 - 16):
-            with pytest.raises(binding.FreezeError):
-                fc.quantised_project(0, codes, scales, out=buf[at:at + 2 * 50 * 256].view(torch.bfloat16).view(50, 256))
-        assert (fc.quantised_project(0, codes, scales, out=buf[50 * 256:3 * 50 * 256].view(torch.bfloat16).view(50, 256)) == 0).all()
+        codes, scales = fc.quantise_rows(want)
+        wanted = fc.quantised_project(0, codes, scales)
+        buf[:50 * 256] = codes.view(torch.uint8).view(-1)
+        buf[50 * 256:50 * 260] = scales.view(-1)
+        got = fc.quantised_project(0, buf[:50 * 256].view(50, 256).view(torch.float8_e4m3fn), buf[50 * 256:50 * 260].view(50, 4),
+                                   out=buf[:4 * 50 * 256].view(torch.float32).view(50, 256))
+        assert torch.equal(got, wanted)
     finally:
         fc.close()
 
