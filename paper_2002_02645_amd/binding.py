@@ -355,7 +355,15 @@ def _here(*tensors: Optional[torch.Tensor]) -> None:
     """The library's kernels run on the current device."""
     dev = torch.cuda.current_device()
     for t in tensors:
-        assert t is None or (t.is_cuda and t.device.index == dev), "tensors of the current device are needed"
+        assert t is None or t.get_device() == dev, "tensors of the current device are needed"
+
+
+def _at(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _on(stream) -> int:
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 def _rows_of(t: torch.Tensor) -> int:
@@ -364,8 +372,11 @@ def _rows_of(t: torch.Tensor) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
+_DTYPES = {torch.float32: FREEZE_F32, torch.bfloat16: FREEZE_BF16, torch.float8_e4m3fn: FREEZE_E4M3}
+
+
 def _values_dtype(t: torch.Tensor) -> int:
-    return {torch.float32: FREEZE_F32, torch.bfloat16: FREEZE_BF16, torch.float8_e4m3fn: FREEZE_E4M3}[t.dtype]
+    return _DTYPES[t.dtype]
 
 
 def freeze_quantise_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
@@ -375,7 +386,7 @@ def freeze_quantise_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     assert x.dtype in (torch.float32, torch.bfloat16)
     assert codes.dtype == torch.float8_e4m3fn and codes.is_contiguous() and codes.shape == (rows, freeze_quantised_code_stride(d))
     assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (rows, freeze_quantised_scale_stride(d))
-    _check(lib().freeze_quantise_rows(_ptr(x), _values_dtype(x), rows, d, _rows_of(x), _ptr(codes), _ptr(scales), _stream(stream)),
+    _check(lib().freeze_quantise_rows(_at(x), _values_dtype(x), rows, d, _rows_of(x), _at(codes), _at(scales), _on(stream)),
            "freeze_quantise_rows")
 
 
@@ -395,8 +406,8 @@ def freeze_quantised_build(ctx, slot: int, weights: torch.Tensor, scales: Option
     else:
         assert weights.dtype == torch.float8_e4m3fn and weights.shape[1] == freeze_quantised_code_stride(d)
         assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (m, freeze_quantised_scale_stride(d))
-    _check(lib().freeze_quantised_build(ctx, slot, _ptr(weights), _values_dtype(weights), _ptr(scales), m, d, _ptr(bias), _ptr(storage),
-                                        storage.numel() * storage.element_size(), _stream(stream)), "freeze_quantised_build")
+    _check(lib().freeze_quantised_build(ctx, slot, _at(weights), _values_dtype(weights), _at(scales), m, d, _at(bias), _at(storage),
+                                        storage.nbytes, _on(stream)), "freeze_quantised_build")
 
 
 def freeze_quantised_workspace_bytes(ctx, slot: int, b: int, x_dtype: int) -> int:
@@ -416,9 +427,9 @@ def freeze_quantised_project(ctx, slot: int, x: torch.Tensor, scales: Optional[t
         assert x.dtype == torch.float8_e4m3fn and x.is_contiguous() and x.shape[1] == freeze_quantised_code_stride(d)
         assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (b, freeze_quantised_scale_stride(d))
         stride = 0
-    _check(lib().freeze_quantised_project(ctx, slot, _ptr(x), _values_dtype(x), _ptr(scales), b, stride, int(relu), _ptr(out),
-                                          _values_dtype(out), _rows_of(out), _ptr(workspace),
-                                          workspace.numel() * workspace.element_size(), _stream(stream)), "freeze_quantised_project")
+    _check(lib().freeze_quantised_project(ctx, slot, _at(x), _values_dtype(x), _at(scales), b, stride, int(relu), _at(out),
+                                          _values_dtype(out), _rows_of(out), _at(workspace),
+                                          workspace.nbytes, _on(stream)), "freeze_quantised_project")
 
 
 def freeze_beam_workspace_bytes(groups: int, beams: int, vocab: int, k: int) -> int:
@@ -436,10 +447,10 @@ def freeze_beam_select(logits: torch.Tensor, scores: torch.Tensor, finished: Opt
     groups = rows // beams
     for t, dt in ((out_scores, torch.float32), (out_tokens, torch.int32), (out_parents, torch.int32), (out_finished, torch.uint8)):
         assert t is None or (t.dtype == dt and t.is_contiguous() and t.numel() == groups * k)
-    _check(lib().freeze_beam_select(_ptr(logits), _values_dtype(logits), groups, beams, vocab, _rows_of(logits), _ptr(scores),
-                                    _ptr(finished), end_token, k, _ptr(out_scores), _ptr(out_tokens), _ptr(out_parents),
-                                    _ptr(out_finished), _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                    _stream(stream)), "freeze_beam_select")
+    _check(lib().freeze_beam_select(_at(logits), _values_dtype(logits), groups, beams, vocab, _rows_of(logits), _at(scores),
+                                    _at(finished), end_token, k, _at(out_scores), _at(out_tokens), _at(out_parents),
+                                    _at(out_finished), _at(workspace), workspace.nbytes,
+                                    _on(stream)), "freeze_beam_select")
 
 
 def state_of(src: torch.Tensor, dst: torch.Tensor, used: Optional[int] = None, row_dim: int = 0) -> FreezeState:
@@ -475,8 +486,8 @@ def freeze_reorder_states(states: Sequence[FreezeState], parents: torch.Tensor, 
     _here(parents)
     assert parents.dtype == torch.int32 and parents.is_contiguous()
     arr = (FreezeState * len(states))(*states)
-    _check(lib().freeze_reorder_states(ctypes.cast(arr, ctypes.c_void_p), len(states), _ptr(parents), parents.numel(), src_rows,
-                                       _stream(stream)), "freeze_reorder_states")
+    _check(lib().freeze_reorder_states(ctypes.addressof(arr), len(states), _at(parents), parents.numel(), src_rows,
+                                       _on(stream)), "freeze_reorder_states")
 
 
 def freeze_compact_misses(hit: torch.Tensor, sel_in: Optional[torch.Tensor], sel_out: torch.Tensor,

@@ -19,7 +19,7 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
 namespace {
 
-constexpr float kLowest = -3.402823466e38f;
+constexpr float kLowest = -3.402823466e38f, kLog2E = 1.44269504f;
 constexpr int kBeamLoads = 4;   // loads of 16 bytes a lane has in flight
 
 struct BeamArgs {
@@ -68,22 +68,15 @@ __device__ __forceinline__ bool insert(BestList<V, I> &list, V cv, I ci, int k, 
     return true;
 }
 
-__device__ __forceinline__ uint64_t ordered_bits64(double x)
-{
-    const uint64_t u = (uint64_t)__double_as_longlong(x);
-    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
-}
-__device__ __forceinline__ double from_ordered_bits64(uint64_t u)
-{
-    return __longlong_as_double((long long)((u >> 63) ? (u & 0x7fffffffffffffffull) : ~u));
-}
-
 template <typename T>
 __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 {
-    constexpr int V = 16 / (int)sizeof(T), E = V * kBeamLoads;
-    const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int V = 16 / (int)sizeof(T), E = V * kBeamLoads, B = 8;   // B values of a lane are looked at together
+    __shared__ float floors[4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (lane == 0) floors[wave] = kLowest;
+    __syncthreads();
+    const int64_t unit0 = (int64_t)blockIdx.x * 4, unit = unit0 + wave;
     if (unit >= (int64_t)p.rows * p.parts) return;   // uniform in the wave
     const int row = (int)(unit / p.parts), part = (int)(unit % p.parts);
     if (p.scores[row] == -__builtin_inff() || (p.finished && p.finished[row])) return;
@@ -92,51 +85,72 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     const int64_t shift = (int64_t)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
     const int64_t all = (p.vocab + shift + V - 1) / V;
     const int64_t g0 = part * p.groups_per_part, g1 = g0 + p.groups_per_part < all ? g0 + p.groups_per_part : all;
+    // what the workgroup's other waves found on the same row
+    const bool same_row = lane < 4 && (int)((unit0 + lane) / p.parts) == row;
+
+    auto load = [&](int64_t base, u32x4(&raw)[kBeamLoads]) {
+#pragma unroll
+        for (int l = 0; l < kBeamLoads; ++l) {
+            const int64_t g = base + l * 64 + lane, at = g * V - shift;
+            if (g < g1 && at >= 0 && at + V <= p.vocab) {
+                raw[l] = *reinterpret_cast<const u32x4 *>(src + at);
+            } else {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    uint32_t word = 0;
+#pragma unroll
+                    for (int e = 0; e < V / 4; ++e) {
+                        const int64_t i = at + w * (V / 4) + e;
+                        const bool in = g < g1 && i >= 0 && i < p.vocab;
+                        if constexpr (sizeof(T) == 4) word = in ? __float_as_uint(src[i]) : 0xff800000u;
+                        else word |= (in ? (uint32_t)src[i] : 0xff80u) << (16 * e);
+                    }
+                    raw[l][w] = word;
+                }
+            }
+        }
+    };
+    auto value = [](const u32x4(&raw)[kBeamLoads], int e) {
+        const uint32_t w = raw[e / V][(e % V) * 4 / V];
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+        else return __uint_as_float(e % 2 ? w & 0xffff0000u : w << 16);
+    };
 
     BestList<float, uint32_t> list;
     list.clear(-__builtin_inff());
     float floor_v = kLowest;   // what a value has to reach
     float top = -__builtin_inff(), sum = 0.f;
+    u32x4 raw[kBeamLoads], next[kBeamLoads];
+    if (g0 < g1) load(g0, next);
     for (int64_t base = g0; base < g1; base += 64 * kBeamLoads) {
-        float v[E];
 #pragma unroll
-        for (int l = 0; l < kBeamLoads; ++l) {
-            const int64_t g = base + l * 64 + lane, at = g * V - shift;
-            if (g < g1 && at >= 0 && at + V <= p.vocab) {
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(src + at);
+        for (int l = 0; l < kBeamLoads; ++l) raw[l] = next[l];
+        if (base + 64 * kBeamLoads < g1) load(base + 64 * kBeamLoads, next);
+        float most8[E / B];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (sizeof(T) == 4) {
-                        v[l * V + e] = __uint_as_float(w[e]);
-                    } else {
-                        v[l * V + 2 * e] = __uint_as_float(w[e] << 16);
-                        v[l * V + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-                    }
-                }
-            } else {
+        for (int b = 0; b < E / B; ++b) {
+            most8[b] = value(raw, b * B);
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    v[l * V + e] = -__builtin_inff();
-                    if (g < g1 && at + e >= 0 && at + e < p.vocab) {
-                        if constexpr (sizeof(T) == 4) v[l * V + e] = src[at + e];
-                        else v[l * V + e] = __uint_as_float((uint32_t)src[at + e] << 16);
-                    }
-                }
-            }
+            for (int e = 1; e < B; ++e) most8[b] = __builtin_fmaxf(most8[b], value(raw, b * B + e));
         }
-        float most = v[0];
+        float most = most8[0];
 #pragma unroll
-        for (int e = 1; e < E; ++e) most = __builtin_fmaxf(most, v[e]);
+        for (int b = 1; b < E / B; ++b) most = __builtin_fmaxf(most, most8[b]);
         if (most > top) {
-            sum *= expf(top - most);
+            sum *= __builtin_amdgcn_exp2f((top - most) * kLog2E);
             top = most;
         }
         if (top >= kLowest) {
+            // differences to the largest value first: the rounding of the factor then goes by them, not by the values
             float part_sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) part_sum += expf(v[e] - top);
+            for (int e = 0; e < E; ++e) part_sum += __builtin_amdgcn_exp2f((value(raw, e) - top) * kLog2E);
             sum += part_sum;
         }
+        float others = same_row ? *const_cast<volatile float *>(&floors[lane & 3]) : kLowest;
+        others = __builtin_fmaxf(others, __shfl_xor(others, 1, 64));
+        others = __builtin_fmaxf(others, __shfl_xor(others, 2, 64));
+        floor_v = __builtin_fmaxf(floor_v, __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(others))));
         const uint64_t lanes = __ballot(most >= floor_v);
         if (lanes == 0) continue;   // uniform
         if (__popcll(lanes) >= p.k) {
@@ -145,23 +159,29 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
             floor_v = __builtin_fmaxf(floor_v, from_ordered_bits(~(uint32_t)__shfl((int)sorted, p.k - 1, 64)));
         }
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            uint64_t who = __ballot(v[e] >= floor_v);
-            while (who) {
-                const int l = __ffsll((unsigned long long)who) - 1;
-                who &= who - 1;
-                const float cv = __shfl(v[e], l, 64);
-                const int64_t at = (base + (e / V) * 64 + l) * V - shift + e % V;
-                if (cv >= floor_v && insert(list, cv, (uint32_t)at, p.k, lane))
-                    floor_v = __builtin_fmaxf(floor_v, __shfl(list.v, p.k - 1, 64));
+        for (int b = 0; b < E / B; ++b) {
+            if (__ballot(most8[b] >= floor_v) == 0) continue;   // uniform
+#pragma unroll
+            for (int e = b * B; e < (b + 1) * B; ++e) {
+                const float v = value(raw, e);
+                uint64_t who = __ballot(v >= floor_v);
+                while (who) {
+                    const int l = __ffsll((unsigned long long)who) - 1;
+                    who &= who - 1;
+                    const float cv = __shfl(v, l, 64);
+                    const int64_t at = (base + (e / V) * 64 + l) * V - shift + e % V;
+                    if (cv >= floor_v && insert(list, cv, (uint32_t)at, p.k, lane))
+                        floor_v = __builtin_fmaxf(floor_v, __shfl(list.v, p.k - 1, 64));
+                }
             }
         }
+        if (lane == 0) *const_cast<volatile float *>(&floors[wave]) = floor_v;
     }
     // the piece's sum, relative to its largest value
     float m = top;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, o, 64));
-    double s = top >= kLowest ? (double)sum * (double)expf(top - m) : 0.0;
+    double s = top >= kLowest ? (double)sum * (double)__builtin_amdgcn_exp2f((top - m) * kLog2E) : 0.0;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if (lane == 0) {
@@ -174,104 +194,150 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     }
 }
 
-// One workgroup a group: the rows' offsets score - log sum exp, then the k best of the pieces' lists.
-constexpr int kMeetThreads = 256;
+// One workgroup a group: the rows' offsets score - log sum exp, then the k best of the pieces' lists.  What reaches the k-th largest of some
+// wave's lanes' largest is gathered, as a rule a few more than k, and every one of them counts those before it; where
+// too many reach it (or there are more than kMeetHeld a thread), the waves keep lists as the pieces did.
+constexpr int kMeetThreads = 256, kMeetHeld = 16, kMeetGathered = 512;
 __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
 {
     __shared__ double off[FREEZE_MAX_BEAMS];     // -inf: nothing in the row
     __shared__ uint8_t ended[FREEZE_MAX_BEAMS];
-    __shared__ double list_v[kMeetThreads / 64][FREEZE_MAX_K];
-    __shared__ uint64_t list_i[kMeetThreads / 64][FREEZE_MAX_K];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    __shared__ double list_v[kMeetGathered];
+    __shared__ uint64_t list_i[kMeetGathered];
+    __shared__ float floors[kMeetThreads / 64];
+    __shared__ int gathered;
+    static_assert(kMeetThreads / 64 * FREEZE_MAX_K <= kMeetGathered, "the waves' lists");
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row0 = (int64_t)blockIdx.x * p.beams;
-    for (int j = wave; j < p.beams; j += kMeetThreads / 64) {
-        const float score = p.scores[row0 + j];
-        const bool end = p.finished && p.finished[row0 + j];
-        double o = score;
-        if (!end && score > -__builtin_inff()) {
-            const float *tops = p.tops + (row0 + j) * p.parts;
-            const double *sums = p.sums + (row0 + j) * p.parts;
-            float m = -__builtin_inff();
-            for (int q = lane; q < p.parts; q += 64) m = __builtin_fmaxf(m, tops[q]);
-#pragma unroll
-            for (int x = 32; x > 0; x >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, x, 64));
-            double s = 0.0;
-            if (m >= kLowest)
-                for (int q = lane; q < p.parts; q += 64)
-                    if (tops[q] >= kLowest) s += sums[q] * exp((double)tops[q] - (double)m);
-#pragma unroll
-            for (int x = 32; x > 0; x >>= 1) s += __shfl_xor(s, x, 64);
-            o = m >= kLowest ? (double)score - (double)m - log(s) : -__builtin_inf();
-        }
-        if (lane == 0) {
-            off[j] = o;
+    if (tid == 0) gathered = 0;
+    {
+        // a row for as many threads as there are for each: a power of two of them, within a wave
+        int per = 64;
+        while (per > 1 && kMeetThreads / per < p.beams) per >>= 1;
+        const int j = tid / per, at = tid & (per - 1);
+        const bool in = j < p.beams;
+        const float score = in ? p.scores[row0 + j] : -__builtin_inff();
+        const bool end = in && p.finished && p.finished[row0 + j];
+        const bool open = !end && score > -__builtin_inff();
+        const float *tops = p.tops + (row0 + j) * p.parts;
+        const double *sums = p.sums + (row0 + j) * p.parts;
+        float m = -__builtin_inff();
+        if (open)
+            for (int q = at; q < p.parts; q += per) m = __builtin_fmaxf(m, tops[q]);
+        for (int x = per >> 1; x > 0; x >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, x, 64));
+        double s = 0.0;
+        if (open && m >= kLowest)
+            for (int q = at; q < p.parts; q += per)
+                if (tops[q] >= kLowest) s += sums[q] * exp((double)tops[q] - (double)m);
+        for (int x = per >> 1; x > 0; x >>= 1) s += __shfl_xor(s, x, 64);
+        if (in && at == 0) {
+            off[j] = !open ? (double)score : (m >= kLowest ? (double)score - (double)m - log(s) : -__builtin_inf());
             ended[j] = end;
         }
     }
     __syncthreads();
+    const int per_row = p.parts * p.k, all = p.beams * per_row;
+    auto put = [&](int64_t place, double v, uint64_t i) {
+        const bool some = v > -__builtin_inf();
+        const int32_t token = some ? (int32_t)(uint32_t)i : (p.end > 0 ? p.end : 0);
+        const int64_t at = (int64_t)blockIdx.x * p.k + place;
+        p.out_scores[at] = some ? (float)v : -__builtin_inff();
+        p.out_tokens[at] = token;
+        p.out_parents[at] = (int32_t)(row0 + (some ? (int64_t)(i >> 32) : 0));
+        if (p.out_finished) p.out_finished[at] = token == p.end;
+    };
+    // candidate q of the group: value (-inf: none) and place (row, token)
+    auto candidate = [&](int q, uint64_t &i) {
+        double c = -__builtin_inf();
+        if (q < all) {
+            const int j = q / per_row;
+            const float v = p.best_v[row0 * per_row + q];   // (not written where the row is empty or has ended)
+            const int32_t t = p.best_i[row0 * per_row + q];
+            const double o = off[j];
+            if (ended[j]) {
+                i = ((uint64_t)j << 32) | (uint32_t)p.end;
+                if (q == j * per_row) c = o;
+            } else if (o > -__builtin_inf() && v >= kLowest) {
+                i = ((uint64_t)j << 32) | (uint32_t)t;
+                c = o + (double)v;
+            }
+        }
+        return c;
+    };
+    if (all <= kMeetThreads * kMeetHeld) {
+        double c[kMeetHeld], most = -__builtin_inf();
+        uint64_t ci[kMeetHeld];
+        const int rounds = (all + kMeetThreads - 1) / kMeetThreads;   // uniform
+#pragma unroll
+        for (int e = 0; e < kMeetHeld; ++e) {
+            c[e] = -__builtin_inf();
+            ci[e] = 0;
+            if (e < rounds) c[e] = candidate(e * kMeetThreads + tid, ci[e]);
+            most = c[e] > most ? c[e] : most;
+        }
+        // (in fp32, one step down: what it stands for is not more than the k-th largest)
+        const uint32_t sorted = wave_sort32(~ordered_bits((float)most), lane);
+        const uint32_t kth = ~(uint32_t)__shfl((int)sorted, p.k - 1, 64);
+        if (lane == 0) floors[wave] = from_ordered_bits(kth);
+        __syncthreads();
+        const float f = __builtin_fmaxf(__builtin_fmaxf(floors[0], floors[1]), __builtin_fmaxf(floors[2], floors[3]));
+        const double floor_v = f > kLowest ? (double)from_ordered_bits(ordered_bits(f) - 1) : -1.7976931348623157e308;
+#pragma unroll
+        for (int e = 0; e < kMeetHeld; ++e)
+            if (c[e] >= floor_v) {
+                const int at = atomicAdd(&gathered, 1);   // (their order does not matter)
+                if (at < kMeetGathered) {
+                    list_v[at] = c[e];
+                    list_i[at] = ci[e];
+                }
+            }
+        __syncthreads();
+        const int n = gathered;
+        if (n <= kMeetGathered) {   // uniform
+            for (int q = tid; q < n; q += kMeetThreads) {
+                const double v = list_v[q];
+                const uint64_t i = list_i[q];
+                int before = 0;
+                for (int o = 0; o < n; ++o) before += list_v[o] > v || (list_v[o] == v && list_i[o] < i);
+                if (before < p.k) put(before, v, i);
+            }
+            for (int q = n + tid; q < p.k; q += kMeetThreads) put(q, -__builtin_inf(), 0);
+            return;
+        }
+        __syncthreads();
+    }
     BestList<double, uint64_t> list;
     list.clear(-__builtin_inf());
     double floor_v = -1.7976931348623157e308;
-    const int lists = p.beams * p.parts;
-    for (int base = wave * 64; base < lists; base += kMeetThreads) {
-        const int id = base + lane, j = id < lists ? id / p.parts : 0, part = id < lists ? id - j * p.parts : 0;
-        const bool one = id < lists && ended[j], live = id < lists && off[j] > -__builtin_inf();
-        const float *bv = p.best_v + ((row0 + j) * p.parts + part) * p.k;
-        const int32_t *bi = p.best_i + ((row0 + j) * p.parts + part) * p.k;
-        for (int t = 0; t < p.k; ++t) {   // the lists are in order: depth by depth
-            double c = -__builtin_inf();
-            uint64_t ci = ~0ull;
-            if (live && one) {
-                if (t == 0 && part == 0) {
-                    c = off[j];
-                    ci = ((uint64_t)j << 32) | (uint32_t)p.end;
-                }
-            } else if (live && bv[t] >= kLowest) {
-                c = off[j] + (double)bv[t];
-                ci = ((uint64_t)j << 32) | (uint32_t)bi[t];
-            }
-            uint64_t who = __ballot(c >= floor_v);
-            if (who == 0) break;   // uniform
-            if (t == 0 && __popcll(who) >= p.k) {
-                const uint64_t sorted = wave_sort64(~ordered_bits64(c), lane);
-                const double f = from_ordered_bits64(~shfl_any(sorted, p.k - 1));
+    for (int base = wave * 64; base < all; base += kMeetThreads) {
+        uint64_t ci = 0;
+        const double c = candidate(base + lane, ci);
+        uint64_t who = __ballot(c >= floor_v);
+        while (who) {
+            const int l = __ffsll((unsigned long long)who) - 1;
+            who &= who - 1;
+            const double cv = shfl_any(c, l);
+            if (cv >= floor_v && insert(list, cv, shfl_any(ci, l), p.k, lane)) {
+                const double f = shfl_any(list.v, p.k - 1);
                 floor_v = f > floor_v ? f : floor_v;
-                who = __ballot(c >= floor_v);
-            }
-            while (who) {
-                const int l = __ffsll((unsigned long long)who) - 1;
-                who &= who - 1;
-                const double cv = shfl_any(c, l);
-                if (cv >= floor_v && insert(list, cv, shfl_any(ci, l), p.k, lane)) {
-                    const double f = shfl_any(list.v, p.k - 1);
-                    floor_v = f > floor_v ? f : floor_v;
-                }
             }
         }
     }
     if (lane < p.k) {
-        list_v[wave][lane] = list.v;
-        list_i[wave][lane] = list.i;
+        list_v[wave * FREEZE_MAX_K + lane] = list.v;
+        list_i[wave * FREEZE_MAX_K + lane] = list.i;
     }
     __syncthreads();
     if (wave != 0) return;
     for (int w = 1; w < kMeetThreads / 64; ++w)
         for (int t = 0; t < p.k; ++t) {
-            const double cv = list_v[w][t];
-            if (!(cv > -__builtin_inf()) || !insert(list, cv, list_i[w][t], p.k, lane)) break;   // uniform
+            const double cv = list_v[w * FREEZE_MAX_K + t];
+            if (!(cv > -__builtin_inf()) || !insert(list, cv, list_i[w * FREEZE_MAX_K + t], p.k, lane)) break;   // uniform
         }
-    if (lane < p.k) {
-        const int64_t at = (int64_t)blockIdx.x * p.k + lane;
-        const bool some = list.v > -__builtin_inf();
-        const int32_t token = some ? (int32_t)(uint32_t)list.i : (p.end > 0 ? p.end : 0);
-        p.out_scores[at] = some ? (float)list.v : -__builtin_inff();
-        p.out_tokens[at] = token;
-        p.out_parents[at] = (int32_t)(row0 + (some ? (int64_t)(list.i >> 32) : 0));
-        if (p.out_finished) p.out_finished[at] = token == p.end;
-    }
+    if (lane < p.k) put(lane, list.v, list.i);
 }
 
-// How a row is cut: pieces of whole batches, as many as fill the chip with waves (16 a CU) and no more.
+// How a row is cut: pieces of whole batches, as many as fill the chip with waves (8 a CU) and no more.
 struct BeamPlan {
     int64_t groups_per_part;
     int parts;
@@ -280,7 +346,7 @@ BeamPlan beam_plan(int64_t rows, int64_t vocab, int size)
 {
     const int64_t v = 16 / size, batch = 64 * kBeamLoads;
     const int64_t batches = ((vocab + v - 1 + v - 1) / v + batch - 1) / batch;   // (a misaligned row's groups are one more)
-    int64_t parts = (4096 + rows - 1) / rows;
+    int64_t parts = (2048 + rows - 1) / rows;
     parts = parts < 1 ? 1 : (parts > batches ? batches : parts);
     BeamPlan pl;
     const int64_t per = (batches + parts - 1) / parts;
@@ -305,7 +371,7 @@ struct StateRun {
     int64_t outer_stride, row_stride, piece_stride;
     int64_t per_run;        // units of a run
     uint32_t pieces, rows;
-    int64_t first;          // units of the states before this one
+    int64_t first;          // workgroups, or units, of the states before this one
 };
 struct ReorderArgs {
     StateRun state[kStatesPerLaunch];
@@ -314,17 +380,47 @@ struct ReorderArgs {
     int states;
 };
 
+// Long runs: a workgroup copies kRunChunk units of a run, four a thread on their way at once.
+constexpr int kRunChunk = 1024;
 template <typename U>
-__global__ __launch_bounds__(256) void reorder_kernel(ReorderArgs p)
+__global__ __launch_bounds__(256) void reorder_runs_kernel(ReorderArgs p)
+{
+    const int64_t block = blockIdx.x;
+    int s = 0;
+    while (s + 1 < p.states && block >= p.state[s + 1].first) ++s;
+    const StateRun &t = p.state[s];
+    const uint32_t in = (uint32_t)(block - t.first), chunks = (uint32_t)((t.per_run + kRunChunk - 1) / kRunChunk);
+    const uint32_t run = in / chunks, chunk = in - run * chunks;
+    const uint32_t rest = run / t.pieces, piece = run - rest * t.pieces;
+    const uint32_t outer = rest / t.rows, row = rest - outer * t.rows;
+    const int64_t parent = p.parents[row];
+    if (parent < 0 || parent >= p.src_rows) return;
+    const int64_t place = outer * t.outer_stride + piece * t.piece_stride;
+    const U *src = reinterpret_cast<const U *>(t.src + place + parent * t.row_stride) + (int64_t)chunk * kRunChunk;
+    U *dst = reinterpret_cast<U *>(t.dst + place + row * t.row_stride) + (int64_t)chunk * kRunChunk;
+    const int64_t left = t.per_run - (int64_t)chunk * kRunChunk;
+    U v[kRunChunk / 256];
+#pragma unroll
+    for (int i = 0; i < kRunChunk / 256; ++i)
+        if (i * 256 + (int)threadIdx.x < left) v[i] = __builtin_nontemporal_load(src + i * 256 + threadIdx.x);
+#pragma unroll
+    for (int i = 0; i < kRunChunk / 256; ++i)
+        if (i * 256 + (int)threadIdx.x < left) __builtin_nontemporal_store(v[i], dst + i * 256 + threadIdx.x);
+}
+
+// Short runs: a unit a thread.
+template <typename U>
+__global__ __launch_bounds__(256) void reorder_units_kernel(ReorderArgs p)
 {
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < p.total; u += (int64_t)gridDim.x * 256) {
         int s = 0;
         while (s + 1 < p.states && u >= p.state[s + 1].first) ++s;
         const StateRun &t = p.state[s];
-        const int64_t run = (u - t.first) / t.per_run, at = (u - t.first) - run * t.per_run;
-        const uint32_t piece = (uint32_t)(run % t.pieces);
-        const int64_t rest = run / t.pieces;
-        const int64_t row = rest % t.rows, outer = rest / t.rows;
+        const int64_t rel = u - t.first;
+        const uint32_t run = (rel | t.per_run) < 0x100000000ll ? (uint32_t)rel / (uint32_t)t.per_run : (uint32_t)(rel / t.per_run);
+        const int64_t at = rel - run * t.per_run;
+        const uint32_t rest = run / t.pieces, piece = run - rest * t.pieces;
+        const uint32_t outer = rest / t.rows, row = rest - outer * t.rows;
         const int64_t parent = p.parents[row];
         if (parent < 0 || parent >= p.src_rows) continue;
         const int64_t place = outer * t.outer_stride + piece * t.piece_stride + at * (int64_t)sizeof(U);
@@ -482,17 +578,30 @@ int freeze_reorder_states(const freeze_state *states, int num_states, const int3
         }
         if (a.states == 0) continue;
         const int unit = bits % 16 == 0 ? 16 : (bits % 4 == 0 ? 4 : 1);
+        int64_t blocks = 0, units = 0;
         for (int j = 0; j < a.states; ++j) {
             a.state[j].per_run /= unit;
-            a.state[j].first = a.total;
-            a.total += a.state[j].per_run * runs[j];
+            blocks += (a.state[j].per_run + kRunChunk - 1) / kRunChunk * runs[j];
+            units += a.state[j].per_run * runs[j];
         }
-        const int64_t blocks = (a.total + 255) / 256;
-        const dim3 grid((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20)));
+        // a workgroup for each piece of a run where it has half a piece to do on average, and a grid holds them
+        const bool long_runs = units >= blocks * (kRunChunk / 2) && blocks < 0x7fffffff;
+        for (int j = 0; j < a.states; ++j) {
+            a.state[j].first = a.total;
+            a.total += long_runs ? (a.state[j].per_run + kRunChunk - 1) / kRunChunk * runs[j] : a.state[j].per_run * runs[j];
+        }
+        const int64_t wanted = long_runs ? blocks : (units + 255) / 256;
+        const dim3 grid((unsigned)(long_runs || wanted < (1 << 20) ? wanted : (1 << 20)));
         hipStream_t s = static_cast<hipStream_t>(stream);
-        if (unit == 16) hipLaunchKernelGGL(reorder_kernel<u32x4>, grid, dim3(256), 0, s, a);
-        else if (unit == 4) hipLaunchKernelGGL(reorder_kernel<uint32_t>, grid, dim3(256), 0, s, a);
-        else hipLaunchKernelGGL(reorder_kernel<uint8_t>, grid, dim3(256), 0, s, a);
+        if (long_runs) {
+            if (unit == 16) hipLaunchKernelGGL(reorder_runs_kernel<u32x4>, grid, dim3(256), 0, s, a);
+            else if (unit == 4) hipLaunchKernelGGL(reorder_runs_kernel<uint32_t>, grid, dim3(256), 0, s, a);
+            else hipLaunchKernelGGL(reorder_runs_kernel<uint8_t>, grid, dim3(256), 0, s, a);
+        } else {
+            if (unit == 16) hipLaunchKernelGGL(reorder_units_kernel<u32x4>, grid, dim3(256), 0, s, a);
+            else if (unit == 4) hipLaunchKernelGGL(reorder_units_kernel<uint32_t>, grid, dim3(256), 0, s, a);
+            else hipLaunchKernelGGL(reorder_units_kernel<uint8_t>, grid, dim3(256), 0, s, a);
+        }
         if (hipGetLastError() != hipSuccess) return FREEZE_EHIP;
     }
     return FREEZE_OK;
