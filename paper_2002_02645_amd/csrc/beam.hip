@@ -45,10 +45,22 @@ struct BestList {
     __device__ __forceinline__ void clear(V lowest) { v = lowest; i = (I)-1; }   // (unsigned: the largest index)
     __device__ __forceinline__ bool before(V cv, I ci) const { return v > cv || (v == cv && i < ci); }
 };
-__device__ __forceinline__ float shfl_any(float x, int l) { return __shfl(x, l, 64); }
-__device__ __forceinline__ double shfl_any(double x, int l) { return __shfl(x, l, 64); }
-__device__ __forceinline__ uint32_t shfl_any(uint32_t x, int l) { return (uint32_t)__shfl((int)x, l, 64); }
-__device__ __forceinline__ uint64_t shfl_any(uint64_t x, int l) { return (uint64_t)__shfl((unsigned long long)x, l, 64); }
+// the value of lane l, which is the same in all lanes
+__device__ __forceinline__ uint32_t of_lane(uint32_t x, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); }
+__device__ __forceinline__ float of_lane(float x, int l) { return __uint_as_float(of_lane(__float_as_uint(x), l)); }
+__device__ __forceinline__ uint64_t of_lane(uint64_t x, int l)
+{
+    return (uint64_t)of_lane((uint32_t)x, l) | ((uint64_t)of_lane((uint32_t)(x >> 32), l) << 32);
+}
+__device__ __forceinline__ double of_lane(double x, int l) { return __longlong_as_double((long long)of_lane((uint64_t)__double_as_longlong(x), l)); }
+// the value of the lane before (lane 0: its own)
+__device__ __forceinline__ uint32_t of_previous(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x138, 0xf, 0xf, false); }   // wave_shr:1
+__device__ __forceinline__ float of_previous(float x) { return __uint_as_float(of_previous(__float_as_uint(x))); }
+__device__ __forceinline__ uint64_t of_previous(uint64_t x)
+{
+    return (uint64_t)of_previous((uint32_t)x) | ((uint64_t)of_previous((uint32_t)(x >> 32)) << 32);
+}
+__device__ __forceinline__ double of_previous(double x) { return __longlong_as_double((long long)of_previous((uint64_t)__double_as_longlong(x))); }
 
 // inserts (cv, ci), the same in all lanes; false where k others are before it
 template <typename V, typename I>
@@ -56,8 +68,8 @@ __device__ __forceinline__ bool insert(BestList<V, I> &list, V cv, I ci, int k, 
 {
     const int pos = __popcll(__ballot(lane < k && list.before(cv, ci)));
     if (pos >= k) return false;
-    const V pv = shfl_any(list.v, lane > 0 ? lane - 1 : 0);
-    const I pi = shfl_any(list.i, lane > 0 ? lane - 1 : 0);
+    const V pv = of_previous(list.v);
+    const I pi = of_previous(list.i);
     if (lane > pos) {
         list.v = pv;
         list.i = pi;
@@ -66,6 +78,20 @@ __device__ __forceinline__ bool insert(BestList<V, I> &list, V cv, I ci, int k, 
         list.i = ci;
     }
     return true;
+}
+
+// A value that k lanes reach at least, cut off to the bits from LOW on of its place in order: near the k-th largest, and not above it.
+template <int LOW>
+__device__ __forceinline__ float kth_reached(float x, int k)
+{
+    const uint32_t u = ordered_bits(x);
+    uint32_t t = 0;
+#pragma unroll
+    for (int bit = 31; bit >= LOW; --bit) {
+        const uint32_t more = t | (1u << bit);
+        if (__popcll(__ballot(u >= more)) >= k) t = more;   // uniform
+    }
+    return from_ordered_bits(t);
 }
 
 template <typename T>
@@ -155,8 +181,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
         if (lanes == 0) continue;   // uniform
         if (__popcll(lanes) >= p.k) {
             // at least k values of this batch reach the k-th largest of the lanes' largest
-            const uint32_t sorted = wave_sort32(~ordered_bits(most), lane);
-            floor_v = __builtin_fmaxf(floor_v, from_ordered_bits(~(uint32_t)__shfl((int)sorted, p.k - 1, 64)));
+            floor_v = __builtin_fmaxf(floor_v, kth_reached<16>(most, p.k));
         }
 #pragma unroll
         for (int b = 0; b < E / B; ++b) {
@@ -168,10 +193,10 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
                 while (who) {
                     const int l = __ffsll((unsigned long long)who) - 1;
                     who &= who - 1;
-                    const float cv = __shfl(v, l, 64);
+                    const float cv = of_lane(v, l);
                     const int64_t at = (base + (e / V) * 64 + l) * V - shift + e % V;
                     if (cv >= floor_v && insert(list, cv, (uint32_t)at, p.k, lane))
-                        floor_v = __builtin_fmaxf(floor_v, __shfl(list.v, p.k - 1, 64));
+                        floor_v = __builtin_fmaxf(floor_v, of_lane(list.v, p.k - 1));
                 }
             }
         }
@@ -196,20 +221,22 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 
 // One workgroup a group: the rows' offsets score - log sum exp, then the k best of the pieces' lists.  What reaches the k-th largest of some
 // wave's lanes' largest is gathered, as a rule a few more than k, and every one of them counts those before it; where
-// too many reach it (or there are more than kMeetHeld a thread), the waves keep lists as the pieces did.
-constexpr int kMeetThreads = 256, kMeetHeld = 16, kMeetGathered = 512;
+// too many reach it (or there are more than kMeetHeld), the waves keep lists as the pieces did.
+constexpr int kMeetThreads = 256, kMeetHeld = 4096, kMeetGathered = 512;
 __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
 {
     __shared__ double off[FREEZE_MAX_BEAMS];     // -inf: nothing in the row
     __shared__ uint8_t ended[FREEZE_MAX_BEAMS];
     __shared__ double list_v[kMeetGathered];
     __shared__ uint64_t list_i[kMeetGathered];
+    __shared__ double held[kMeetHeld];
     __shared__ float floors[kMeetThreads / 64];
     __shared__ int gathered;
     static_assert(kMeetThreads / 64 * FREEZE_MAX_K <= kMeetGathered, "the waves' lists");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t row0 = (int64_t)blockIdx.x * p.beams;
     if (tid == 0) gathered = 0;
+    const int per_row = p.parts * p.k, all = p.beams * per_row;
     {
         // a row for as many threads as there are for each: a power of two of them, within a wave
         int per = 64;
@@ -236,7 +263,6 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
         }
     }
     __syncthreads();
-    const int per_row = p.parts * p.k, all = p.beams * per_row;
     auto put = [&](int64_t place, double v, uint64_t i) {
         const bool some = v > -__builtin_inf();
         const int32_t token = some ? (int32_t)(uint32_t)i : (p.end > 0 ? p.end : 0);
@@ -246,51 +272,43 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
         p.out_parents[at] = (int32_t)(row0 + (some ? (int64_t)(i >> 32) : 0));
         if (p.out_finished) p.out_finished[at] = token == p.end;
     };
-    // candidate q of the group: value (-inf: none) and place (row, token)
-    auto candidate = [&](int q, uint64_t &i) {
-        double c = -__builtin_inf();
-        if (q < all) {
-            const int j = q / per_row;
-            const float v = p.best_v[row0 * per_row + q];   // (not written where the row is empty or has ended)
-            const int32_t t = p.best_i[row0 * per_row + q];
-            const double o = off[j];
-            if (ended[j]) {
-                i = ((uint64_t)j << 32) | (uint32_t)p.end;
-                if (q == j * per_row) c = o;
-            } else if (o > -__builtin_inf() && v >= kLowest) {
-                i = ((uint64_t)j << 32) | (uint32_t)t;
-                c = o + (double)v;
-            }
-        }
-        return c;
+    // candidate q of the group: what it is worth (-inf: none) and its place (row, token).  (Where a row is empty or has ended, no list was written.)
+    auto worth = [&](int q) {
+        const int j = q / per_row;
+        const float v = p.best_v[row0 * per_row + q];
+        const double o = off[j];
+        if (ended[j]) return q == j * per_row ? o : -__builtin_inf();
+        return o > -__builtin_inf() && v >= kLowest ? o + (double)v : -__builtin_inf();
     };
-    if (all <= kMeetThreads * kMeetHeld) {
-        double c[kMeetHeld], most = -__builtin_inf();
-        uint64_t ci[kMeetHeld];
-        const int rounds = (all + kMeetThreads - 1) / kMeetThreads;   // uniform
-#pragma unroll
-        for (int e = 0; e < kMeetHeld; ++e) {
-            c[e] = -__builtin_inf();
-            ci[e] = 0;
-            if (e < rounds) c[e] = candidate(e * kMeetThreads + tid, ci[e]);
-            most = c[e] > most ? c[e] : most;
+    auto place = [&](int q) {
+        const int j = q / per_row;
+        return ((uint64_t)j << 32) | (uint32_t)(ended[j] ? p.end : p.best_i[row0 * per_row + q]);
+    };
+    if (all <= kMeetHeld) {   // uniform
+        double most = -__builtin_inf();
+#pragma unroll 1
+        for (int q = tid; q < all; q += kMeetThreads) {
+            const double c = worth(q);
+            held[q] = c;
+            most = c > most ? c : most;
         }
         // (in fp32, one step down: what it stands for is not more than the k-th largest)
-        const uint32_t sorted = wave_sort32(~ordered_bits((float)most), lane);
-        const uint32_t kth = ~(uint32_t)__shfl((int)sorted, p.k - 1, 64);
-        if (lane == 0) floors[wave] = from_ordered_bits(kth);
+        const float kth = kth_reached<6>((float)most, p.k);
+        if (lane == 0) floors[wave] = kth;
         __syncthreads();
         const float f = __builtin_fmaxf(__builtin_fmaxf(floors[0], floors[1]), __builtin_fmaxf(floors[2], floors[3]));
         const double floor_v = f > kLowest ? (double)from_ordered_bits(ordered_bits(f) - 1) : -1.7976931348623157e308;
-#pragma unroll
-        for (int e = 0; e < kMeetHeld; ++e)
-            if (c[e] >= floor_v) {
+#pragma unroll 1
+        for (int q = tid; q < all; q += kMeetThreads) {
+            const double c = held[q];
+            if (c >= floor_v) {
                 const int at = atomicAdd(&gathered, 1);   // (their order does not matter)
                 if (at < kMeetGathered) {
-                    list_v[at] = c[e];
-                    list_i[at] = ci[e];
+                    list_v[at] = c;
+                    list_i[at] = place(q);
                 }
             }
+        }
         __syncthreads();
         const int n = gathered;
         if (n <= kMeetGathered) {   // uniform
@@ -298,7 +316,8 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
                 const double v = list_v[q];
                 const uint64_t i = list_i[q];
                 int before = 0;
-                for (int o = 0; o < n; ++o) before += list_v[o] > v || (list_v[o] == v && list_i[o] < i);
+#pragma unroll 4
+                for (int o = 0; o < n; ++o) before += (int)(list_v[o] > v) | ((int)(list_v[o] == v) & (int)(list_i[o] < i));
                 if (before < p.k) put(before, v, i);
             }
             for (int q = n + tid; q < p.k; q += kMeetThreads) put(q, -__builtin_inf(), 0);
@@ -310,15 +329,16 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
     list.clear(-__builtin_inf());
     double floor_v = -1.7976931348623157e308;
     for (int base = wave * 64; base < all; base += kMeetThreads) {
-        uint64_t ci = 0;
-        const double c = candidate(base + lane, ci);
+        const int q = base + lane;
+        const double c = q < all ? worth(q) : -__builtin_inf();
+        const uint64_t ci = c >= floor_v ? place(q) : 0;
         uint64_t who = __ballot(c >= floor_v);
         while (who) {
             const int l = __ffsll((unsigned long long)who) - 1;
             who &= who - 1;
-            const double cv = shfl_any(c, l);
-            if (cv >= floor_v && insert(list, cv, shfl_any(ci, l), p.k, lane)) {
-                const double f = shfl_any(list.v, p.k - 1);
+            const double cv = of_lane(c, l);
+            if (cv >= floor_v && insert(list, cv, of_lane(ci, l), p.k, lane)) {
+                const double f = of_lane(list.v, p.k - 1);
                 floor_v = f > floor_v ? f : floor_v;
             }
         }
@@ -337,7 +357,7 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
     if (lane < p.k) put(lane, list.v, list.i);
 }
 
-// How a row is cut: pieces of whole batches, as many as fill the chip with waves (8 a CU) and no more.
+// How a row is cut: pieces of whole batches, as many as fill the chip with waves (16 a CU) and no more.
 struct BeamPlan {
     int64_t groups_per_part;
     int parts;
@@ -346,7 +366,7 @@ BeamPlan beam_plan(int64_t rows, int64_t vocab, int size)
 {
     const int64_t v = 16 / size, batch = 64 * kBeamLoads;
     const int64_t batches = ((vocab + v - 1 + v - 1) / v + batch - 1) / batch;   // (a misaligned row's groups are one more)
-    int64_t parts = (2048 + rows - 1) / rows;
+    int64_t parts = (4096 + rows - 1) / rows;
     parts = parts < 1 ? 1 : (parts > batches ? batches : parts);
     BeamPlan pl;
     const int64_t per = (batches + parts - 1) / parts;
