@@ -363,7 +363,7 @@ size_t freeze_quantised_storage_bytes(int64_t m, int64_t d);
 int freeze_quantised_build(freeze_ctx *ctx, int slot, const void *weights, int weights_dtype,
                            const uint8_t *weight_scales, int64_t m, int64_t d, const float *bias,
                            void *storage, size_t storage_bytes, void *stream);
-size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t b, int x_dtype);
+size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t b, int out_dtype);
 int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dtype, const uint8_t *x_scales,
                              int64_t b, int64_t x_stride, int relu, void *out, int out_dtype, int64_t out_stride,
                              void *workspace, size_t workspace_bytes, void *stream);

@@ -410,8 +410,8 @@ def freeze_quantised_build(ctx, slot: int, weights: torch.Tensor, scales: Option
                                         storage.nbytes, _on(stream)), "freeze_quantised_build")
 
 
-def freeze_quantised_workspace_bytes(ctx, slot: int, b: int, x_dtype: int) -> int:
-    return int(lib().freeze_quantised_workspace_bytes(ctx, slot, b, x_dtype))
+def freeze_quantised_workspace_bytes(ctx, slot: int, b: int, out_dtype: int) -> int:
+    return int(lib().freeze_quantised_workspace_bytes(ctx, slot, b, out_dtype))
 
 
 def freeze_quantised_project(ctx, slot: int, x: torch.Tensor, scales: Optional[torch.Tensor], d: int, relu: bool, out: torch.Tensor,
@@ -723,7 +723,7 @@ class FreezeCache:
         if out is None:
             out = torch.empty((x.shape[0], m), dtype=out_dtype, device=self.device)
         assert out.shape == (x.shape[0], m)
-        nbytes = freeze_quantised_workspace_bytes(self.ctx, slot, x.shape[0], _values_dtype(x))
+        nbytes = freeze_quantised_workspace_bytes(self.ctx, slot, x.shape[0], _values_dtype(out))
         if nbytes == 0:
             raise FreezeError(FREEZE_EINVAL, "freeze_quantised_workspace_bytes")
         freeze_quantised_project(self.ctx, slot, x, scales, d, relu, out, self._workspace(nbytes))

@@ -740,6 +740,13 @@ const LayerCache *get_quantised(const freeze_ctx *ctx, int slot, int *err)
     return *err == FREEZE_OK ? &ctx->layers[slot] : nullptr;
 }
 
+// workspace of a product: its rows in tiles, the sums of cut tiles
+size_t quant_bytes(const QuantPlan &pl, int64_t b, int64_t d)
+{
+    const int64_t rows = quant_tiled_rows(b, pl.bm);
+    return align_up((size_t)(rows * quant_code_stride(d))) + align_up((size_t)(rows * quant_scale_stride(d))) + align_up(pl.part * 4);
+}
+
 QuantRows take_rows(Carver &c, int64_t rows, int64_t d, int tile)
 {
     const int64_t n = quant_tiled_rows(rows, tile);
@@ -1340,21 +1347,13 @@ int freeze_quantised_build(freeze_ctx *ctx, int slot, const void *weights, int w
     return FREEZE_OK;
 }
 
-size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t b, int x_dtype)
+size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t b, int out_dtype)
 {
     int err;
     const LayerCache *P = get_quantised(ctx, slot, &err);
-    if (!P || b < 0 || b > (int64_t)1 << 30 || x_dtype < FREEZE_F32 || x_dtype > FREEZE_E4M3) return 0;
+    if (!P || b < 0 || b > (int64_t)1 << 30 || (out_dtype != FREEZE_F32 && out_dtype != FREEZE_BF16)) return 0;
     if (b < 1) b = 1;
-    // the largest of what the two types of outputs take
-    size_t most = 0;
-    for (int half = 0; half < 2; ++half) {
-        const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), half != 0, ctx->num_cus);
-        const int64_t rows = quant_tiled_rows(b, pl.bm);
-        const size_t bytes = align_up((size_t)(rows * quant_code_stride(P->d))) + align_up((size_t)(rows * quant_scale_stride(P->d))) + align_up(pl.part * 4);
-        most = bytes > most ? bytes : most;
-    }
-    return most;
+    return quant_bytes(plan_quant_product(b, P->n, quant_code_stride(P->d), out_dtype == FREEZE_BF16, ctx->num_cus), b, P->d);
 }
 
 int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dtype, const uint8_t *x_scales, int64_t b, int64_t x_stride,
@@ -1373,9 +1372,9 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
     if (!x || !out || !workspace || given != (x_scales != nullptr) || !aligned(out, out_size) ||
         !aligned(x, given ? 16 : (x_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(x_scales, 4))
         return FREEZE_EINVAL;
-    if (workspace_bytes < freeze_quantised_workspace_bytes(ctx, slot, b, x_dtype) || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
-    hipStream_t s = static_cast<hipStream_t>(stream);
     const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), out_dtype == FREEZE_BF16, ctx->num_cus);
+    if (workspace_bytes < quant_bytes(pl, b, P->d) || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
     Carver ws(workspace);
     const QuantRows rows = take_rows(ws, b, P->d, pl.bm);
     const hipError_t e = given ? launch_tile_codes(static_cast<const uint8_t *>(x), x_scales, b, P->d, rows, s)

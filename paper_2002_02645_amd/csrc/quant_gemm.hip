@@ -67,16 +67,33 @@ __device__ __forceinline__ void store_outputs(const QuantProduct &p, int64_t row
     }
 }
 
-// Tiles in the order in which ranges take them: four tiles of x rows side by side, so that the workgroups of an XCD, which
-// are at neighbouring places of that order, share both operands in its L2.
+// What a workgroup forms: a tile, or the k-steps [ka, kb) of it.  Units are in order of (cut, group of four tiles of x rows, tile of w
+// rows, x tile), and each XCD (block id modulo 8) takes a run of them: its workgroups are in the same k-steps at about the same time and
+// share the rows of both operands in its L2.  (Ranges one after the other along a tile's depth shared nothing: 256 x 8,192 -> 8,192 55 us.)
 constexpr int kTileGroup = 4;
-__device__ __forceinline__ void tile_place(const QuantProduct &p, int64_t tile, int *xt, int *wt)
+struct Unit {
+    int xt, wt, ka, kb;
+    uint32_t slot;   // of the sums: tile * splits + cut
+};
+__device__ __forceinline__ void tile_place(const QuantProduct &p, uint32_t tile, int *xt, int *wt)
 {
-    const int64_t group = tile / (kTileGroup * (int64_t)p.w_tiles);
+    const uint32_t group = tile / (uint32_t)(kTileGroup * p.w_tiles);
     const int first = (int)group * kTileGroup, wide = p.x_tiles - first < kTileGroup ? p.x_tiles - first : kTileGroup;
-    const int r = (int)(tile - group * kTileGroup * p.w_tiles);
-    *xt = first + r % wide;
+    const int r = (int)(tile - group * (uint32_t)(kTileGroup * p.w_tiles));
     *wt = r / wide;
+    *xt = first + r - *wt * wide;
+}
+__device__ __forceinline__ Unit unit_of(const QuantProduct &p)
+{
+    const uint32_t n = gridDim.x, share = n >> 3, more = n & 7, xcd = blockIdx.x & 7, at = blockIdx.x >> 3;
+    const uint32_t id = xcd * share + (xcd < more ? xcd : more) + at;   // the first `more` XCDs have one unit more
+    const uint32_t tiles = (uint32_t)p.x_tiles * (uint32_t)p.w_tiles, cut = id / tiles, tile = id - cut * tiles;
+    Unit u;
+    tile_place(p, tile, &u.xt, &u.wt);
+    u.ka = (int)((int64_t)p.nk * cut / p.splits);
+    u.kb = (int)((int64_t)p.nk * (cut + 1) / p.splits);
+    u.slot = tile * (uint32_t)p.splits + cut;
+    return u;
 }
 
 // LDS-direct loads to a constant distance behind a wave's place (formed in M0 itself: as many places as a stage has loads, kept over
@@ -100,17 +117,16 @@ __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F f)
 // A wave's sums: the matrix instructions take w as their rows, so a lane holds four consecutive outputs (from col on, and 16 j behind)
 // of one x row (row, and 16 i behind).
 template <int XB, int NB, int BM, int BN>
-__device__ __forceinline__ void tile_out(const QuantProduct &p, const f32x4 (&acc)[XB][NB], int64_t range, int64_t tile, bool whole, int row, int col,
+__device__ __forceinline__ void tile_out(const QuantProduct &p, const f32x4 (&acc)[XB][NB], const Unit &u, int row, int col,
                                          int64_t x0, int64_t w0, int x_last)
 {
-    if (whole) {   // uniform
+    if (p.splits == 1) {   // uniform
         each(std::make_integer_sequence<int, XB * NB>{}, [&](auto ij) {
             constexpr int i = decltype(ij)::value / NB, j = decltype(ij)::value % NB;
             if (row + 16 * i <= x_last) store_outputs(p, x0 + row + 16 * i, w0 + col + 16 * j, acc[i][j]);
         });
     } else {
-        const int slot = (int)(range - tile * p.nk / p.len);   // how many ranges before this one touch the tile
-        float *dst = p.part + ((tile * p.slots + slot) * BM + row) * BN + col;
+        float *dst = p.part + ((int64_t)u.slot * BM + row) * BN + col;
         each(std::make_integer_sequence<int, XB * NB>{}, [&](auto ij) {
             constexpr int i = decltype(ij)::value / NB, j = decltype(ij)::value % NB;
             *reinterpret_cast<f32x4 *>(dst + i * 16 * BN + j * 16) = acc[i][j];
@@ -135,11 +151,8 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wx = w / WN, wn = w % WN;
     const uint32_t smem_base = (uint32_t)(uintptr_t)(lds_void_ptr)smem;
-    const int nk = p.nk;
-
-    const int64_t range = p.xcd_share ? (int64_t)(blockIdx.x & 7) * p.xcd_share + (blockIdx.x >> 3) : blockIdx.x;
-    const int64_t total = (int64_t)p.x_tiles * p.w_tiles * nk;
-    const int64_t g_begin = range * p.len, g_end = g_begin + p.len < total ? g_begin + p.len : total;
+    const Unit u = unit_of(p);
+    const int ka = u.ka, kb = u.kb;
 
     const int g4 = lane >> 4;
     const int rX = wx * XB * 16 + (lane & 15), rW = wn * NB * 16 + (lane & 15);   // + 16 i: leaves the swizzle as it is
@@ -150,269 +163,285 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
     // (of fewer rows than lanes the last row's scales are loaded again)
     const uint32_t off4 = (ls < BN / 64 || BM >= 64 || lane < BM ? lane : BM - 1) * 4;
 
-    for (int64_t g = g_begin; g < g_end;) {
-        const int64_t tile = g / nk;
-        const int ka = (int)(g - tile * nk);
-        const int kb = g_end - tile * nk < nk ? (int)(g_end - tile * nk) : nk;
-        int xt, wt;
-        tile_place(p, tile, &xt, &wt);
-        const int64_t x0 = (int64_t)xt * BM, w0 = (int64_t)wt * BN;
-        const int x_last = (int)(p.b - x0 < BM ? p.b - x0 : BM) - 1;
-        const int64_t wbig = w0 / kQuantTile * kQuantTile, win = w0 - wbig;   // the tile of the weights, the place within it
-        const uint64_t gX = uniform_u64((uint64_t)(uintptr_t)(p.x + x0 * p.d_pad) + lx * 1024);
-        const uint64_t gW = uniform_u64((uint64_t)(uintptr_t)(p.w + wbig * p.d_pad + win * 128) + w * 1024);
-        const uint64_t gS = uniform_u64((uint64_t)(uintptr_t)(ls < BN / 64 ? p.ws + wbig * p.sd + win * 4 + ls * 256 : p.xs + x0 * p.sd + (ls - BN / 64) * 256));
-        const uint32_t s_rows = ls < BN / 64 ? kQuantTile * 4 : BM * 4;
-        auto issue = [&](int buf, int kt) {
-            const uint32_t to = smem_base + buf * kStage;
-            const uint64_t kw = gW + (uint64_t)kt * (kQuantTile * 128), kx = gX + (uint64_t)kt * (BM * 128);
-            each(std::make_integer_sequence<int, IW>{}, [&](auto i) {
-                load16_to_lds_at<decltype(i)::value * 8192>(kw + decltype(i)::value * 8192, off16, to + w * 1024);
-            });
-            each(std::make_integer_sequence<int, IX>{}, [&](auto i) {
-                load16_to_lds_at<kX + decltype(i)::value * 8192>(kx + decltype(i)::value * 8192, off16, to + lx * 1024);
-            });
-            load4_to_lds_at<kS>(gS + (uint64_t)(kt >> 2) * s_rows, off4, to + ls * 256);
-        };
+    const int64_t x0 = (int64_t)u.xt * BM, w0 = (int64_t)u.wt * BN;
+    const int x_last = (int)(p.b - x0 < BM ? p.b - x0 : BM) - 1;
+    const int64_t wbig = w0 / kQuantTile * kQuantTile, win = w0 - wbig;   // the tile of the weights, the place within it
+    const uint64_t gX = uniform_u64((uint64_t)(uintptr_t)(p.x + x0 * p.d_pad) + lx * 1024);
+    const uint64_t gW = uniform_u64((uint64_t)(uintptr_t)(p.w + wbig * p.d_pad + win * 128) + w * 1024);
+    const uint64_t gS = uniform_u64((uint64_t)(uintptr_t)(ls < BN / 64 ? p.ws + wbig * p.sd + win * 4 + ls * 256 : p.xs + x0 * p.sd + (ls - BN / 64) * 256));
+    const uint32_t s_rows = ls < BN / 64 ? kQuantTile * 4 : BM * 4;
+    auto issue = [&](int buf, int kt) {
+        const uint32_t to = smem_base + buf * kStage;
+        const uint64_t kw = gW + (uint64_t)kt * (kQuantTile * 128), kx = gX + (uint64_t)kt * (BM * 128);
+        each(std::make_integer_sequence<int, IW>{}, [&](auto i) {
+            load16_to_lds_at<decltype(i)::value * 8192>(kw + decltype(i)::value * 8192, off16, to + w * 1024);
+        });
+        each(std::make_integer_sequence<int, IX>{}, [&](auto i) {
+            load16_to_lds_at<kX + decltype(i)::value * 8192>(kx + decltype(i)::value * 8192, off16, to + lx * 1024);
+        });
+        load4_to_lds_at<kS>(gS + (uint64_t)(kt >> 2) * s_rows, off4, to + ls * 256);
+    };
 
-        f32x4 acc[XB][NB];
+    f32x4 acc[XB][NB];
 #pragma unroll
-        for (int i = 0; i < XB; ++i)
+    for (int i = 0; i < XB; ++i)
 #pragma unroll
-            for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        const int klast = kb - 1;
-        __syncthreads();   // the LDS is free (a range's previous tile)
+    const int klast = kb - 1;
 #pragma unroll
-        for (int s = 0; s < NS - 1; ++s) issue(s, ka + s < klast ? ka + s : klast);
-        int st = 0;
-        for (int kt = ka; kt < kb; ++kt) {
-            wait_global_loads_le<(NS - 2) * NL>();
-            __syncthreads();   // this step's stage is there, the one before has been read
-            const int fill = st == 0 ? NS - 1 : st - 1;
-            issue(fill, kt + NS - 1 < klast ? kt + NS - 1 : klast);
-            const unsigned char *stage = smem + st * kStage;
-            const u32x4 *tw = reinterpret_cast<const u32x4 *>(stage), *tx = reinterpret_cast<const u32x4 *>(stage + kX);
-            const uint32_t *sw = reinterpret_cast<const uint32_t *>(stage + kS), *sx = sw + BN;
-            const int sh = 8 * (kt & 3);
-            float fx[XB], fw[NB];
+    for (int s = 0; s < NS - 1; ++s) issue(s, ka + s < klast ? ka + s : klast);
+    int st = 0;
+    for (int kt = ka; kt < kb; ++kt) {
+        wait_global_loads_le<(NS - 2) * NL>();
+        __syncthreads();   // this step's stage is there, the one before has been read
+        const int fill = st == 0 ? NS - 1 : st - 1;
+        issue(fill, kt + NS - 1 < klast ? kt + NS - 1 : klast);
+        const unsigned char *stage = smem + st * kStage;
+        const u32x4 *tw = reinterpret_cast<const u32x4 *>(stage), *tx = reinterpret_cast<const u32x4 *>(stage + kX);
+        const uint32_t *sw = reinterpret_cast<const uint32_t *>(stage + kS), *sx = sw + BN;
+        const int sh = 8 * (kt & 3);
+        float fx[XB], fw[NB];
 #pragma unroll
-            for (int i = 0; i < XB; ++i) fx[i] = __uint_as_float((sx[rX + 16 * i] >> sh & 255u) << 23);
+        for (int i = 0; i < XB; ++i) fx[i] = __uint_as_float((sx[rX + 16 * i] >> sh & 255u) << 23);
 #pragma unroll
-            for (int j = 0; j < NB; ++j) fw[j] = __uint_as_float((sw[rW + 16 * j] >> sh & 255u) << 23);
+        for (int j = 0; j < NB; ++j) fw[j] = __uint_as_float((sw[rW + 16 * j] >> sh & 255u) << 23);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bf16x8 xa[2][XB];
+        for (int h = 0; h < 2; ++h) {
+            bf16x8 xa[2][XB];
 #pragma unroll
-                for (int i = 0; i < XB; ++i) {
-                    const u32x4 a = tx[(rX + 16 * i) * 8 + ((2 * g4 + h) ^ swX)];
-                    xa[0][i] = widen8(a[0], a[1], fx[i]);
-                    xa[1][i] = widen8(a[2], a[3], fx[i]);
-                }
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    const u32x4 a = tw[(rW + 16 * j) * 8 + ((2 * g4 + h) ^ swW)];
-                    const bf16x8 w0v = widen8(a[0], a[1], fw[j]), w1v = widen8(a[2], a[3], fw[j]);
-#pragma unroll
-                    for (int i = 0; i < XB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0v, xa[0][i], acc[i][j], 0, 0, 0);
-#pragma unroll
-                    for (int i = 0; i < XB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1v, xa[1][i], acc[i][j], 0, 0, 0);
-                }
+            for (int i = 0; i < XB; ++i) {
+                const u32x4 a = tx[(rX + 16 * i) * 8 + ((2 * g4 + h) ^ swX)];
+                xa[0][i] = widen8(a[0], a[1], fx[i]);
+                xa[1][i] = widen8(a[2], a[3], fx[i]);
             }
-            st = st + 1 == NS ? 0 : st + 1;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                const u32x4 a = tw[(rW + 16 * j) * 8 + ((2 * g4 + h) ^ swW)];
+                const bf16x8 w0v = widen8(a[0], a[1], fw[j]), w1v = widen8(a[2], a[3], fw[j]);
+#pragma unroll
+                for (int i = 0; i < XB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0v, xa[0][i], acc[i][j], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < XB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1v, xa[1][i], acc[i][j], 0, 0, 0);
+            }
         }
-        wait_global_loads_le<0>();   // the refills past the last k-step
-        tile_out<XB, NB, BM, BN>(p, acc, range, tile, ka == 0 && kb == nk, wx * XB * 16 + (lane & 15), wn * NB * 16 + g4 * 4, x0, w0, x_last);
-        g = tile * nk + kb;
+        st = st + 1 == NS ? 0 : st + 1;
     }
+    wait_global_loads_le<0>();   // the refills past the last k-step
+    tile_out<XB, NB, BM, BN>(p, acc, u, wx * XB * 16 + (lane & 15), wn * NB * 16 + g4 * 4, x0, w0, x_last);
 }
 
-// Tiles of 256 x 256 for the batches that the matrix pipes bound.  A wave forms 16 XB x 128 outputs: 8-bit form XB = 8, four waves, one a
-// SIMD (the sums take half of its registers; a k-step reads 128 KiB of fragments out of LDS, with eight waves it would be 192 in
-// half the time of the bf16 form); bf16 form XB = 4, eight waves, so that one of a SIMD's widens codes while the other's matrix instructions run.  A
-// step goes through its blocks of 16 w rows, in the bf16 form twice (64 codes each); fragments are read kAhead blocks ahead.  The step's
-// barrier comes before its last kAhead blocks of matrix instructions, which need nothing newer: it publishes the
-// next step's stage and frees this one, which is refilled from there on.
+// Larger batches, which the matrix pipes bound: tiles of 32 XB x rows by 256 w rows, eight waves of 16 XB x 64 outputs, two stages.  A wave
+// keeps its four blocks of w rows' fragments (16 rows each) for a step (8-bit form) or half a step (bf16 form, 64 codes) and goes through
+// its XB blocks of x rows, a group of matrix instructions each; their fragments are read kAhead groups ahead.  The step's barrier comes
+// before its last kAhead groups, which need nothing newer: it publishes the next step's stage and frees this one, which is refilled from there on.
+// (Four waves of 128 x 128 outputs read a third less out of LDS, but their sums fill a register file and the compiler moves them about: 290 us for
+// 4,096 x 8,192 -> 8,192 in the 8-bit form, 236 so.)
 template <bool F8, int XB>
-__global__ __launch_bounds__(2048 / XB, 8 / XB) void quant_tile_kernel(QuantProduct p)
+__global__ __launch_bounds__(512, 2) void quant_tile_kernel(QuantProduct p)
 {
     using frag = std::conditional_t<F8, i32x8, u32x4>;
-    constexpr int BM = 256, BN = 256, NB = 8, kWaves = 32 / XB;
-    static_assert(BM == kQuantTile && BN == kQuantTile, "a stage is a run of memory");
-    constexpr int kX = BN * 128, kS = kX + BM * 128, kStage = kS + (BN + BM) * 4;
-    constexpr int kHalves = F8 ? 1 : 2, kAhead = 2, kRing = 4;
-    constexpr int NC = 32 / kWaves, NS = 8 / kWaves, NL = 2 * NC + NS;   // load instructions of a wave and step: codes of an operand, scales, all
+    constexpr int BM = 32 * XB, BN = 256, NB = 4;
+    static_assert(BN == kQuantTile, "a stage of the weights is a run of memory");
+    constexpr int kX = BN * 128, kS = kX + BM * 128, kStage = kS + (BN + (BM + 63) / 64 * 64) * 4;
+    constexpr int kHalves = F8 ? 1 : 2, kGroups = kHalves * XB, kAhead = F8 ? 2 : 3;
+    constexpr int kRing = kGroups % 4 == 0 ? 4 : (kGroups % 3 == 0 && F8 ? 3 : (kGroups % 5 == 0 ? 5 : 6));   // fragments ahead, in step with the groups
+    constexpr int IW = BN / 64, LX = BM / 8, IX = (LX + 7) / 8, LS = BN / 64 + (BM + 63) / 64, NL = IW + IX + 1;   // load instructions: see above
     constexpr int kPerGroup = (NL + kAhead - 1) / kAhead;
-    static_assert(2 * kStage <= 163840 && NB % kRing == 0, "");
+    static_assert(2 * kStage <= 163840 && kGroups % kRing == 0 && kRing > kAhead && LS <= 8, "");
     __shared__ __attribute__((aligned(16))) unsigned char smem[2 * kStage];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wx = w >> 1, wn = w & 1;
+    const int wx = w >> 2, wn = w & 3;
     const uint32_t smem_base = (uint32_t)(uintptr_t)(lds_void_ptr)smem;
-    const int nk = p.nk;
-
-    const int64_t range = p.xcd_share ? (int64_t)(blockIdx.x & 7) * p.xcd_share + (blockIdx.x >> 3) : blockIdx.x;
-    const int64_t total = (int64_t)p.x_tiles * p.w_tiles * nk;
-    const int64_t g_begin = range * p.len, g_end = g_begin + p.len < total ? g_begin + p.len : total;
+    const Unit u = unit_of(p);
+    const int ka = u.ka, kb = u.kb;
 
     const int g4 = lane >> 4;
-    const int rX = wx * 16 * XB + (lane & 15), rW = wn * 128 + (lane & 15);   // + 16 i: leaves the swizzle as it is
+    const int rX = wx * 16 * XB + (lane & 15), rW = wn * 64 + (lane & 15);   // + 16 i: leaves the swizzle as it is
     const int swX = row128_swizzle(rX), swW = row128_swizzle(rW);
-    const uint32_t off16 = lane * 16, off4 = lane * 4;
-    const uint32_t lds16 = smem_base + w * 1024, lds4 = smem_base + w * 256;
+    const uint32_t off16 = lane * 16;
+    const int lx_last = (IX - 1) * 8 + w < LX ? (IX - 1) * 8 + w : LX - 1, ls = w < LS ? w : LS - 1;   // (surplus waves repeat a load)
+    // (of fewer rows than lanes the last row's scales are loaded again)
+    const int x_scales = BM - (ls - BN / 64) * 64;
+    const uint32_t off4 = (ls < BN / 64 || lane < x_scales ? lane : x_scales - 1) * 4;
+    const uint32_t lds16 = smem_base + w * 1024;
 
-    for (int64_t g = g_begin; g < g_end;) {
-        const int64_t tile = g / nk;
-        const int ka = (int)(g - tile * nk);
-        const int kb = g_end - tile * nk < nk ? (int)(g_end - tile * nk) : nk;
-        int xt, wt;
-        tile_place(p, tile, &xt, &wt);
-        const int64_t x0 = (int64_t)xt * BM, w0 = (int64_t)wt * BN;
-        const int x_last = (int)(p.b - x0 < BM ? p.b - x0 : BM) - 1;
-        const uint64_t gX = uniform_u64((uint64_t)(uintptr_t)(p.x + x0 * p.d_pad) + w * 1024), gW = uniform_u64((uint64_t)(uintptr_t)(p.w + w0 * p.d_pad) + w * 1024);
-        // scales: four waves bring both operands', or four each one's
-        const bool s_of_w = NS == 2 || w < 4;
-        const uint64_t gS = uniform_u64((uint64_t)(uintptr_t)(s_of_w ? p.ws + w0 * p.sd : p.xs + x0 * p.sd) + (w & 3) * 256);
-        const uint64_t gS2 = uniform_u64((uint64_t)(uintptr_t)(p.xs + x0 * p.sd) + (w & 3) * 256);
-        // load l of k-step kt's stage
-        auto issue = [&](int buf, int kt, auto l_) {
-            constexpr int l = decltype(l_)::value;
-            const uint32_t st = buf * kStage;
-            const uint64_t k = (uint64_t)kt * 32768, q = (uint64_t)(kt >> 2) * 1024;
-            if constexpr (l < NC) load16_to_lds_at<l * kWaves * 1024>(gW + k + l * kWaves * 1024, off16, lds16 + st);
-            else if constexpr (l < 2 * NC) load16_to_lds_at<kX + (l - NC) * kWaves * 1024>(gX + k + (l - NC) * kWaves * 1024, off16, lds16 + st);
-            else if constexpr (l == 2 * NC) load4_to_lds_at<kS>(gS + q, off4, lds4 + st);   // (eight waves: the second four's lie behind the first's)
-            else if constexpr (l < NL) load4_to_lds_at<kS + BN * 4>(gS2 + q, off4, lds4 + st);
-        };
+    const int64_t x0 = (int64_t)u.xt * BM, w0 = (int64_t)u.wt * BN;
+    const int x_last = (int)(p.b - x0 < BM ? p.b - x0 : BM) - 1;
+    const uint64_t gX = uniform_u64((uint64_t)(uintptr_t)(p.x + x0 * p.d_pad)), gW = uniform_u64((uint64_t)(uintptr_t)(p.w + w0 * p.d_pad) + w * 1024);
+    const uint64_t gS = uniform_u64((uint64_t)(uintptr_t)(ls < BN / 64 ? p.ws + w0 * p.sd + ls * 256 : p.xs + x0 * p.sd + (ls - BN / 64) * 256));
+    const uint32_t s_rows = ls < BN / 64 ? BN * 4 : BM * 4;
+    // load l of k-step kt's stage
+    auto issue = [&](int buf, int kt, auto l_) {
+        constexpr int l = decltype(l_)::value;
+        const uint32_t st = buf * kStage;
+        if constexpr (l < IW) load16_to_lds_at<l * 8192>(gW + (uint64_t)kt * (BN * 128) + l * 8192, off16, lds16 + st);
+        else if constexpr (l < IW + IX - 1) load16_to_lds_at<kX + (l - IW) * 8192>(gX + (uint64_t)kt * (BM * 128) + (l - IW) * 8192 + w * 1024, off16, lds16 + st);
+        else if constexpr (l == IW + IX - 1) load16_to_lds_at<kX>(gX + (uint64_t)kt * (BM * 128) + lx_last * 1024, off16, smem_base + lx_last * 1024 + st);
+        else if constexpr (l == NL - 1) load4_to_lds_at<kS>(gS + (uint64_t)(kt >> 2) * s_rows, off4, smem_base + ls * 256 + st);
+    };
 
-        f32x4 acc[XB][NB];
+    f32x4 acc[XB][NB];
 #pragma unroll
-        for (int i = 0; i < XB; ++i)
+    for (int i = 0; i < XB; ++i)
 #pragma unroll
-            for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        frag wr[kRing];            // fragments of w ahead, with the scale bytes of their rows
-        uint32_t ew[kRing];
-        frag xr[XB];               // of x: 8-bit form, this step's; bf16 form, the next 64 codes
-        bf16x8 xa[F8 ? 1 : XB][2];
-        uint32_t ex[XB];
-        auto read = [&](frag &to, const unsigned char *base, int row, int sw, int h) {
-            const u32x4 *t = reinterpret_cast<const u32x4 *>(base) + row * 8;
-            if constexpr (F8) {
-                const u32x4 a = t[(2 * g4) ^ sw], b = t[(2 * g4 + 1) ^ sw];
-                to = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
-            } else {
-                to = t[(2 * g4 + h) ^ sw];
-            }
-        };
-        auto read_w = [&](int set, int buf, int j, int h) {
-            read(wr[set], smem + buf * kStage, rW + 16 * j, swW, h);
-            ew[set] = *reinterpret_cast<const uint32_t *>(smem + buf * kStage + kS + (rW + 16 * j) * 4);
-        };
-        auto read_x = [&](int buf, int i, int h) { read(xr[i], smem + buf * kStage + kX, rX + 16 * i, swX, h); };
-        auto read_xs = [&](int buf, int i) { ex[i] = *reinterpret_cast<const uint32_t *>(smem + buf * kStage + kS + (BN + rX + 16 * i) * 4); };
-
-        const int klast = kb - 1;
-        auto at_most = [&](int kt) { return kt < klast ? kt : klast; };
-        __syncthreads();   // the LDS is free (a range's previous tile)
-        each(std::make_integer_sequence<int, NL>{}, [&](auto l) { issue(0, ka, l); });
-        each(std::make_integer_sequence<int, NL>{}, [&](auto l) { issue(1, at_most(ka + 1), l); });
-        wait_global_loads_le<NL>();
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < XB; ++i) {
-            read_x(0, i, 0);
-            read_xs(0, i);
+    frag xr[kRing], wr[NB];    // of x, ahead; of w: 8-bit form, this step's; bf16 form, codes yet to be widened
+    uint32_t ex[kRing], ew[NB];   // with the scale bytes of their rows
+    auto read = [&](frag &to, const unsigned char *base, int row, int sw, int h) {
+        const u32x4 *t = reinterpret_cast<const u32x4 *>(base) + row * 8;
+        if constexpr (F8) {
+            const u32x4 a = t[(2 * g4) ^ sw], b = t[(2 * g4 + 1) ^ sw];
+            to = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+        } else {
+            to = t[(2 * g4 + h) ^ sw];
         }
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) read_w(j, 0, j, 0);
-        int st = 0;
+    };
+    auto read_x = [&](int set, int buf, int i, int h) {
+        read(xr[set], smem + buf * kStage + kX, rX + 16 * i, swX, h);
+        ex[set] = *reinterpret_cast<const uint32_t *>(smem + buf * kStage + kS + (BN + rX + 16 * i) * 4);
+    };
+    auto read_w = [&](int buf, int j, int h) { read(wr[j], smem + buf * kStage, rW + 16 * j, swW, h); };
+    auto read_ws = [&](int buf, int j) { ew[j] = *reinterpret_cast<const uint32_t *>(smem + buf * kStage + kS + (rW + 16 * j) * 4); };
+
+    const int klast = kb - 1;
+    auto at_most = [&](int kt) { return kt < klast ? kt : klast; };
+    each(std::make_integer_sequence<int, NL>{}, [&](auto l) { issue(0, ka, l); });
+    each(std::make_integer_sequence<int, NL>{}, [&](auto l) { issue(1, at_most(ka + 1), l); });
+    wait_global_loads_le<NL>();
+    __syncthreads();
+    each(std::make_integer_sequence<int, NB>{}, [&](auto j) {
+        read_w(0, decltype(j)::value, 0);
+        read_ws(0, decltype(j)::value);
+    });
+    each(std::make_integer_sequence<int, kAhead>{}, [&](auto i) { read_x(decltype(i)::value, 0, decltype(i)::value, 0); });
+    // group g of a step: the barrier where the reads reach the next step, this group's share of the refill, the reads of the group kAhead further
+    auto group_head = [&](int kt, int st, auto g_) {
+        constexpr int g = decltype(g_)::value, ahead = g + kAhead;
+        if constexpr (g == kGroups - kAhead) {
+            wait_global_loads_le<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __syncthreads();
+        }
+        read_x(ahead % kRing, ahead < kGroups ? st : st ^ 1, ahead % XB, ahead / XB % kHalves);
+        if constexpr (g >= kGroups - kAhead)
+            each(std::make_integer_sequence<int, kPerGroup>{}, [&](auto l) {
+                issue(st, at_most(kt + 2), std::integral_constant<int, (g - kGroups + kAhead) * kPerGroup + decltype(l)::value>{});
+            });
+    };
+    int st = 0;
+    if constexpr (F8) {
         for (int kt = ka; kt < kb; ++kt) {
-            const int nst = st ^ 1, sh = 8 * (kt & 3);
-            if constexpr (F8) {
+            const int sh = 8 * (kt & 3);
 #pragma unroll
-                for (int i = 0; i < XB; ++i) ex[i] >>= sh;
-            }
-            each(std::make_integer_sequence<int, kHalves * NB>{}, [&](auto hj) {
-                constexpr int h = decltype(hj)::value / NB, j = decltype(hj)::value % NB;
-                constexpr bool last_half = h == kHalves - 1;
-                if constexpr (last_half && j == NB - kAhead) {
-                    wait_global_loads_le<0>();
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    __syncthreads();
-                }
-                if constexpr (j + kAhead < NB) read_w((j + kAhead) % kRing, st, j + kAhead, h);
-                else read_w((j + kAhead) % kRing, last_half ? nst : st, j + kAhead - NB, last_half ? 0 : h + 1);
-                if constexpr (!F8 && j >= NB - kAhead) {
-#pragma unroll
-                    for (int i = (j - NB + kAhead) * XB / kAhead; i < (j - NB + kAhead + 1) * XB / kAhead; ++i) {
-                        read_x(last_half ? nst : st, i, last_half ? 0 : h + 1);
-                        if (last_half) read_xs(nst, i);
-                    }
-                }
+            for (int j = 0; j < NB; ++j) ew[j] >>= sh;
+            each(std::make_integer_sequence<int, XB>{}, [&](auto g_) {
+                constexpr int i = decltype(g_)::value;
+                group_head(kt, st, g_);
                 __builtin_amdgcn_sched_barrier(0);
-                if constexpr (last_half && j >= NB - kAhead)
-                    each(std::make_integer_sequence<int, kPerGroup>{}, [&](auto l) {
-                        issue(st, at_most(kt + 2), std::integral_constant<int, (j - NB + kAhead) * kPerGroup + decltype(l)::value>{});
-                    });
-                if constexpr (F8) {
-                    const int e = (int)(ew[j % kRing] >> sh);
-#pragma unroll
-                    for (int i = 0; i < XB; ++i) {
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wr[j % kRing], xr[i], acc[i][j], 0, 0, 0, e, 0, (int)ex[i]);
-                        if constexpr (j == NB - 1) {   // the block's last use: the next step's takes its place
-                            read_x(nst, i, 0);
-                            read_xs(nst, i);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
+                const int e = (int)(ex[i % kRing] >> sh);
+                each(std::make_integer_sequence<int, NB>{}, [&](auto j_) {
+                    constexpr int j = decltype(j_)::value;
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wr[j], xr[i % kRing], acc[i][j], 0, 0, 0, (int)ew[j], 0, e);
+                    if constexpr (i == XB - 1) {   // the block's last use: the next step's takes its place
+                        read_w(st ^ 1, j, 0);
+                        read_ws(st ^ 1, j);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
-                } else {
-                    const float fw = __uint_as_float((ew[j % kRing] >> sh & 255u) << 23);
-                    const u32x4 a = wr[j % kRing];
-                    const bf16x8 w0v = widen8(a[0], a[1], fw), w1v = widen8(a[2], a[3], fw);
-#pragma unroll
-                    for (int i = 0; i < XB; ++i) {
-                        if constexpr (j == 0) {
-                            const float fx = __uint_as_float((ex[i] >> sh & 255u) << 23);
-                            xa[i][0] = widen8(xr[i][0], xr[i][1], fx);
-                            xa[i][1] = widen8(xr[i][2], xr[i][3], fx);
-                        }
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w0v, xa[i][0], acc[i][j], 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int i = 0; i < XB; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w1v, xa[i][1], acc[i][j], 0, 0, 0);
-                }
+                });
                 __builtin_amdgcn_sched_barrier(0);
             });
-            st = nst;
+            st ^= 1;
         }
-        wait_global_loads_le<0>();   // the refills past the last k-step
-        tile_out<XB, NB, BM, BN>(p, acc, range, tile, ka == 0 && kb == nk, rX, wn * 128 + g4 * 4, x0, w0, x_last);
-        g = tile * nk + kb;
+    } else {
+        // Codes are widened between the matrix instructions of the group before, a word or two behind each: one after the other, the two kinds
+        // hardly overlap, not even those of a SIMD's two waves (measured: 8 matrix and 16 conversion instructions a wave 359 cycles in blocks,
+        // 307 interleaved, 295 without the conversions).
+        u32x4 wa[2][NB][2], xc[2][2];
+        const auto word = [](u32x4 &to, int half, uint32_t codes, uint32_t e) {
+            const u32x2 v = widen(codes, __uint_as_float(e));
+            to[2 * half] = v[0];
+            to[2 * half + 1] = v[1];
+        };
+        const auto scale = [](uint32_t e, int sh) { return (e >> sh & 255u) << 23; };
+        each(std::make_integer_sequence<int, 4 * NB>{}, [&](auto t_) {
+            constexpr int t = decltype(t_)::value;
+            word(wa[0][t / 4][t % 4 / 2], t % 2, wr[t / 4][t % 4], scale(ew[t / 4], 8 * (ka & 3)));
+        });
+        each(std::make_integer_sequence<int, 4>{}, [&](auto t_) {
+            constexpr int t = decltype(t_)::value;
+            word(xc[0][t / 2], t % 2, xr[0][t], scale(ex[0], 8 * (ka & 3)));
+        });
+        for (int kt = ka; kt < kb; ++kt) {
+            const int sh = 8 * (kt & 3), nsh = 8 * ((kt + 1) & 3);
+            each(std::make_integer_sequence<int, kGroups>{}, [&](auto g_) {
+                constexpr int g = decltype(g_)::value, h = g / XB, i = g % XB;
+                group_head(kt, st, g_);
+                // w blocks of the other half: of this step early in its first half, of the next one when its stage is there
+                if constexpr (g < 2) {
+                    read_w(st, 2 * g, 1);
+                    read_w(st, 2 * g + 1, 1);
+                } else if constexpr (g == kGroups - 3 || g == kGroups - 2) {
+                    constexpr int j = 2 * (g - kGroups + 3);
+                    read_w(st ^ 1, j, 0);
+                    read_ws(st ^ 1, j);
+                    read_w(st ^ 1, j + 1, 0);
+                    read_ws(st ^ 1, j + 1);
+                }
+                // ... and those of them that are widened in this group: the first half ends with one a group (of four groups, the last takes two)
+                constexpr int late = XB == 4 ? 1 : XB - 4;
+                constexpr int w_first = h == 0 ? i - late : 2 * (g - kGroups + 2);
+                constexpr int w_count = h == 0 ? (i < late ? 0 : (XB == 4 && i == 3 ? 2 : 1)) : (g >= kGroups - 2 ? 2 : 0);
+                constexpr int words = 4 + 4 * w_count;
+                const uint32_t fx = scale(ex[(g + 1) % kRing], g + 1 < kGroups ? sh : nsh);
+                uint32_t fw[2];
+                each(std::make_integer_sequence<int, w_count>{}, [&](auto n) { fw[decltype(n)::value] = scale(ew[w_first + decltype(n)::value], h == 0 ? sh : nsh); });
+                __builtin_amdgcn_sched_barrier(0);
+                each(std::make_integer_sequence<int, 2 * NB>{}, [&](auto q_) {
+                    constexpr int q = decltype(q_)::value, j = q % NB, half = q / NB;
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[h][j][half]), __builtin_bit_cast(bf16x8, xc[g & 1][half]),
+                                                                        acc[i][j], 0, 0, 0);
+                    each(std::make_integer_sequence<int, words>{}, [&](auto t_) {
+                        constexpr int t = decltype(t_)::value;
+                        if constexpr (t * 2 * NB / words == q) {
+                            if constexpr (t < 4) {
+                                word(xc[(g + 1) & 1][t / 2], t % 2, xr[(g + 1) % kRing][t], fx);
+                            } else {
+                                constexpr int n = t - 4, wj = w_first + n / 4;
+                                word(wa[h ^ 1][wj][n % 4 / 2], n % 2, wr[wj][n % 4], fw[n / 4]);
+                            }
+                        }
+                    });
+                    __builtin_amdgcn_sched_barrier(0);
+                });
+            });
+            st ^= 1;
+        }
     }
+    wait_global_loads_le<0>();   // the refills past the last k-step
+    tile_out<XB, NB, BM, BN>(p, acc, u, rX, wn * 64 + g4 * 4, x0, w0, x_last);
 }
 
-// The outputs of cut tiles: the sums of a tile's slots in order, 256 threads for 1,024 outputs.
+// The outputs of cut tiles: the sums of a tile's cuts in order, 256 threads for 1,024 outputs.
 __global__ __launch_bounds__(256) void quant_sum_kernel(QuantProduct p, int bm, int bn)
 {
-    const int per_tile = bm * bn / 1024;
-    const int64_t tile = blockIdx.x / per_tile;
-    const int64_t first = tile * p.nk / p.len, last = (tile * p.nk + p.nk - 1) / p.len;
-    if (first == last) return;   // uniform: written by its range
+    const uint32_t per_tile = (uint32_t)(bm * bn) / 1024, tile = blockIdx.x / per_tile;
     int xt, wt;
     tile_place(p, tile, &xt, &wt);
-    const int at = (int)(blockIdx.x % per_tile) * 1024 + threadIdx.x * 4, row = at / bn, col = at % bn;
-    if ((int64_t)xt * bm + row >= p.b) return;
-    const float *src = p.part + (tile * p.slots) * bm * bn + at;
-    const int ns = (int)(last - first) + 1;
+    const int at = (int)(blockIdx.x - tile * per_tile) * 1024 + threadIdx.x * 4, row = at / bn, col = at % bn;
+    if ((int64_t)xt * bm + row >= p.b || (int64_t)wt * bn + col >= p.m) return;
+    const int64_t step = (int64_t)bm * bn;
+    const float *src = p.part + (int64_t)tile * p.splits * step + at;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < ns; s += 4) {   // four in flight, and summed before they are added
+    for (int s = 0; s < p.splits; s += 4) {   // four in flight, and summed before they are added
         f32x4 t[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            t[u] = *reinterpret_cast<const f32x4 *>(src + (int64_t)(s + u < ns ? s + u : s) * bm * bn);
-            if (s + u >= ns) t[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < 4; ++e) {
+            t[e] = *reinterpret_cast<const f32x4 *>(src + (s + e < p.splits ? s + e : s) * step);
+            if (s + e >= p.splits) t[e] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
         v += (t[0] + t[1]) + (t[2] + t[3]);
     }
@@ -423,15 +452,20 @@ struct Variant {
     int bm, bn, per_cu;
     float step_us;   // of a k-step of a workgroup, all CUs at work
     void (*kernel)(QuantProduct);
-    int threads;
+    bool narrow;     // the 8-bit form
 };
+constexpr int kNarrowRows = 64;
 const Variant kVariants[] = {
-    {16, 128, 2, 1.2f, quant_gemm_kernel<1, 8, 1, 1, 4>, 512},
-    {32, 128, 2, 1.2f, quant_gemm_kernel<1, 8, 2, 1, 3>, 512},
-    {64, 128, 2, 1.3f, quant_gemm_kernel<1, 8, 4, 1, 3>, 512},
-    {128, 256, 1, 1.5f, quant_gemm_kernel<2, 4, 4, 4, 3>, 512},
-    {256, 256, 1, 2.2f, quant_tile_kernel<false, 4>, 512},
-    {256, 256, 1, 1.2f, quant_tile_kernel<true, 4>, 512},
+    {16, 128, 2, 1.2f, quant_gemm_kernel<1, 8, 1, 1, 4>, false},
+    {32, 128, 2, 1.2f, quant_gemm_kernel<1, 8, 2, 1, 3>, false},
+    {64, 128, 2, 1.3f, quant_gemm_kernel<1, 8, 4, 1, 3>, false},
+    {128, 256, 1, 1.8f, quant_tile_kernel<false, 4>, false},
+    {160, 256, 1, 2.1f, quant_tile_kernel<false, 5>, false},
+    {192, 256, 1, 2.4f, quant_tile_kernel<false, 6>, false},
+    {256, 256, 1, 3.2f, quant_tile_kernel<false, 8>, false},
+    {128, 256, 1, 1.0f, quant_tile_kernel<true, 4>, true},
+    {192, 256, 1, 1.4f, quant_tile_kernel<true, 6>, true},
+    {256, 256, 1, 1.7f, quant_tile_kernel<true, 8>, true},
 };
 
 }  // namespace
@@ -439,40 +473,48 @@ const Variant kVariants[] = {
 QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16, int num_cus)
 {
     QuantPlan pl{};
-    pl.variant = b <= 16 ? 0 : (b <= 32 ? 1 : (b <= 64 ? 2 : (b <= 128 ? 3 : (out_bf16 ? 5 : 4))));
-    const Variant &v = kVariants[pl.variant];
-    pl.bm = v.bm;
-    pl.bn = v.bn;
-    pl.x_tiles = (int)((b + v.bm - 1) / v.bm);
-    pl.w_tiles = (int)((m + v.bn - 1) / v.bn);
     pl.nk = (int)(d_pad / kQuantBlock);
-    const int64_t tiles = (int64_t)pl.x_tiles * pl.w_tiles, total = tiles * pl.nk, wgs = (int64_t)num_cus * v.per_cu;
-    // Whole tiles, or even ranges with the sums of cut tiles through memory (written and read at 4 TB/s, and a launch).
-    const int64_t whole = (tiles + wgs - 1) / wgs * pl.nk;
-    int64_t even = (total + wgs - 1) / wgs;
-    even = even < 4 ? 4 : even;
-    const double join_us = 5.0 + 2.0 * 4.0 * (double)std::min<int64_t>(tiles, wgs) * v.bm * v.bn * (even < pl.nk ? (double)pl.nk / even : 1.0) / 4e6;
-    pl.len = (double)whole * v.step_us <= (double)even * v.step_us + join_us ? pl.nk : even;   // (whole tiles: a workgroup each)
-    pl.wgs = (int)((total + pl.len - 1) / pl.len);
-    if (pl.len % pl.nk != 0) {
-        pl.slots = (int)((pl.nk - 1) / pl.len + 2);
-        pl.part = (size_t)tiles * pl.slots * v.bm * v.bn;
+    double best = 0;
+    for (int i = 0; i < (int)(sizeof kVariants / sizeof kVariants[0]); ++i) {
+        const Variant &v = kVariants[i];
+        // the 8-bit form: bf16 outputs of more than kNarrowRows rows
+        if (v.narrow ? !out_bf16 || b <= kNarrowRows : out_bf16 && b > kNarrowRows) continue;
+        const int64_t xt = (b + v.bm - 1) / v.bm, wt = (m + v.bn - 1) / v.bn, tiles = xt * wt, places = (int64_t)num_cus * v.per_cu;
+        // whole tiles, or each cut along the depth so that one to four rounds of workgroups are full, with the sums through memory
+        // (written and read at 4 TB/s, and a launch)
+        for (int r = 0; r <= 4; ++r) {
+            const int64_t fit = r == 0 ? 1 : std::min<int64_t>(places * r / tiles, std::min(pl.nk, 64));
+            if (r > 0 && fit < 2) continue;
+            const int splits = (int)fit;
+            const double rounds = (double)((tiles * splits + places - 1) / places);
+            double us = rounds * ((double)((pl.nk + splits - 1) / splits) * v.step_us + 3.0);
+            if (splits > 1) us += 5.0 + 2.0 * 4.0 * (double)(tiles * splits) * v.bm * v.bn / 4e6;
+            if (pl.wgs == 0 || us < best) {
+                best = us;
+                pl.variant = i;
+                pl.bm = v.bm;
+                pl.bn = v.bn;
+                pl.x_tiles = (int)xt;
+                pl.w_tiles = (int)wt;
+                pl.splits = splits;
+                pl.wgs = tiles * splits;
+            }
+        }
     }
+    pl.part = pl.splits > 1 ? (size_t)pl.wgs * pl.bm * pl.bn : 0;
     return pl;
 }
 
 hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t s)
 {
-    p.len = pl.len;
     p.nk = pl.nk;
     p.x_tiles = pl.x_tiles;
     p.w_tiles = pl.w_tiles;
-    p.slots = pl.slots;
-    p.xcd_share = pl.wgs % 8 == 0 ? pl.wgs / 8 : 0;
+    p.splits = pl.splits;
     const int size = p.out_bf16 ? 2 : 4;
     p.vec = p.out_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * size) == 0;
     const Variant &v = kVariants[pl.variant];
-    hipLaunchKernelGGL(v.kernel, dim3((unsigned)pl.wgs), dim3((unsigned)v.threads), 0, s, p);
+    hipLaunchKernelGGL(v.kernel, dim3((unsigned)pl.wgs), dim3(512), 0, s, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || pl.part == 0) return e;
     const int64_t tiles = (int64_t)pl.x_tiles * pl.w_tiles;
     hipLaunchKernelGGL(quant_sum_kernel, dim3((unsigned)(tiles * (pl.bm * pl.bn / 1024))), dim3(256), 0, s, p, pl.bm, pl.bn);

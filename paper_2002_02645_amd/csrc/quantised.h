@@ -23,13 +23,13 @@ struct QuantRows {
     __host__ __device__ int64_t code_at(int64_t r, int64_t chunk) const   // chunk: 16 codes
     {
         if (tile == 0) return r * d_pad + chunk * 16;
-        const int64_t t = r >> __builtin_ctz(tile), in = r - t * tile;   // (a power of two)
+        const int64_t t = (uint32_t)r / (uint32_t)tile, in = r - t * tile;   // (at most 2^31 rows)
         return t * tile * d_pad + ((chunk >> 3) * tile + in) * 128 + (((int)chunk & 7) ^ row128_swizzle((int)in)) * 16;
     }
     __host__ __device__ int64_t scale_at(int64_t r, int64_t block) const
     {
         if (tile == 0) return r * sd + block;
-        const int64_t t = r >> __builtin_ctz(tile), in = r - t * tile;
+        const int64_t t = (uint32_t)r / (uint32_t)tile, in = r - t * tile;
         return t * tile * sd + ((block >> 2) * tile + in) * 4 + (block & 3);
     }
 };
@@ -49,16 +49,15 @@ struct QuantProduct {
     int out_bf16, relu;
     int vec;                 // four outputs of a row from a multiple of four on are one aligned store
     float *part;             // plan's floats of scratch (none: null)
-    // the plan's
-    int64_t len;             // k-steps of a workgroup's range of the flattened (tile, k-step) space
-    int nk, x_tiles, w_tiles, slots, xcd_share;
+    int nk, x_tiles, w_tiles, splits;   // the plan's
 };
 // How a product is cut.
 struct QuantPlan {
     int variant;        // of quant_gemm_kernel
     int bm, bn;         // rows of x, rows of w of a tile
-    int x_tiles, w_tiles, nk, slots, wgs;
-    int64_t len;
+    int x_tiles, w_tiles, nk;
+    int splits;         // cuts of a tile along the depth
+    int64_t wgs;
     size_t part;        // floats of the sums of cut tiles
 };
 QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16, int num_cus);

@@ -183,7 +183,7 @@ def test_rows_apart_exact_workspace_and_guards(b, d, m, ot):
         fc.build_quantised(0, w.cuda(), bias.cuda())
         wide = _inputs(b, d + 13, torch.float32, 40 + b).cuda()
         out = torch.full((b + 2, m + 9), 77.0, dtype=ot, device="cuda")
-        need = binding.freeze_quantised_workspace_bytes(fc.ctx, 0, b, binding.FREEZE_F32)
+        need = binding.freeze_quantised_workspace_bytes(fc.ctx, 0, b, binding.FREEZE_F32 if ot == torch.float32 else binding.FREEZE_BF16)
         raw = torch.full((need + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
         binding.freeze_quantised_project(fc.ctx, 0, wide[:, 5:5 + d], None, d, False, out[1:b + 1, 3:3 + m], raw[4096:4096 + need])
         torch.cuda.synchronize()
@@ -264,7 +264,7 @@ def test_other_streams_and_replays():
         want = [fc.quantised_project(0, x).clone() for x in xs]
         torch.cuda.synchronize()
         side = torch.cuda.Stream()
-        ws = torch.empty(binding.freeze_quantised_workspace_bytes(fc.ctx, 0, b, binding.FREEZE_BF16), dtype=torch.uint8, device="cuda")
+        ws = torch.empty(binding.freeze_quantised_workspace_bytes(fc.ctx, 0, b, binding.FREEZE_F32), dtype=torch.uint8, device="cuda")
         out = torch.empty(b, m, device="cuda")
         binding.freeze_quantised_project(fc.ctx, 0, xs[0], None, d, False, out, ws, stream=side)
         side.synchronize()

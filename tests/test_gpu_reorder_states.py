@@ -146,7 +146,7 @@ def test_decoding_behind_a_cache():
         out = dict(score=torch.empty(groups, beams, device="cuda"), token=torch.empty(groups, beams, dtype=torch.int32, device="cuda"),
                    parent=torch.empty(groups, beams, dtype=torch.int32, device="cuda"),
                    finished=torch.empty(groups, beams, dtype=torch.uint8, device="cuda"))
-        ws = torch.empty(max(binding.freeze_quantised_workspace_bytes(fc.ctx, 1, rows, binding.FREEZE_BF16),
+        ws = torch.empty(max(binding.freeze_quantised_workspace_bytes(fc.ctx, 1, rows, binding.FREEZE_F32),
                              binding.freeze_beam_workspace_bytes(groups, beams, vocab, beams)), dtype=torch.uint8, device="cuda")
 
         def choose():
