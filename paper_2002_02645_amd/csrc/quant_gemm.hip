@@ -42,7 +42,13 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t c0, uint32_t c1, float s)
     return __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], b[0], b[1]});
 }
 
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) { return (uint32_t)bf16_rne(a) | ((uint32_t)bf16_rne(b) << 16); }
+// two bf16, to nearest even
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b)
+{
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
 
 // outputs col .. col + 3 of a row
 __device__ __forceinline__ void store_outputs(const QuantProduct &p, int64_t row, int64_t col, f32x4 v)
@@ -114,22 +120,73 @@ __device__ __forceinline__ void each(std::integer_sequence<int, I...>, F f)
     (f(std::integral_constant<int, I>{}), ...);
 }
 
-// A wave's sums: the matrix instructions take w as their rows, so a lane holds four consecutive outputs (from col on, and 16 j behind)
-// of one x row (row, and 16 i behind).
+// A wave's sums: the matrix instructions take w as their rows, so a lane holds four consecutive outputs (from col on, and 16 j behind) of one
+// x row (row, and 16 i behind).  Two blocks' bf16 outputs change places between a lane and the one 16 further, so that each has eight in a row.
 template <int XB, int NB, int BM, int BN>
-__device__ __forceinline__ void tile_out(const QuantProduct &p, const f32x4 (&acc)[XB][NB], const Unit &u, int row, int col,
-                                         int64_t x0, int64_t w0, int x_last)
+__device__ __forceinline__ void tile_out(const QuantProduct &p, const f32x4 (&acc)[XB][NB], const Unit &u, int row, int wave_col, int g4, int64_t x0,
+                                         int64_t w0, int x_last)
 {
-    if (p.splits == 1) {   // uniform
-        each(std::make_integer_sequence<int, XB * NB>{}, [&](auto ij) {
-            constexpr int i = decltype(ij)::value / NB, j = decltype(ij)::value % NB;
-            if (row + 16 * i <= x_last) store_outputs(p, x0 + row + 16 * i, w0 + col + 16 * j, acc[i][j]);
-        });
-    } else {
+    const int col = wave_col + 4 * g4;
+    if (p.splits > 1) {   // uniform
         float *dst = p.part + ((int64_t)u.slot * BM + row) * BN + col;
         each(std::make_integer_sequence<int, XB * NB>{}, [&](auto ij) {
             constexpr int i = decltype(ij)::value / NB, j = decltype(ij)::value % NB;
-            *reinterpret_cast<f32x4 *>(dst + i * 16 * BN + j * 16) = acc[i][j];
+            if (row + 16 * i <= x_last) *reinterpret_cast<f32x4 *>(dst + i * 16 * BN + j * 16) = acc[i][j];
+        });
+        return;
+    }
+    if (p.vec && w0 + wave_col + 16 * NB <= p.m) {   // uniform in the wave
+        f32x4 bias[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) bias[j][e] = p.bias ? p.bias[w0 + col + 16 * j + e] : 0.f;
+        each(std::make_integer_sequence<int, XB>{}, [&](auto i_) {
+            constexpr int i = decltype(i_)::value;
+            const int64_t to = (x0 + row + 16 * i) * p.out_stride + w0 + wave_col;
+            const bool in = row + 16 * i <= x_last;
+            f32x4 v[NB];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                v[j] = acc[i][j] + bias[j];
+                if (p.relu)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[j][e] = __builtin_fmaxf(v[j][e], 0.f);
+            }
+            if (!p.out_bf16) {
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    if (in) *reinterpret_cast<f32x4 *>(static_cast<float *>(p.out) + to + 4 * g4 + 16 * j) = v[j];
+                return;
+            }
+            uint32_t h[NB][2];
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) h[j][e] = bf16_pair(v[j][2 * e], v[j][2 * e + 1]);
+            uint16_t *out = static_cast<uint16_t *>(p.out) + to;
+            if (p.vec > 1 && NB % 2 == 0) {
+#pragma unroll
+                for (int j = 0; j + 1 < NB; j += 2) {
+                    u32x4 t;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const auto s = __builtin_amdgcn_permlane16_swap(h[j][e], h[j + 1][e], false, false);
+                        t[e] = s[0];
+                        t[2 + e] = s[1];
+                    }
+                    if (in) *reinterpret_cast<u32x4 *>(out + 16 * (j + (g4 & 1)) + 8 * (g4 >> 1)) = t;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+                    if (in) *reinterpret_cast<u32x2 *>(out + 4 * g4 + 16 * j) = u32x2{h[j][0], h[j][1]};
+            }
+        });
+    } else {
+        each(std::make_integer_sequence<int, XB * NB>{}, [&](auto ij) {
+            constexpr int i = decltype(ij)::value / NB, j = decltype(ij)::value % NB;
+            if (row + 16 * i <= x_last) store_outputs(p, x0 + row + 16 * i, w0 + col + 16 * j, acc[i][j]);
         });
     }
 }
@@ -228,7 +285,7 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
         st = st + 1 == NS ? 0 : st + 1;
     }
     wait_global_loads_le<0>();   // the refills past the last k-step
-    tile_out<XB, NB, BM, BN>(p, acc, u, wx * XB * 16 + (lane & 15), wn * NB * 16 + g4 * 4, x0, w0, x_last);
+    tile_out<XB, NB, BM, BN>(p, acc, u, rX, wn * NB * 16, g4, x0, w0, x_last);
 }
 
 // Larger batches, which the matrix pipes bound: tiles of 32 XB x rows by 256 w rows, eight waves of 16 XB x 64 outputs, two stages.  A wave
@@ -422,7 +479,7 @@ __global__ __launch_bounds__(512, 2) void quant_tile_kernel(QuantProduct p)
         }
     }
     wait_global_loads_le<0>();   // the refills past the last k-step
-    tile_out<XB, NB, BM, BN>(p, acc, u, rX, wn * 64 + g4 * 4, x0, w0, x_last);
+    tile_out<XB, NB, BM, BN>(p, acc, u, rX, wn * 64, g4, x0, w0, x_last);
 }
 
 // The outputs of cut tiles: the sums of a tile's cuts in order, 256 threads for 1,024 outputs.
@@ -436,37 +493,43 @@ __global__ __launch_bounds__(256) void quant_sum_kernel(QuantProduct p, int bm, 
     const int64_t step = (int64_t)bm * bn;
     const float *src = p.part + (int64_t)tile * p.splits * step + at;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < p.splits; s += 4) {   // four in flight, and summed before they are added
-        f32x4 t[4];
+    auto add = [&](int s, auto n_) {   // n cuts, all on their way at once, summed in pairs before they are added
+        constexpr int n = decltype(n_)::value;
+        f32x4 t[n];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            t[e] = *reinterpret_cast<const f32x4 *>(src + (s + e < p.splits ? s + e : s) * step);
-            if (s + e >= p.splits) t[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        v += (t[0] + t[1]) + (t[2] + t[3]);
-    }
+        for (int e = 0; e < n; ++e) t[e] = s + e < p.splits ? *reinterpret_cast<const f32x4 *>(src + (s + e) * step) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 1; d < n; d <<= 1)
+#pragma unroll
+            for (int e = 0; e < n; e += 2 * d) t[e] += t[e + d];
+        v += t[0];
+    };
+    int s = 0;
+    for (; p.splits - s > 4; s += 16) add(s, std::integral_constant<int, 16>{});
+    if (s < p.splits) add(s, std::integral_constant<int, 4>{});
     store_outputs(p, (int64_t)xt * bm + row, (int64_t)wt * bn + col, v);
 }
 
 struct Variant {
     int bm, bn, per_cu;
-    float step_us;   // of a k-step of a workgroup, all CUs at work
+    float step_us;   // of a k-step of a workgroup where neither memory nor L2 bounds it
     void (*kernel)(QuantProduct);
     bool narrow;     // the 8-bit form
 };
-constexpr int kNarrowRows = 64;
 const Variant kVariants[] = {
-    {16, 128, 2, 1.2f, quant_gemm_kernel<1, 8, 1, 1, 4>, false},
-    {32, 128, 2, 1.2f, quant_gemm_kernel<1, 8, 2, 1, 3>, false},
-    {64, 128, 2, 1.3f, quant_gemm_kernel<1, 8, 4, 1, 3>, false},
-    {128, 256, 1, 1.8f, quant_tile_kernel<false, 4>, false},
-    {160, 256, 1, 2.1f, quant_tile_kernel<false, 5>, false},
-    {192, 256, 1, 2.4f, quant_tile_kernel<false, 6>, false},
-    {256, 256, 1, 3.2f, quant_tile_kernel<false, 8>, false},
-    {128, 256, 1, 1.0f, quant_tile_kernel<true, 4>, true},
-    {192, 256, 1, 1.4f, quant_tile_kernel<true, 6>, true},
-    {256, 256, 1, 1.7f, quant_tile_kernel<true, 8>, true},
+    {16, 128, 2, 0.60f, quant_gemm_kernel<1, 8, 1, 1, 4>, false},
+    {32, 128, 2, 0.75f, quant_gemm_kernel<1, 8, 2, 1, 3>, false},
+    {64, 128, 2, 1.00f, quant_gemm_kernel<1, 8, 4, 1, 3>, false},
+    {128, 256, 1, 1.55f, quant_tile_kernel<false, 4>, false},
+    {160, 256, 1, 1.80f, quant_tile_kernel<false, 5>, false},
+    {192, 256, 1, 2.20f, quant_tile_kernel<false, 6>, false},
+    {256, 256, 1, 2.95f, quant_tile_kernel<false, 8>, false},
+    {128, 256, 1, 1.10f, quant_tile_kernel<true, 4>, true},
+    {192, 256, 1, 1.40f, quant_tile_kernel<true, 6>, true},
+    {256, 256, 1, 1.70f, quant_tile_kernel<true, 8>, true},
 };
+// bf16 outputs of more rows than this go by the 8-bit form (8,192 -> 8,192 of 128 rows: 35.7 us, 36.6 by the other one; of 256 rows 42 and 50)
+constexpr int kNarrowRows = 64;
 
 }  // namespace
 
@@ -480,15 +543,19 @@ QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16,
         // the 8-bit form: bf16 outputs of more than kNarrowRows rows
         if (v.narrow ? !out_bf16 || b <= kNarrowRows : out_bf16 && b > kNarrowRows) continue;
         const int64_t xt = (b + v.bm - 1) / v.bm, wt = (m + v.bn - 1) / v.bn, tiles = xt * wt, places = (int64_t)num_cus * v.per_cu;
-        // whole tiles, or each cut along the depth so that one to four rounds of workgroups are full, with the sums through memory
-        // (written and read at 4 TB/s, and a launch)
-        for (int r = 0; r <= 4; ++r) {
-            const int64_t fit = r == 0 ? 1 : std::min<int64_t>(places * r / tiles, std::min(pl.nk, 64));
+        // whole tiles, or each cut along the depth so that a quarter or half a round of workgroups, or one to four rounds are full, with the
+        // sums through memory (written and read at 4 TB/s, and a launch)
+        constexpr int kQuarters[] = {0, 1, 2, 4, 8, 12, 16};
+        for (int r : kQuarters) {
+            const int64_t fit = r == 0 ? 1 : std::min<int64_t>(places * r / 4 / tiles, std::min(pl.nk, 64));
             if (r > 0 && fit < 2) continue;
             const int splits = (int)fit;
             const double rounds = (double)((tiles * splits + places - 1) / places);
+            // workgroups in rounds, the weights out of memory (5.3 TB/s), the stages out of L2 and beyond (10 TB/s)
             double us = rounds * ((double)((pl.nk + splits - 1) / splits) * v.step_us + 3.0);
-            if (splits > 1) us += 5.0 + 2.0 * 4.0 * (double)(tiles * splits) * v.bm * v.bn / 4e6;
+            us = std::max(us, (double)wt * v.bn * (double)d_pad / 5.3e6);
+            us = std::max(us, (double)tiles * (v.bm + v.bn) * (double)d_pad / 10e6);
+            if (splits > 1) us += 5.0 + 2.0 * 4.0 * (double)wt * v.bn * (double)b * splits / 4e6 + 0.1 * splits;
             if (pl.wgs == 0 || us < best) {
                 best = us;
                 pl.variant = i;
@@ -513,6 +580,7 @@ hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t
     p.splits = pl.splits;
     const int size = p.out_bf16 ? 2 : 4;
     p.vec = p.out_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * size) == 0;
+    if (p.vec && p.out_stride % 8 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0) p.vec = 2;
     const Variant &v = kVariants[pl.variant];
     hipLaunchKernelGGL(v.kernel, dim3((unsigned)pl.wgs), dim3(512), 0, s, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || pl.part == 0) return e;

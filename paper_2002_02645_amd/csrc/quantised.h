@@ -23,13 +23,15 @@ struct QuantRows {
     __host__ __device__ int64_t code_at(int64_t r, int64_t chunk) const   // chunk: 16 codes
     {
         if (tile == 0) return r * d_pad + chunk * 16;
-        const int64_t t = (uint32_t)r / (uint32_t)tile, in = r - t * tile;   // (at most 2^31 rows)
-        return t * tile * d_pad + ((chunk >> 3) * tile + in) * 128 + (((int)chunk & 7) ^ row128_swizzle((int)in)) * 16;
+        const int64_t t = (uint32_t)r / (uint32_t)tile;   // (at most 2^31 rows)
+        const int in = (int)(r - t * tile);
+        return t * tile * d_pad + ((chunk >> 3) * tile + in) * 128 + (((int)chunk & 7) ^ row128_swizzle(in)) * 16;
     }
     __host__ __device__ int64_t scale_at(int64_t r, int64_t block) const
     {
         if (tile == 0) return r * sd + block;
-        const int64_t t = (uint32_t)r / (uint32_t)tile, in = r - t * tile;
+        const int64_t t = (uint32_t)r / (uint32_t)tile;
+        const int in = (int)(r - t * tile);
         return t * tile * sd + ((block >> 2) * tile + in) * 4 + (block & 3);
     }
 };
@@ -47,7 +49,7 @@ struct QuantProduct {
     int64_t out_stride;
     int64_t b, m, d_pad, sd;
     int out_bf16, relu;
-    int vec;                 // four outputs of a row from a multiple of four on are one aligned store
+    int vec;                 // 1: four outputs of a row from a multiple of four on are one aligned store; 2: and eight bf16 are
     float *part;             // plan's floats of scratch (none: null)
     int nk, x_tiles, w_tiles, splits;   // the plan's
 };
