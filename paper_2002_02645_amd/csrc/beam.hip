@@ -186,15 +186,16 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 #pragma unroll
         for (int b = 0; b < E / B; ++b) {
             if (__ballot(most8[b] >= floor_v) == 0) continue;   // uniform
+            uint64_t who[B];   // (compared all at once; the limit that rises meanwhile is looked at again)
 #pragma unroll
-            for (int e = b * B; e < (b + 1) * B; ++e) {
-                const float v = value(raw, e);
-                uint64_t who = __ballot(v >= floor_v);
-                while (who) {
-                    const int l = __ffsll((unsigned long long)who) - 1;
-                    who &= who - 1;
-                    const float cv = of_lane(v, l);
-                    const int64_t at = (base + (e / V) * 64 + l) * V - shift + e % V;
+            for (int e = 0; e < B; ++e) who[e] = __ballot(value(raw, b * B + e) >= floor_v);
+#pragma unroll
+            for (int e = 0; e < B; ++e) {
+                while (who[e]) {
+                    const int l = __ffsll((unsigned long long)who[e]) - 1;
+                    who[e] &= who[e] - 1;
+                    const float cv = of_lane(value(raw, b * B + e), l);
+                    const int64_t at = (base + ((b * B + e) / V) * 64 + l) * V - shift + (b * B + e) % V;
                     if (cv >= floor_v && insert(list, cv, (uint32_t)at, p.k, lane))
                         floor_v = __builtin_fmaxf(floor_v, of_lane(list.v, p.k - 1));
                 }
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
     if (lane < p.k) put(lane, list.v, list.i);
 }
 
-// How a row is cut: pieces of whole batches, as many as fill the chip with waves (16 a CU) and no more.
+// How a row is cut: pieces of whole batches, as many as fill the chip with waves (12 a CU) and no more.
 struct BeamPlan {
     int64_t groups_per_part;
     int parts;
@@ -366,7 +367,7 @@ BeamPlan beam_plan(int64_t rows, int64_t vocab, int size)
 {
     const int64_t v = 16 / size, batch = 64 * kBeamLoads;
     const int64_t batches = ((vocab + v - 1 + v - 1) / v + batch - 1) / batch;   // (a misaligned row's groups are one more)
-    int64_t parts = (4096 + rows - 1) / rows;
+    int64_t parts = (3072 + rows - 1) / rows;
     parts = parts < 1 ? 1 : (parts > batches ? batches : parts);
     BeamPlan pl;
     const int64_t per = (batches + parts - 1) / parts;

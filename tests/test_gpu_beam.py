@@ -148,6 +148,42 @@ def test_exact_workspace_and_guards():
                                        raw[4096:4096 + need - 256])
 
 
+def test_logits_beyond_4_gib():
+    # 1.2e9 fp32 values: the last group's rows lie behind byte 4.7e9
+    groups, beams, vocab, k = 300, 4, 1000003, 5
+    logits = torch.zeros(groups * beams, vocab, device="cuda")
+    rows = [0, 1, 1073, 1074, 1196, 1197, 1198, 1199]
+    for n, r in enumerate(rows):
+        logits[r, vocab - 1 - n] = 20.0 + n
+        logits[r, n] = 18.0
+    scores = torch.zeros(groups * beams, device="cuda")
+    fc = binding.FreezeCache(1)
+    try:
+        out = fc.beam_select(logits, scores, beams, k)
+    finally:
+        fc.close()
+    for g in (0, 268, 299):
+        part = slice(g * beams, (g + 1) * beams)
+        _check(logits[part], scores[part], None, beams, k, -1, dict(score=out["score"][g:g + 1], token=out["token"][g:g + 1],
+                                                                   parent=out["parent"][g:g + 1] - g * beams, finished=out["finished"][g:g + 1]))
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_random_sizes(seed):
+    rng = np.random.RandomState(100 + seed)
+    beams, vocab = int(rng.choice([1, 2, 3, 5, 8, 16, 33])), int(2 ** rng.uniform(0, 15.5))
+    groups, k = int(2 ** rng.uniform(0, 5)), int(rng.choice([1, 2, beams, 2 * beams, 64]))
+    k = min(k, 64)
+    dtype = [torch.float32, torch.bfloat16][seed % 2]
+    logits, scores = _make(groups * beams, vocab, dtype, 200 + seed)
+    g = torch.Generator().manual_seed(300 + seed)
+    if rng.rand() < 0.6:
+        logits[torch.rand(logits.shape, generator=g).cuda() < rng.uniform(0, 1)] = -INF
+    done = (torch.rand(groups * beams, generator=g) < 0.2).to(torch.uint8).cuda()
+    scores[torch.rand(groups * beams, generator=g).cuda() < 0.1] = -INF
+    _run(logits, scores, beams, k, finished=done, end=int(rng.randint(vocab)))
+
+
 def test_replays_and_other_streams():
     groups, beams, vocab, k = 3, 4, 20000, 8
     sets = [_make(groups * beams, vocab, torch.float32, 20 + i) for i in range(3)]

@@ -172,6 +172,82 @@ def test_layer(b, d, m, xt, ot, relu, with_bias, given):
         fc.close()
 
 
+def _values64(x):
+    """The values that rows of x are held as, in 64 bits on the GPU (for sizes that numpy takes long for)."""
+    rows, d = x.shape
+    t = torch.zeros(rows, -(-d // 128) * 128, dtype=torch.float64, device="cuda")
+    t[:, :d] = x
+    t = t.view(rows, -1, 128)
+    e = torch.ceil(torch.log2(t.abs().amax(2, keepdim=True) / 448)).clamp(min=-126)
+    t = t / torch.exp2(e)
+    step = torch.exp2(torch.frexp(t).exponent.double().clamp(min=-5) - 4)
+    return (torch.round(t / step) * step * torch.exp2(e)).view(rows, -1)
+
+
+def test_the_two_references_agree():
+    x = _inputs(20, 700, torch.float32, 2)
+    assert torch.equal(_values64(x.cuda()).cpu(), torch.from_numpy(ref.values(*ref.quantise(x.double().numpy()))))
+
+
+@pytest.mark.parametrize("b,d,m,ot", [
+    # every height of tiles, whole and cut along the depth
+    (1466, 64, 16, torch.float32), (3, 1466, 16, torch.float32), (4363, 64, 141, torch.float32), (142, 2730, 156, torch.float32),
+    (5442, 68, 291, torch.float32), (5486, 4172, 22, torch.float32), (73, 64, 32879, torch.float32), (69, 4161, 11590, torch.float32),
+    (144, 70, 33170, torch.float32), (132, 7266, 7287, torch.float32), (166, 69, 35740, torch.float32), (163, 6654, 11726, torch.float32),
+    (214, 72, 32799, torch.float32), (195, 11281, 10761, torch.float32), (71, 69, 16, torch.bfloat16), (72, 776, 16, torch.bfloat16),
+    (144, 70, 33170, torch.bfloat16), (1314, 4563, 23, torch.bfloat16), (214, 72, 32799, torch.bfloat16), (4830, 51288, 20, torch.bfloat16),
+    (1000, 515, 4104, torch.bfloat16), (1000, 515, 4104, torch.float32), (2500, 1152, 1032, torch.float32),
+])
+def test_every_tile(b, d, m, ot):
+    x = _inputs(b, d, torch.bfloat16, 70 + b + d).cuda()
+    w = _inputs(m, d, torch.bfloat16, 71 + m + d, channels=False).cuda()
+    bias = torch.linspace(-1, 1, m, device="cuda")
+    fc = binding.FreezeCache(1)
+    try:
+        fc.build_quantised(0, w, bias)
+        got = fc.quantised_project(0, x, out_dtype=ot)
+        again = fc.quantised_project(0, x, out_dtype=ot)
+        assert torch.equal(got, again)
+        xv, wv = _values64(x), _values64(w)
+        y = xv @ wv.t().contiguous() + bias.double()
+        tol = _tolerance(xv, wv, bias.double(), y, xv.shape[1], ot)
+        off = (got.double() - y).abs()
+        assert (off <= tol).all(), (off / tol).max().item()
+    finally:
+        fc.close()
+
+
+def test_weights_and_rows_beyond_4_gib():
+    # 4.4e9 codes of weights, then as many of rows: the last ones and a few between
+    d, n = 8192, 540007
+    g = torch.Generator(device="cuda").manual_seed(3)
+    codes = torch.randint(0, 0x7F, (n, d), generator=g, dtype=torch.uint8, device="cuda")
+    scales = torch.randint(100, 130, (n, 64), generator=g, dtype=torch.uint8, device="cuda")
+    few = torch.randn(3, d, generator=g, device="cuda")
+    table = torch.from_numpy(np.nan_to_num(ref.CODE_VALUES)).cuda()
+    some = torch.tensor([0, 1, 255, 256, 131071, 262144, 300001, 524287, 524288, n - 2, n - 1], device="cuda")
+    at = (table[codes[some].long()].view(-1, 64, 128) * torch.exp2(scales[some].double() - 127).unsqueeze(2)).view(-1, d)
+    fc = binding.FreezeCache(2)
+    try:
+        fc.build_quantised(0, codes.view(torch.float8_e4m3fn), scales=scales)
+        fc.build_quantised(1, few)
+        vf = _values64(few)
+        y = vf @ at.t().contiguous()
+        tol = _tolerance(vf, at, None, y, d, torch.float32)
+        assert ((fc.quantised_project(0, few)[:, some].double() - y).abs() <= tol).all()
+        del fc.storage[0]
+        got = fc.quantised_project(1, codes.view(torch.float8_e4m3fn), scales)[some]
+        assert ((got.double() - y.t()).abs() <= tol.t()).all()
+        del codes, scales, got
+        x = torch.zeros(n - 400000, d, device="cuda")     # 4.6e9 bytes of fp32
+        x[-5:] = torch.randn(5, d, generator=g, device="cuda")
+        c, s = fc.quantise_rows(x)
+        want = ref.quantise(x[-5:].double().cpu().numpy())
+        assert np.array_equal(_bits(c[-5:]), want[0]) and np.array_equal(s[-5:].cpu().numpy(), want[1])
+    finally:
+        fc.close()
+
+
 @pytest.mark.parametrize("b,d,m,ot", [(1, 300, 70, torch.float32), (40, 1000, 131, torch.bfloat16), (150, 700, 259, torch.float32),
                                       (300, 1100, 258, torch.bfloat16), (300, 1100, 258, torch.float32)])
 def test_rows_apart_exact_workspace_and_guards(b, d, m, ot):
@@ -280,6 +356,26 @@ def test_other_streams_and_replays():
             assert torch.equal(out, want[i])
             ws.fill_(255)
             assert torch.equal(fc.quantised_project(0, xs[i]), want[i])
+    finally:
+        fc.close()
+
+
+def test_two_streams_at_once():
+    w = _inputs(3000, 900, torch.float32, 30, channels=False).cuda()
+    fc = binding.FreezeCache(1)
+    try:
+        fc.build_quantised(0, w)
+        xs = [_inputs(b, 900, torch.bfloat16, 31 + b).cuda() for b in (40, 300)]
+        want = [fc.quantised_project(0, x).clone() for x in xs]
+        outs = [torch.empty_like(y) for y in want]
+        ws = [torch.empty(binding.freeze_quantised_workspace_bytes(fc.ctx, 0, x.shape[0], binding.FREEZE_F32), dtype=torch.uint8, device="cuda") for x in xs]
+        streams = [torch.cuda.Stream() for _ in xs]
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for x, out, w8, s in zip(xs, outs, ws, streams):
+                binding.freeze_quantised_project(fc.ctx, 0, x, None, 900, False, out, w8, stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
     finally:
         fc.close()
 
