@@ -292,6 +292,9 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
 // keeps its four blocks of w rows' fragments (16 rows each) for a step (8-bit form) or half a step (bf16 form, 64 codes) and goes through
 // its XB blocks of x rows, a group of matrix instructions each; their fragments are read kAhead groups ahead.  The step's barrier comes
 // before its last kAhead groups, which need nothing newer: it publishes the next step's stage and frees this one, which is refilled from there on.
+// The 8-bit form, whose steps are half as long as what is loaded in them takes (133 us without matrix instructions, 216 with them, for
+// 4,096 x 8,192 -> 8,192), has another barrier where the step's w rows have been read: those of the step after the next are loaded in their place
+// before the x rows are free (208 us).
 // (Four waves of 128 x 128 outputs read a third less out of LDS, but their sums fill a register file and the compiler moves them about: 290 us for
 // 4,096 x 8,192 -> 8,192 in the 8-bit form, 236 so.)
 template <bool F8, int XB>
@@ -304,7 +307,8 @@ __global__ __launch_bounds__(512, 2) void quant_tile_kernel(QuantProduct p)
     constexpr int kHalves = F8 ? 1 : 2, kGroups = kHalves * XB, kAhead = F8 ? 2 : 3;
     constexpr int kRing = kGroups % 4 == 0 ? 4 : (kGroups % 3 == 0 && F8 ? 3 : (kGroups % 5 == 0 ? 5 : 6));   // fragments ahead, in step with the groups
     constexpr int IW = BN / 64, LX = BM / 8, IX = (LX + 7) / 8, LS = BN / 64 + (BM + 63) / 64, NL = IW + IX + 1;   // load instructions: see above
-    constexpr int kPerGroup = (NL + kAhead - 1) / kAhead;
+    constexpr int kFirst = F8 ? IW : 0, kPerGroup = (NL - kFirst + kAhead - 1) / kAhead;   // loads that the step's last groups issue
+    constexpr int kWRead = 1;   // 8-bit form: the group at whose start the step's w rows have been read
     static_assert(2 * kStage <= 163840 && kGroups % kRing == 0 && kRing > kAhead && LS <= 8, "");
     __shared__ __attribute__((aligned(16))) unsigned char smem[2 * kStage];
 
@@ -375,18 +379,22 @@ __global__ __launch_bounds__(512, 2) void quant_tile_kernel(QuantProduct p)
         read_ws(0, decltype(j)::value);
     });
     each(std::make_integer_sequence<int, kAhead>{}, [&](auto i) { read_x(decltype(i)::value, 0, decltype(i)::value, 0); });
-    // group g of a step: the barrier where the reads reach the next step, this group's share of the refill, the reads of the group kAhead further
+    // group g of a step: its barriers, the loads that they make room for, the reads of the group kAhead further
     auto group_head = [&](int kt, int st, auto g_) {
         constexpr int g = decltype(g_)::value, ahead = g + kAhead;
         if constexpr (g == kGroups - kAhead) {
-            wait_global_loads_le<0>();
+            wait_global_loads_le<F8 ? IW : 0>();   // (the w rows of the step after the next are on their way)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __syncthreads();
+        } else if constexpr (F8 && g == kWRead) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __syncthreads();
         }
         read_x(ahead % kRing, ahead < kGroups ? st : st ^ 1, ahead % XB, ahead / XB % kHalves);
+        if constexpr (F8 && g == kWRead) each(std::make_integer_sequence<int, IW>{}, [&](auto l) { issue(st, at_most(kt + 2), l); });
         if constexpr (g >= kGroups - kAhead)
             each(std::make_integer_sequence<int, kPerGroup>{}, [&](auto l) {
-                issue(st, at_most(kt + 2), std::integral_constant<int, (g - kGroups + kAhead) * kPerGroup + decltype(l)::value>{});
+                issue(st, at_most(kt + 2), std::integral_constant<int, kFirst + (g - kGroups + kAhead) * kPerGroup + decltype(l)::value>{});
             });
     };
     int st = 0;
