@@ -528,6 +528,9 @@ const Variant kVariants[] = {
     {16, 128, 2, 0.60f, quant_gemm_kernel<1, 8, 1, 1, 4>, false},
     {32, 128, 2, 0.75f, quant_gemm_kernel<1, 8, 2, 1, 3>, false},
     {64, 128, 2, 1.00f, quant_gemm_kernel<1, 8, 4, 1, 3>, false},
+    {16, 256, 1, 0.75f, quant_gemm_kernel<1, 8, 1, 2, 4>, false},
+    {32, 256, 1, 0.90f, quant_gemm_kernel<1, 8, 2, 2, 4>, false},
+    {64, 256, 1, 1.10f, quant_gemm_kernel<1, 8, 4, 2, 3>, false},
     {128, 256, 1, 1.55f, quant_tile_kernel<false, 4>, false},
     {160, 256, 1, 1.80f, quant_tile_kernel<false, 5>, false},
     {192, 256, 1, 2.20f, quant_tile_kernel<false, 6>, false},
@@ -536,9 +539,6 @@ const Variant kVariants[] = {
     {192, 256, 1, 1.40f, quant_tile_kernel<true, 6>, true},
     {256, 256, 1, 1.70f, quant_tile_kernel<true, 8>, true},
 };
-// bf16 outputs of more rows than this go by the 8-bit form (8,192 -> 8,192 of 128 rows: 35.7 us, 36.6 by the other one; of 256 rows 42 and 50)
-constexpr int kNarrowRows = 64;
-
 }  // namespace
 
 QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16, int num_cus)
@@ -548,22 +548,24 @@ QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16,
     double best = 0;
     for (int i = 0; i < (int)(sizeof kVariants / sizeof kVariants[0]); ++i) {
         const Variant &v = kVariants[i];
-        // the 8-bit form: bf16 outputs of more than kNarrowRows rows
-        if (v.narrow ? !out_bf16 || b <= kNarrowRows : out_bf16 && b > kNarrowRows) continue;
+        if (v.narrow && !out_bf16) continue;
         const int64_t xt = (b + v.bm - 1) / v.bm, wt = (m + v.bn - 1) / v.bn, tiles = xt * wt, places = (int64_t)num_cus * v.per_cu;
         // whole tiles, or each cut along the depth so that a quarter or half a round of workgroups, or one to four rounds are full, with the
-        // sums through memory (written and read at 4 TB/s, and a launch)
+        // sums through memory (written and read at 2.5 TB/s, and a launch)
         constexpr int kQuarters[] = {0, 1, 2, 4, 8, 12, 16};
         for (int r : kQuarters) {
             const int64_t fit = r == 0 ? 1 : std::min<int64_t>(places * r / 4 / tiles, std::min(pl.nk, 64));
             if (r > 0 && fit < 2) continue;
             const int splits = (int)fit;
             const double rounds = (double)((tiles * splits + places - 1) / places);
-            // workgroups in rounds, the weights out of memory (5.3 TB/s), the stages out of L2 and beyond (10 TB/s)
-            double us = rounds * ((double)((pl.nk + splits - 1) / splits) * v.step_us + 3.0);
+            // Workgroups in rounds; the weights out of memory (5.3 TB/s); what a CU takes in (40 GB/s; all of them 10 TB/s), of which a part shows
+            // beside either.
+            const double steps = (double)((pl.nk + splits - 1) / splits);
+            const double fed = (double)((tiles * splits + num_cus - 1) / num_cus) * steps * (double)(v.bm + v.bn) * 132.0 / 40e3;
+            double us = rounds * (steps * v.step_us + 3.0);
             us = std::max(us, (double)wt * v.bn * (double)d_pad / 5.3e6);
-            us = std::max(us, (double)tiles * (v.bm + v.bn) * (double)d_pad / 10e6);
-            if (splits > 1) us += 5.0 + 2.0 * 4.0 * (double)wt * v.bn * (double)b * splits / 4e6 + 0.1 * splits;
+            us = std::max(us, fed) + 0.15 * fed;
+            if (splits > 1) us += 5.0 + 2.0 * 4.0 * (double)wt * v.bn * (double)b * splits / 2.5e6 + 0.1 * splits;
             if (pl.wgs == 0 || us < best) {
                 best = us;
                 pl.variant = i;

@@ -190,12 +190,14 @@ def test_the_two_references_agree():
 
 
 @pytest.mark.parametrize("b,d,m,ot", [
-    # every height of tiles, whole and cut along the depth
-    (1466, 64, 16, torch.float32), (3, 1466, 16, torch.float32), (4363, 64, 141, torch.float32), (142, 2730, 156, torch.float32),
-    (5442, 68, 291, torch.float32), (5486, 4172, 22, torch.float32), (73, 64, 32879, torch.float32), (69, 4161, 11590, torch.float32),
-    (144, 70, 33170, torch.float32), (132, 7266, 7287, torch.float32), (166, 69, 35740, torch.float32), (163, 6654, 11726, torch.float32),
-    (214, 72, 32799, torch.float32), (195, 11281, 10761, torch.float32), (71, 69, 16, torch.bfloat16), (72, 776, 16, torch.bfloat16),
-    (144, 70, 33170, torch.bfloat16), (1314, 4563, 23, torch.bfloat16), (214, 72, 32799, torch.bfloat16), (4830, 51288, 20, torch.bfloat16),
+    # every shape of tiles, whole and cut along the depth
+    (1466, 64, 16, torch.float32), (3, 1466, 16, torch.float32), (4363, 64, 141, torch.float32), (106, 2553, 273, torch.float32),
+    (5442, 68, 291, torch.float32), (5486, 4172, 22, torch.float32), (1, 392, 61910, torch.float32), (18, 5647, 16, torch.float32),
+    (4138, 2193, 130, torch.float32), (17, 7390, 5298, torch.float32), (39, 697, 65486, torch.float32), (328, 3871, 2063, torch.float32),
+    (73, 64, 32879, torch.float32), (66, 4137, 11021, torch.float32), (144, 70, 33170, torch.float32), (132, 9715, 7318, torch.float32),
+    (166, 69, 35740, torch.float32), (176, 7477, 11082, torch.float32), (214, 72, 32799, torch.float32), (194, 8149, 18562, torch.float32),
+    (73, 64, 32879, torch.bfloat16), (166, 3941, 3744, torch.bfloat16), (144, 70, 33170, torch.bfloat16), (135, 5904, 11349, torch.bfloat16),
+    (214, 72, 32799, torch.bfloat16), (5496, 63304, 27, torch.bfloat16),
     (1000, 515, 4104, torch.bfloat16), (1000, 515, 4104, torch.float32), (2500, 1152, 1032, torch.float32),
 ])
 def test_every_tile(b, d, m, ot):
