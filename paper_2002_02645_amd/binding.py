@@ -445,8 +445,11 @@ def freeze_beam_select(logits: torch.Tensor, scores: torch.Tensor, finished: Opt
     assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
     assert finished is None or (finished.dtype in (torch.uint8, torch.bool) and finished.is_contiguous() and finished.numel() == rows)
     groups = rows // beams
-    for t, dt in ((out_scores, torch.float32), (out_tokens, torch.int32), (out_parents, torch.int32), (out_finished, torch.uint8)):
-        assert t is None or (t.dtype == dt and t.is_contiguous() and t.numel() == groups * k)
+    n = groups * k
+    assert out_scores.dtype == torch.float32 and out_scores.is_contiguous() and out_scores.numel() == n
+    assert out_tokens.dtype == torch.int32 and out_tokens.is_contiguous() and out_tokens.numel() == n
+    assert out_parents.dtype == torch.int32 and out_parents.is_contiguous() and out_parents.numel() == n
+    assert out_finished is None or (out_finished.dtype == torch.uint8 and out_finished.is_contiguous() and out_finished.numel() == n)
     _check(lib().freeze_beam_select(_at(logits), _values_dtype(logits), groups, beams, vocab, _rows_of(logits), _at(scores),
                                     _at(finished), end_token, k, _at(out_scores), _at(out_tokens), _at(out_parents),
                                     _at(out_finished), _at(workspace), workspace.nbytes,
@@ -564,6 +567,7 @@ class FreezeCache:
             self.ctx = None
 
     def _workspace(self, nbytes: int) -> torch.Tensor:
+        # (a larger one replaces it: what is captured into a graph has to be called with a workspace of its own, as the functions above take it)
         if self._ws is None or self._ws.numel() < nbytes:
             self._ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
         return self._ws
@@ -696,10 +700,13 @@ class FreezeCache:
 
     def quantise_rows(self, x: torch.Tensor):
         """Rows in 8 bits: codes [rows, d rounded up to 128] float8_e4m3fn and a scale byte for each block of 128 values."""
+        _here(x)
+        assert x.dtype in (torch.float32, torch.bfloat16)
         rows, d = x.shape
-        codes = torch.empty((rows, freeze_quantised_code_stride(d)), dtype=torch.float8_e4m3fn, device=self.device)
-        scales = torch.empty((rows, freeze_quantised_scale_stride(d)), dtype=torch.uint8, device=self.device)
-        freeze_quantise_rows(x, codes, scales)
+        codes = torch.empty((rows, -(-d // 128) * 128), dtype=torch.float8_e4m3fn, device=self.device)
+        scales = torch.empty((rows, -(-d // 512) * 4), dtype=torch.uint8, device=self.device)
+        _check(lib().freeze_quantise_rows(x.data_ptr(), _values_dtype(x), rows, d, _rows_of(x), codes.data_ptr(), scales.data_ptr(), _on(None)),
+               "freeze_quantise_rows")
         return codes, scales
 
     def build_quantised(self, slot: int, weights: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -733,9 +740,8 @@ class FreezeCache:
                     end_token: int = -1) -> dict:
         """The k best continuations of every group of `beams` rows: score, token, parent (row), finished; each [groups, k]."""
         groups = logits.shape[0] // beams
-        out = dict(score=torch.empty((groups, k), dtype=torch.float32, device=self.device),
-                   token=torch.empty((groups, k), dtype=torch.int32, device=self.device),
-                   parent=torch.empty((groups, k), dtype=torch.int32, device=self.device),
+        score, token, parent = torch.empty((3, groups, k), dtype=torch.int32, device=self.device).unbind(0)
+        out = dict(score=score.view(torch.float32), token=token, parent=parent,
                    finished=torch.empty((groups, k), dtype=torch.uint8, device=self.device))
         nbytes = freeze_beam_workspace_bytes(groups, beams, logits.shape[1], k)
         if nbytes == 0:
@@ -746,9 +752,12 @@ class FreezeCache:
 
     def reorder_states(self, src, dst, parents: torch.Tensor, used: Optional[int] = None, row_dim: int = 0) -> None:
         """Row r of every dst becomes row parents[r] of its src (tensors or lists of tensors; see state_of)."""
-        src, dst = ([t] if isinstance(t, torch.Tensor) else list(t) for t in (src, dst))
-        assert len(src) == len(dst) and all(t.shape[row_dim] == src[0].shape[row_dim] for t in src)
-        assert all(parents.numel() <= t.shape[row_dim] for t in dst)
+        if isinstance(src, torch.Tensor):
+            src, dst = (src,), (dst,)
+        assert len(src) == len(dst)
+        if not src:
+            return
         _here(*src, *dst)
-        freeze_reorder_states([state_of(s, d, used, row_dim) for s, d in zip(src, dst)], parents,
-                              src[0].shape[row_dim] if src else 0)
+        rows = src[0].shape[row_dim]
+        assert parents.numel() <= rows and all(t.shape[row_dim] == rows for t in src)   # (state_of: a dst is like its src)
+        freeze_reorder_states([state_of(s, d, used, row_dim) for s, d in zip(src, dst)], parents, rows)

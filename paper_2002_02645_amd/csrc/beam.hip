@@ -98,11 +98,8 @@ template <typename T>
 __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 {
     constexpr int V = 16 / (int)sizeof(T), E = V * kBeamLoads, B = 8;   // B values of a lane are looked at together
-    __shared__ float floors[4];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (lane == 0) floors[wave] = kLowest;
-    __syncthreads();
-    const int64_t unit0 = (int64_t)blockIdx.x * 4, unit = unit0 + wave;
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= (int64_t)p.rows * p.parts) return;   // uniform in the wave
     const int row = (int)(unit / p.parts), part = (int)(unit % p.parts);
     if (p.scores[row] == -__builtin_inff() || (p.finished && p.finished[row])) return;
@@ -111,9 +108,6 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     const int64_t shift = (int64_t)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
     const int64_t all = (p.vocab + shift + V - 1) / V;
     const int64_t g0 = part * p.groups_per_part, g1 = g0 + p.groups_per_part < all ? g0 + p.groups_per_part : all;
-    // what the workgroup's other waves found on the same row
-    const bool same_row = lane < 4 && (int)((unit0 + lane) / p.parts) == row;
-
     auto load = [&](int64_t base, u32x4(&raw)[kBeamLoads]) {
 #pragma unroll
         for (int l = 0; l < kBeamLoads; ++l) {
@@ -173,10 +167,6 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
             for (int e = 0; e < E; ++e) part_sum += __builtin_amdgcn_exp2f((value(raw, e) - top) * kLog2E);
             sum += part_sum;
         }
-        float others = same_row ? *const_cast<volatile float *>(&floors[lane & 3]) : kLowest;
-        others = __builtin_fmaxf(others, __shfl_xor(others, 1, 64));
-        others = __builtin_fmaxf(others, __shfl_xor(others, 2, 64));
-        floor_v = __builtin_fmaxf(floor_v, __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(others))));
         const uint64_t lanes = __ballot(most >= floor_v);
         if (lanes == 0) continue;   // uniform
         if (__popcll(lanes) >= p.k) {
@@ -201,7 +191,6 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
                 }
             }
         }
-        if (lane == 0) *const_cast<volatile float *>(&floors[wave]) = floor_v;
     }
     // the piece's sum, relative to its largest value
     float m = top;
