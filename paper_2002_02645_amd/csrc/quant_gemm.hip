@@ -109,6 +109,12 @@ __device__ __forceinline__ void load16_to_lds_at(uint64_t sbase, uint32_t voff, 
 {
     asm volatile("s_add_u32 m0, %0, %3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(voff), "s"(sbase), "n"(TO) : "memory", "m0", "scc");
 }
+// of memory that nobody else reads soon: not kept in L2
+template <int TO>
+__device__ __forceinline__ void load16_once_to_lds_at(uint64_t sbase, uint32_t voff, uint32_t lds)
+{
+    asm volatile("s_add_u32 m0, %0, %3\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(voff), "s"(sbase), "n"(TO) : "memory", "m0", "scc");
+}
 template <int TO>
 __device__ __forceinline__ void load4_to_lds_at(uint64_t sbase, uint32_t voff, uint32_t lds)
 {
@@ -192,7 +198,9 @@ __device__ __forceinline__ void tile_out(const QuantProduct &p, const f32x4 (&ac
 }
 
 // Batches of few rows: eight waves of XB x NB blocks of 16 x 16 outputs, WX of them along x; NS stages.  Bound by the memory that the
-// weights come from: what counts is how many bytes are on their way.
+// weights come from: what counts is how many bytes are on their way.  Weights that one workgroup reads and that L2 cannot hold until the
+// next call pass it by: 134 MB (1 x 4,096 -> 32,768) in 21.2 us against 25.5, 1.07 GB (32 x 8,192 -> 131,072) in 172.7 against 190.7,
+// 6.2 - 6.9 TB/s.  Not so where tiles of x share them (300 rows of x: 25.1 us against 23.8), nor where L2 holds them: 16.8 MB 6.9 against 5.8.
 template <int WX, int WN, int XB, int NB, int NS>
 __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
 {
@@ -231,7 +239,8 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
         const uint32_t to = smem_base + buf * kStage;
         const uint64_t kw = gW + (uint64_t)kt * (kQuantTile * 128), kx = gX + (uint64_t)kt * (BM * 128);
         each(std::make_integer_sequence<int, IW>{}, [&](auto i) {
-            load16_to_lds_at<decltype(i)::value * 8192>(kw + decltype(i)::value * 8192, off16, to + w * 1024);
+            if (p.w_once) load16_once_to_lds_at<decltype(i)::value * 8192>(kw + decltype(i)::value * 8192, off16, to + w * 1024);   // uniform
+            else load16_to_lds_at<decltype(i)::value * 8192>(kw + decltype(i)::value * 8192, off16, to + w * 1024);
         });
         each(std::make_integer_sequence<int, IX>{}, [&](auto i) {
             load16_to_lds_at<kX + decltype(i)::value * 8192>(kx + decltype(i)::value * 8192, off16, to + lx * 1024);
@@ -558,12 +567,12 @@ QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16,
             if (r > 0 && fit < 2) continue;
             const int splits = (int)fit;
             const double rounds = (double)((tiles * splits + places - 1) / places);
-            // Workgroups in rounds; the weights out of memory (5.3 TB/s); what a CU takes in (40 GB/s; all of them 10 TB/s), of which a part shows
+            // Workgroups in rounds; the weights out of memory (6.5 TB/s where one workgroup reads them, else 5.3); what a CU takes in (40 GB/s; all of them 10 TB/s), of which a part shows
             // beside either.
             const double steps = (double)((pl.nk + splits - 1) / splits);
             const double fed = (double)((tiles * splits + num_cus - 1) / num_cus) * steps * (double)(v.bm + v.bn) * 132.0 / 40e3;
             double us = rounds * (steps * v.step_us + 3.0);
-            us = std::max(us, (double)wt * v.bn * (double)d_pad / 5.3e6);
+            us = std::max(us, (double)wt * v.bn * (double)d_pad / (xt == 1 ? 6.5e6 : 5.3e6));
             us = std::max(us, fed) + 0.15 * fed;
             if (splits > 1) us += 5.0 + 2.0 * 4.0 * (double)wt * v.bn * (double)b * splits / 2.5e6 + 0.1 * splits;
             if (pl.wgs == 0 || us < best) {
@@ -591,6 +600,7 @@ hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t
     const int size = p.out_bf16 ? 2 : 4;
     p.vec = p.out_stride % 4 == 0 && reinterpret_cast<uintptr_t>(p.out) % (4 * size) == 0;
     if (p.vec && p.out_stride % 8 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0) p.vec = 2;
+    p.w_once = pl.x_tiles == 1 && p.m * p.d_pad > kL2Bytes;
     const Variant &v = kVariants[pl.variant];
     hipLaunchKernelGGL(v.kernel, dim3((unsigned)pl.wgs), dim3(512), 0, s, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || pl.part == 0) return e;

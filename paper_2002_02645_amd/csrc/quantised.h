@@ -5,6 +5,7 @@
 namespace fz {
 
 constexpr int kQuantBlock = 128;             // values that share an exponent: one k-step of the product
+constexpr int64_t kL2Bytes = 32 << 20;       // of the eight XCDs together
 constexpr int64_t kQuantMaxD = 1 << 22;      // a tile of 256 rows spans 32-bit offsets
 
 inline int64_t quant_code_stride(int64_t d) { return (d + kQuantBlock - 1) / kQuantBlock * kQuantBlock; }
@@ -50,6 +51,7 @@ struct QuantProduct {
     int64_t b, m, d_pad, sd;
     int out_bf16, relu;
     int vec;                 // 1: four outputs of a row from a multiple of four on are one aligned store; 2: and eight bf16 are
+    int w_once;              // the weights are read by one workgroup each, and more than L2 holds
     float *part;             // plan's floats of scratch (none: null)
     int nk, x_tiles, w_tiles, splits;   // the plan's
 };
