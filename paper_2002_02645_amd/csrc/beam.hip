@@ -3,10 +3,15 @@
 // Choice.  total(j, v) = score_j + l_jv - log sum_u exp l_ju, the k best of a group's rows j and tokens v.  Within a row the
 // values themselves decide, so that a row's sum of exponentials and its k best tokens come from one pass over it; rows are
 // brought together by a second, small kernel.
-//   - A wave takes a piece of a row, batches of 64 lanes x 4 loads of 16 bytes.  Its k best so far lie in its lanes in order
-//     (value, then index), a new one is inserted by a ballot and a shuffle.  Values below the k-th best so far are passed over by one
-//     comparison a batch; where k lanes or more have better ones, the k-th best of the lanes' largest raises that limit first.
-//   - The sums of exponentials are kept per lane in fp32 relative to the lane's largest value (a batch at a time), joined in fp64.
+//   - A wave takes a piece of a row, batches of 64 lanes x 4 loads of 16 bytes, the next batch on its way while one is looked at.  Its k
+//     best so far lie in its lanes in order (value, then index).  A new one is inserted by a ballot and a shift of the lanes; that is
+//     some hundred cycles, so that few may come to it: of a run of 16 batches only the lanes' largest values are kept at first, the k-th of
+//     64 lanes' largest is a limit that about k values of the run reach, and the loads that hold these are read again, out of L2 as a
+//     rule.  512 rows of 131,072 bf16 with k 16: 31.4 us; with every batch looked through at once for the k best so far 39.8.
+//   - The sums of exponentials are kept per lane relative to the lane's largest value: a batch in fp32, the batches in fp64 (a batch's sum
+//     may be lost in a large one that was there before it; a row of a million would add that up).
+// 121 MB (a tenth of the rows has ended) at 31.4 us are 3.9 TB/s: without the choice 24 us, of which the exponentials and the comparisons
+// are 17 us of issue; small calls (4 rows of 32,000 fp32: 6.0 us) are bound by the way through the code.
 #include "../../include/freeze.h"
 #include "freeze_internal.h"
 #include "select_common.h"
@@ -21,6 +26,7 @@ namespace {
 
 constexpr float kLowest = -3.402823466e38f, kLog2E = 1.44269504f;
 constexpr int kBeamLoads = 4;   // loads of 16 bytes a lane has in flight
+constexpr int kBeamRun = 16;    // batches that are looked through together for the best
 
 struct BeamArgs {
     const void *logits;
@@ -43,7 +49,7 @@ struct BestList {
     V v;
     I i;
     __device__ __forceinline__ void clear(V lowest) { v = lowest; i = (I)-1; }   // (unsigned: the largest index)
-    __device__ __forceinline__ bool before(V cv, I ci) const { return v > cv || (v == cv && i < ci); }
+    __device__ __forceinline__ bool before(V cv, I ci) const { return (v > cv) | ((v == cv) & (i < ci)); }
 };
 // the value of lane l, which is the same in all lanes
 __device__ __forceinline__ uint32_t of_lane(uint32_t x, int l) { return (uint32_t)__builtin_amdgcn_readlane((int)x, l); }
@@ -66,7 +72,7 @@ __device__ __forceinline__ double of_previous(double x) { return __longlong_as_d
 template <typename V, typename I>
 __device__ __forceinline__ bool insert(BestList<V, I> &list, V cv, I ci, int k, int lane)
 {
-    const int pos = __popcll(__ballot(lane < k && list.before(cv, ci)));
+    const int pos = __popcll(__ballot((lane < k) & list.before(cv, ci)));
     if (pos >= k) return false;
     const V pv = of_previous(list.v);
     const I pi = of_previous(list.i);
@@ -78,6 +84,12 @@ __device__ __forceinline__ bool insert(BestList<V, I> &list, V cv, I ci, int k, 
         list.i = ci;
     }
     return true;
+}
+
+// of the lanes of `who`, how many are before this one
+__device__ __forceinline__ int lanes_before(uint64_t who)
+{
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
 }
 
 // A value that k lanes reach at least, cut off to the bits from LOW on of its place in order: near the k-th largest, and not above it.
@@ -97,40 +109,32 @@ __device__ __forceinline__ float kth_reached(float x, int k)
 template <typename T>
 __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 {
-    constexpr int V = 16 / (int)sizeof(T), E = V * kBeamLoads, B = 8;   // B values of a lane are looked at together
-    const int lane = threadIdx.x & 63;
+    constexpr int V = 16 / (int)sizeof(T), E = V * kBeamLoads;
+    __shared__ float run_most[4][kBeamRun][64];      // a run's largest values, by batch and lane
+    __shared__ uint16_t run_lane[4][128];            // (batch, lane) of those that may hold one of the best
+    __shared__ float near_v[4][2 * 64 * V];          // values that may be among the best
+    __shared__ uint32_t near_i[4][2 * 64 * V];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (unit >= (int64_t)p.rows * p.parts) return;   // uniform in the wave
     const int row = (int)(unit / p.parts), part = (int)(unit % p.parts);
     if (p.scores[row] == -__builtin_inff() || (p.finished && p.finished[row])) return;
     const T *src = static_cast<const T *>(p.logits) + (int64_t)row * p.row_stride;
-    // groups of V values on 16-byte boundaries; the first and the last may reach over the row's ends
+    // Groups of V values on 16-byte boundaries.  The row's first and last ones may reach over its ends: their values come one by one, the
+    // whole groups [f0, f1) of the piece in batches.  Of a batch that reaches past f1 the last group is loaded again and put out of the way:
+    // loads that no branch decides about, so that a batch is on its way while the one before is looked at.
     const int64_t shift = (int64_t)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
     const int64_t all = (p.vocab + shift + V - 1) / V;
     const int64_t g0 = part * p.groups_per_part, g1 = g0 + p.groups_per_part < all ? g0 + p.groups_per_part : all;
-    auto load = [&](int64_t base, u32x4(&raw)[kBeamLoads]) {
+    const int64_t full = (p.vocab + shift) / V;
+    const int64_t f0 = g0 == 0 && shift > 0 ? 1 : g0, f1 = g1 < full ? g1 : full;
+    auto load = [&](int64_t base, u32x4(&raw)[kBeamLoads]) {   // base < f1
+        const T *at = src + (base * V - shift);
+        const int last = (int)(f1 - base < 64 * kBeamLoads ? f1 - base : 64 * kBeamLoads) - 1;
 #pragma unroll
-        for (int l = 0; l < kBeamLoads; ++l) {
-            const int64_t g = base + l * 64 + lane, at = g * V - shift;
-            if (g < g1 && at >= 0 && at + V <= p.vocab) {
-                raw[l] = *reinterpret_cast<const u32x4 *>(src + at);
-            } else {
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    uint32_t word = 0;
-#pragma unroll
-                    for (int e = 0; e < V / 4; ++e) {
-                        const int64_t i = at + w * (V / 4) + e;
-                        const bool in = g < g1 && i >= 0 && i < p.vocab;
-                        if constexpr (sizeof(T) == 4) word = in ? __float_as_uint(src[i]) : 0xff800000u;
-                        else word |= (in ? (uint32_t)src[i] : 0xff80u) << (16 * e);
-                    }
-                    raw[l][w] = word;
-                }
-            }
-        }
+        for (int l = 0; l < kBeamLoads; ++l) raw[l] = *reinterpret_cast<const u32x4 *>(at + (l * 64 + lane < last ? l * 64 + lane : last) * V);
     };
-    auto value = [](const u32x4(&raw)[kBeamLoads], int e) {
+    auto value = [](const u32x4 *raw, int e) {
         const uint32_t w = raw[e / V][(e % V) * 4 / V];
         if constexpr (sizeof(T) == 4) return __uint_as_float(w);
         else return __uint_as_float(e % 2 ? w & 0xffff0000u : w << 16);
@@ -138,65 +142,163 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 
     BestList<float, uint32_t> list;
     list.clear(-__builtin_inff());
-    float floor_v = kLowest;   // what a value has to reach
-    float top = -__builtin_inff(), sum = 0.f;
-    u32x4 raw[kBeamLoads], next[kBeamLoads];
-    if (g0 < g1) load(g0, next);
-    for (int64_t base = g0; base < g1; base += 64 * kBeamLoads) {
+    // what a value has to be before, or the same: the k-th best so far, or a value that k others reach
+    float floor_v = kLowest;
+    uint32_t floor_i = ~0u;
+    auto may = [&](float v, uint32_t i) { return (v > floor_v) | ((v == floor_v) & (i <= floor_i)); };
+    auto take = [&](uint64_t who, float v, uint32_t i) {   // the lanes' values
+        while (who) {
+            const int l = __ffsll((unsigned long long)who) - 1;
+            who &= who - 1;
+            const float cv = of_lane(v, l);
+            const uint32_t ci = of_lane(i, l);
+            if (may(cv, ci) && insert(list, cv, ci, p.k, lane)) {
+                const float kv = of_lane(list.v, p.k - 1);
+                if (kv >= floor_v) {
+                    floor_v = kv;
+                    floor_i = of_lane(list.i, p.k - 1);
+                }
+            }
+        }
+    };
+    float top = -__builtin_inff();
+    double sum = 0.0;   // (in fp32 a large value in front would take hundreds of batches of small ones in without a trace)
+    u32x4 next[kBeamLoads];
+    {
+        // the ends: lanes 0 .. 7 before the whole groups, 8 .. 15 behind them (of a row within one group all are before)
+        const int64_t i = lane < 8 ? (g0 == 0 && shift > 0 && lane < V - shift ? lane : p.vocab)
+                                   : (lane < 16 && full >= g0 && full < g1 && (full > 0 || shift == 0) ? full * V - shift + lane - 8 : p.vocab);
+        float x = -__builtin_inff();
+        if (i < p.vocab) {
+            if constexpr (sizeof(T) == 4) x = src[i];
+            else x = __uint_as_float((uint32_t)src[i] << 16);
+        }
+        if (f0 < f1) load(f0, next);
+        if (x >= kLowest) {
+            top = x;
+            sum = 1.0;
+        }
+        take(__ballot(x >= kLowest), x, (uint32_t)i);
+    }
+    // the best of the lanes' loads from group g on, those of a lane 64 groups apart
+    auto scan = [&](const u32x4(&raw)[kBeamLoads], int64_t g, bool mine) {
+        int near = 0;
+#pragma unroll
+        for (int l = 0; l < kBeamLoads; ++l) {
+            const bool in = mine & (g + l * 64 < f1);
+            const uint32_t i = (uint32_t)((g + l * 64) * V - shift);
+            uint64_t who[V];   // (compared all at once; equals behind the k-th best fall out below)
+#pragma unroll
+            for (int e = 0; e < V; ++e) who[e] = __ballot(in & (value(raw, l * V + e) >= floor_v));
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (who[e] == 0) continue;   // uniform
+                if (who[e] >> lane & 1) {
+                    near_v[wave][near + lanes_before(who[e])] = value(raw, l * V + e);
+                    near_i[wave][near + lanes_before(who[e])] = i + e;
+                }
+                near += __popcll(who[e]);
+            }
+            if (l < kBeamLoads - 1 && near <= 64 * V) continue;   // the next load's find room
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int from = 0; from < near; from += 64) {
+                const bool some = from + lane < near;
+                const int place = some ? from + lane : near - 1;
+                const float v = near_v[wave][place];
+                const uint32_t vi = near_i[wave][place];
+                take(__ballot(some & may(v, vi)), v, vi);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            near = 0;
+        }
+    };
+    // The best of a run of n batches from base on, of which `last` is the last one; most: the lane's largest value.  A limit that k values
+    // reach comes from the lanes' largest ones; the batches' largest ones say then which loads to look at again.
+    auto look = [&](int64_t base, int n, float most, const u32x4(&last)[kBeamLoads]) {
+        const uint64_t lanes = __ballot(most >= floor_v);
+        if (lanes == 0) return;   // uniform
+        if (__popcll(lanes) >= p.k) {
+            const float reached = kth_reached<16>(most, p.k);
+            if (reached > floor_v) {
+                floor_v = reached;
+                floor_i = ~0u;
+            }
+        }
+        int q = 0, held = 0;
+        do {
+            u32x4 raw[kBeamLoads];
+            int64_t g = base + lane;
+            bool mine = true;
+            if (n == 1) {
+#pragma unroll
+                for (int l = 0; l < kBeamLoads; ++l) raw[l] = last[l];
+            } else {
+                for (; q < n && held < 64; ++q) {
+                    const bool pass = may(run_most[wave][q][lane], (uint32_t)((base + q * (64 * kBeamLoads) + lane) * V - shift));
+                    const uint64_t who = __ballot(pass);
+                    if (pass) run_lane[wave][held + lanes_before(who)] = (uint16_t)(q * 64 + lane);
+                    held += __popcll(who);
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                mine = lane < held;
+                const uint32_t at = mine ? run_lane[wave][lane] : 0;
+                g = base + (int64_t)(at >> 6) * (64 * kBeamLoads) + (at & 63);
+#pragma unroll
+                for (int l = 0; l < kBeamLoads; ++l) raw[l] = *reinterpret_cast<const u32x4 *>(src + ((g + l * 64 < f1 ? g + l * 64 : f1 - 1) * V - shift));
+                held = held > 64 ? held - 64 : 0;
+                if (lane < held) run_lane[wave][lane] = run_lane[wave][64 + lane];
+            }
+            scan(raw, g, mine);
+        } while (n > 1 && (q < n || held > 0));
+    };
+    int in_run = 0;
+    float most_run = -__builtin_inff();
+    u32x4 raw[kBeamLoads];
+    for (int64_t base = f0; base < f1; base += 64 * kBeamLoads) {
 #pragma unroll
         for (int l = 0; l < kBeamLoads; ++l) raw[l] = next[l];
-        if (base + 64 * kBeamLoads < g1) load(base + 64 * kBeamLoads, next);
-        float most8[E / B];
+        load(base + 64 * kBeamLoads < f1 ? base + 64 * kBeamLoads : base, next);
+        if (f1 - base < 64 * kBeamLoads) {   // uniform
+            const int n = (int)(f1 - base);
 #pragma unroll
-        for (int b = 0; b < E / B; ++b) {
-            most8[b] = value(raw, b * B);
-#pragma unroll
-            for (int e = 1; e < B; ++e) most8[b] = __builtin_fmaxf(most8[b], value(raw, b * B + e));
+            for (int l = 0; l < kBeamLoads; ++l)
+                if (l * 64 + lane >= n) raw[l] = sizeof(T) == 4 ? u32x4{0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u} : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
         }
-        float most = most8[0];
+        float most = value(raw, 0);
 #pragma unroll
-        for (int b = 1; b < E / B; ++b) most = __builtin_fmaxf(most, most8[b]);
+        for (int e = 1; e < E; ++e) most = __builtin_fmaxf(most, value(raw, e));
+        run_most[wave][in_run][lane] = most;
+        most_run = __builtin_fmaxf(most_run, most);
         if (most > top) {
-            sum *= __builtin_amdgcn_exp2f((top - most) * kLog2E);
+            sum *= (double)__builtin_amdgcn_exp2f((top - most) * kLog2E);
             top = most;
         }
         if (top >= kLowest) {
-            // differences to the largest value first: the rounding of the factor then goes by them, not by the values
-            float part_sum = 0.f;
+            // l log2(e) - top log2(e) in one rounding, which goes by the difference; what the subtrahend lost by its own is given back to the sum
+            const float t = top * kLog2E, lost = __builtin_fmaf(top, kLog2E, -t);
+            float part_sum[2] = {0.f, 0.f};
+            if (__builtin_fabsf(top) < 1e38f) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) part_sum += __builtin_amdgcn_exp2f((value(raw, e) - top) * kLog2E);
-            sum += part_sum;
-        }
-        const uint64_t lanes = __ballot(most >= floor_v);
-        if (lanes == 0) continue;   // uniform
-        if (__popcll(lanes) >= p.k) {
-            // at least k values of this batch reach the k-th largest of the lanes' largest
-            floor_v = __builtin_fmaxf(floor_v, kth_reached<16>(most, p.k));
-        }
+                for (int e = 0; e < E; ++e) part_sum[e & 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(value(raw, e), kLog2E, -t));
+                sum += (double)((part_sum[0] + part_sum[1]) * __builtin_amdgcn_exp2f(-lost));
+            } else {   // (the product overflows)
 #pragma unroll
-        for (int b = 0; b < E / B; ++b) {
-            if (__ballot(most8[b] >= floor_v) == 0) continue;   // uniform
-            uint64_t who[B];   // (compared all at once; the limit that rises meanwhile is looked at again)
-#pragma unroll
-            for (int e = 0; e < B; ++e) who[e] = __ballot(value(raw, b * B + e) >= floor_v);
-#pragma unroll
-            for (int e = 0; e < B; ++e) {
-                while (who[e]) {
-                    const int l = __ffsll((unsigned long long)who[e]) - 1;
-                    who[e] &= who[e] - 1;
-                    const float cv = of_lane(value(raw, b * B + e), l);
-                    const int64_t at = (base + ((b * B + e) / V) * 64 + l) * V - shift + (b * B + e) % V;
-                    if (cv >= floor_v && insert(list, cv, (uint32_t)at, p.k, lane))
-                        floor_v = __builtin_fmaxf(floor_v, of_lane(list.v, p.k - 1));
-                }
+                for (int e = 0; e < E; ++e) part_sum[0] += __builtin_amdgcn_exp2f((value(raw, e) - top) * kLog2E);
+                sum += (double)part_sum[0];
             }
+        }
+        ++in_run;
+        if (in_run == kBeamRun || base + 64 * kBeamLoads >= f1) {   // uniform
+            look(base - (int64_t)(in_run - 1) * (64 * kBeamLoads), in_run, most_run, raw);
+            in_run = 0;
+            most_run = -__builtin_inff();
         }
     }
     // the piece's sum, relative to its largest value
     float m = top;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, o, 64));
-    double s = top >= kLowest ? (double)sum * (double)__builtin_amdgcn_exp2f((top - m) * kLog2E) : 0.0;
+    double s = top >= kLowest ? sum * (double)__builtin_amdgcn_exp2f((top - m) * kLog2E) : 0.0;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
     if (lane == 0) {

@@ -168,6 +168,42 @@ def test_logits_beyond_4_gib():
                                                                    parent=out["parent"][g:g + 1] - g * beams, finished=out["finished"][g:g + 1]))
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_large_value_before_many_small_ones(dtype):
+    # the small ones are a fifth of the sum, each 4e-7 of the large one
+    logits = torch.zeros(4, 500009, device="cuda")
+    logits[:, 0] = 14.75
+    logits[2, 0] = 0
+    logits[2, -1] = 14.75
+    _run(logits.to(dtype), torch.zeros(4, device="cuda"), 2, 3)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_whole_rows_to_a_wave(dtype):
+    # 4,000 rows: a piece is a row of several runs of batches; the best ones last, first, spread, all alike, and within one load
+    groups, beams, vocab, k = 1000, 4, 50021, 6
+    g = torch.Generator(device="cuda").manual_seed(12)
+    logits = torch.randn(groups * beams, vocab, generator=g, device="cuda").to(dtype)
+    logits[0] = torch.linspace(-9, 9, vocab).to(dtype)
+    logits[1] = torch.linspace(9, -9, vocab).to(dtype)
+    logits[2] = 0.5
+    logits[3] = torch.where(torch.arange(vocab) % 4001 == 17, 4.0, -1.0).to(dtype)
+    logits[3996, 16384 * 2 + 8:16384 * 2 + 16] = 7.0
+    logits[3997, :] = -INF
+    logits[3997, 50020] = -2.0
+    logits[3998, vocab // 2:] = -INF
+    scores = -torch.rand(groups * beams, generator=g, device="cuda")
+    fc = binding.FreezeCache(1)
+    try:
+        out = fc.beam_select(logits, scores, beams, k)
+    finally:
+        fc.close()
+    for n in (0, 500, 999):
+        part = slice(n * beams, (n + 1) * beams)
+        _check(logits[part], scores[part], None, beams, k, -1, dict(score=out["score"][n:n + 1], token=out["token"][n:n + 1],
+                                                                   parent=out["parent"][n:n + 1] - n * beams, finished=out["finished"][n:n + 1]))
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_random_sizes(seed):
     rng = np.random.RandomState(100 + seed)
