@@ -356,7 +356,8 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
  *            FREEZE_F32: products are exact and summed in fp32.  FREEZE_BF16: larger batches go through the 8-bit matrix
  *            instructions, which cut the products of eight neighbouring elements off 13 bits below the largest of them
  *            before they are summed in fp32: less than the rounding of the output, but not what the fp32 output rounds to.
- *   workspace  freeze_quantised_workspace_bytes() bytes, 256-byte aligned; scratch only.
+ *   workspace  freeze_quantised_workspace_bytes() bytes, 256-byte aligned; scratch only.  Calls that share a workspace (replays of
+ *            captured ones too) must follow one another on the device.
  * 1 <= m < 2^31 - 512, 0 <= b <= 2^30; b == 0 is a no-op.
  */
 size_t freeze_quantised_storage_bytes(int64_t m, int64_t d);
@@ -384,7 +385,7 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
  *             and freeze_reorder_states take it;
  *   out_finished [groups, k] uint8 or NULL: token == end_token.
  *   A group with fewer than k continuations: its last places get score -inf, token end_token (0 for -1), parent its first row.
- *   workspace  freeze_beam_workspace_bytes() bytes, 256-byte aligned; scratch only.
+ *   workspace  freeze_beam_workspace_bytes() bytes, 256-byte aligned; scratch only, shared by calls that follow one another only.
  * 1 <= beams <= 64, 1 <= k <= FREEZE_MAX_K, 1 <= vocab < 2^31 - 512, groups * beams <= 2^20; groups == 0 is a no-op.  Totals are formed in
  * fp64 from fp32 exponentials and rounded once; within a row, the values themselves decide.  No output may lie over an input.
  */

