@@ -459,7 +459,7 @@ BeamPlan beam_plan(int64_t rows, int64_t vocab, int size)
 {
     const int64_t v = 16 / size, batch = 64 * kBeamLoads;
     const int64_t batches = ((vocab + v - 1 + v - 1) / v + batch - 1) / batch;   // (a misaligned row's groups are one more)
-    int64_t parts = (3072 + rows - 1) / rows;
+    int64_t parts = (12 * 256 + rows - 1) / rows;
     parts = parts < 1 ? 1 : (parts > batches ? batches : parts);
     BeamPlan pl;
     const int64_t per = (batches + parts - 1) / parts;
