@@ -346,8 +346,8 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
  *   weights  [m, d] row-major, fp32 or bf16, quantised by the call (weight_scales NULL); or FREEZE_E4M3: codes and
  *            weight_scales as of freeze_quantise_rows (codes behind d are not looked at).
  *   bias     [m] fp32, or NULL for none.
- *   storage  >= freeze_quantised_storage_bytes() bytes, 256-byte aligned; everything is copied into it; it must outlive
- *            the calls of freeze_quantised_project on the slot.
+ *   storage  >= freeze_quantised_storage_bytes() bytes, 256-byte aligned, none of them of the operands; everything is copied into it;
+ *            it must outlive the calls of freeze_quantised_project on the slot.
  *   x        [b, d] fp32 or bf16, x_stride elements from row to row, quantised by the call (x_scales NULL); or
  *            FREEZE_E4M3: codes and x_scales as of freeze_quantise_rows (16 and 4 bytes aligned, their own strides; codes behind d
  *            and x_stride are not looked at).
@@ -357,7 +357,7 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
  *            instructions, which cut the products of eight neighbouring elements off 13 bits below the largest of them
  *            before they are summed in fp32: less than the rounding of the output, but not what the fp32 output rounds to.
  *   workspace  freeze_quantised_workspace_bytes() bytes, 256-byte aligned; scratch only.  Calls that share a workspace (replays of
- *            captured ones too) must follow one another on the device.
+ *            captured ones too) must follow one another on the device.  It may not lie over x or out.
  * 1 <= m < 2^31 - 512, 0 <= b <= 2^30; b == 0 is a no-op.
  */
 size_t freeze_quantised_storage_bytes(int64_t m, int64_t d);
@@ -387,7 +387,8 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
  *   A group with fewer than k continuations: its last places get score -inf, token end_token (0 for -1), parent its first row.
  *   workspace  freeze_beam_workspace_bytes() bytes, 256-byte aligned; scratch only, shared by calls that follow one another only.
  * 1 <= beams <= 64, 1 <= k <= FREEZE_MAX_K, 1 <= vocab < 2^31 - 512, groups * beams <= 2^20; groups == 0 is a no-op.  Totals are formed in
- * fp64 from fp32 exponentials and rounded once; within a row, the values themselves decide.  No output may lie over an input.
+ * fp64 from fp32 exponentials and rounded once; within a row, the values themselves decide.  No output, nor the workspace, may lie
+ * over an input or another output: FREEZE_EINVAL.
  */
 #define FREEZE_MAX_BEAMS 64
 size_t freeze_beam_workspace_bytes(int64_t groups, int beams, int64_t vocab, int k);
@@ -404,7 +405,7 @@ int freeze_beam_select(const void *logits, int logits_dtype, int64_t groups, int
  *            dst).  Keys and values of attention, [layers, rows, heads, places, width], the first `used` places filled: outer =
  *            layers, pieces = heads, piece_bytes = used * width * element size; what lies behind the runs is left as it is.
  *   parents  [rows] int32 (device); a row whose parent is outside [0, src_rows) is left as it was.
- * No dst may share a byte of its whole extent (first to last run) with any src or another dst: FREEZE_EINVAL.
+ * No dst may share a byte of its whole extent (first to last run) with any src, another dst or parents: FREEZE_EINVAL.
  * 0 <= num_states <= 1024, strides >= 0, piece_bytes >= 0, at most 2^31 - 1 runs a state; rows == 0 is a no-op.
  */
 typedef struct freeze_state {

@@ -585,6 +585,18 @@ struct Extent {
     uintptr_t begin, end;
     bool dst;
 };
+// whether a dst shares a byte with another extent (sorts them)
+bool written_twice(Extent *e, int n)
+{
+    std::sort(e, e + n, [](const Extent &a, const Extent &b) { return a.begin < b.begin; });
+    uintptr_t any_end = 0, dst_end = 0;   // how far the extents so far reach
+    for (int i = 0; i < n; ++i) {
+        if (e[i].begin < (e[i].dst ? any_end : dst_end)) return true;
+        any_end = std::max(any_end, e[i].end);
+        if (e[i].dst) dst_end = std::max(dst_end, e[i].end);
+    }
+    return false;
+}
 
 }  // namespace
 }  // namespace fz
@@ -606,7 +618,8 @@ int freeze_beam_select(const void *logits, int logits_dtype, int64_t groups, int
                        int32_t *out_tokens, int32_t *out_parents, uint8_t *out_finished, void *workspace, size_t workspace_bytes,
                        void *stream)
 {
-    if (!beam_sizes(groups, beams, vocab, k) || (logits_dtype != FREEZE_F32 && logits_dtype != FREEZE_BF16) || row_stride < vocab)
+    if (!beam_sizes(groups, beams, vocab, k) || (logits_dtype != FREEZE_F32 && logits_dtype != FREEZE_BF16) || row_stride < vocab ||
+        row_stride > (int64_t)1 << 40)
         return FREEZE_EINVAL;
     if (end_token < -1 || end_token >= vocab || (finished && end_token < 0)) return FREEZE_EINVAL;
     if (groups == 0) return FREEZE_OK;
@@ -616,6 +629,22 @@ int freeze_beam_select(const void *logits, int logits_dtype, int64_t groups, int
     if (workspace_bytes < freeze_beam_workspace_bytes(groups, beams, vocab, k) || reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
         return FREEZE_EWORKSPACE;
     const int64_t rows = groups * beams;
+    {
+        Extent e[8];
+        int n = 0;
+        auto add = [&](const void *p, size_t bytes, bool dst) {
+            const uintptr_t b = reinterpret_cast<uintptr_t>(p);
+            if (p) e[n++] = Extent{b, b + bytes, dst};
+            return b % 4 == 0;
+        };
+        const size_t places = (size_t)groups * k;
+        add(logits, (size_t)((rows - 1) * row_stride + vocab) * size, false);
+        add(finished, (size_t)rows, false);
+        add(out_finished, places, true);
+        if (!add(scores, (size_t)rows * 4, false) || !add(out_scores, places * 4, true) || !add(out_tokens, places * 4, true) ||
+            !add(out_parents, places * 4, true) || !add(workspace, freeze_beam_workspace_bytes(groups, beams, vocab, k), true) || written_twice(e, n))
+            return FREEZE_EINVAL;
+    }
     const BeamPlan pl = beam_plan(rows, vocab, size);
     const size_t units = (size_t)rows * pl.parts;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
@@ -659,7 +688,7 @@ int freeze_reorder_states(const freeze_state *states, int num_states, const int3
         return FREEZE_EINVAL;
     // every size and stride first, then no dst over another extent
     constexpr int64_t kMost = (int64_t)1 << 46;
-    Extent extents[2048];
+    Extent extents[2049];
     int n = 0;
     for (int i = 0; i < num_states; ++i) {
         const freeze_state &t = states[i];
@@ -682,13 +711,10 @@ int freeze_reorder_states(const freeze_state *states, int num_states, const int3
     }
     if (rows == 0 || num_states == 0) return FREEZE_OK;
     if (!parents) return FREEZE_EINVAL;
-    std::sort(extents, extents + n, [](const Extent &a, const Extent &b) { return a.begin < b.begin; });
-    uintptr_t any_end = 0, dst_end = 0;   // how far the extents so far reach
-    for (int i = 0; i < n; ++i) {
-        if (extents[i].begin < (extents[i].dst ? any_end : dst_end)) return FREEZE_EINVAL;
-        any_end = std::max(any_end, extents[i].end);
-        if (extents[i].dst) dst_end = std::max(dst_end, extents[i].end);
-    }
+    const uintptr_t pb = reinterpret_cast<uintptr_t>(parents);
+    if (pb % 4 != 0) return FREEZE_EINVAL;
+    extents[n++] = Extent{pb, pb + (uintptr_t)rows * 4, false};
+    if (written_twice(extents, n)) return FREEZE_EINVAL;
     for (int i = 0; i < num_states;) {
         ReorderArgs a{};
         a.parents = parents;

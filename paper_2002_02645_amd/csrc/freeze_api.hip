@@ -1330,6 +1330,10 @@ int freeze_quantised_build(freeze_ctx *ctx, int slot, const void *weights, int w
         return FREEZE_EINVAL;
     if (!aligned(weights, given ? 16 : (weights_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(weight_scales, 4) || !aligned(bias, 4)) return FREEZE_EINVAL;
     if (storage_bytes < bytes || !aligned(storage, kAlign)) return FREEZE_EWORKSPACE;
+    const size_t wb = (size_t)m * (given ? (size_t)quant_code_stride(d) : (size_t)d * (weights_dtype == FREEZE_F32 ? 4 : 2));
+    if (share_bytes(weights, wb, storage, bytes) || (given && share_bytes(weight_scales, (size_t)(m * quant_scale_stride(d)), storage, bytes)) ||
+        (bias && share_bytes(bias, (size_t)m * 4, storage, bytes)))
+        return FREEZE_EINVAL;
     Carver st(storage);
     const QuantRows w = take_rows(st, m, d, kQuantTile);
     float *q_bias = bias ? st.take<float>((size_t)m) : nullptr;
@@ -1373,7 +1377,12 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
         !aligned(x, given ? 16 : (x_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(x_scales, 4))
         return FREEZE_EINVAL;
     const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), out_dtype == FREEZE_BF16, ctx->num_cus);
-    if (workspace_bytes < quant_bytes(pl, b, P->d) || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
+    const size_t need = quant_bytes(pl, b, P->d);
+    if (workspace_bytes < need || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
+    const size_t xb = given ? (size_t)(b * quant_code_stride(P->d)) : (size_t)((b - 1) * x_stride + P->d) * (x_dtype == FREEZE_F32 ? 4 : 2);
+    if (share_bytes(workspace, need, out, (size_t)((b - 1) * out_stride + P->n) * out_size) || share_bytes(workspace, need, x, xb) ||
+        (given && share_bytes(workspace, need, x_scales, (size_t)(b * quant_scale_stride(P->d)))))
+        return FREEZE_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(stream);
     Carver ws(workspace);
     const QuantRows rows = take_rows(ws, b, P->d, pl.bm);

@@ -64,6 +64,12 @@ def test_layer_refusals(ctx):
     assert build(ctx, 0, P((1 << 20) + 8), 2, sc, 4, 8, None, st, 1 << 20, None) == EINVAL
     x, out, ws = P(1 << 25), P(1 << 26), P(1 << 27)
     assert L.freeze_quantised_project(ctx, 0, x, 0, None, 2, 8, 0, out, 0, 4, ws, 1 << 20, None) == ENOTBUILT
+    need = binding.freeze_quantised_storage_bytes(4, 8)
+    for at in ((1 << 24) - 64, (1 << 24) + need - 64):      # weights, bias, codes and scales that reach into the storage
+        assert build(ctx, 0, P(at), 0, None, 4, 8, None, st, 1 << 20, None) == EINVAL
+        assert build(ctx, 0, w, 0, None, 32, 8, P(at), st, 1 << 20, None) == EINVAL
+        assert build(ctx, 0, P(at), 2, sc, 4, 8, None, st, 1 << 20, None) == EINVAL
+        assert build(ctx, 0, w, 2, P(at), 32, 8, None, st, 1 << 20, None) == EINVAL
     assert L.freeze_quantised_project(ctx, 5, x, 0, None, 2, 8, 0, out, 0, 4, ws, 1 << 20, None) == ELAYER
     assert L.freeze_quantised_project(None, 0, x, 0, None, 2, 8, 0, out, 0, 4, ws, 1 << 20, None) == EINVAL
 
@@ -90,6 +96,27 @@ def test_beam_refusals():
     assert call(a2=0, a0=None, a14=None) == 0
 
 
+def test_beam_outputs_over_other_buffers():
+    # 2 groups of 4 rows, k = 4: 8 places of 4 bytes each; every buffer alone, then one of them moved over another one's last byte
+    L = binding.lib()
+    need = binding.freeze_beam_workspace_bytes(2, 4, 1000, 4)
+    lo, sc, fi, oS, oT, oP, oF, ws = (n << 20 for n in range(1, 9))
+    at = dict(lo=(lo, 8 * 1000 * 4), sc=(sc, 32), fi=(fi, 8), oS=(oS, 32), oT=(oT, 32), oP=(oP, 32), oF=(oF, 8), ws=(ws, need))
+
+    def call(**moved):
+        p = {k: P(moved.get(k, v[0])) for k, v in at.items()}
+        return L.freeze_beam_select(p["lo"], 0, 2, 4, 1000, 1000, p["sc"], p["fi"], 5, 4, p["oS"], p["oT"], p["oP"], p["oF"], p["ws"], need, None)
+    for out in ("oS", "oT", "oP", "oF"):
+        for other, (begin, size) in at.items():
+            if other != out:
+                assert call(**{out: begin}) == EINVAL, (out, other)
+                assert call(**{out: begin + (size - 1) // 4 * 4}) == EINVAL, (out, other)
+    for other in ("lo", "sc", "fi"):
+        assert call(**{other: ws + 256}) == EINVAL
+    for name in ("sc", "oS", "oT", "oP"):
+        assert call(**{name: at[name][0] + 2}) == EINVAL
+
+
 def test_reorder_refusals():
     f = binding.lib().freeze_reorder_states
 
@@ -109,6 +136,7 @@ def test_reorder_refusals():
     assert call([good], parents=None) == EINVAL and call([good], rows=-1) == EINVAL and call([good], src_rows=-1) == EINVAL
     assert call([good, S(b + 100, 1 << 26, 1, 0, 64, 1, 0, 64)]) == EINVAL         # a source within another's destination
     assert call([good, S(1 << 27, b + 200, 1, 0, 64, 1, 0, 64)]) == EINVAL         # two destinations
+    assert call([good], parents=P(b + 252)) == EINVAL and call([good], parents=P(4098)) == EINVAL
 
 
 def test_state_of_layouts():

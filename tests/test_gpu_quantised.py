@@ -316,6 +316,30 @@ def test_output_over_its_input():
         fc.close()
 
 
+def test_workspace_over_operands_is_refused():
+    b, d, m = 50, 256, 256
+    fc = binding.FreezeCache(1)
+    try:
+        fc.build_quantised(0, _inputs(m, d, torch.float32, 5, channels=False).cuda())
+        need = binding.freeze_quantised_workspace_bytes(fc.ctx, 0, b, binding.FREEZE_F32)
+        size = b * 256 * 4
+        buf = torch.zeros(2 * need + 2 * size, dtype=torch.uint8, device="cuda")
+        ws, other = buf[size:size + need], torch.zeros(b, 256, device="cuda")
+        codes, scales = fc.quantise_rows(other)
+        for at in (size - 256, size + need // 256 * 256 - 256):   # over the first and the last bytes
+            rows = buf[at:at + size].view(torch.float32).view(b, 256)
+            given = buf[at:at + b * 256].view(torch.float8_e4m3fn).view(b, 256), buf[at:at + b * 4].view(b, 4)
+            for x, sc, out in ((rows, None, other), (other, None, rows), (given[0], scales, other), (codes, given[1] if at >= size else None, other)):
+                if x is codes and sc is None:
+                    continue
+                with pytest.raises(binding.FreezeError):
+                    binding.freeze_quantised_project(fc.ctx, 0, x, sc, d, False, out, ws)
+        torch.cuda.synchronize()
+        assert (buf == 0).all()
+    finally:
+        fc.close()
+
+
 def test_a_row_does_not_depend_on_its_batch():
     # the same sums for a row alone and in the middle of others of the same tile
     x = _inputs(48, 1000, torch.bfloat16, 6).cuda()
