@@ -11,7 +11,7 @@
 //   - The sums of exponentials are kept per lane relative to the lane's largest value: a batch in fp32, the batches in fp64 (a batch's sum
 //     may be lost in a large one that was there before it; a row of a million would add that up).
 // 121 MB (a tenth of the rows has ended) at 31.4 us are 3.9 TB/s: without the choice 24 us, of which the exponentials and the comparisons
-// are 17 us of issue; small calls (4 rows of 32,000 fp32: 6.0 us) are bound by the way through the code.
+// are 17 us of issue; small calls (4 rows of 32,000 fp32: 5.8 us) are bound by the way through the code.
 #include "../../include/freeze.h"
 #include "freeze_internal.h"
 #include "select_common.h"
@@ -115,10 +115,9 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     __shared__ float near_v[4][2 * 64 * V];          // values that may be among the best
     __shared__ uint32_t near_i[4][2 * 64 * V];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (unit >= (int64_t)p.rows * p.parts) return;   // uniform in the wave
-    const int row = (int)(unit / p.parts), part = (int)(unit % p.parts);
-    if (p.scores[row] == -__builtin_inff() || (p.finished && p.finished[row])) return;
+    const uint32_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);   // (at most 2^20 rows, or 12 pieces a CU and one a row)
+    if (unit >= (uint32_t)p.rows * (uint32_t)p.parts) return;   // uniform in the wave
+    const int row = (int)(unit / (uint32_t)p.parts), part = (int)(unit - (uint32_t)row * (uint32_t)p.parts);
     const T *src = static_cast<const T *>(p.logits) + (int64_t)row * p.row_stride;
     // Groups of V values on 16-byte boundaries.  The row's first and last ones may reach over its ends: their values come one by one, the
     // whole groups [f0, f1) of the piece in batches.  Of a batch that reaches past f1 the last group is loaded again and put out of the way:
@@ -174,6 +173,8 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
             else x = __uint_as_float((uint32_t)src[i] << 16);
         }
         if (f0 < f1) load(f0, next);
+        // (with the first loads on their way: an empty row or one that has ended has nothing to choose from)
+        if (p.scores[row] == -__builtin_inff() || (p.finished && p.finished[row])) return;
         if (x >= kLowest) {
             top = x;
             sum = 1.0;
@@ -306,16 +307,16 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
         p.sums[unit] = s;
     }
     if (lane < p.k) {
-        p.best_v[unit * p.k + lane] = list.v;
-        p.best_i[unit * p.k + lane] = (int32_t)list.i;
+        p.best_v[(int64_t)unit * p.k + lane] = list.v;
+        p.best_i[(int64_t)unit * p.k + lane] = (int32_t)list.i;
     }
 }
 
 // One workgroup a group: the rows' offsets score - log sum exp, then the k best of the pieces' lists.  What reaches the k-th largest of some
 // wave's lanes' largest is gathered, as a rule a few more than k, and every one of them counts those before it; where
 // too many reach it (or there are more than kMeetHeld), the waves keep lists as the pieces did.  Bound by its chain of dependent steps: one
-// group of 4 rows 5.9 us, 64 groups of 8 rows 8.6.
-constexpr int kMeetThreads = 256, kMeetHeld = 4096, kMeetGathered = 512;
+// group of 4 rows 5.2 us, 64 groups of 8 rows 7.0 (5.9 and 8.6 with each load where its value is needed).
+constexpr int kMeetThreads = 256, kMeetHeld = 4096, kMeetGathered = 512, kMeetEarly = 4;
 __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
 {
     __shared__ double off[FREEZE_MAX_BEAMS];     // -inf: nothing in the row
@@ -330,6 +331,16 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
     const int64_t row0 = (int64_t)blockIdx.x * p.beams;
     if (tid == 0) gathered = 0;
     const int per_row = p.parts * p.k, all = p.beams * per_row;
+    // A thread's first candidates are loaded before it is known whether their row has any, beside what tells that (an empty row's are
+    // whatever the workspace held, and passed over): one round trip in the place of four.
+    float early_v[kMeetEarly];
+    int32_t early_i[kMeetEarly];
+#pragma unroll
+    for (int e = 0; e < kMeetEarly; ++e) {
+        const int q = tid + e * kMeetThreads < all ? tid + e * kMeetThreads : all - 1;
+        early_v[e] = p.best_v[row0 * per_row + q];
+        early_i[e] = p.best_i[row0 * per_row + q];
+    }
     {
         // a row for as many threads as there are for each: a power of two of them, within a wave
         int per = 64;
@@ -339,16 +350,21 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
         const float score = in ? p.scores[row0 + j] : -__builtin_inff();
         const bool end = in && p.finished && p.finished[row0 + j];
         const bool open = !end && score > -__builtin_inff();
-        const float *tops = p.tops + (row0 + j) * p.parts;
-        const double *sums = p.sums + (row0 + j) * p.parts;
+        const float *tops = p.tops + (row0 + (in ? j : 0)) * p.parts;
+        const double *sums = p.sums + (row0 + (in ? j : 0)) * p.parts;
+        const int first = at < p.parts ? at : p.parts - 1;
+        const float first_top = tops[first];
+        const double first_sum = sums[first];
         float m = -__builtin_inff();
         if (open)
-            for (int q = at; q < p.parts; q += per) m = __builtin_fmaxf(m, tops[q]);
+            for (int q = at; q < p.parts; q += per) m = __builtin_fmaxf(m, q == at ? first_top : tops[q]);
         for (int x = per >> 1; x > 0; x >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, x, 64));
         double s = 0.0;
         if (open && m >= kLowest)
-            for (int q = at; q < p.parts; q += per)
-                if (tops[q] >= kLowest) s += sums[q] * exp((double)tops[q] - (double)m);
+            for (int q = at; q < p.parts; q += per) {
+                const float t = q == at ? first_top : tops[q];
+                if (t >= kLowest) s += (q == at ? first_sum : sums[q]) * exp((double)t - (double)m);
+            }
         for (int x = per >> 1; x > 0; x >>= 1) s += __shfl_xor(s, x, 64);
         if (in && at == 0) {
             off[j] = !open ? (double)score : (m >= kLowest ? (double)score - (double)m - log(s) : -__builtin_inf());
@@ -366,42 +382,51 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
         if (p.out_finished) p.out_finished[at] = token == p.end;
     };
     // candidate q of the group: what it is worth (-inf: none) and its place (row, token).  (Where a row is empty or has ended, no list was written.)
-    auto worth = [&](int q) {
+    auto worth = [&](int q, float v) {
         const int j = q / per_row;
-        const float v = p.best_v[row0 * per_row + q];
         const double o = off[j];
         if (ended[j]) return q == j * per_row ? o : -__builtin_inf();
         return o > -__builtin_inf() && v >= kLowest ? o + (double)v : -__builtin_inf();
     };
-    auto place = [&](int q) {
+    auto place = [&](int q, int32_t i) {
         const int j = q / per_row;
-        return ((uint64_t)j << 32) | (uint32_t)(ended[j] ? p.end : p.best_i[row0 * per_row + q]);
+        return ((uint64_t)j << 32) | (uint32_t)(ended[j] ? p.end : i);
     };
+    const float *const best_v = p.best_v + row0 * per_row;
+    const int32_t *const best_i = p.best_i + row0 * per_row;
     if (all <= kMeetHeld) {   // uniform
         double most = -__builtin_inf();
-#pragma unroll 1
-        for (int q = tid; q < all; q += kMeetThreads) {
-            const double c = worth(q);
+        auto hold = [&](int q, float v) {
+            const double c = worth(q, v);
             held[q] = c;
             most = c > most ? c : most;
-        }
+        };
+#pragma unroll
+        for (int e = 0; e < kMeetEarly; ++e)
+            if (tid + e * kMeetThreads < all) hold(tid + e * kMeetThreads, early_v[e]);
+#pragma unroll 1
+        for (int q = tid + kMeetEarly * kMeetThreads; q < all; q += kMeetThreads) hold(q, best_v[q]);
         // (in fp32, one step down: what it stands for is not more than the k-th largest)
         const float kth = kth_reached<6>((float)most, p.k);
         if (lane == 0) floors[wave] = kth;
         __syncthreads();
         const float f = __builtin_fmaxf(__builtin_fmaxf(floors[0], floors[1]), __builtin_fmaxf(floors[2], floors[3]));
         const double floor_v = f > kLowest ? (double)from_ordered_bits(ordered_bits(f) - 1) : -1.7976931348623157e308;
-#pragma unroll 1
-        for (int q = tid; q < all; q += kMeetThreads) {
+        auto gather = [&](int q, const int32_t *i) {
             const double c = held[q];
             if (c >= floor_v) {
                 const int at = atomicAdd(&gathered, 1);   // (their order does not matter)
                 if (at < kMeetGathered) {
                     list_v[at] = c;
-                    list_i[at] = place(q);
+                    list_i[at] = place(q, *i);
                 }
             }
-        }
+        };
+#pragma unroll
+        for (int e = 0; e < kMeetEarly; ++e)
+            if (tid + e * kMeetThreads < all) gather(tid + e * kMeetThreads, &early_i[e]);
+#pragma unroll 1
+        for (int q = tid + kMeetEarly * kMeetThreads; q < all; q += kMeetThreads) gather(q, &best_i[q]);
         __syncthreads();
         const int n = gathered;
         if (n <= kMeetGathered) {   // uniform
@@ -423,8 +448,8 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
     double floor_v = -1.7976931348623157e308;
     for (int base = wave * 64; base < all; base += kMeetThreads) {
         const int q = base + lane;
-        const double c = q < all ? worth(q) : -__builtin_inf();
-        const uint64_t ci = c >= floor_v ? place(q) : 0;
+        const double c = q < all ? worth(q, best_v[q]) : -__builtin_inf();
+        const uint64_t ci = c >= floor_v ? place(q, best_i[q]) : 0;
         uint64_t who = __ballot(c >= floor_v);
         while (who) {
             const int l = __ffsll((unsigned long long)who) - 1;
