@@ -727,28 +727,48 @@ class FreezeCache:
                           out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x: fp32 / bf16 rows, or codes with their scales."""
         m, d, _ = self.meta[slot]
+        b = x.shape[0]
         if out is None:
-            out = torch.empty((x.shape[0], m), dtype=out_dtype, device=self.device)
-        assert out.shape == (x.shape[0], m)
-        nbytes = freeze_quantised_workspace_bytes(self.ctx, slot, x.shape[0], _values_dtype(out))
+            out = torch.empty((b, m), dtype=out_dtype, device=self.device)
+        _here(x, scales, out)
+        assert out.shape == (b, m) and out.dtype in (torch.float32, torch.bfloat16)
+        if scales is None:
+            assert x.shape[1] == d and x.dtype in (torch.float32, torch.bfloat16)
+            stride = _rows_of(x)
+        else:
+            assert x.dtype == torch.float8_e4m3fn and x.is_contiguous() and x.shape == (b, -(-d // 128) * 128)
+            assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (b, -(-d // 512) * 4)
+            stride = 0
+        out_type = _values_dtype(out)
+        nbytes = lib().freeze_quantised_workspace_bytes(self.ctx, slot, b, out_type)
         if nbytes == 0:
             raise FreezeError(FREEZE_EINVAL, "freeze_quantised_workspace_bytes")
-        freeze_quantised_project(self.ctx, slot, x, scales, d, relu, out, self._workspace(nbytes))
+        ws = self._workspace(nbytes)
+        _check(lib().freeze_quantised_project(self.ctx, slot, x.data_ptr(), _values_dtype(x), _at(scales), b, stride, int(relu), out.data_ptr(),
+                                              out_type, _rows_of(out), ws.data_ptr(), ws.numel(), _on(None)), "freeze_quantised_project")
         return out
 
     def beam_select(self, logits: torch.Tensor, scores: torch.Tensor, beams: int, k: int, finished: Optional[torch.Tensor] = None,
                     end_token: int = -1) -> dict:
         """The k best continuations of every group of `beams` rows: score, token, parent (row), finished; each [groups, k]."""
-        groups = logits.shape[0] // beams
-        score, token, parent = torch.empty((3, groups, k), dtype=torch.int32, device=self.device).unbind(0)
-        out = dict(score=score.view(torch.float32), token=token, parent=parent,
-                   finished=torch.empty((groups, k), dtype=torch.uint8, device=self.device))
-        nbytes = freeze_beam_workspace_bytes(groups, beams, logits.shape[1], k)
+        rows, vocab = logits.shape
+        _here(logits, scores, finished)
+        assert rows % beams == 0 and scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
+        assert finished is None or (finished.dtype in (torch.uint8, torch.bool) and finished.is_contiguous() and finished.numel() == rows)
+        assert logits.dtype in (torch.float32, torch.bfloat16)
+        groups = rows // beams
+        nbytes = lib().freeze_beam_workspace_bytes(groups, beams, vocab, k)
         if nbytes == 0:
             raise FreezeError(FREEZE_EINVAL, "freeze_beam_workspace_bytes")
-        freeze_beam_select(logits, scores, finished, beams, end_token, k, out["score"], out["token"], out["parent"], out["finished"],
-                           self._workspace(nbytes))
-        return out
+        ws = self._workspace(nbytes)
+        words = torch.empty((3, groups, k), dtype=torch.int32, device=self.device)
+        ended = torch.empty((groups, k), dtype=torch.uint8, device=self.device)
+        at, size = words.data_ptr(), 4 * groups * k
+        _check(lib().freeze_beam_select(logits.data_ptr(), _values_dtype(logits), groups, beams, vocab, _rows_of(logits), scores.data_ptr(),
+                                        _at(finished), end_token, k, at, at + size, at + 2 * size, ended.data_ptr(), ws.data_ptr(), ws.numel(),
+                                        _on(None)), "freeze_beam_select")
+        score, token, parent = words.unbind(0)
+        return dict(score=score.view(torch.float32), token=token, parent=parent, finished=ended)
 
     def reorder_states(self, src, dst, parents: torch.Tensor, used: Optional[int] = None, row_dim: int = 0) -> None:
         """Row r of every dst becomes row parents[r] of its src (tensors or lists of tensors; see state_of)."""
