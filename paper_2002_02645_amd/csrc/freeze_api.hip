@@ -1380,16 +1380,24 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
     const size_t need = quant_bytes(pl, b, P->d);
     if (workspace_bytes < need || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
     const size_t xb = given ? (size_t)(b * quant_code_stride(P->d)) : (size_t)((b - 1) * x_stride + P->d) * (x_dtype == FREEZE_F32 ? 4 : 2);
-    if (share_bytes(workspace, need, out, (size_t)((b - 1) * out_stride + P->n) * out_size) || share_bytes(workspace, need, x, xb) ||
+    const size_t ob = (size_t)((b - 1) * out_stride + P->n) * out_size;
+    if (share_bytes(workspace, need, out, ob) || share_bytes(workspace, need, x, xb) ||
         (given && share_bytes(workspace, need, x_scales, (size_t)(b * quant_scale_stride(P->d)))))
         return FREEZE_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(stream);
     Carver ws(workspace);
     const QuantRows rows = take_rows(ws, b, P->d, pl.bm);
-    const hipError_t e = given ? launch_tile_codes(static_cast<const uint8_t *>(x), x_scales, b, P->d, rows, s)
-                               : launch_quantise_rows(x, x_dtype, b, P->d, x_stride, rows, s);
-    if (e != hipSuccess) return FREEZE_EHIP;
     QuantProduct q{};
+    // (values that the product quantises itself may not lie under its outputs)
+    if (!given && quant_takes_values(pl, x, x_dtype, b, P->d, x_stride) && !share_bytes(x, xb, out, ob)) {
+        q.raw = x;
+        q.raw_bf16 = x_dtype == FREEZE_BF16;
+        q.raw_stride = x_stride;
+        q.d = P->d;
+    } else if ((given ? launch_tile_codes(static_cast<const uint8_t *>(x), x_scales, b, P->d, rows, s)
+                      : launch_quantise_rows(x, x_dtype, b, P->d, x_stride, rows, s)) != hipSuccess) {
+        return FREEZE_EHIP;
+    }
     q.x = rows.codes;
     q.xs = rows.scales;
     q.w = P->codes;

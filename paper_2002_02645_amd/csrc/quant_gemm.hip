@@ -23,7 +23,6 @@ namespace fz {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((address_space(3))) void *lds_void_ptr;
@@ -201,16 +200,21 @@ __device__ __forceinline__ void tile_out(const QuantProduct &p, const f32x4 (&ac
 // weights come from: what counts is how many bytes are on their way.  Weights that one workgroup reads and that L2 cannot hold until the
 // next call pass it by: 134 MB (1 x 4,096 -> 32,768) in 21.2 us against 25.5, 1.07 GB (32 x 8,192 -> 131,072) in 172.7 against 190.7,
 // 6.2 - 6.9 TB/s.  Not so where tiles of x share them (300 rows of x: 25.1 us against 23.8), nor where L2 holds them: 16.8 MB 6.9 against 5.8.
-template <int WX, int WN, int XB, int NB, int NS>
+// RAW: the few rows of x are quantised by every workgroup for itself, for the k-steps it takes, while its first weights are on their way; they stay
+// in LDS as a whole.  As many as that holds: 1 x 4,096 -> 32,768 21.9 us a call, with a launch of its own for the row 24.3.
+constexpr int kRawBytes = 14336;   // beside four stages, twice in a CU
+constexpr int kRawSteps = kRawBytes / 129;   // k-steps of a row: 128 codes and a scale byte
+template <int WX, int WN, int XB, int NB, int NS, bool RAW = false>
 __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
 {
+    static_assert(!RAW || (WX == 1 && XB == 1), "one block of x rows");
     static_assert(WX * WN == 8, "eight waves");
     constexpr int BM = WX * XB * 16, BN = WN * NB * 16;
-    constexpr int kX = BN * 128, kS = kX + BM * 128, kStage = kS + (BN + (BM < 64 ? 64 : BM)) * 4;
-    constexpr int IW = BN / 64, LX = BM / 8, IX = (LX + 7) / 8;        // load instructions: of a wave, of all, of a wave
-    constexpr int LS = BN / 64 + (BM + 63) / 64, NL = IW + IX + 1;
-    static_assert(kQuantTile % BN == 0 && LS <= 8 && NS * kStage <= 163840 && (NS - 2) * NL <= 63, "");
-    __shared__ __attribute__((aligned(16))) unsigned char smem[NS * kStage];
+    constexpr int kX = BN * 128, kS = kX + (RAW ? 0 : BM * 128), kStage = kS + (BN + (RAW ? 0 : BM < 64 ? 64 : BM)) * 4;
+    constexpr int IW = BN / 64, LX = BM / 8, IX = RAW ? 0 : (LX + 7) / 8;        // load instructions: of a wave, of all, of a wave
+    constexpr int LS = BN / 64 + (RAW ? 0 : (BM + 63) / 64), NL = IW + IX + 1;
+    static_assert(kQuantTile % BN == 0 && LS <= 8 && NS * kStage + (RAW ? kRawBytes : 0) <= 163840 && (NS - 2) * NL <= 63, "");
+    __shared__ __attribute__((aligned(16))) unsigned char smem[NS * kStage + (RAW ? kRawBytes : 0)];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -234,6 +238,9 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
     const uint64_t gX = uniform_u64((uint64_t)(uintptr_t)(p.x + x0 * p.d_pad) + lx * 1024);
     const uint64_t gW = uniform_u64((uint64_t)(uintptr_t)(p.w + wbig * p.d_pad + win * 128) + w * 1024);
     const uint64_t gS = uniform_u64((uint64_t)(uintptr_t)(ls < BN / 64 ? p.ws + wbig * p.sd + win * 4 + ls * 256 : p.xs + x0 * p.sd + (ls - BN / 64) * 256));
+    const int steps = kb - ka;
+    const int rows = (int)(p.b < BM ? p.b : BM), own = rX < rows ? rX : rows - 1;   // RAW: one tile of x rows
+    unsigned char *const held = smem + NS * kStage, *const held_scales = held + rows * steps * 128;
     const uint32_t s_rows = ls < BN / 64 ? kQuantTile * 4 : BM * 4;
     auto issue = [&](int buf, int kt) {
         const uint32_t to = smem_base + buf * kStage;
@@ -257,6 +264,28 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
     const int klast = kb - 1;
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s) issue(s, ka + s < klast ? ka + s : klast);
+    if constexpr (RAW) {
+        // sixteen values a thread, eight threads a block; chunk c of row r at c ^ (r & 7)
+        const int per_row = steps * 8, n = rows * per_row;   // (a multiple of 8)
+        for (int t = tid; t < n; t += 512) {
+            const int r = t / per_row, chunk = t - r * per_row;
+            const int64_t c = (int64_t)ka * 128 + chunk * 16;
+            float v[16];
+            if (c >= p.d) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) v[e] = 0.f;
+            } else if (p.raw_bf16) {   // uniform
+                sixteen_of(static_cast<const uint16_t *>(p.raw) + r * p.raw_stride + c, v);
+            } else {
+                sixteen_of(static_cast<const float *>(p.raw) + r * p.raw_stride + c, v);
+            }
+            int ex;
+            const u32x4 codes = codes_of(v, &ex);
+            const int step = r * steps + (chunk >> 3);
+            *reinterpret_cast<u32x4 *>(held + step * 128 + ((chunk & 7) ^ (r & 7)) * 16) = codes;
+            if ((chunk & 7) == 0) held_scales[step] = (unsigned char)(ex + 127);
+        }
+    }
     int st = 0;
     for (int kt = ka; kt < kb; ++kt) {
         wait_global_loads_le<(NS - 2) * NL>();
@@ -269,7 +298,9 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
         const int sh = 8 * (kt & 3);
         float fx[XB], fw[NB];
 #pragma unroll
-        for (int i = 0; i < XB; ++i) fx[i] = __uint_as_float((sx[rX + 16 * i] >> sh & 255u) << 23);
+        for (int i = 0; i < XB; ++i)
+            fx[i] = __uint_as_float((RAW ? (uint32_t)held_scales[own * steps + kt - ka] : sx[rX + 16 * i] >> sh & 255u) << 23);
+        const u32x4 *const hx = reinterpret_cast<const u32x4 *>(held + (own * steps + kt - ka) * 128);
 #pragma unroll
         for (int j = 0; j < NB; ++j) fw[j] = __uint_as_float((sw[rW + 16 * j] >> sh & 255u) << 23);
 #pragma unroll
@@ -277,7 +308,7 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
             bf16x8 xa[2][XB];
 #pragma unroll
             for (int i = 0; i < XB; ++i) {
-                const u32x4 a = tx[(rX + 16 * i) * 8 + ((2 * g4 + h) ^ swX)];
+                const u32x4 a = RAW ? hx[(2 * g4 + h) ^ (own & 7)] : tx[(rX + 16 * i) * 8 + ((2 * g4 + h) ^ swX)];
                 xa[0][i] = widen8(a[0], a[1], fx[i]);
                 xa[1][i] = widen8(a[2], a[3], fx[i]);
             }
@@ -534,21 +565,22 @@ struct Variant {
     float step_us;   // of a k-step of a workgroup where neither memory nor L2 bounds it
     void (*kernel)(QuantProduct);
     bool narrow;     // the 8-bit form
+    void (*raw)(QuantProduct);   // the form that quantises its rows itself
 };
 const Variant kVariants[] = {
-    {16, 128, 2, 0.60f, quant_gemm_kernel<1, 8, 1, 1, 4>, false},
-    {32, 128, 2, 0.75f, quant_gemm_kernel<1, 8, 2, 1, 3>, false},
-    {64, 128, 2, 1.00f, quant_gemm_kernel<1, 8, 4, 1, 3>, false},
-    {16, 256, 1, 0.75f, quant_gemm_kernel<1, 8, 1, 2, 4>, false},
-    {32, 256, 1, 0.90f, quant_gemm_kernel<1, 8, 2, 2, 4>, false},
-    {64, 256, 1, 1.10f, quant_gemm_kernel<1, 8, 4, 2, 3>, false},
-    {128, 256, 1, 1.55f, quant_tile_kernel<false, 4>, false},
-    {160, 256, 1, 1.80f, quant_tile_kernel<false, 5>, false},
-    {192, 256, 1, 2.20f, quant_tile_kernel<false, 6>, false},
-    {256, 256, 1, 2.95f, quant_tile_kernel<false, 8>, false},
-    {128, 256, 1, 1.10f, quant_tile_kernel<true, 4>, true},
-    {192, 256, 1, 1.40f, quant_tile_kernel<true, 6>, true},
-    {256, 256, 1, 1.70f, quant_tile_kernel<true, 8>, true},
+    {16, 128, 2, 0.60f, quant_gemm_kernel<1, 8, 1, 1, 4>, false, quant_gemm_kernel<1, 8, 1, 1, 4, true>},
+    {32, 128, 2, 0.75f, quant_gemm_kernel<1, 8, 2, 1, 3>, false, nullptr},
+    {64, 128, 2, 1.00f, quant_gemm_kernel<1, 8, 4, 1, 3>, false, nullptr},
+    {16, 256, 1, 0.75f, quant_gemm_kernel<1, 8, 1, 2, 4>, false, quant_gemm_kernel<1, 8, 1, 2, 4, true>},
+    {32, 256, 1, 0.90f, quant_gemm_kernel<1, 8, 2, 2, 4>, false, nullptr},
+    {64, 256, 1, 1.10f, quant_gemm_kernel<1, 8, 4, 2, 3>, false, nullptr},
+    {128, 256, 1, 1.55f, quant_tile_kernel<false, 4>, false, nullptr},
+    {160, 256, 1, 1.80f, quant_tile_kernel<false, 5>, false, nullptr},
+    {192, 256, 1, 2.20f, quant_tile_kernel<false, 6>, false, nullptr},
+    {256, 256, 1, 2.95f, quant_tile_kernel<false, 8>, false, nullptr},
+    {128, 256, 1, 1.10f, quant_tile_kernel<true, 4>, true, nullptr},
+    {192, 256, 1, 1.40f, quant_tile_kernel<true, 6>, true, nullptr},
+    {256, 256, 1, 1.70f, quant_tile_kernel<true, 8>, true, nullptr},
 };
 }  // namespace
 
@@ -593,6 +625,13 @@ QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16,
     return pl;
 }
 
+bool quant_takes_values(const QuantPlan &pl, const void *x, int dtype, int64_t b, int64_t d, int64_t row_stride)
+{
+    const int64_t size = dtype == FREEZE_F32 ? 4 : 2;
+    return kVariants[pl.variant].raw && pl.x_tiles == 1 && b * ((pl.nk + pl.splits - 1) / pl.splits) <= kRawSteps && d % 16 == 0 &&
+           reinterpret_cast<uintptr_t>(x) % 16 == 0 && row_stride * size % 16 == 0;
+}
+
 hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t s)
 {
     p.nk = pl.nk;
@@ -604,7 +643,7 @@ hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t
     if (p.vec && p.out_stride % 8 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0) p.vec = 2;
     p.w_once = pl.x_tiles == 1 && p.m * p.d_pad > kL2Bytes;
     const Variant &v = kVariants[pl.variant];
-    hipLaunchKernelGGL(v.kernel, dim3((unsigned)pl.wgs), dim3(512), 0, s, p);
+    hipLaunchKernelGGL(p.raw ? v.raw : v.kernel, dim3((unsigned)pl.wgs), dim3(512), 0, s, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || pl.part == 0) return e;
     const int64_t tiles = (int64_t)pl.x_tiles * pl.w_tiles;
     hipLaunchKernelGGL(quant_sum_kernel, dim3((unsigned)(tiles * (pl.bm * pl.bn / 1024))), dim3(256), 0, s, p, pl.bm, pl.bn);

@@ -37,6 +37,62 @@ struct QuantRows {
     }
 };
 
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+
+// The exponent of a block from the bits of its largest magnitude 1.f * 2^(E - 127): 448 = 1.75 * 2^8, so 2^(E - 135),
+// or twice that where 1.f is above 1.75; not below 2^-126, so that both the factor and its inverse are normal numbers.
+__device__ __forceinline__ int block_exponent(uint32_t amax_bits)
+{
+    const int e = (int)(amax_bits >> 23) - 135 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return e < -126 ? -126 : e;
+}
+
+// sixteen values from a 16-byte boundary on
+__device__ __forceinline__ void sixteen_of(const float *src, float (&v)[16])
+{
+    u32x4 w[4];
+#pragma unroll
+    for (int l = 0; l < 4; ++l) w[l] = reinterpret_cast<const u32x4 *>(src)[l];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(w[e / 4][e % 4]);
+}
+__device__ __forceinline__ void sixteen_of(const uint16_t *src, float (&v)[16])
+{
+    u32x4 w[2];
+#pragma unroll
+    for (int l = 0; l < 2; ++l) w[l] = reinterpret_cast<const u32x4 *>(src)[l];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(e % 2 ? w[e / 8][e % 8 / 2] & 0xffff0000u : w[e / 8][e % 8 / 2] << 16);
+}
+
+// codes of sixteen values; eight neighbouring lanes hold a block
+__device__ __forceinline__ u32x4 codes_of(const float (&v)[16], int *exponent)
+{
+    uint32_t amax = 0;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const uint32_t u = __float_as_uint(v[e]) & 0x7fffffffu;
+        amax = u > amax ? u : amax;
+    }
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1) {
+        const uint32_t u = (uint32_t)__shfl_xor((int)amax, o, 8);
+        amax = u > amax ? u : amax;
+    }
+    const int ex = block_exponent(amax);
+    *exponent = ex;
+    const float inv = __uint_as_float((uint32_t)(127 - ex) << 23);
+    u32x4 codes;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        int q = 0;
+        q = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w] * inv, v[4 * w + 1] * inv, q, false);
+        q = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w + 2] * inv, v[4 * w + 3] * inv, q, true);
+        codes[w] = (uint32_t)q;
+    }
+    return codes;
+}
+
 // x [rows, d] (dtype: FREEZE_F32 or FREEZE_BF16) -> codes, scales
 hipError_t launch_quantise_rows(const void *x, int dtype, int64_t rows, int64_t d, int64_t row_stride, const QuantRows &out, hipStream_t s);
 // codes and scales row after row -> out, zeros behind d
@@ -52,6 +108,9 @@ struct QuantProduct {
     int out_bf16, relu;
     int vec;                 // 1: four outputs of a row from a multiple of four on are one aligned store; 2: and eight bf16 are
     int w_once;              // the weights are read by one workgroup each, and more than L2 holds
+    const void *raw;         // few rows straight from the caller's values (x, xs: not used); null: none
+    int raw_bf16;
+    int64_t raw_stride, d;
     float *part;             // plan's floats of scratch (none: null)
     int nk, x_tiles, w_tiles, splits;   // the plan's
 };
@@ -65,6 +124,8 @@ struct QuantPlan {
     size_t part;        // floats of the sums of cut tiles
 };
 QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16, int num_cus);
+// whether the product quantises its b rows itself
+bool quant_takes_values(const QuantPlan &pl, const void *x, int dtype, int64_t b, int64_t d, int64_t row_stride);
 hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t s);
 
 }  // namespace fz

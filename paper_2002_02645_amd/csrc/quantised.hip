@@ -4,17 +4,7 @@
 
 namespace fz {
 
-typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
-
 namespace {
-
-// The exponent of a block from the bits of its largest magnitude 1.f * 2^(E - 127): 448 = 1.75 * 2^8, so 2^(E - 135),
-// or twice that where 1.f is above 1.75; not below 2^-126, so that both the factor and its inverse are normal numbers.
-__device__ __forceinline__ int block_exponent(uint32_t amax_bits)
-{
-    const int e = (int)(amax_bits >> 23) - 135 + ((amax_bits & 0x7fffffu) > 0x600000u ? 1 : 0);
-    return e < -126 ? -126 : e;
-}
 
 // Sixteen values a thread (four loads of 16 bytes in fp32, two in bf16, one store), eight threads a block of 128.  Bound by memory:
 // 10,000 x 8,192 fp32 71 - 74 us, 5.5 - 5.8 TB/s read and written.  (A run of memory to each load, a block to 32 lanes: 74, 71 past the
@@ -29,14 +19,7 @@ __global__ __launch_bounds__(256) void quantise_rows_kernel(const T *x, int64_t 
         const T *src = x + r * row_stride + c;
         float v[16];
         if (VEC && c + 16 <= d) {
-            u32x4 w[16 / V];
-#pragma unroll
-            for (int l = 0; l < 16 / V; ++l) w[l] = reinterpret_cast<const u32x4 *>(src)[l];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                if constexpr (V == 4) v[e] = __uint_as_float(w[e / 4][e % 4]);
-                else v[e] = __uint_as_float(e % 2 ? w[e / 8][e % 8 / 2] & 0xffff0000u : w[e / 8][e % 8 / 2] << 16);
-            }
+            sixteen_of(src, v);
         } else {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -47,27 +30,8 @@ __global__ __launch_bounds__(256) void quantise_rows_kernel(const T *x, int64_t 
                 }
             }
         }
-        uint32_t amax = 0;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const uint32_t u = __float_as_uint(v[e]) & 0x7fffffffu;
-            amax = u > amax ? u : amax;
-        }
-#pragma unroll
-        for (int o = 4; o > 0; o >>= 1) {
-            const uint32_t u = (uint32_t)__shfl_xor((int)amax, o, 8);
-            amax = u > amax ? u : amax;
-        }
-        const int ex = block_exponent(amax);
-        const float inv = __uint_as_float((uint32_t)(127 - ex) << 23);
-        u32x4 codes;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            int q = 0;
-            q = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w] * inv, v[4 * w + 1] * inv, q, false);
-            q = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * w + 2] * inv, v[4 * w + 3] * inv, q, true);
-            codes[w] = (uint32_t)q;
-        }
+        int ex;
+        const u32x4 codes = codes_of(v, &ex);
         *reinterpret_cast<u32x4 *>(out.codes + out.code_at(r, c >> 4)) = codes;
         if ((c & 127) == 0) {
             const int64_t b = c >> 7;

@@ -316,6 +316,33 @@ def test_output_over_its_input():
         fc.close()
 
 
+@pytest.mark.parametrize("ot", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_few_rows_straight_from_values(dtype, ot):
+    # quantised within the product or before it: the same codes, so the same outputs bit by bit.  Sizes around what a workgroup holds (16 rows
+    # of 768 values, not 13 of 1,056), cut and whole depths, rows apart, rows off 16 bytes and odd depths (before it), output over x
+    fc = binding.FreezeCache(1)
+    try:
+        for b, d, m in [(1, 16, 1), (1, 128, 300), (1, 4096, 5000), (1, 14208, 700), (1, 14224, 33000), (1, 14464, 33000), (1, 40960, 33000), (2, 4096, 33000),
+                        (2, 7040, 33000), (2, 7168, 33000), (3, 4736, 33000), (7, 1936, 9000), (8, 1024, 40000), (13, 1056, 40000), (16, 768, 40000),
+                        (16, 1024, 40000), (1, 4100, 33000), (16, 16, 129)]:
+            w = torch.randn(m, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(d))
+            fc.build_quantised(0, w, torch.linspace(-1, 1, m, device="cuda"))
+            for pad in (0, 16, 3):
+                x = _inputs(b, d + pad, dtype, 50 + b).cuda()[:, pad:]
+                codes, scales = fc.quantise_rows(x)
+                want = fc.quantised_project(0, codes, scales, relu=True, out_dtype=ot)
+                got = fc.quantised_project(0, x, relu=True, out_dtype=ot)
+                assert torch.equal(got.view(torch.uint8), want.view(torch.uint8)), (b, d, m, pad)
+        x = torch.randn(2, 256, device="cuda").to(ot)
+        fc.build_quantised(0, torch.randn(256, 256, device="cuda"))
+        want = fc.quantised_project(0, x, out_dtype=ot)
+        fc.quantised_project(0, x, out=x)
+        assert torch.equal(x, want)
+    finally:
+        fc.close()
+
+
 def test_workspace_over_operands_is_refused():
     b, d, m = 50, 256, 256
     fc = binding.FreezeCache(1)
