@@ -353,9 +353,7 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
  *            and x_stride are not looked at).
  *   out      [b, m] out_dtype, out_stride elements from row to row (>= m); elements between rows are left as they
  *            are.  It may lie over x.
- *            FREEZE_F32: products are exact and summed in fp32.  FREEZE_BF16: larger batches go through the 8-bit matrix
- *            instructions, which cut the products of eight neighbouring elements off 13 bits below the largest of them
- *            before they are summed in fp32: less than the rounding of the output, but not what the fp32 output rounds to.
+ *            FREEZE_F32: products are exact and summed in fp32.  FREEZE_BF16: the same sums, rounded to nearest even once.
  *   workspace  freeze_quantised_workspace_bytes() bytes, 256-byte aligned; scratch only.  Calls that share a workspace (replays of
  *            captured ones too) must follow one another on the device.  It may not lie over x or out.
  * 1 <= m < 2^31 - 512, 0 <= b <= 2^30; b == 0 is a no-op.

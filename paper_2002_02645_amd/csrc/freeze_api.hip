@@ -1357,7 +1357,7 @@ size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t
     const LayerCache *P = get_quantised(ctx, slot, &err);
     if (!P || b < 0 || b > (int64_t)1 << 30 || (out_dtype != FREEZE_F32 && out_dtype != FREEZE_BF16)) return 0;
     if (b < 1) b = 1;
-    return quant_bytes(plan_quant_product(b, P->n, quant_code_stride(P->d), out_dtype == FREEZE_BF16, ctx->num_cus), b, P->d);
+    return quant_bytes(plan_quant_product(b, P->n, quant_code_stride(P->d), ctx->num_cus), b, P->d);
 }
 
 int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dtype, const uint8_t *x_scales, int64_t b, int64_t x_stride,
@@ -1376,7 +1376,7 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
     if (!x || !out || !workspace || given != (x_scales != nullptr) || !aligned(out, out_size) ||
         !aligned(x, given ? 16 : (x_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(x_scales, 4))
         return FREEZE_EINVAL;
-    const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), out_dtype == FREEZE_BF16, ctx->num_cus);
+    const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), ctx->num_cus);
     const size_t need = quant_bytes(pl, b, P->d);
     if (workspace_bytes < need || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
     const size_t xb = given ? (size_t)(b * quant_code_stride(P->d)) : (size_t)((b - 1) * x_stride + P->d) * (x_dtype == FREEZE_F32 ? 4 : 2);

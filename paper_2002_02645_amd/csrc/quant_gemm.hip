@@ -3,13 +3,11 @@
 //     y[r, c] = act(bias[c] + sum_B 2^(Ex[r, B] + Ew[c, B]) sum_{i in B} x8[r, i] w8[c, i])
 //
 // A k-step is a block of 128 codes: 128 bytes a row, copied as they are into LDS (direct loads) with the scale bytes of the four
-// blocks it belongs to; both operands are laid out so that a stage is a run of memory (QuantRows).  Two forms of the inner product:
-//   - fp32 outputs (and small tiles): codes widen to bf16 in registers, their scale applied by the same instruction, exactly;
-//     bf16 matrix instructions, exact products summed in fp32.
-//   - bf16 outputs of tiles of 256 rows (F8): the 8-bit matrix instructions with their scales, at twice the rate.  They cut the products
-//     of eight neighbours off 13 bits below the largest's exponent: measured against 64 bits 1.4e-5 of the result's
-//     norm on normal values, 8e-5 with a few channels far larger.  A bf16 output is rounded by 1.7e-3; an fp32 one is not
-//     worth its bits then, which is why it does not go this way.
+// blocks it belongs to; both operands are laid out so that a stage is a run of memory (QuantRows).  Codes widen to bf16 in registers, their
+// scale applied by the same instruction; bf16 matrix instructions, exact products summed in fp32.  (The 8-bit matrix instructions have twice the
+// rate, but cut the products of eight neighbours off 13 bits below the largest's exponent: up to 8e-5 of the result's norm, and where large terms
+// cancel nothing is left of the small ones.  Not even a bf16 output is worth its bits then: 2.9 % of them were a step off at
+// 4,096 x 2,048 -> 2,048.)
 // Work: the flattened (tile, k-step) space in ranges, whole tiles where they fill the chip, else even ranges whose cut tiles
 // leave their sums in slots, added in order by quant_sum_kernel.
 #include "../../include/freeze.h"
@@ -23,7 +21,6 @@ namespace fz {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(8))) int i32x8;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((address_space(3))) void *lds_void_ptr;
 
@@ -329,28 +326,20 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
 }
 
 // Larger batches, which the matrix pipes bound: tiles of 32 XB x rows by 256 w rows, eight waves of 16 XB x 64 outputs, two stages.  A wave
-// keeps its four blocks of w rows' fragments (16 rows each) for a step (8-bit form) or half a step (bf16 form, 64 codes) and goes through
-// its XB blocks of x rows, a group of matrix instructions each; their fragments are read kAhead groups ahead.  The step's barrier comes
+// keeps its four blocks of w rows' fragments (16 rows each) for half a step (64 codes) and goes through its XB blocks of x rows, a group of
+// matrix instructions each; their codes are read kAhead groups ahead.  The step's barrier comes
 // before its last kAhead groups, which need nothing newer: it publishes the next step's stage and frees this one, which is refilled from there on.
-// The 8-bit form, whose steps are half as long as what is loaded in them takes (133 us without matrix instructions, 216 with them, for
-// 4,096 x 8,192 -> 8,192), has another barrier where the step's w rows have been read: those of the step after the next are loaded in their place
-// before the x rows are free (208 us).
-// 10,000 x 8,192 -> 1,024 in the bf16 form 130 us, 1.29 PFLOP/s, the matrix pipes busy 55 % of all cycles; the square case in the 8-bit form 62 %,
-// 2.6 PFLOP/s.
-// (Four waves of 128 x 128 outputs read a third less out of LDS, but their sums fill a register file and the compiler moves them about: 290 us for
-// 4,096 x 8,192 -> 8,192 in the 8-bit form, 236 so.)
-template <bool F8, int XB>
+// 10,000 x 8,192 -> 1,024 130 us, 1.29 PFLOP/s, the matrix pipes busy 55 % of all cycles; 4,096 x 8,192 -> 8,192 with its quantisation 400 us, 1.37 PFLOP/s.
+template <int XB>
 __global__ __launch_bounds__(512, 2) void quant_tile_kernel(QuantProduct p)
 {
-    using frag = std::conditional_t<F8, i32x8, u32x4>;
     constexpr int BM = 32 * XB, BN = 256, NB = 4;
     static_assert(BN == kQuantTile, "a stage of the weights is a run of memory");
     constexpr int kX = BN * 128, kS = kX + BM * 128, kStage = kS + (BN + (BM + 63) / 64 * 64) * 4;
-    constexpr int kHalves = F8 ? 1 : 2, kGroups = kHalves * XB, kAhead = F8 ? 2 : 3;
-    constexpr int kRing = kGroups % 4 == 0 ? 4 : (kGroups % 3 == 0 && F8 ? 3 : (kGroups % 5 == 0 ? 5 : 6));   // fragments ahead, in step with the groups
+    constexpr int kGroups = 2 * XB, kAhead = 3;
+    constexpr int kRing = kGroups % 4 == 0 ? 4 : (kGroups % 5 == 0 ? 5 : 6);   // fragments ahead, in step with the groups
     constexpr int IW = BN / 64, LX = BM / 8, IX = (LX + 7) / 8, LS = BN / 64 + (BM + 63) / 64, NL = IW + IX + 1;   // load instructions: see above
-    constexpr int kFirst = F8 ? IW : 0, kPerGroup = (NL - kFirst + kAhead - 1) / kAhead;   // loads that the step's last groups issue
-    constexpr int kWRead = 1;   // 8-bit form: the group at whose start the step's w rows have been read
+    constexpr int kPerGroup = (NL + kAhead - 1) / kAhead;   // loads that each of the step's last groups issues
     static_assert(2 * kStage <= 163840 && kGroups % kRing == 0 && kRing > kAhead && LS <= 8, "");
     __shared__ __attribute__((aligned(16))) unsigned char smem[2 * kStage];
 
@@ -392,17 +381,9 @@ __global__ __launch_bounds__(512, 2) void quant_tile_kernel(QuantProduct p)
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    frag xr[kRing], wr[NB];    // of x, ahead; of w: 8-bit form, this step's; bf16 form, codes yet to be widened
+    u32x4 xr[kRing], wr[NB];   // codes yet to be widened: of x, ahead; of w
     uint32_t ex[kRing], ew[NB];   // with the scale bytes of their rows
-    auto read = [&](frag &to, const unsigned char *base, int row, int sw, int h) {
-        const u32x4 *t = reinterpret_cast<const u32x4 *>(base) + row * 8;
-        if constexpr (F8) {
-            const u32x4 a = t[(2 * g4) ^ sw], b = t[(2 * g4 + 1) ^ sw];
-            to = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
-        } else {
-            to = t[(2 * g4 + h) ^ sw];
-        }
-    };
+    auto read = [&](u32x4 &to, const unsigned char *base, int row, int sw, int h) { to = (reinterpret_cast<const u32x4 *>(base) + row * 8)[(2 * g4 + h) ^ sw]; };
     auto read_x = [&](int set, int buf, int i, int h) {
         read(xr[set], smem + buf * kStage + kX, rX + 16 * i, swX, h);
         ex[set] = *reinterpret_cast<const uint32_t *>(smem + buf * kStage + kS + (BN + rX + 16 * i) * 4);
@@ -425,108 +406,79 @@ __global__ __launch_bounds__(512, 2) void quant_tile_kernel(QuantProduct p)
     auto group_head = [&](int kt, int st, auto g_) {
         constexpr int g = decltype(g_)::value, ahead = g + kAhead;
         if constexpr (g == kGroups - kAhead) {
-            wait_global_loads_le<F8 ? IW : 0>();   // (the w rows of the step after the next are on their way)
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __syncthreads();
-        } else if constexpr (F8 && g == kWRead) {
+            wait_global_loads_le<0>();
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __syncthreads();
         }
-        read_x(ahead % kRing, ahead < kGroups ? st : st ^ 1, ahead % XB, ahead / XB % kHalves);
-        if constexpr (F8 && g == kWRead) each(std::make_integer_sequence<int, IW>{}, [&](auto l) { issue(st, at_most(kt + 2), l); });
+        read_x(ahead % kRing, ahead < kGroups ? st : st ^ 1, ahead % XB, ahead / XB % 2);
         if constexpr (g >= kGroups - kAhead)
             each(std::make_integer_sequence<int, kPerGroup>{}, [&](auto l) {
-                issue(st, at_most(kt + 2), std::integral_constant<int, kFirst + (g - kGroups + kAhead) * kPerGroup + decltype(l)::value>{});
+                issue(st, at_most(kt + 2), std::integral_constant<int, (g - kGroups + kAhead) * kPerGroup + decltype(l)::value>{});
             });
     };
     int st = 0;
-    if constexpr (F8) {
-        for (int kt = ka; kt < kb; ++kt) {
-            const int sh = 8 * (kt & 3);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) ew[j] >>= sh;
-            each(std::make_integer_sequence<int, XB>{}, [&](auto g_) {
-                constexpr int i = decltype(g_)::value;
-                group_head(kt, st, g_);
-                __builtin_amdgcn_sched_barrier(0);
-                const int e = (int)(ex[i % kRing] >> sh);
-                each(std::make_integer_sequence<int, NB>{}, [&](auto j_) {
-                    constexpr int j = decltype(j_)::value;
-                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wr[j], xr[i % kRing], acc[i][j], 0, 0, 0, (int)ew[j], 0, e);
-                    if constexpr (i == XB - 1) {   // the block's last use: the next step's takes its place
-                        read_w(st ^ 1, j, 0);
-                        read_ws(st ^ 1, j);
-                        __builtin_amdgcn_sched_barrier(0);
+    // Codes are widened between the matrix instructions of the group before, a word or two behind each: one after the other, the two kinds
+    // hardly overlap, not even those of a SIMD's two waves (measured: 8 matrix and 16 conversion instructions a wave 359 cycles in blocks,
+    // 307 interleaved, 295 without the conversions).
+    u32x4 wa[2][NB][2], xc[2][2];
+    const auto word = [](u32x4 &to, int half, uint32_t codes, uint32_t e) {
+        const u32x2 v = widen(codes, __uint_as_float(e));
+        to[2 * half] = v[0];
+        to[2 * half + 1] = v[1];
+    };
+    const auto scale = [](uint32_t e, int sh) { return (e >> sh & 255u) << 23; };
+    each(std::make_integer_sequence<int, 4 * NB>{}, [&](auto t_) {
+        constexpr int t = decltype(t_)::value;
+        word(wa[0][t / 4][t % 4 / 2], t % 2, wr[t / 4][t % 4], scale(ew[t / 4], 8 * (ka & 3)));
+    });
+    each(std::make_integer_sequence<int, 4>{}, [&](auto t_) {
+        constexpr int t = decltype(t_)::value;
+        word(xc[0][t / 2], t % 2, xr[0][t], scale(ex[0], 8 * (ka & 3)));
+    });
+    for (int kt = ka; kt < kb; ++kt) {
+        const int sh = 8 * (kt & 3), nsh = 8 * ((kt + 1) & 3);
+        each(std::make_integer_sequence<int, kGroups>{}, [&](auto g_) {
+            constexpr int g = decltype(g_)::value, h = g / XB, i = g % XB;
+            group_head(kt, st, g_);
+            // w blocks of the other half: of this step early in its first half, of the next one when its stage is there
+            if constexpr (g < 2) {
+                read_w(st, 2 * g, 1);
+                read_w(st, 2 * g + 1, 1);
+            } else if constexpr (g == kGroups - 3 || g == kGroups - 2) {
+                constexpr int j = 2 * (g - kGroups + 3);
+                read_w(st ^ 1, j, 0);
+                read_ws(st ^ 1, j);
+                read_w(st ^ 1, j + 1, 0);
+                read_ws(st ^ 1, j + 1);
+            }
+            // ... and those of them that are widened in this group: the first half ends with one a group (of four groups, the last takes two)
+            constexpr int late = XB == 4 ? 1 : XB - 4;
+            constexpr int w_first = h == 0 ? i - late : 2 * (g - kGroups + 2);
+            constexpr int w_count = h == 0 ? (i < late ? 0 : (XB == 4 && i == 3 ? 2 : 1)) : (g >= kGroups - 2 ? 2 : 0);
+            constexpr int words = 4 + 4 * w_count;
+            const uint32_t fx = scale(ex[(g + 1) % kRing], g + 1 < kGroups ? sh : nsh);
+            uint32_t fw[2];
+            each(std::make_integer_sequence<int, w_count>{}, [&](auto n) { fw[decltype(n)::value] = scale(ew[w_first + decltype(n)::value], h == 0 ? sh : nsh); });
+            __builtin_amdgcn_sched_barrier(0);
+            each(std::make_integer_sequence<int, 2 * NB>{}, [&](auto q_) {
+                constexpr int q = decltype(q_)::value, j = q % NB, half = q / NB;
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[h][j][half]), __builtin_bit_cast(bf16x8, xc[g & 1][half]),
+                                                                    acc[i][j], 0, 0, 0);
+                each(std::make_integer_sequence<int, words>{}, [&](auto t_) {
+                    constexpr int t = decltype(t_)::value;
+                    if constexpr (t * 2 * NB / words == q) {
+                        if constexpr (t < 4) {
+                            word(xc[(g + 1) & 1][t / 2], t % 2, xr[(g + 1) % kRing][t], fx);
+                        } else {
+                            constexpr int n = t - 4, wj = w_first + n / 4;
+                            word(wa[h ^ 1][wj][n % 4 / 2], n % 2, wr[wj][n % 4], fw[n / 4]);
+                        }
                     }
                 });
                 __builtin_amdgcn_sched_barrier(0);
             });
-            st ^= 1;
-        }
-    } else {
-        // Codes are widened between the matrix instructions of the group before, a word or two behind each: one after the other, the two kinds
-        // hardly overlap, not even those of a SIMD's two waves (measured: 8 matrix and 16 conversion instructions a wave 359 cycles in blocks,
-        // 307 interleaved, 295 without the conversions).
-        u32x4 wa[2][NB][2], xc[2][2];
-        const auto word = [](u32x4 &to, int half, uint32_t codes, uint32_t e) {
-            const u32x2 v = widen(codes, __uint_as_float(e));
-            to[2 * half] = v[0];
-            to[2 * half + 1] = v[1];
-        };
-        const auto scale = [](uint32_t e, int sh) { return (e >> sh & 255u) << 23; };
-        each(std::make_integer_sequence<int, 4 * NB>{}, [&](auto t_) {
-            constexpr int t = decltype(t_)::value;
-            word(wa[0][t / 4][t % 4 / 2], t % 2, wr[t / 4][t % 4], scale(ew[t / 4], 8 * (ka & 3)));
         });
-        each(std::make_integer_sequence<int, 4>{}, [&](auto t_) {
-            constexpr int t = decltype(t_)::value;
-            word(xc[0][t / 2], t % 2, xr[0][t], scale(ex[0], 8 * (ka & 3)));
-        });
-        for (int kt = ka; kt < kb; ++kt) {
-            const int sh = 8 * (kt & 3), nsh = 8 * ((kt + 1) & 3);
-            each(std::make_integer_sequence<int, kGroups>{}, [&](auto g_) {
-                constexpr int g = decltype(g_)::value, h = g / XB, i = g % XB;
-                group_head(kt, st, g_);
-                // w blocks of the other half: of this step early in its first half, of the next one when its stage is there
-                if constexpr (g < 2) {
-                    read_w(st, 2 * g, 1);
-                    read_w(st, 2 * g + 1, 1);
-                } else if constexpr (g == kGroups - 3 || g == kGroups - 2) {
-                    constexpr int j = 2 * (g - kGroups + 3);
-                    read_w(st ^ 1, j, 0);
-                    read_ws(st ^ 1, j);
-                    read_w(st ^ 1, j + 1, 0);
-                    read_ws(st ^ 1, j + 1);
-                }
-                // ... and those of them that are widened in this group: the first half ends with one a group (of four groups, the last takes two)
-                constexpr int late = XB == 4 ? 1 : XB - 4;
-                constexpr int w_first = h == 0 ? i - late : 2 * (g - kGroups + 2);
-                constexpr int w_count = h == 0 ? (i < late ? 0 : (XB == 4 && i == 3 ? 2 : 1)) : (g >= kGroups - 2 ? 2 : 0);
-                constexpr int words = 4 + 4 * w_count;
-                const uint32_t fx = scale(ex[(g + 1) % kRing], g + 1 < kGroups ? sh : nsh);
-                uint32_t fw[2];
-                each(std::make_integer_sequence<int, w_count>{}, [&](auto n) { fw[decltype(n)::value] = scale(ew[w_first + decltype(n)::value], h == 0 ? sh : nsh); });
-                __builtin_amdgcn_sched_barrier(0);
-                each(std::make_integer_sequence<int, 2 * NB>{}, [&](auto q_) {
-                    constexpr int q = decltype(q_)::value, j = q % NB, half = q / NB;
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, wa[h][j][half]), __builtin_bit_cast(bf16x8, xc[g & 1][half]),
-                                                                        acc[i][j], 0, 0, 0);
-                    each(std::make_integer_sequence<int, words>{}, [&](auto t_) {
-                        constexpr int t = decltype(t_)::value;
-                        if constexpr (t * 2 * NB / words == q) {
-                            if constexpr (t < 4) {
-                                word(xc[(g + 1) & 1][t / 2], t % 2, xr[(g + 1) % kRing][t], fx);
-                            } else {
-                                constexpr int n = t - 4, wj = w_first + n / 4;
-                                word(wa[h ^ 1][wj][n % 4 / 2], n % 2, wr[wj][n % 4], fw[n / 4]);
-                            }
-                        }
-                    });
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-            });
-            st ^= 1;
-        }
+        st ^= 1;
     }
     wait_global_loads_le<0>();   // the refills past the last k-step
     tile_out<XB, NB, BM, BN>(p, acc, u, rX, wn * 64, g4, x0, w0, x_last);
@@ -564,34 +516,29 @@ struct Variant {
     int bm, bn, per_cu;
     float step_us;   // of a k-step of a workgroup where neither memory nor L2 bounds it
     void (*kernel)(QuantProduct);
-    bool narrow;     // the 8-bit form
     void (*raw)(QuantProduct);   // the form that quantises its rows itself
 };
 const Variant kVariants[] = {
-    {16, 128, 2, 0.60f, quant_gemm_kernel<1, 8, 1, 1, 4>, false, quant_gemm_kernel<1, 8, 1, 1, 4, true>},
-    {32, 128, 2, 0.75f, quant_gemm_kernel<1, 8, 2, 1, 3>, false, nullptr},
-    {64, 128, 2, 1.00f, quant_gemm_kernel<1, 8, 4, 1, 3>, false, nullptr},
-    {16, 256, 1, 0.75f, quant_gemm_kernel<1, 8, 1, 2, 4>, false, quant_gemm_kernel<1, 8, 1, 2, 4, true>},
-    {32, 256, 1, 0.90f, quant_gemm_kernel<1, 8, 2, 2, 4>, false, nullptr},
-    {64, 256, 1, 1.10f, quant_gemm_kernel<1, 8, 4, 2, 3>, false, nullptr},
-    {128, 256, 1, 1.55f, quant_tile_kernel<false, 4>, false, nullptr},
-    {160, 256, 1, 1.80f, quant_tile_kernel<false, 5>, false, nullptr},
-    {192, 256, 1, 2.20f, quant_tile_kernel<false, 6>, false, nullptr},
-    {256, 256, 1, 2.95f, quant_tile_kernel<false, 8>, false, nullptr},
-    {128, 256, 1, 1.10f, quant_tile_kernel<true, 4>, true, nullptr},
-    {192, 256, 1, 1.40f, quant_tile_kernel<true, 6>, true, nullptr},
-    {256, 256, 1, 1.70f, quant_tile_kernel<true, 8>, true, nullptr},
+    {16, 128, 2, 0.60f, quant_gemm_kernel<1, 8, 1, 1, 4>, quant_gemm_kernel<1, 8, 1, 1, 4, true>},
+    {32, 128, 2, 0.75f, quant_gemm_kernel<1, 8, 2, 1, 3>, nullptr},
+    {64, 128, 2, 1.00f, quant_gemm_kernel<1, 8, 4, 1, 3>, nullptr},
+    {16, 256, 1, 0.75f, quant_gemm_kernel<1, 8, 1, 2, 4>, quant_gemm_kernel<1, 8, 1, 2, 4, true>},
+    {32, 256, 1, 0.90f, quant_gemm_kernel<1, 8, 2, 2, 4>, nullptr},
+    {64, 256, 1, 1.10f, quant_gemm_kernel<1, 8, 4, 2, 3>, nullptr},
+    {128, 256, 1, 1.55f, quant_tile_kernel<4>, nullptr},
+    {160, 256, 1, 1.80f, quant_tile_kernel<5>, nullptr},
+    {192, 256, 1, 2.20f, quant_tile_kernel<6>, nullptr},
+    {256, 256, 1, 2.95f, quant_tile_kernel<8>, nullptr},
 };
 }  // namespace
 
-QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16, int num_cus)
+QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, int num_cus)
 {
     QuantPlan pl{};
     pl.nk = (int)(d_pad / kQuantBlock);
     double best = 0;
     for (int i = 0; i < (int)(sizeof kVariants / sizeof kVariants[0]); ++i) {
         const Variant &v = kVariants[i];
-        if (v.narrow && !out_bf16) continue;
         const int64_t xt = (b + v.bm - 1) / v.bm, wt = (m + v.bn - 1) / v.bn, tiles = xt * wt, places = (int64_t)num_cus * v.per_cu;
         // whole tiles, or each cut along the depth so that a quarter or half a round of workgroups, or one to four rounds are full, with the
         // sums through memory (written and read at 2.5 TB/s, and a launch)

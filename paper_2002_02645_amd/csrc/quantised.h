@@ -123,7 +123,7 @@ struct QuantPlan {
     int64_t wgs;
     size_t part;        // floats of the sums of cut tiles
 };
-QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, bool out_bf16, int num_cus);
+QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, int num_cus);
 // whether the product quantises its b rows itself
 bool quant_takes_values(const QuantPlan &pl, const void *x, int dtype, int64_t b, int64_t d, int64_t row_stride);
 hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t s);

@@ -1,0 +1,46 @@
+"""What numbers the dense layer in 8 bits gives: sums that cancel, bf16 outputs, infinities and no numbers, the smallest values."""
+import pytest
+import torch
+
+from paper_2002_02645_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+
+def _noise(rows, d, seed):
+    return torch.randn(rows, d, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+@pytest.mark.parametrize("b,d,m", [(1, 4096, 1000), (40, 1000, 131), (150, 700, 259), (300, 1100, 258), (1100, 1024, 1040), (2500, 1152, 1032),
+                                   (1000, 515, 4104), (4096, 2048, 2048)])
+@pytest.mark.parametrize("relu", [False, True])
+def test_bf16_outputs_are_the_fp32_ones_rounded(b, d, m, relu):
+    x, w = _noise(b, d, b + d) * torch.where(_noise(1, d, 5).abs() > 2.3, 20.0, 1.0), _noise(m, d, m) / d ** 0.5
+    fc = binding.FreezeCache(1)
+    try:
+        fc.build_quantised(0, w, torch.linspace(-1, 1, m, device="cuda"))
+        want = fc.quantised_project(0, x, relu=relu).to(torch.bfloat16)
+        got = fc.quantised_project(0, x, relu=relu, out_dtype=torch.bfloat16)
+        assert torch.equal(got, want), (got != want).float().mean().item()
+    finally:
+        fc.close()
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_sums_that_cancel(out):
+    # Each output: neighbours 1 and -1 times 448, which cancel, beside products of 2^-9 * k: whole numbers of 2^-9 below 2^24, so that every
+    # order of fp32 sums of exact products gives them without rounding
+    b, d, m = 4096, 512, 2048
+    x = torch.zeros(b, d, device="cuda")
+    x[:, 0::8], x[:, 1::8] = 448.0, -448.0
+    x[:, 2::8] = 2.0 ** -9 * (1 + torch.arange(b, device="cuda") % 7).view(-1, 1)
+    w = torch.zeros(m, d, device="cuda")
+    w[:, 0::8], w[:, 1::8], w[:, 2::8] = 1.0, 1.0, 1.0
+    w[:, 3] = 448.0   # (x: zero) every block's exponent is 0
+    want = (x.double() @ w.double().t().contiguous()).to(out)
+    fc = binding.FreezeCache(1)
+    try:
+        fc.build_quantised(0, w)
+        assert torch.equal(fc.quantised_project(0, x, out_dtype=out), want)
+    finally:
+        fc.close()
