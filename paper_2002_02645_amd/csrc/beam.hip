@@ -21,6 +21,7 @@
 namespace fz {
 
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef u32x4 __attribute__((aligned(1))) u32x4_any;   // loads of it need no alignment
 
 namespace {
 
@@ -119,19 +120,18 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     if (unit >= (uint32_t)p.rows * (uint32_t)p.parts) return;   // uniform in the wave
     const int row = (int)(unit / (uint32_t)p.parts), part = (int)(unit - (uint32_t)row * (uint32_t)p.parts);
     const T *src = static_cast<const T *>(p.logits) + (int64_t)row * p.row_stride;
-    // Groups of V values on 16-byte boundaries.  The row's first and last ones may reach over its ends: their values come one by one, the
-    // whole groups [f0, f1) of the piece in batches.  Of a batch that reaches past f1 the last group is loaded again and put out of the way:
+    // Groups of V values from the row's first one on, wherever it lies: which values are summed together goes by their place in the row alone, so that
+    // rows that are alike have the same sum to the last bit.  The row's last values, less than a group, come one by one, the
+    // whole groups [g0, f1) of the piece in batches.  Of a batch that reaches past f1 the last group is loaded again and put out of the way:
     // loads that no branch decides about, so that a batch is on its way while the one before is looked at.
-    const int64_t shift = (int64_t)((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
-    const int64_t all = (p.vocab + shift + V - 1) / V;
+    const int64_t all = (p.vocab + V - 1) / V, full = p.vocab / V;
     const int64_t g0 = part * p.groups_per_part, g1 = g0 + p.groups_per_part < all ? g0 + p.groups_per_part : all;
-    const int64_t full = (p.vocab + shift) / V;
-    const int64_t f0 = g0 == 0 && shift > 0 ? 1 : g0, f1 = g1 < full ? g1 : full;
+    const int64_t f1 = g1 < full ? g1 : full;
     auto load = [&](int64_t base, u32x4(&raw)[kBeamLoads]) {   // base < f1
-        const T *at = src + (base * V - shift);
+        const T *at = src + base * V;
         const int last = (int)(f1 - base < 64 * kBeamLoads ? f1 - base : 64 * kBeamLoads) - 1;
 #pragma unroll
-        for (int l = 0; l < kBeamLoads; ++l) raw[l] = *reinterpret_cast<const u32x4 *>(at + (l * 64 + lane < last ? l * 64 + lane : last) * V);
+        for (int l = 0; l < kBeamLoads; ++l) raw[l] = *reinterpret_cast<const u32x4_any *>(at + (l * 64 + lane < last ? l * 64 + lane : last) * V);
     };
     auto value = [](const u32x4 *raw, int e) {
         const uint32_t w = raw[e / V][(e % V) * 4 / V];
@@ -164,15 +164,14 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     double sum = 0.0;   // (in fp32 a large value in front would take hundreds of batches of small ones in without a trace)
     u32x4 next[kBeamLoads];
     {
-        // the ends: lanes 0 .. 7 before the whole groups, 8 .. 15 behind them (of a row within one group all are before)
-        const int64_t i = lane < 8 ? (g0 == 0 && shift > 0 && lane < V - shift ? lane : p.vocab)
-                                   : (lane < 16 && full >= g0 && full < g1 && (full > 0 || shift == 0) ? full * V - shift + lane - 8 : p.vocab);
+        // the values behind the whole groups
+        const int64_t i = lane < V && full >= g0 && full < g1 ? full * V + lane : p.vocab;
         float x = -__builtin_inff();
         if (i < p.vocab) {
             if constexpr (sizeof(T) == 4) x = src[i];
             else x = __uint_as_float((uint32_t)src[i] << 16);
         }
-        if (f0 < f1) load(f0, next);
+        if (g0 < f1) load(g0, next);
         // (with the first loads on their way: an empty row or one that has ended has nothing to choose from)
         if (p.scores[row] == -__builtin_inff() || (p.finished && p.finished[row])) return;
         if (x >= kLowest) {
@@ -187,7 +186,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 #pragma unroll
         for (int l = 0; l < kBeamLoads; ++l) {
             const bool in = mine & (g + l * 64 < f1);
-            const uint32_t i = (uint32_t)((g + l * 64) * V - shift);
+            const uint32_t i = (uint32_t)((g + l * 64) * V);
             uint64_t who[V];   // (compared all at once; equals behind the k-th best fall out below)
 #pragma unroll
             for (int e = 0; e < V; ++e) who[e] = __ballot(in & (value(raw, l * V + e) >= floor_v));
@@ -235,7 +234,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
                 for (int l = 0; l < kBeamLoads; ++l) raw[l] = last[l];
             } else {
                 for (; q < n && held < 64; ++q) {
-                    const bool pass = may(run_most[wave][q][lane], (uint32_t)((base + q * (64 * kBeamLoads) + lane) * V - shift));
+                    const bool pass = may(run_most[wave][q][lane], (uint32_t)((base + q * (64 * kBeamLoads) + lane) * V));
                     const uint64_t who = __ballot(pass);
                     if (pass) run_lane[wave][held + lanes_before(who)] = (uint16_t)(q * 64 + lane);
                     held += __popcll(who);
@@ -245,7 +244,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
                 const uint32_t at = mine ? run_lane[wave][lane] : 0;
                 g = base + (int64_t)(at >> 6) * (64 * kBeamLoads) + (at & 63);
 #pragma unroll
-                for (int l = 0; l < kBeamLoads; ++l) raw[l] = *reinterpret_cast<const u32x4 *>(src + ((g + l * 64 < f1 ? g + l * 64 : f1 - 1) * V - shift));
+                for (int l = 0; l < kBeamLoads; ++l) raw[l] = *reinterpret_cast<const u32x4_any *>(src + (g + l * 64 < f1 ? g + l * 64 : f1 - 1) * V);
                 held = held > 64 ? held - 64 : 0;
                 if (lane < held) run_lane[wave][lane] = run_lane[wave][64 + lane];
             }
@@ -255,7 +254,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     int in_run = 0;
     float most_run = -__builtin_inff();
     u32x4 raw[kBeamLoads];
-    for (int64_t base = f0; base < f1; base += 64 * kBeamLoads) {
+    for (int64_t base = g0; base < f1; base += 64 * kBeamLoads) {
 #pragma unroll
         for (int l = 0; l < kBeamLoads; ++l) raw[l] = next[l];
         load(base + 64 * kBeamLoads < f1 ? base + 64 * kBeamLoads : base, next);
@@ -483,7 +482,7 @@ struct BeamPlan {
 BeamPlan beam_plan(int64_t rows, int64_t vocab, int size)
 {
     const int64_t v = 16 / size, batch = 64 * kBeamLoads;
-    const int64_t batches = ((vocab + v - 1 + v - 1) / v + batch - 1) / batch;   // (a misaligned row's groups are one more)
+    const int64_t batches = ((vocab + v - 1) / v + batch - 1) / batch;
     int64_t parts = (12 * 256 + rows - 1) / rows;
     parts = parts < 1 ? 1 : (parts > batches ? batches : parts);
     BeamPlan pl;
@@ -520,7 +519,6 @@ struct ReorderArgs {
 
 // A run is copied by windows: the 16-byte places of dst that it touches, the first and the last in part (byte by byte).  A whole one is one
 // load, aligned or not, and one aligned store.
-typedef u32x4 __attribute__((aligned(1))) u32x4_any;
 __device__ __forceinline__ void copy_part(uint8_t *dst, const uint8_t *src, int64_t bytes, int64_t from)
 {
     for (int64_t i = from < 0 ? 0 : from; i < from + 16 && i < bytes; ++i) dst[i] = src[i];
