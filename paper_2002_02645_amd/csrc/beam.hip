@@ -274,14 +274,15 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
             top = most;
         }
         if (top >= kLowest) {
-            // l log2(e) - top log2(e) in one rounding, which goes by the difference; what the subtrahend lost by its own is given back to the sum
+            // l log2(e) - top log2(e) in one rounding, which goes by the difference; what the subtrahend lost by its own is given back to the sum:
+            // half a step of it, which has to stay far below the exponents of fp32 (beyond 2^31 the powers overflow)
             const float t = top * kLog2E, lost = __builtin_fmaf(top, kLog2E, -t);
             float part_sum[2] = {0.f, 0.f};
-            if (__builtin_fabsf(top) < 1e38f) {
+            if (__builtin_fabsf(top) < 8388608.f) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) part_sum[e & 1] += __builtin_amdgcn_exp2f(__builtin_fmaf(value(raw, e), kLog2E, -t));
                 sum += (double)((part_sum[0] + part_sum[1]) * __builtin_amdgcn_exp2f(-lost));
-            } else {   // (the product overflows)
+            } else {
 #pragma unroll
                 for (int e = 0; e < E; ++e) part_sum[0] += __builtin_amdgcn_exp2f((value(raw, e) - top) * kLog2E);
                 sum += (double)part_sum[0];

@@ -60,3 +60,15 @@ def test_rows_alike(vocab, dtype):
     wide = torch.zeros(8, vocab + 9, dtype=dtype, device="cuda")
     wide[:, 3:3 + vocab] = rows[:1]
     _run(wide[:, 3:3 + vocab], torch.zeros(8, device="cuda"), 8, 16)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("size", [1e7, 3e9, 1e10])
+def test_values_far_from_zero(size, dtype):
+    # 50,021 values of 1e7 and more away from zero, some of them alike: a row is worth its score and the log of a share of its sum
+    g = torch.Generator().manual_seed(8)
+    for sign in (1, -1):
+        x = sign * size * (1 + torch.rand(8, 50021, generator=g))
+        for r in range(8):
+            x[r, torch.randint(0, 50021, (3,), generator=g)] = x[r].max()
+        _run(x.to(dtype).cuda(), -torch.rand(8, generator=g).cuda(), 4, 9)
