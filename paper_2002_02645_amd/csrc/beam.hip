@@ -312,14 +312,15 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     }
 }
 
-// One workgroup a group: the rows' offsets score - log sum exp, then the k best of the pieces' lists.  What reaches the k-th largest of some
+// One workgroup a group: the rows' offsets score - log sum exp(l - largest l), then the k best of the pieces' lists.  What reaches the k-th largest of some
 // wave's lanes' largest is gathered, as a rule a few more than k, and every one of them counts those before it; where
 // too many reach it (or there are more than kMeetHeld), the waves keep lists as the pieces did.  Bound by its chain of dependent steps: one
 // group of 4 rows 5.2 us, 64 groups of 8 rows 7.0 (5.9 and 8.6 with each load where its value is needed).
 constexpr int kMeetThreads = 256, kMeetHeld = 4096, kMeetGathered = 512, kMeetEarly = 4;
 __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
 {
-    __shared__ double off[FREEZE_MAX_BEAMS];     // -inf: nothing in the row
+    __shared__ double off[FREEZE_MAX_BEAMS];     // score - log sum exp(l - largest l); -inf: nothing in the row
+    __shared__ float largest[FREEZE_MAX_BEAMS];
     __shared__ uint8_t ended[FREEZE_MAX_BEAMS];
     __shared__ double list_v[kMeetGathered];
     __shared__ uint64_t list_i[kMeetGathered];
@@ -367,7 +368,8 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
             }
         for (int x = per >> 1; x > 0; x >>= 1) s += __shfl_xor(s, x, 64);
         if (in && at == 0) {
-            off[j] = !open ? (double)score : (m >= kLowest ? (double)score - (double)m - log(s) : -__builtin_inf());
+            off[j] = !open ? (double)score : (m >= kLowest ? (double)score - log(s) : -__builtin_inf());
+            largest[j] = m;
             ended[j] = end;
         }
     }
@@ -386,7 +388,8 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
         const int j = q / per_row;
         const double o = off[j];
         if (ended[j]) return q == j * per_row ? o : -__builtin_inf();
-        return o > -__builtin_inf() && v >= kLowest ? o + (double)v : -__builtin_inf();
+        // (the difference first: a score beside a value far from zero would be lost, and a row of nothing but the type's lowest would be worth 0)
+        return o > -__builtin_inf() && v >= kLowest ? o + ((double)v - (double)largest[j]) : -__builtin_inf();
     };
     auto place = [&](int q, int32_t i) {
         const int j = q / per_row;

@@ -71,9 +71,9 @@ def beam_select(logits, scores, finished, beams, end, k):
             x = logits[r]
             if not (x > -np.inf).any():
                 continue
-            lse = x.max() + np.log(np.exp(x - x.max()).sum())
+            offset = scores[r] - np.log(np.exp(x - x.max()).sum())   # (beside x.max() itself a score would be lost where that is far from zero)
             best = np.lexsort((np.arange(vocab), -x))[:k]
-            cand += [(scores[r] + x[v] - lse, r, int(v)) for v in best if x[v] > -np.inf]
+            cand += [(offset + (x[v] - x.max()), r, int(v)) for v in best if x[v] > -np.inf]
         cand.sort(key=lambda c: (-c[0], c[1], c[2]))
         cand = cand[:k]
         out.append(cand + [(-np.inf, g * beams, max(end, 0))] * (k - len(cand)))

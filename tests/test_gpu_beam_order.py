@@ -63,7 +63,7 @@ def test_rows_alike(vocab, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("size", [1e7, 3e9, 1e10])
+@pytest.mark.parametrize("size", [1e7, 3e9, 1e10, 1e20, 1e37, 1e38])
 def test_values_far_from_zero(size, dtype):
     # 50,021 values of 1e7 and more away from zero, some of them alike: a row is worth its score and the log of a share of its sum
     g = torch.Generator().manual_seed(8)
@@ -72,3 +72,15 @@ def test_values_far_from_zero(size, dtype):
         for r in range(8):
             x[r, torch.randint(0, 50021, (3,), generator=g)] = x[r].max()
         _run(x.to(dtype).cuda(), -torch.rand(8, generator=g).cuda(), 4, 9)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("fill", ["lowest", "highest", "lowest_and_few"])
+def test_rows_of_the_type_s_ends(fill, dtype):
+    # a row whose every value is the mark of a forbidden token: all tokens alike, none of them better than the other rows' best
+    x = _noise(12, 5003, 6).to(dtype)
+    info = torch.finfo(dtype)
+    if fill == "lowest_and_few":
+        x[torch.rand(x.shape, generator=torch.Generator().manual_seed(1)) < 0.999] = info.min
+    x[1] = x[6] = info.max if fill == "highest" else info.min
+    _run(x.cuda(), -torch.arange(12).float().cuda() / 8, 4, 12)
