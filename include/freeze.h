@@ -372,7 +372,7 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
  * holds the output layer's values for every token of the vocabulary and has a score so far.  A continuation (row j, token v)
  * is worth
  *     scores[j] + logits[j, v] - log sum_u exp logits[j, u]
- * and the k best continuations of each group are returned, best first; equal ones: lower row, then lower token.
+ * and the k best continuations of each group are returned, best first; equal ones: lower row, larger value, lower token.
  *   logits    [groups * beams, vocab] fp32 or bf16, row_stride elements from row to row.  -inf: the token is forbidden
  *             (any number of them, whole rows too).  Other values must be finite.
  *   scores    [groups * beams] fp32; -inf: an empty row, whose logits are not looked at.

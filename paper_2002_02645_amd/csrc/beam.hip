@@ -44,12 +44,25 @@ struct BeamArgs {
     uint8_t *out_finished;
 };
 
+// Where a continuation stands among those that are worth the same: the lower row first, in a row the larger value, then the lower token.
+struct Place {
+    uint64_t key;     // from the top: 6 bits of the row, 32 of the value in falling order, the token without its last 5
+    uint32_t token;
+    static __device__ __forceinline__ Place of(uint32_t row, float v, uint32_t token)
+    {
+        return Place{((uint64_t)row << 58) | ((uint64_t)~ordered_bits(v) << 26) | (token >> 5), token};   // (a token has 31 bits)
+    }
+    __device__ __forceinline__ uint32_t row() const { return (uint32_t)(key >> 58); }
+    __device__ __forceinline__ bool operator<(const Place &o) const { return (key < o.key) | ((key == o.key) & (token < o.token)); }
+};
+static_assert(FREEZE_MAX_BEAMS <= 64, "a row in 6 bits");
+
 // The wave's k best so far, one a lane, in order.
 template <typename V, typename I>
 struct BestList {
     V v;
     I i;
-    __device__ __forceinline__ void clear(V lowest) { v = lowest; i = (I)-1; }   // (unsigned: the largest index)
+    __device__ __forceinline__ void clear(V lowest, I last) { v = lowest; i = last; }
     __device__ __forceinline__ bool before(V cv, I ci) const { return (v > cv) | ((v == cv) & (i < ci)); }
 };
 // the value of lane l, which is the same in all lanes
@@ -60,6 +73,7 @@ __device__ __forceinline__ uint64_t of_lane(uint64_t x, int l)
     return (uint64_t)of_lane((uint32_t)x, l) | ((uint64_t)of_lane((uint32_t)(x >> 32), l) << 32);
 }
 __device__ __forceinline__ double of_lane(double x, int l) { return __longlong_as_double((long long)of_lane((uint64_t)__double_as_longlong(x), l)); }
+__device__ __forceinline__ Place of_lane(Place x, int l) { return Place{of_lane(x.key, l), of_lane(x.token, l)}; }
 // the value of the lane before (lane 0: its own)
 __device__ __forceinline__ uint32_t of_previous(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp((int)x, (int)x, 0x138, 0xf, 0xf, false); }   // wave_shr:1
 __device__ __forceinline__ float of_previous(float x) { return __uint_as_float(of_previous(__float_as_uint(x))); }
@@ -68,6 +82,7 @@ __device__ __forceinline__ uint64_t of_previous(uint64_t x)
     return (uint64_t)of_previous((uint32_t)x) | ((uint64_t)of_previous((uint32_t)(x >> 32)) << 32);
 }
 __device__ __forceinline__ double of_previous(double x) { return __longlong_as_double((long long)of_previous((uint64_t)__double_as_longlong(x))); }
+__device__ __forceinline__ Place of_previous(Place x) { return Place{of_previous(x.key), of_previous(x.token)}; }
 
 // inserts (cv, ci), the same in all lanes; false where k others are before it
 template <typename V, typename I>
@@ -140,7 +155,7 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
     };
 
     BestList<float, uint32_t> list;
-    list.clear(-__builtin_inff());
+    list.clear(-__builtin_inff(), ~0u);
     // what a value has to be before, or the same: the k-th best so far, or a value that k others reach
     float floor_v = kLowest;
     uint32_t floor_i = ~0u;
@@ -323,7 +338,8 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
     __shared__ float largest[FREEZE_MAX_BEAMS];
     __shared__ uint8_t ended[FREEZE_MAX_BEAMS];
     __shared__ double list_v[kMeetGathered];
-    __shared__ uint64_t list_i[kMeetGathered];
+    __shared__ uint64_t list_key[kMeetGathered];   // (the parts of a Place)
+    __shared__ uint32_t list_token[kMeetGathered];
     __shared__ double held[kMeetHeld];
     __shared__ float floors[kMeetThreads / 64];
     __shared__ int gathered;
@@ -374,13 +390,13 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
         }
     }
     __syncthreads();
-    auto put = [&](int64_t place, double v, uint64_t i) {
+    auto put = [&](int64_t place, double v, Place i) {
         const bool some = v > -__builtin_inf();
-        const int32_t token = some ? (int32_t)(uint32_t)i : (p.end > 0 ? p.end : 0);
+        const int32_t token = some ? (int32_t)i.token : (p.end > 0 ? p.end : 0);
         const int64_t at = (int64_t)blockIdx.x * p.k + place;
         p.out_scores[at] = some ? (float)v : -__builtin_inff();
         p.out_tokens[at] = token;
-        p.out_parents[at] = (int32_t)(row0 + (some ? (int64_t)(i >> 32) : 0));
+        p.out_parents[at] = (int32_t)(row0 + (some ? (int64_t)i.row() : 0));
         if (p.out_finished) p.out_finished[at] = token == p.end;
     };
     // candidate q of the group: what it is worth (-inf: none) and its place (row, token).  (Where a row is empty or has ended, no list was written.)
@@ -391,9 +407,10 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
         // (the difference first: a score beside a value far from zero would be lost, and a row of nothing but the type's lowest would be worth 0)
         return o > -__builtin_inf() && v >= kLowest ? o + ((double)v - (double)largest[j]) : -__builtin_inf();
     };
-    auto place = [&](int q, int32_t i) {
+    // (totals that are equal need not have equal values: beside a score of -1e30 no value shows.  A zero counts as one, whatever its sign.)
+    auto place = [&](int q, float v, int32_t i) {
         const int j = q / per_row;
-        return ((uint64_t)j << 32) | (uint32_t)(ended[j] ? p.end : i);
+        return Place::of((uint32_t)j, v + 0.f, (uint32_t)(ended[j] ? p.end : i));
     };
     const float *const best_v = p.best_v + row0 * per_row;
     const int32_t *const best_i = p.best_i + row0 * per_row;
@@ -415,44 +432,52 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
         __syncthreads();
         const float f = __builtin_fmaxf(__builtin_fmaxf(floors[0], floors[1]), __builtin_fmaxf(floors[2], floors[3]));
         const double floor_v = f > kLowest ? (double)from_ordered_bits(ordered_bits(f) - 1) : -1.7976931348623157e308;
-        auto gather = [&](int q, const int32_t *i) {
+        auto gather = [&](int q, const float *v, const int32_t *i) {
             const double c = held[q];
             if (c >= floor_v) {
                 const int at = atomicAdd(&gathered, 1);   // (their order does not matter)
                 if (at < kMeetGathered) {
+                    const Place place_of = place(q, *v, *i);
                     list_v[at] = c;
-                    list_i[at] = place(q, *i);
+                    list_key[at] = place_of.key;
+                    list_token[at] = place_of.token;
                 }
             }
         };
 #pragma unroll
         for (int e = 0; e < kMeetEarly; ++e)
-            if (tid + e * kMeetThreads < all) gather(tid + e * kMeetThreads, &early_i[e]);
+            if (tid + e * kMeetThreads < all) gather(tid + e * kMeetThreads, &early_v[e], &early_i[e]);
 #pragma unroll 1
-        for (int q = tid + kMeetEarly * kMeetThreads; q < all; q += kMeetThreads) gather(q, &best_i[q]);
+        for (int q = tid + kMeetEarly * kMeetThreads; q < all; q += kMeetThreads) gather(q, &best_v[q], &best_i[q]);
         __syncthreads();
         const int n = gathered;
         if (n <= kMeetGathered) {   // uniform
             for (int q = tid; q < n; q += kMeetThreads) {
                 const double v = list_v[q];
-                const uint64_t i = list_i[q];
-                int before = 0;
+                const Place i{list_key[q], list_token[q]};
+                int before = 0, same = 0;
 #pragma unroll 4
-                for (int o = 0; o < n; ++o) before += (int)(list_v[o] > v) | ((int)(list_v[o] == v) & (int)(list_i[o] < i));
+                for (int o = 0; o < n; ++o) {
+                    before += (int)(list_v[o] > v) | ((int)(list_v[o] == v) & (int)(list_key[o] < i.key));
+                    same += (int)(list_v[o] == v) & (int)(list_key[o] == i.key);
+                }
+                if (same > 1)   // (itself, and equal values of a row within 32 tokens)
+                    for (int o = 0; o < n; ++o) before += (int)(list_v[o] == v) & (int)(list_key[o] == i.key) & (int)(list_token[o] < i.token);
                 if (before < p.k) put(before, v, i);
             }
-            for (int q = n + tid; q < p.k; q += kMeetThreads) put(q, -__builtin_inf(), 0);
+            for (int q = n + tid; q < p.k; q += kMeetThreads) put(q, -__builtin_inf(), Place{0, 0});
             return;
         }
         __syncthreads();
     }
-    BestList<double, uint64_t> list;
-    list.clear(-__builtin_inf());
+    BestList<double, Place> list;
+    list.clear(-__builtin_inf(), Place{~0ull, ~0u});
     double floor_v = -1.7976931348623157e308;
     for (int base = wave * 64; base < all; base += kMeetThreads) {
         const int q = base + lane;
-        const double c = q < all ? worth(q, best_v[q]) : -__builtin_inf();
-        const uint64_t ci = c >= floor_v ? place(q, best_i[q]) : 0;
+        const float v = q < all ? best_v[q] : 0.f;
+        const double c = q < all ? worth(q, v) : -__builtin_inf();
+        const Place ci = c >= floor_v ? place(q, v, best_i[q]) : Place{0, 0};
         uint64_t who = __ballot(c >= floor_v);
         while (who) {
             const int l = __ffsll((unsigned long long)who) - 1;
@@ -466,14 +491,15 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
     }
     if (lane < p.k) {
         list_v[wave * FREEZE_MAX_K + lane] = list.v;
-        list_i[wave * FREEZE_MAX_K + lane] = list.i;
+        list_key[wave * FREEZE_MAX_K + lane] = list.i.key;
+        list_token[wave * FREEZE_MAX_K + lane] = list.i.token;
     }
     __syncthreads();
     if (wave != 0) return;
     for (int w = 1; w < kMeetThreads / 64; ++w)
         for (int t = 0; t < p.k; ++t) {
             const double cv = list_v[w * FREEZE_MAX_K + t];
-            if (!(cv > -__builtin_inf()) || !insert(list, cv, list_i[w * FREEZE_MAX_K + t], p.k, lane)) break;   // uniform
+            if (!(cv > -__builtin_inf()) || !insert(list, cv, Place{list_key[w * FREEZE_MAX_K + t], list_token[w * FREEZE_MAX_K + t]}, p.k, lane)) break;   // uniform
         }
     if (lane < p.k) put(lane, list.v, list.i);
 }

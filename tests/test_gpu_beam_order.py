@@ -84,3 +84,19 @@ def test_rows_of_the_type_s_ends(fill, dtype):
         x[torch.rand(x.shape, generator=torch.Generator().manual_seed(1)) < 0.999] = info.min
     x[1] = x[6] = info.max if fill == "highest" else info.min
     _run(x.cuda(), -torch.arange(12).float().cuda() / 8, 4, 12)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("beams,vocab,k", [(4, 50021, 1), (4, 50021, 2), (4, 50021, 12), (1, 131075, 64), (8, 20000, 16), (64, 700, 64), (3, 300, 5)])
+def test_totals_that_swallow_the_values(beams, vocab, k, dtype):
+    # marks of rows that are out of use, and values that a total of -10 does not resolve: the values themselves decide within a row
+    x = _noise(2 * beams, vocab, 3 + beams).to(dtype).cuda()
+    for mark in (-1e30, torch.finfo(torch.float32).min):
+        scores = torch.full((2 * beams,), mark, device="cuda")
+        _run(x, scores, beams, k)
+        scores[beams + beams // 2] = -2.0
+        _run(x, scores, beams, k)
+    tiny = torch.zeros(2 * beams, vocab)
+    for i in range(min(5, vocab)):
+        tiny[:, (i * 977 + 131) % vocab] = (i + 1) * 1e-18
+    _run(tiny.to(dtype).cuda(), torch.zeros(2 * beams, device="cuda"), beams, k)
