@@ -354,7 +354,8 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
  *   out      [b, m] out_dtype, out_stride elements from row to row (>= m); elements between rows are left as they
  *            are.  It may lie over x.
  *            FREEZE_F32: products are exact and summed in fp32.  FREEZE_BF16: the same sums, rounded to nearest even once.
- *   workspace  freeze_quantised_workspace_bytes() bytes, 256-byte aligned; scratch only.  Calls that share a workspace (replays of
+ *   workspace  freeze_quantised_workspace_bytes() bytes, 256-byte aligned; scratch only.  The bytes for a batch serve every
+ *            smaller one too, and either type of output.  Calls that share a workspace (replays of
  *            captured ones too) must follow one another on the device.  It may not lie over x or out.
  * 1 <= m < 2^31 - 512, 0 <= b <= 2^30; b == 0 is a no-op.
  */

@@ -740,11 +740,11 @@ const LayerCache *get_quantised(const freeze_ctx *ctx, int slot, int *err)
     return *err == FREEZE_OK ? &ctx->layers[slot] : nullptr;
 }
 
-// workspace of a product: its rows in tiles, the sums of cut tiles
-size_t quant_bytes(const QuantPlan &pl, int64_t b, int64_t d)
+// workspace of a product: its rows in tiles of any height, the sums of cut tiles
+size_t quant_bytes(const freeze_ctx *ctx, const LayerCache &P, int64_t b)
 {
-    const int64_t rows = quant_tiled_rows(b, pl.bm);
-    return align_up((size_t)(rows * quant_code_stride(d))) + align_up((size_t)(rows * quant_scale_stride(d))) + align_up(pl.part * 4);
+    const int64_t rows = quant_workspace_rows(b), d_pad = quant_code_stride(P.d);
+    return align_up((size_t)(rows * d_pad)) + align_up((size_t)(rows * quant_scale_stride(P.d))) + align_up(quant_room(b, P.n, d_pad, ctx->num_cus));
 }
 
 QuantRows take_rows(Carver &c, int64_t rows, int64_t d, int tile)
@@ -1356,8 +1356,7 @@ size_t freeze_quantised_workspace_bytes(const freeze_ctx *ctx, int slot, int64_t
     int err;
     const LayerCache *P = get_quantised(ctx, slot, &err);
     if (!P || b < 0 || b > (int64_t)1 << 30 || (out_dtype != FREEZE_F32 && out_dtype != FREEZE_BF16)) return 0;
-    if (b < 1) b = 1;
-    return quant_bytes(plan_quant_product(b, P->n, quant_code_stride(P->d), ctx->num_cus), b, P->d);
+    return quant_bytes(ctx, *P, b < 1 ? 1 : b);
 }
 
 int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dtype, const uint8_t *x_scales, int64_t b, int64_t x_stride,
@@ -1376,14 +1375,14 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
     if (!x || !out || !workspace || given != (x_scales != nullptr) || !aligned(out, out_size) ||
         !aligned(x, given ? 16 : (x_dtype == FREEZE_F32 ? 4 : 2)) || !aligned(x_scales, 4))
         return FREEZE_EINVAL;
-    const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), ctx->num_cus);
-    const size_t need = quant_bytes(pl, b, P->d);
+    const size_t need = quant_bytes(ctx, *P, b);
     if (workspace_bytes < need || !aligned(workspace, kAlign)) return FREEZE_EWORKSPACE;
     const size_t xb = given ? (size_t)(b * quant_code_stride(P->d)) : (size_t)((b - 1) * x_stride + P->d) * (x_dtype == FREEZE_F32 ? 4 : 2);
     const size_t ob = (size_t)((b - 1) * out_stride + P->n) * out_size;
     if (share_bytes(workspace, need, out, ob) || share_bytes(workspace, need, x, xb) ||
         (given && share_bytes(workspace, need, x_scales, (size_t)(b * quant_scale_stride(P->d)))))
         return FREEZE_EINVAL;
+    const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), ctx->num_cus);
     hipStream_t s = static_cast<hipStream_t>(stream);
     Carver ws(workspace);
     const QuantRows rows = take_rows(ws, b, P->d, pl.bm);

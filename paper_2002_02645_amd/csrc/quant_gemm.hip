@@ -13,7 +13,6 @@
 #include "../../include/freeze.h"
 #include "quantised.h"
 
-#include <algorithm>
 #include <type_traits>
 #include <utility>
 
@@ -512,65 +511,25 @@ __global__ __launch_bounds__(256) void quant_sum_kernel(QuantProduct p, int bm, 
     store_outputs(p, (int64_t)xt * bm + row, (int64_t)wt * bn + col, v);
 }
 
+// The kernels of kQuantVariants.
 struct Variant {
-    int bm, bn, per_cu;
-    float step_us;   // of a k-step of a workgroup where neither memory nor L2 bounds it
     void (*kernel)(QuantProduct);
     void (*raw)(QuantProduct);   // the form that quantises its rows itself
 };
 const Variant kVariants[] = {
-    {16, 128, 2, 0.60f, quant_gemm_kernel<1, 8, 1, 1, 4>, quant_gemm_kernel<1, 8, 1, 1, 4, true>},
-    {32, 128, 2, 0.75f, quant_gemm_kernel<1, 8, 2, 1, 3>, nullptr},
-    {64, 128, 2, 1.00f, quant_gemm_kernel<1, 8, 4, 1, 3>, nullptr},
-    {16, 256, 1, 0.75f, quant_gemm_kernel<1, 8, 1, 2, 4>, quant_gemm_kernel<1, 8, 1, 2, 4, true>},
-    {32, 256, 1, 0.90f, quant_gemm_kernel<1, 8, 2, 2, 4>, nullptr},
-    {64, 256, 1, 1.10f, quant_gemm_kernel<1, 8, 4, 2, 3>, nullptr},
-    {128, 256, 1, 1.55f, quant_tile_kernel<4>, nullptr},
-    {160, 256, 1, 1.80f, quant_tile_kernel<5>, nullptr},
-    {192, 256, 1, 2.20f, quant_tile_kernel<6>, nullptr},
-    {256, 256, 1, 2.95f, quant_tile_kernel<8>, nullptr},
+    {quant_gemm_kernel<1, 8, 1, 1, 4>, quant_gemm_kernel<1, 8, 1, 1, 4, true>},
+    {quant_gemm_kernel<1, 8, 2, 1, 3>, nullptr},
+    {quant_gemm_kernel<1, 8, 4, 1, 3>, nullptr},
+    {quant_gemm_kernel<1, 8, 1, 2, 4>, quant_gemm_kernel<1, 8, 1, 2, 4, true>},
+    {quant_gemm_kernel<1, 8, 2, 2, 4>, nullptr},
+    {quant_gemm_kernel<1, 8, 4, 2, 3>, nullptr},
+    {quant_tile_kernel<4>, nullptr},
+    {quant_tile_kernel<5>, nullptr},
+    {quant_tile_kernel<6>, nullptr},
+    {quant_tile_kernel<8>, nullptr},
 };
+static_assert(sizeof kVariants / sizeof kVariants[0] == kQuantNumVariants, "a kernel for each");
 }  // namespace
-
-QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, int num_cus)
-{
-    QuantPlan pl{};
-    pl.nk = (int)(d_pad / kQuantBlock);
-    double best = 0;
-    for (int i = 0; i < (int)(sizeof kVariants / sizeof kVariants[0]); ++i) {
-        const Variant &v = kVariants[i];
-        const int64_t xt = (b + v.bm - 1) / v.bm, wt = (m + v.bn - 1) / v.bn, tiles = xt * wt, places = (int64_t)num_cus * v.per_cu;
-        // whole tiles, or each cut along the depth so that a quarter or half a round of workgroups, or one to four rounds are full, with the
-        // sums through memory (written and read at 2.5 TB/s, and a launch)
-        constexpr int kQuarters[] = {0, 1, 2, 4, 8, 12, 16};
-        for (int r : kQuarters) {
-            const int64_t fit = r == 0 ? 1 : std::min<int64_t>(places * r / 4 / tiles, std::min(pl.nk, 64));
-            if (r > 0 && fit < 2) continue;
-            const int splits = (int)fit;
-            const double rounds = (double)((tiles * splits + places - 1) / places);
-            // Workgroups in rounds; the weights out of memory (6.5 TB/s where one workgroup reads them, else 5.3); what a CU takes in (40 GB/s; all of them 10 TB/s), of which a part shows
-            // beside either.
-            const double steps = (double)((pl.nk + splits - 1) / splits);
-            const double fed = (double)((tiles * splits + num_cus - 1) / num_cus) * steps * (double)(v.bm + v.bn) * 132.0 / 40e3;
-            double us = rounds * (steps * v.step_us + 3.0);
-            us = std::max(us, (double)wt * v.bn * (double)d_pad / (xt == 1 ? 6.5e6 : 5.3e6));
-            us = std::max(us, fed) + 0.15 * fed;
-            if (splits > 1) us += 5.0 + 2.0 * 4.0 * (double)wt * v.bn * (double)b * splits / 2.5e6 + 0.1 * splits;
-            if (pl.wgs == 0 || us < best) {
-                best = us;
-                pl.variant = i;
-                pl.bm = v.bm;
-                pl.bn = v.bn;
-                pl.x_tiles = (int)xt;
-                pl.w_tiles = (int)wt;
-                pl.splits = splits;
-                pl.wgs = tiles * splits;
-            }
-        }
-    }
-    pl.part = pl.splits > 1 ? (size_t)pl.wgs * pl.bm * pl.bn : 0;
-    return pl;
-}
 
 bool quant_takes_values(const QuantPlan &pl, const void *x, int dtype, int64_t b, int64_t d, int64_t row_stride)
 {

@@ -1,10 +1,10 @@
 // Rows held in 8 bits and the dense layer on them: what the host dispatcher and the kernels share.  Not part of the C ABI.
 #pragma once
 #include "freeze_internal.h"
+#include "quant_plan.h"
 
 namespace fz {
 
-constexpr int kQuantBlock = 128;             // values that share an exponent: one k-step of the product
 constexpr int64_t kL2Bytes = 32 << 20;       // of the eight XCDs together
 constexpr int64_t kQuantMaxD = 1 << 22;      // a tile of 256 rows spans 32-bit offsets
 
@@ -15,8 +15,6 @@ inline int64_t quant_scale_stride(int64_t d) { return ((d + kQuantBlock - 1) / k
 // (128 codes), so that a stage of the product is one run of memory; of a row's 128 bytes, chunk c (16 bytes) lies at
 // c ^ row128_swizzle(row), as in LDS.  The scale bytes of four k-steps lie together, 4 bytes a row.  Rows behind the last one are
 // whatever they were: they meet outputs that are not stored.
-constexpr int kQuantTile = 256;
-inline int64_t quant_tiled_rows(int64_t rows, int64_t tile) { return (rows + tile - 1) / tile * tile; }
 struct QuantRows {
     uint8_t *codes, *scales;
     int64_t d_pad, sd;      // bytes of a row
@@ -114,16 +112,6 @@ struct QuantProduct {
     float *part;             // plan's floats of scratch (none: null)
     int nk, x_tiles, w_tiles, splits;   // the plan's
 };
-// How a product is cut.
-struct QuantPlan {
-    int variant;        // of quant_gemm_kernel
-    int bm, bn;         // rows of x, rows of w of a tile
-    int x_tiles, w_tiles, nk;
-    int splits;         // cuts of a tile along the depth
-    int64_t wgs;
-    size_t part;        // floats of the sums of cut tiles
-};
-QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, int num_cus);
 // whether the product quantises its b rows itself
 bool quant_takes_values(const QuantPlan &pl, const void *x, int dtype, int64_t b, int64_t d, int64_t row_stride);
 hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t s);

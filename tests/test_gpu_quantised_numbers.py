@@ -44,3 +44,18 @@ def test_sums_that_cancel(out):
         assert torch.equal(fc.quantised_project(0, x, out_dtype=out), want)
     finally:
         fc.close()
+
+
+@pytest.mark.parametrize("m,d", [(8192, 8192), (32768, 4096)])
+def test_one_workspace_for_a_batch_that_shrinks(m, d):
+    fc = binding.FreezeCache(1)
+    try:
+        fc.build_quantised(0, _noise(m, d, 1))
+        ws = torch.empty(binding.freeze_quantised_workspace_bytes(fc.ctx, 0, 400, binding.FREEZE_F32), dtype=torch.uint8, device="cuda")
+        x = _noise(400, d, 2)
+        for b in (400, 375, 257, 256, 129, 39, 33, 17, 1):
+            for out in (torch.full((b, m), 7.0, device="cuda"), torch.full((b, m), 7.0, device="cuda", dtype=torch.bfloat16)):
+                binding.freeze_quantised_project(fc.ctx, 0, x[:b], None, d, False, out, ws)
+                assert torch.equal(out, fc.quantised_project(0, x[:b].clone(), out_dtype=out.dtype))
+    finally:
+        fc.close()
