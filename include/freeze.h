@@ -384,7 +384,8 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
  *             and freeze_reorder_states take it;
  *   out_finished [groups, k] uint8 or NULL: token == end_token.
  *   A group with fewer than k continuations: its last places get score -inf, token end_token (0 for -1), parent its first row.
- *   workspace  freeze_beam_workspace_bytes() bytes, 256-byte aligned; scratch only, shared by calls that follow one another only.
+ *   workspace  freeze_beam_workspace_bytes() bytes, 256-byte aligned; scratch only, shared by calls that follow one another only.  The
+ *             bytes for some groups serve fewer ones too (and smaller vocabularies, fewer beams, a smaller k).
  * 1 <= beams <= 64, 1 <= k <= FREEZE_MAX_K, 1 <= vocab < 2^31 - 512, groups * beams <= 2^20; groups == 0 is a no-op.  Totals are formed in
  * fp64 from fp32 exponentials, (scores[j] - log sum exp(l - largest l)) + (l - largest l), and rounded once; within a row, the values
  * themselves decide.  No output, nor the workspace, may lie

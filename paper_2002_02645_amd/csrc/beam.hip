@@ -505,6 +505,7 @@ __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
 }
 
 // How a row is cut: pieces of whole batches, as many as fill the chip with waves (12 a CU) and no more.
+constexpr int64_t kBeamWaves = 12 * 256;
 struct BeamPlan {
     int64_t groups_per_part;
     int parts;
@@ -513,13 +514,20 @@ BeamPlan beam_plan(int64_t rows, int64_t vocab, int size)
 {
     const int64_t v = 16 / size, batch = 64 * kBeamLoads;
     const int64_t batches = ((vocab + v - 1) / v + batch - 1) / batch;
-    int64_t parts = (12 * 256 + rows - 1) / rows;
+    int64_t parts = (kBeamWaves + rows - 1) / rows;
     parts = parts < 1 ? 1 : (parts > batches ? batches : parts);
     BeamPlan pl;
     const int64_t per = (batches + parts - 1) / parts;
     pl.groups_per_part = per * batch;
     pl.parts = (int)((batches + per - 1) / per);
     return pl;
+}
+// Places for the pieces' lists: as many as fewer rows may take too (a plan's own number goes up and down: 3,068 rows are cut in two, 3,072 not
+// at all), so that a workspace serves every smaller call.
+size_t beam_units(int64_t rows, int64_t vocab)
+{
+    const int64_t batch = 4 * 64 * kBeamLoads;   // values of a batch at least (fp32)
+    return (size_t)std::min<int64_t>(rows * ((vocab + batch - 1) / batch), rows + kBeamWaves - 1);
 }
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
@@ -662,7 +670,7 @@ size_t freeze_beam_workspace_bytes(int64_t groups, int beams, int64_t vocab, int
 {
     if (!beam_sizes(groups, beams, vocab, k)) return 0;
     const int64_t rows = groups > 0 ? groups * beams : 1;
-    const size_t units = (size_t)rows * std::max(beam_plan(rows, vocab, 4).parts, beam_plan(rows, vocab, 2).parts);
+    const size_t units = beam_units(rows, vocab);
     return 2 * up256(units * k * 4) + up256(units * 8) + up256(units * 4);
 }
 
