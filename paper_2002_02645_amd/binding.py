@@ -366,6 +366,12 @@ def _on(stream) -> int:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
+def _here_and_now() -> tuple:
+    """The current device and its current stream."""
+    dev = torch.cuda.current_device()
+    return dev, torch._C._cuda_getCurrentRawStream(dev)
+
+
 def _rows_of(t: torch.Tensor) -> int:
     """Elements from row to row of a two-dimensional tensor whose rows are dense."""
     assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)
@@ -554,23 +560,35 @@ def freeze_calibrate_hbm_read(buffer: torch.Tensor) -> float:
 # ---- convenience holder: owns the context, the per-layer storage and a reusable workspace ---------
 
 class FreezeCache:
+    """A context, the storage of its slots and scratch memory for each stream: calls on several streams may overlap, and calls may be captured into
+    graphs (their scratch and outputs are of the graph's memory).  Building a slot and calls that use it on another stream are the caller's to order."""
+
     def __init__(self, num_layers: int, device="cuda:0"):
         self.device = torch.device(device)
         self.ctx = freeze_create(num_layers)
         self.storage: Dict[int, torch.Tensor] = {}
         self.meta: Dict[int, tuple] = {}
-        self._ws: Optional[torch.Tensor] = None
+        self._scratch: Dict[tuple, torch.Tensor] = {}   # by device and stream
 
     def close(self):
         if self.ctx is not None:
             freeze_destroy(self.ctx)
             self.ctx = None
 
+    @property
+    def _ws(self) -> Optional[torch.Tensor]:
+        return self._scratch.get(_here_and_now())
+
     def _workspace(self, nbytes: int) -> torch.Tensor:
-        # (a larger one replaces it: what is captured into a graph has to be called with a workspace of its own, as the functions above take it)
-        if self._ws is None or self._ws.numel() < nbytes:
-            self._ws = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
-        return self._ws
+        # One for each stream: calls on a stream follow one another, those on two may overlap.  (Where a larger one replaces it, the old one's memory
+        # goes back to the stream it is used on.)  A captured call keeps none: its replays run beside whatever the stream does then.
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        at = _here_and_now()
+        ws = self._scratch.get(at)
+        if ws is None or ws.numel() < nbytes:
+            ws = self._scratch[at] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
+        return ws
 
     def build_layer(self, layer: int, entries: torch.Tensor, labels: torch.Tensor, num_classes: int):
         n, d = entries.shape

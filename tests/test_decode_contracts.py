@@ -16,3 +16,28 @@ def test_a_choice_s_workspace_serves_smaller_calls():
         g, beams, vocab, k = rng.randint(1, 2000), rng.randint(1, 64), int(2 ** rng.uniform(0, 18)), rng.randint(1, 64)
         most = f(g, beams, vocab, k)
         assert most >= f(rng.randint(1, g), rng.randint(1, beams), rng.randint(1, vocab), rng.randint(1, k)) > 0
+
+
+def test_a_holder_s_streams_have_scratch_of_their_own(monkeypatch):
+    now = dict(device=0, stream=7, capturing=False)
+    monkeypatch.setattr(binding.torch.cuda, "current_device", lambda: now["device"])
+    monkeypatch.setattr(binding.torch.cuda, "is_current_stream_capturing", lambda: now["capturing"])
+    monkeypatch.setattr(binding.torch._C, "_cuda_getCurrentRawStream", lambda device: now["stream"], raising=False)
+    fc = binding.FreezeCache(1, "cpu")
+    try:
+        one = fc._workspace(1000)
+        assert fc._workspace(10) is one and fc._workspace(1000) is one and fc._ws is one
+        now["stream"] = 8
+        two = fc._workspace(500)
+        assert two is not one and two.data_ptr() != one.data_ptr() and fc._workspace(500) is two
+        larger = fc._workspace(5000)
+        assert larger.numel() >= 5000 and fc._workspace(500) is larger
+        now["capturing"] = True      # what a graph holds is nobody else's
+        captured = [fc._workspace(500) for _ in range(2)]
+        assert all(c is not larger and c is not one and c.numel() >= 500 for c in captured) and captured[0] is not captured[1]
+        now.update(stream=7, capturing=False)
+        assert fc._workspace(1000) is one
+        now["device"] = 1            # (streams of two devices may have the same handle)
+        assert fc._workspace(1000) is not one
+    finally:
+        fc.close()

@@ -1,0 +1,69 @@
+"""A holder's calls on several streams at once, and captured into graphs: each has scratch memory of its own."""
+import pytest
+import torch
+
+from paper_2002_02645_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+
+def _noise(rows, d, seed):
+    return torch.randn(rows, d, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda")
+
+
+@pytest.fixture()
+def holder():
+    fc = binding.FreezeCache(3)
+    fc.build_quantised(0, _noise(3000, 900, 1))
+    fc.build_layer(1, _noise(3000, 256, 2), torch.zeros(3000, dtype=torch.int32, device="cuda"), 1)
+    yield fc
+    torch.cuda.synchronize()
+    fc.close()
+
+
+def _calls(fc):
+    small, large = _noise(40, 900, 3), _noise(300, 900, 4)
+    logits, scores, queries = _noise(32, 40021, 5), -_noise(32, 1, 6).abs().view(-1), _noise(200, 256, 7)
+    return [lambda: (fc.quantised_project(0, small),), lambda: (fc.quantised_project(0, large, out_dtype=torch.bfloat16),),
+            lambda: tuple(fc.beam_select(logits, scores, 4, 8).values()), lambda: tuple(fc.lookup(1, queries, 5, 3).values())]
+
+
+def _same(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b)) and len(a) == len(b)
+
+
+def test_streams_at_once(holder):
+    calls = _calls(holder)
+    want = [tuple(t.clone() for t in call()) for call in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(10):
+        got = []
+        for call, stream in zip(calls, streams):
+            with torch.cuda.stream(stream):
+                got.append(call())
+        torch.cuda.synchronize()
+        assert all(_same(a, b) for a, b in zip(got, want))
+
+
+def test_captured_calls_beside_eager_ones(holder):
+    calls = _calls(holder)
+    want = [tuple(t.clone() for t in call()) for call in calls]
+    graphs = []
+    for call in calls[:3]:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = call()
+        graphs.append((graph, out))
+    for n in range(6):
+        for graph, out in graphs:
+            for t in out:
+                t.zero_()
+            graph.replay()
+        eager = [call() for call in calls]
+        if n == 2:      # a larger call replaces the stream's scratch: the graphs keep their own
+            holder.quantised_project(0, _noise(2000, 900, 9))
+            torch.full((1 << 24,), 255, dtype=torch.uint8, device="cuda")
+        torch.cuda.synchronize()
+        assert all(_same(a, b) for a, b in zip(eager, want))
+        assert all(_same(out, b) for (_, out), b in zip(graphs, want))
