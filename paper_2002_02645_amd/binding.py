@@ -351,9 +351,10 @@ def freeze_quantised_scale_stride(d: int) -> int:
     return int(lib().freeze_quantised_scale_stride(d))
 
 
-def _here(*tensors: Optional[torch.Tensor]) -> None:
-    """The library's kernels run on the current device."""
+def _here(*tensors: Optional[torch.Tensor], holder: Optional["FreezeCache"] = None) -> None:
+    """The library's kernels run on the current device, and a holder's outputs, scratch and weights are on its own."""
     dev = torch.cuda.current_device()
+    assert holder is None or (holder.device.type == "cuda" and holder.device.index in (None, dev)), "the holder's device is not the current one"
     for t in tensors:
         assert t is None or t.get_device() == dev, "tensors of the current device are needed"
 
@@ -718,7 +719,7 @@ class FreezeCache:
 
     def quantise_rows(self, x: torch.Tensor):
         """Rows in 8 bits: codes [rows, d rounded up to 128] float8_e4m3fn and a scale byte for each block of 128 values."""
-        _here(x)
+        _here(x, holder=self)
         assert x.dtype in (torch.float32, torch.bfloat16)
         rows, d = x.shape
         codes = torch.empty((rows, -(-d // 128) * 128), dtype=torch.float8_e4m3fn, device=self.device)
@@ -731,6 +732,7 @@ class FreezeCache:
                         scales: Optional[torch.Tensor] = None, d: Optional[int] = None):
         """A dense layer y = W x + bias in 8 bits (a model's output layer, or the layer in front of a look-up); occupies one slot.
         weights: fp32 / bf16, quantised here, or codes with their scales (d: the values of a row, where fewer than the codes)."""
+        _here(weights, scales, bias, holder=self)
         m = weights.shape[0]
         d = weights.shape[1] if d is None else d
         nbytes = freeze_quantised_storage_bytes(m, d)
@@ -744,11 +746,11 @@ class FreezeCache:
     def quantised_project(self, slot: int, x: torch.Tensor, scales: Optional[torch.Tensor] = None, relu: bool = False,
                           out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x: fp32 / bf16 rows, or codes with their scales."""
+        _here(x, scales, out, holder=self)
         m, d, _ = self.meta[slot]
         b = x.shape[0]
         if out is None:
             out = torch.empty((b, m), dtype=out_dtype, device=self.device)
-        _here(x, scales, out)
         assert out.shape == (b, m) and out.dtype in (torch.float32, torch.bfloat16)
         if scales is None:
             assert x.shape[1] == d and x.dtype in (torch.float32, torch.bfloat16)
@@ -770,7 +772,7 @@ class FreezeCache:
                     end_token: int = -1) -> dict:
         """The k best continuations of every group of `beams` rows: score, token, parent (row), finished; each [groups, k]."""
         rows, vocab = logits.shape
-        _here(logits, scores, finished)
+        _here(logits, scores, finished, holder=self)
         assert rows % beams == 0 and scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
         assert finished is None or (finished.dtype in (torch.uint8, torch.bool) and finished.is_contiguous() and finished.numel() == rows)
         assert logits.dtype in (torch.float32, torch.bfloat16)

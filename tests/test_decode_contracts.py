@@ -41,3 +41,27 @@ def test_a_holder_s_streams_have_scratch_of_their_own(monkeypatch):
         assert fc._workspace(1000) is not one
     finally:
         fc.close()
+
+
+class _There:
+    """Stands for a tensor of device 1."""
+    dtype, shape, device = binding.torch.float32, (4, 8), binding.torch.device("cuda:1")
+
+    def get_device(self):
+        return 1
+
+
+def test_a_holder_of_another_device_is_refused(monkeypatch):
+    # its outputs, scratch and weights would be on another device than the one whose stream the kernels go to
+    monkeypatch.setattr(binding.torch.cuda, "current_device", lambda: 1)
+    fc, t = binding.FreezeCache(1, "cuda:0"), _There()
+    try:
+        fc.meta[0] = (8, 8, 0)
+        for call in (lambda: fc.quantise_rows(t), lambda: fc.build_quantised(0, t), lambda: fc.quantised_project(0, t), lambda: fc.quantised_project(0, t, out=t),
+                     lambda: fc.beam_select(t, t, 2, 2)):
+            with pytest.raises(AssertionError, match="holder's device"):
+                call()
+        binding._here(t, holder=binding.FreezeCache(1, "cuda:1"))
+        binding._here(t, holder=binding.FreezeCache(1, "cuda"))
+    finally:
+        fc.close()
