@@ -343,6 +343,12 @@ def freeze_gather_rows(x: torch.Tensor, sel: torch.Tensor, count: Optional[torch
                                     _stream(stream)), "freeze_gather_rows")
 
 
+def _refused(why: str = "an argument's shape, type or layout is not what the call takes") -> AssertionError:
+    """Raised in the place of an assert statement, which an optimised interpreter (-O) takes out: the library sees pointers alone, and would read or
+    write past a wrong shape."""
+    return AssertionError(why)
+
+
 def freeze_quantised_code_stride(d: int) -> int:
     return int(lib().freeze_quantised_code_stride(d))
 
@@ -351,12 +357,15 @@ def freeze_quantised_scale_stride(d: int) -> int:
     return int(lib().freeze_quantised_scale_stride(d))
 
 
-def _here(*tensors: Optional[torch.Tensor], holder: Optional["FreezeCache"] = None) -> None:
-    """The library's kernels run on the current device, and a holder's outputs, scratch and weights are on its own."""
+def _here(*tensors: Optional[torch.Tensor], holder: Optional["FreezeCache"] = None) -> int:
+    """The library's kernels run on the current device, and a holder's outputs, scratch and weights are on its own.  Returns the device."""
     dev = torch.cuda.current_device()
-    assert holder is None or (holder.device.type == "cuda" and holder.device.index in (None, dev)), "the holder's device is not the current one"
+    if holder is not None and holder._index != dev and holder._index is not None:
+        raise _refused("the holder's device is not the current one")
     for t in tensors:
-        assert t is None or t.get_device() == dev, "tensors of the current device are needed"
+        if t is not None and t.get_device() != dev:
+            raise _refused("tensors of the current device are needed")
+    return dev
 
 
 def _at(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -375,7 +384,8 @@ def _here_and_now() -> tuple:
 
 def _rows_of(t: torch.Tensor) -> int:
     """Elements from row to row of a two-dimensional tensor whose rows are dense."""
-    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)
+    if not (t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)):
+        raise _refused()
     return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
 
 
@@ -390,9 +400,12 @@ def freeze_quantise_rows(x: torch.Tensor, codes: torch.Tensor, scales: torch.Ten
     """codes [rows, freeze_quantised_code_stride(d)] float8_e4m3fn, scales [rows, freeze_quantised_scale_stride(d)] uint8."""
     _here(x, codes, scales)
     rows, d = x.shape
-    assert x.dtype in (torch.float32, torch.bfloat16)
-    assert codes.dtype == torch.float8_e4m3fn and codes.is_contiguous() and codes.shape == (rows, freeze_quantised_code_stride(d))
-    assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (rows, freeze_quantised_scale_stride(d))
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise _refused()
+    if not (codes.dtype == torch.float8_e4m3fn and codes.is_contiguous() and codes.shape == (rows, freeze_quantised_code_stride(d))):
+        raise _refused()
+    if not (scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (rows, freeze_quantised_scale_stride(d))):
+        raise _refused()
     _check(lib().freeze_quantise_rows(_at(x), _values_dtype(x), rows, d, _rows_of(x), _at(codes), _at(scales), _on(stream)),
            "freeze_quantise_rows")
 
@@ -406,13 +419,18 @@ def freeze_quantised_build(ctx, slot: int, weights: torch.Tensor, scales: Option
     """weights [m, d] fp32 / bf16 (scales None), or codes [m, freeze_quantised_code_stride(d)] with their scales."""
     _here(weights, scales, bias, storage)
     m = weights.shape[0]
-    assert weights.is_contiguous() and weights.dim() == 2
-    assert bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == m)
+    if not (weights.is_contiguous() and weights.dim() == 2):
+        raise _refused()
+    if not (bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == m)):
+        raise _refused()
     if scales is None:
-        assert weights.shape[1] == d
+        if weights.shape[1] != d:
+            raise _refused()
     else:
-        assert weights.dtype == torch.float8_e4m3fn and weights.shape[1] == freeze_quantised_code_stride(d)
-        assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (m, freeze_quantised_scale_stride(d))
+        if not (weights.dtype == torch.float8_e4m3fn and weights.shape[1] == freeze_quantised_code_stride(d)):
+            raise _refused()
+        if not (scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (m, freeze_quantised_scale_stride(d))):
+            raise _refused()
     _check(lib().freeze_quantised_build(ctx, slot, _at(weights), _values_dtype(weights), _at(scales), m, d, _at(bias), _at(storage),
                                         storage.nbytes, _on(stream)), "freeze_quantised_build")
 
@@ -426,13 +444,17 @@ def freeze_quantised_project(ctx, slot: int, x: torch.Tensor, scales: Optional[t
     """x [b, d] fp32 / bf16 (scales None), or codes with their scales; out [b, m] fp32 or bf16.  d, m: the built layer's."""
     _here(x, scales, out, workspace)
     b = x.shape[0]
-    assert out.dtype in (torch.float32, torch.bfloat16) and out.shape[0] == b
+    if not (out.dtype in (torch.float32, torch.bfloat16) and out.shape[0] == b):
+        raise _refused()
     if scales is None:
-        assert x.shape[1] == d
+        if x.shape[1] != d:
+            raise _refused()
         stride = _rows_of(x)
     else:
-        assert x.dtype == torch.float8_e4m3fn and x.is_contiguous() and x.shape[1] == freeze_quantised_code_stride(d)
-        assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (b, freeze_quantised_scale_stride(d))
+        if not (x.dtype == torch.float8_e4m3fn and x.is_contiguous() and x.shape[1] == freeze_quantised_code_stride(d)):
+            raise _refused()
+        if not (scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (b, freeze_quantised_scale_stride(d))):
+            raise _refused()
         stride = 0
     _check(lib().freeze_quantised_project(ctx, slot, _at(x), _values_dtype(x), _at(scales), b, stride, int(relu), _at(out),
                                           _values_dtype(out), _rows_of(out), _at(workspace),
@@ -448,15 +470,22 @@ def freeze_beam_select(logits: torch.Tensor, scores: torch.Tensor, finished: Opt
                        out_finished: Optional[torch.Tensor], workspace: torch.Tensor, stream=None) -> None:
     _here(logits, scores, finished, out_scores, out_tokens, out_parents, out_finished, workspace)
     rows, vocab = logits.shape
-    assert logits.dtype in (torch.float32, torch.bfloat16) and rows % beams == 0
-    assert scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
-    assert finished is None or (finished.dtype in (torch.uint8, torch.bool) and finished.is_contiguous() and finished.numel() == rows)
+    if not (logits.dtype in (torch.float32, torch.bfloat16) and rows % beams == 0):
+        raise _refused()
+    if not (scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows):
+        raise _refused()
+    if not (finished is None or (finished.dtype in (torch.uint8, torch.bool) and finished.is_contiguous() and finished.numel() == rows)):
+        raise _refused()
     groups = rows // beams
     n = groups * k
-    assert out_scores.dtype == torch.float32 and out_scores.is_contiguous() and out_scores.numel() == n
-    assert out_tokens.dtype == torch.int32 and out_tokens.is_contiguous() and out_tokens.numel() == n
-    assert out_parents.dtype == torch.int32 and out_parents.is_contiguous() and out_parents.numel() == n
-    assert out_finished is None or (out_finished.dtype == torch.uint8 and out_finished.is_contiguous() and out_finished.numel() == n)
+    if not (out_scores.dtype == torch.float32 and out_scores.is_contiguous() and out_scores.numel() == n):
+        raise _refused()
+    if not (out_tokens.dtype == torch.int32 and out_tokens.is_contiguous() and out_tokens.numel() == n):
+        raise _refused()
+    if not (out_parents.dtype == torch.int32 and out_parents.is_contiguous() and out_parents.numel() == n):
+        raise _refused()
+    if not (out_finished is None or (out_finished.dtype == torch.uint8 and out_finished.is_contiguous() and out_finished.numel() == n)):
+        raise _refused()
     _check(lib().freeze_beam_select(_at(logits), _values_dtype(logits), groups, beams, vocab, _rows_of(logits), _at(scores),
                                     _at(finished), end_token, k, _at(out_scores), _at(out_tokens), _at(out_parents),
                                     _at(out_finished), _at(workspace), workspace.nbytes,
@@ -466,19 +495,23 @@ def freeze_beam_select(logits: torch.Tensor, scores: torch.Tensor, finished: Opt
 def state_of(src: torch.Tensor, dst: torch.Tensor, used: Optional[int] = None, row_dim: int = 0) -> FreezeState:
     """The freeze_state of two tensors of one shape, type and layout [outer..., rows, pieces..., places, width] (row_dim: the place of
     the rows; after it at most three dimensions, before it at most one).  used: how many places are taken along; None: all."""
-    assert src.shape == dst.shape and src.dtype == dst.dtype and src.stride() == dst.stride(), "src and dst of one layout are needed"
-    assert 0 <= row_dim <= 1 and src.dim() - row_dim <= 4 and src.dim() > row_dim
+    if not (src.shape == dst.shape and src.dtype == dst.dtype and src.stride() == dst.stride()):
+        raise _refused("src and dst of one layout are needed")
+    if not (0 <= row_dim <= 1 and src.dim() - row_dim <= 4 and src.dim() > row_dim):
+        raise _refused()
     size = src.element_size()
     shape, stride = list(src.shape), list(src.stride())
     outer, outer_stride = (shape[0], stride[0]) if row_dim else (1, 0)
     row_stride = stride[row_dim]
     inner, istr = shape[row_dim + 1:], stride[row_dim + 1:]
     if used is not None:
-        assert len(inner) >= 2 and 0 <= used <= inner[-2]
+        if not (len(inner) >= 2 and 0 <= used <= inner[-2]):
+            raise _refused()
         inner[-2] = used
     pieces, piece_stride, run = 1, 0, size
     if inner:
-        assert istr[-1] == 1 or inner[-1] <= 1, "the last dimension has to be dense"
+        if not (istr[-1] == 1 or inner[-1] <= 1):
+            raise _refused("the last dimension has to be dense")
         run *= inner[-1]
     if len(inner) >= 2:
         if istr[-2] * size == run or inner[-2] <= 1:
@@ -486,7 +519,8 @@ def state_of(src: torch.Tensor, dst: torch.Tensor, used: Optional[int] = None, r
             if len(inner) == 3:
                 pieces, piece_stride = inner[0], istr[0]
         else:
-            assert len(inner) == 2 or inner[0] == 1, "places that do not follow each other, in several pieces"
+            if not (len(inner) == 2 or inner[0] == 1):
+                raise _refused("places that do not follow each other, in several pieces")
             pieces, piece_stride = inner[-2], istr[-2]
     return FreezeState(src.data_ptr(), dst.data_ptr(), outer, outer_stride * size, row_stride * size, pieces, piece_stride * size, run)
 
@@ -494,7 +528,8 @@ def state_of(src: torch.Tensor, dst: torch.Tensor, used: Optional[int] = None, r
 def freeze_reorder_states(states: Sequence[FreezeState], parents: torch.Tensor, src_rows: int, stream=None) -> None:
     """states as of state_of; row r of every dst becomes row parents[r] of its src."""
     _here(parents)
-    assert parents.dtype == torch.int32 and parents.is_contiguous()
+    if not (parents.dtype == torch.int32 and parents.is_contiguous()):
+        raise _refused()
     arr = (FreezeState * len(states))(*states)
     _check(lib().freeze_reorder_states(ctypes.addressof(arr), len(states), _at(parents), parents.numel(), src_rows,
                                        _on(stream)), "freeze_reorder_states")
@@ -566,6 +601,7 @@ class FreezeCache:
 
     def __init__(self, num_layers: int, device="cuda:0"):
         self.device = torch.device(device)
+        self._index = self.device.index if self.device.type == "cuda" else -1   # None: whichever device is the current one
         self.ctx = freeze_create(num_layers)
         self.storage: Dict[int, torch.Tensor] = {}
         self.meta: Dict[int, tuple] = {}
@@ -580,12 +616,12 @@ class FreezeCache:
     def _ws(self) -> Optional[torch.Tensor]:
         return self._scratch.get(_here_and_now())
 
-    def _workspace(self, nbytes: int) -> torch.Tensor:
+    def _workspace(self, nbytes: int, at: Optional[tuple] = None) -> torch.Tensor:
         # One for each stream: calls on a stream follow one another, those on two may overlap.  (Where a larger one replaces it, the old one's memory
         # goes back to the stream it is used on.)  A captured call keeps none: its replays run beside whatever the stream does then.
         if torch.cuda.is_current_stream_capturing():
             return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
-        at = _here_and_now()
+        at = at or _here_and_now()
         ws = self._scratch.get(at)
         if ws is None or ws.numel() < nbytes:
             ws = self._scratch[at] = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
@@ -719,12 +755,13 @@ class FreezeCache:
 
     def quantise_rows(self, x: torch.Tensor):
         """Rows in 8 bits: codes [rows, d rounded up to 128] float8_e4m3fn and a scale byte for each block of 128 values."""
-        _here(x, holder=self)
-        assert x.dtype in (torch.float32, torch.bfloat16)
+        dev = _here(x, holder=self)
+        if x.dtype not in (torch.float32, torch.bfloat16):
+            raise _refused()
         rows, d = x.shape
         codes = torch.empty((rows, -(-d // 128) * 128), dtype=torch.float8_e4m3fn, device=self.device)
         scales = torch.empty((rows, -(-d // 512) * 4), dtype=torch.uint8, device=self.device)
-        _check(lib().freeze_quantise_rows(x.data_ptr(), _values_dtype(x), rows, d, _rows_of(x), codes.data_ptr(), scales.data_ptr(), _on(None)),
+        _check(lib().freeze_quantise_rows(x.data_ptr(), _values_dtype(x), rows, d, _rows_of(x), codes.data_ptr(), scales.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)),
                "freeze_quantise_rows")
         return codes, scales
 
@@ -746,47 +783,56 @@ class FreezeCache:
     def quantised_project(self, slot: int, x: torch.Tensor, scales: Optional[torch.Tensor] = None, relu: bool = False,
                           out_dtype: torch.dtype = torch.float32, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """x: fp32 / bf16 rows, or codes with their scales."""
-        _here(x, scales, out, holder=self)
+        dev = _here(x, scales, out, holder=self)
         m, d, _ = self.meta[slot]
         b = x.shape[0]
         if out is None:
             out = torch.empty((b, m), dtype=out_dtype, device=self.device)
-        assert out.shape == (b, m) and out.dtype in (torch.float32, torch.bfloat16)
+        if not (out.shape == (b, m) and out.dtype in (torch.float32, torch.bfloat16)):
+            raise _refused()
         if scales is None:
-            assert x.shape[1] == d and x.dtype in (torch.float32, torch.bfloat16)
+            if not (x.shape[1] == d and x.dtype in (torch.float32, torch.bfloat16)):
+                raise _refused()
             stride = _rows_of(x)
         else:
-            assert x.dtype == torch.float8_e4m3fn and x.is_contiguous() and x.shape == (b, -(-d // 128) * 128)
-            assert scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (b, -(-d // 512) * 4)
+            if not (x.dtype == torch.float8_e4m3fn and x.is_contiguous() and x.shape == (b, -(-d // 128) * 128)):
+                raise _refused()
+            if not (scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (b, -(-d // 512) * 4)):
+                raise _refused()
             stride = 0
         out_type = _values_dtype(out)
         nbytes = lib().freeze_quantised_workspace_bytes(self.ctx, slot, b, out_type)
         if nbytes == 0:
             raise FreezeError(FREEZE_EINVAL, "freeze_quantised_workspace_bytes")
-        ws = self._workspace(nbytes)
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+        ws = self._workspace(nbytes, (dev, stream))
         _check(lib().freeze_quantised_project(self.ctx, slot, x.data_ptr(), _values_dtype(x), _at(scales), b, stride, int(relu), out.data_ptr(),
-                                              out_type, _rows_of(out), ws.data_ptr(), ws.numel(), _on(None)), "freeze_quantised_project")
+                                              out_type, _rows_of(out), ws.data_ptr(), ws.numel(), stream), "freeze_quantised_project")
         return out
 
     def beam_select(self, logits: torch.Tensor, scores: torch.Tensor, beams: int, k: int, finished: Optional[torch.Tensor] = None,
                     end_token: int = -1) -> dict:
         """The k best continuations of every group of `beams` rows: score, token, parent (row), finished; each [groups, k]."""
         rows, vocab = logits.shape
-        _here(logits, scores, finished, holder=self)
-        assert rows % beams == 0 and scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows
-        assert finished is None or (finished.dtype in (torch.uint8, torch.bool) and finished.is_contiguous() and finished.numel() == rows)
-        assert logits.dtype in (torch.float32, torch.bfloat16)
+        dev = _here(logits, scores, finished, holder=self)
+        if not (rows % beams == 0 and scores.dtype == torch.float32 and scores.is_contiguous() and scores.numel() == rows):
+            raise _refused()
+        if not (finished is None or (finished.dtype in (torch.uint8, torch.bool) and finished.is_contiguous() and finished.numel() == rows)):
+            raise _refused()
+        if logits.dtype not in (torch.float32, torch.bfloat16):
+            raise _refused()
         groups = rows // beams
         nbytes = lib().freeze_beam_workspace_bytes(groups, beams, vocab, k)
         if nbytes == 0:
             raise FreezeError(FREEZE_EINVAL, "freeze_beam_workspace_bytes")
-        ws = self._workspace(nbytes)
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+        ws = self._workspace(nbytes, (dev, stream))
         words = torch.empty((3, groups, k), dtype=torch.int32, device=self.device)
         ended = torch.empty((groups, k), dtype=torch.uint8, device=self.device)
         at, size = words.data_ptr(), 4 * groups * k
         _check(lib().freeze_beam_select(logits.data_ptr(), _values_dtype(logits), groups, beams, vocab, _rows_of(logits), scores.data_ptr(),
                                         _at(finished), end_token, k, at, at + size, at + 2 * size, ended.data_ptr(), ws.data_ptr(), ws.numel(),
-                                        _on(None)), "freeze_beam_select")
+                                        stream), "freeze_beam_select")
         score, token, parent = words.unbind(0)
         return dict(score=score.view(torch.float32), token=token, parent=parent, finished=ended)
 
@@ -794,10 +840,12 @@ class FreezeCache:
         """Row r of every dst becomes row parents[r] of its src (tensors or lists of tensors; see state_of)."""
         if isinstance(src, torch.Tensor):
             src, dst = (src,), (dst,)
-        assert len(src) == len(dst)
+        if len(src) != len(dst):
+            raise _refused()
         if not src:
             return
         _here(*src, *dst)
         rows = src[0].shape[row_dim]
-        assert parents.numel() <= rows and all(t.shape[row_dim] == rows for t in src)   # (state_of: a dst is like its src)
+        if not (parents.numel() <= rows and all(t.shape[row_dim] == rows for t in src)):   # (state_of: a dst is like its src)
+            raise _refused()
         freeze_reorder_states([state_of(s, d, used, row_dim) for s, d in zip(src, dst)], parents, rows)

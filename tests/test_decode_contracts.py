@@ -1,9 +1,15 @@
 """What callers of the 8-bit layer, the choice of tokens and the reordering of states may rely on, as far as no GPU is needed."""
+import ast
+import os
 import random
+import subprocess
+import sys
 
 import pytest
 
 from paper_2002_02645_amd import binding
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def test_a_choice_s_workspace_serves_smaller_calls():
@@ -65,3 +71,24 @@ def test_a_holder_of_another_device_is_refused(monkeypatch):
         binding._here(t, holder=binding.FreezeCache(1, "cuda"))
     finally:
         fc.close()
+
+
+def test_shapes_are_checked_in_an_optimised_interpreter_too():
+    # `python -O` takes assert statements out, and a wrong shape would have the kernels read or write past a tensor's end
+    code = """
+import torch
+from paper_2002_02645_amd import binding
+t = torch.zeros(2, 3, 4, 5, 6)
+for args in ((t, t.transpose(0, 1)), (t[..., ::2], t[..., ::2])):
+    try:
+        binding.state_of(*args, row_dim=1)
+    except AssertionError:
+        continue
+    raise SystemExit("not refused")
+"""
+    subprocess.run([sys.executable, "-O", "-c", code], cwd=ROOT, check=True, timeout=300)
+    tree = ast.parse(open(binding.__file__).read())
+    found = {n.name: n for n in ast.walk(tree) if isinstance(n, ast.FunctionDef)}
+    for name in ("_here", "_rows_of", "freeze_quantise_rows", "freeze_quantised_build", "freeze_quantised_project", "freeze_beam_select", "state_of",
+                 "freeze_reorder_states", "quantise_rows", "build_quantised", "quantised_project", "beam_select", "reorder_states"):
+        assert not any(isinstance(n, ast.Assert) for n in ast.walk(found[name])), name
