@@ -1383,6 +1383,7 @@ int freeze_quantised_project(freeze_ctx *ctx, int slot, const void *x, int x_dty
         (given && share_bytes(workspace, need, x_scales, (size_t)(b * quant_scale_stride(P->d)))))
         return FREEZE_EINVAL;
     const QuantPlan pl = plan_quant_product(b, P->n, quant_code_stride(P->d), ctx->num_cus);
+    if (pl.wgs == 0) return FREEZE_EINVAL;
     hipStream_t s = static_cast<hipStream_t>(stream);
     Carver ws(workspace);
     const QuantRows rows = take_rows(ws, b, P->d, pl.bm);

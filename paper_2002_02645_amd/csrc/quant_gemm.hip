@@ -201,7 +201,7 @@ __device__ __forceinline__ void tile_out(const QuantProduct &p, const f32x4 (&ac
 constexpr int kRawBytes = 14336;   // beside four stages, twice in a CU
 constexpr int kRawSteps = kRawBytes / 129;   // k-steps of a row: 128 codes and a scale byte
 template <int WX, int WN, int XB, int NB, int NS, bool RAW = false>
-__global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
+__global__ __launch_bounds__(kQuantThreads, 2) void quant_gemm_kernel(QuantProduct p)
 {
     static_assert(!RAW || (WX == 1 && XB == 1), "one block of x rows");
     static_assert(WX * WN == 8, "eight waves");
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(512, 2) void quant_gemm_kernel(QuantProduct p)
 // before its last kAhead groups, which need nothing newer: it publishes the next step's stage and frees this one, which is refilled from there on.
 // 10,000 x 8,192 -> 1,024 130 us, 1.29 PFLOP/s, the matrix pipes busy 55 % of all cycles; 4,096 x 8,192 -> 8,192 with its quantisation 400 us, 1.37 PFLOP/s.
 template <int XB>
-__global__ __launch_bounds__(512, 2) void quant_tile_kernel(QuantProduct p)
+__global__ __launch_bounds__(kQuantThreads, 2) void quant_tile_kernel(QuantProduct p)
 {
     constexpr int BM = 32 * XB, BN = 256, NB = 4;
     static_assert(BN == kQuantTile, "a stage of the weights is a run of memory");
@@ -549,9 +549,9 @@ hipError_t launch_quant_product(const QuantPlan &pl, QuantProduct p, hipStream_t
     if (p.vec && p.out_stride % 8 == 0 && reinterpret_cast<uintptr_t>(p.out) % 16 == 0) p.vec = 2;
     p.w_once = pl.x_tiles == 1 && p.m * p.d_pad > kL2Bytes;
     const Variant &v = kVariants[pl.variant];
-    hipLaunchKernelGGL(p.raw ? v.raw : v.kernel, dim3((unsigned)pl.wgs), dim3(512), 0, s, p);
+    hipLaunchKernelGGL(p.raw ? v.raw : v.kernel, dim3((unsigned)pl.wgs), dim3(kQuantThreads), 0, s, p);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess || pl.part == 0) return e;
-    const int64_t tiles = (int64_t)pl.x_tiles * pl.w_tiles;
+    const int64_t tiles = (int64_t)pl.x_tiles * pl.w_tiles;   // (cut ones: a few rounds)
     hipLaunchKernelGGL(quant_sum_kernel, dim3((unsigned)(tiles * (pl.bm * pl.bn / 1024))), dim3(256), 0, s, p, pl.bm, pl.bn);
     return hipGetLastError();
 }

@@ -10,6 +10,8 @@ constexpr int kQuantBlock = 128;             // values that share an exponent: o
 constexpr int kQuantTile = 256;              // rows of a tile of the weights
 constexpr int kQuantMostCuts = 64;           // of a tile along the depth
 constexpr int kQuantMostRounds = 4;          // of workgroups, of cut tiles
+constexpr int kQuantThreads = 512;           // of a workgroup of the product
+constexpr int64_t kQuantMostWorkgroups = 0xffffffffll / kQuantThreads;   // a grid has less than 2^32 threads
 
 // Tiles of the product's kernels.
 struct QuantVariant {
@@ -52,6 +54,7 @@ inline size_t quant_room(int64_t b, int64_t m, int64_t d_pad, int num_cus)
     return (size_t)std::min(std::min(rounds, cuts), held);
 }
 
+// wgs 0: more tiles than a launch has workgroups (outputs that no memory holds).
 inline QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, int num_cus)
 {
     QuantPlan pl{};
@@ -68,7 +71,7 @@ inline QuantPlan plan_quant_product(int64_t b, int64_t m, int64_t d_pad, int num
             const int64_t fit = r == 0 ? 1 : std::min<int64_t>(places * r / 4 / tiles, std::min(pl.nk, kQuantMostCuts));
             if (r > 0 && fit < 2) continue;
             const int splits = (int)fit;
-            if (splits > 1 && tiles * splits * v.bm * v.bn > room) continue;
+            if (tiles * splits > kQuantMostWorkgroups || (splits > 1 && tiles * splits * v.bm * v.bn > room)) continue;
             const double rounds = (double)((tiles * splits + places - 1) / places);
             // Workgroups in rounds; the weights out of memory (6.5 TB/s where one workgroup reads them, else 5.3); what a CU takes in (40 GB/s; all of them 10 TB/s), of which a part shows
             // beside either.

@@ -6,7 +6,7 @@
 namespace fz {
 
 constexpr int64_t kL2Bytes = 32 << 20;       // of the eight XCDs together
-constexpr int64_t kQuantMaxD = 1 << 22;      // a tile of 256 rows spans 32-bit offsets
+constexpr int64_t kQuantMaxD = 1 << 22;      // 2^31 rows of it stay within 64 bits of bytes
 
 inline int64_t quant_code_stride(int64_t d) { return (d + kQuantBlock - 1) / kQuantBlock * kQuantBlock; }
 inline int64_t quant_scale_stride(int64_t d) { return ((d + kQuantBlock - 1) / kQuantBlock + 3) / 4 * 4; }

@@ -52,6 +52,9 @@ def test_a_workspace_serves_every_smaller_batch(plans, m, d_pad):
     most_rows = most_part = 0
     for b in batches:
         p, rows, room = plans.plan(b, m, d_pad), plans.rows(b), plans.room(b, m, d_pad)
+        if p["wgs"] == 0:     # refused: more tiles than a launch has workgroups
+            assert b * m > 1 << 38
+            continue
         assert p["x_tiles"] * p["bm"] >= b and p["w_tiles"] * p["bn"] >= m and p["nk"] * 128 == d_pad
         assert 1 <= p["splits"] <= min(p["nk"], 64) and p["wgs"] == p["x_tiles"] * p["w_tiles"] * p["splits"]
         # what any smaller batch takes fits what this one asks for
@@ -60,3 +63,17 @@ def test_a_workspace_serves_every_smaller_batch(plans, m, d_pad):
         assert p["part"] == (p["wgs"] * p["bm"] * p["bn"] if p["splits"] > 1 else 0)
     sizes = [(plans.rows(b), plans.room(b, m, d_pad)) for b in batches]
     assert all(a[0] <= c[0] and a[1] <= c[1] for a, c in zip(sizes, sizes[1:]))
+
+
+def test_every_accepted_layer_has_a_launch(plans):
+    # a grid dimension has less than 2^32 threads, a workgroup 512 of them
+    rng = random.Random(5)
+    sizes = [(1, m, d) for m in (2147483647 - 513, 1100000000, 1 << 30, 1073741824 + 1, 1 << 23) for d in (128, 256, 1024)]
+    sizes += [(int(2 ** rng.uniform(0, 14)), int(2 ** rng.uniform(0, 31)) - 600, 128 * int(2 ** rng.uniform(0, 8))) for _ in range(3000)]
+    for b, m, d in sizes:
+        if m < 1 or b * m > 1 << 38:     # (beyond the memory of any device)
+            continue
+        p = plans.plan(b, m, d)
+        assert 0 < p["wgs"] * 512 < 1 << 32, (b, m, d, p)
+        assert p["splits"] == 1 or p["x_tiles"] * p["w_tiles"] * p["bm"] * p["bn"] // 4 < 1 << 32
+    assert plans.plan(1 << 30, 1 << 30, 128)["wgs"] == 0
