@@ -326,7 +326,8 @@ int freeze_gather_rows(const float *x, int64_t d, const int32_t *sel, const int3
  *
  * Quantised rows: a row of d values is cut into blocks of 128 (the last one may be shorter).  A block is held as codes
  * and an exponent E, the smallest integer >= -126 with max|x| <= 448 * 2^E; its codes are x * 2^-E rounded to nearest even
- * (FREEZE_E4M3).  Every factor is a power of two, so that a code is one rounding of the value.
+ * (FREEZE_E4M3).  Every factor is a power of two, so that a code is one rounding of the value.  An infinity or a NaN has a code that is
+ * no number, and its block an exponent of 120 or 121.
  *   codes   [rows, freeze_quantised_code_stride(d)] bytes, zero behind d;
  *   scales  [rows, freeze_quantised_scale_stride(d)] bytes E + 127, 1 behind the last block.
  * Strides: d rounded up to 128, the number of blocks rounded up to 4; 0 on invalid d.  1 <= d <= 2^22.
@@ -340,7 +341,8 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
                          uint8_t *codes, uint8_t *scales, void *stream);
 
 /*
- * Dense layer with quantised weights: y = W x + bias, optionally through ReLU, W and x as quantised rows.  It occupies
+ * Dense layer with quantised weights: y = W x + bias, optionally through ReLU (of NaN: NaN), W and x as quantised rows.  A row of x or W
+ * with a code that is no number has outputs that are NaN, no other row's outputs show it.  It occupies
  * one of the context's slots (look-ups and freeze_project on that slot fail with FREEZE_ENOTBUILT, and
  * freeze_quantised_project does on every other slot).
  *   weights  [m, d] row-major, fp32 or bf16, quantised by the call (weight_scales NULL); or FREEZE_E4M3: codes and

@@ -45,6 +45,9 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b)
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
 }
 
+// no number stays what it is
+__device__ __forceinline__ float relu_of(float v) { return v <= 0.f ? 0.f : v; }
+
 // outputs col .. col + 3 of a row
 __device__ __forceinline__ void store_outputs(const QuantProduct &p, int64_t row, int64_t col, f32x4 v)
 {
@@ -52,7 +55,7 @@ __device__ __forceinline__ void store_outputs(const QuantProduct &p, int64_t row
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         if (p.bias) v[e] += p.bias[col + e < p.m ? col + e : p.m - 1];
-        if (p.relu) v[e] = __builtin_fmaxf(v[e], 0.f);
+        if (p.relu) v[e] = relu_of(v[e]);
     }
     const int64_t at = row * p.out_stride + col;
     if (p.vec && col + 4 <= p.m) {
@@ -152,7 +155,7 @@ __device__ __forceinline__ void tile_out(const QuantProduct &p, const f32x4 (&ac
                 v[j] = acc[i][j] + bias[j];
                 if (p.relu)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v[j][e] = __builtin_fmaxf(v[j][e], 0.f);
+                    for (int e = 0; e < 4; ++e) v[j][e] = relu_of(v[j][e]);
             }
             if (!p.out_bf16) {
 #pragma unroll

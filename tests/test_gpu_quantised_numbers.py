@@ -59,3 +59,41 @@ def test_one_workspace_for_a_batch_that_shrinks(m, d):
                 assert torch.equal(out, fc.quantised_project(0, x[:b].clone(), out_dtype=out.dtype))
     finally:
         fc.close()
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("xt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("b,d,m", [(1, 256, 40), (7, 256, 500), (9, 4097, 200), (70, 300, 300), (300, 1024, 1000), (2100, 512, 1032)])
+def test_no_numbers_show_in_their_rows_alone(b, d, m, xt, out):
+    inf, nan = float("inf"), float("nan")
+    x, w, bias = _noise(b, d, 11), _noise(m, d, 12), torch.linspace(-1, 1, m, device="cuda")
+    x = x.to(xt)
+    clean = x.clone()
+    bad = {b // 2: nan, b - 1: inf, 0: -inf}
+    for row, value in bad.items():
+        x[row, (row * 37 + 5) % d] = value
+    fc = binding.FreezeCache(1)
+    try:
+        fc.build_quantised(0, w, bias)
+        codes, scales = fc.quantise_rows(x)
+        assert (scales[:, :-(-d // 128)].amax(1)[list(bad)] >= 247).all()
+        for relu in (False, True):
+            want = fc.quantised_project(0, clean, relu=relu, out_dtype=out)
+            rows = torch.tensor([r not in bad for r in range(b)], device="cuda")
+            for got in (fc.quantised_project(0, x, relu=relu, out_dtype=out), fc.quantised_project(0, codes, scales, relu=relu, out_dtype=out)):
+                assert torch.isnan(got[list(bad)]).all() and torch.equal(got[rows], want[rows])
+        # in the weights: their output alone, for every row
+        w[m // 3, d // 2], w[m - 1, 0] = nan, inf
+        fc.build_quantised(0, w, bias)
+        got = fc.quantised_project(0, clean, relu=True, out_dtype=out)
+        assert torch.isnan(got[:, [m // 3, m - 1]]).all()
+        keep = torch.tensor([c not in (m // 3, m - 1) for c in range(m)], device="cuda")
+        assert torch.equal(got[:, keep], want[:, keep])
+        # (a bias that is no number; infinite outputs)
+        bias[3], w[:] = nan, 1.0
+        w[5], w[6] = 3e38, -3e38
+        fc.build_quantised(0, w, bias)
+        got = fc.quantised_project(0, torch.full((b, d), 4.0, device="cuda").to(xt), relu=True, out_dtype=out)
+        assert torch.isnan(got[:, 3]).all() and (got[:, 5] == inf).all() and (got[:, 6] == 0).all()
+    finally:
+        fc.close()
