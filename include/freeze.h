@@ -355,7 +355,10 @@ int freeze_quantise_rows(const void *x, int x_dtype, int64_t rows, int64_t d, in
  *            and x_stride are not looked at).
  *   out      [b, m] out_dtype, out_stride elements from row to row (>= m); elements between rows are left as they
  *            are.  It may lie over x.
- *            FREEZE_F32: products are exact and summed in fp32.  FREEZE_BF16: the same sums, rounded to nearest even once.
+ *            FREEZE_F32: the values that codes stand for are taken as bf16, their products are exact and summed in fp32.  A value is its bf16
+ *            number, but for the ends of the range: below 2^-126 it counts as the nearest multiple of 2^-133, and 2^128, which the largest fp32
+ *            numbers round up to, as infinite.  FREEZE_BF16: the same sums, rounded to nearest even once.
+ *            How many rows a call has decides in which order an output's products are added: its last bits may go by b.
  *   workspace  freeze_quantised_workspace_bytes() bytes, 256-byte aligned; scratch only.  The bytes for a batch serve every
  *            smaller one too, and either type of output.  Calls that share a workspace (replays of
  *            captured ones too) must follow one another on the device.  It may not lie over x or out.

@@ -4,7 +4,7 @@
 //
 // A k-step is a block of 128 codes: 128 bytes a row, copied as they are into LDS (direct loads) with the scale bytes of the four
 // blocks it belongs to; both operands are laid out so that a stage is a run of memory (QuantRows).  Codes widen to bf16 in registers, their
-// scale applied by the same instruction; bf16 matrix instructions, exact products summed in fp32.  (The 8-bit matrix instructions have twice the
+// scale applied by the same instruction; bf16 matrix instructions, exact products (see widen) summed in fp32.  (The 8-bit matrix instructions have twice the
 // rate, but cut the products of eight neighbours off 13 bits below the largest's exponent: up to 8e-5 of the result's norm, and where large terms
 // cancel nothing is left of the small ones.  Not even a bf16 output is worth its bits then: 2.9 % of them were a step off at
 // 4,096 x 2,048 -> 2,048.)
@@ -25,7 +25,8 @@ typedef __attribute__((address_space(3))) void *lds_void_ptr;
 
 namespace {
 
-// four codes of a word times 2^(exponent of s): four bf16, exact
+// four codes of a word times 2^(exponent of s): four bf16, exact from 2^-126 on; below that to the nearest multiple of 2^-133, where codes of the
+// lowest exponents reach 2^-135.  (The matrix instructions take such numbers as they are.)  256 * 2^120 is infinite.
 __device__ __forceinline__ u32x2 widen(uint32_t codes, float s)
 {
     return u32x2{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)codes, s, false)),

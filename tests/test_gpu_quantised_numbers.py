@@ -97,3 +97,36 @@ def test_no_numbers_show_in_their_rows_alone(b, d, m, xt, out):
         assert torch.isnan(got[:, 3]).all() and (got[:, 5] == inf).all() and (got[:, 6] == 0).all()
     finally:
         fc.close()
+
+
+@pytest.mark.parametrize("b", [1, 40, 300])
+def test_the_ends_of_the_range(b):
+    """Values below 2^-126 count as the nearest multiple of 2^-133 (off by 2^-134 at most), beside weights that make them matter; a row of fp32's
+    largest numbers is held as 2^128."""
+    d, m = 512, 260
+    w = _noise(m, d, 3)
+    w = w.clamp(-3.5, 3.5) * 2.0 ** 100
+    x = _noise(b, d, 4) * torch.exp2(torch.tensor([-118.0, -120.0, -124.0, -128.0], device="cuda")).repeat_interleave(128)
+    fc = binding.FreezeCache(1)
+    try:
+        fc.build_quantised(0, w)
+        values = []
+        for t in (x, w):
+            codes, scales = fc.quantise_rows(t)
+            values.append((codes.double().view(-1, d // 128, 128) * torch.exp2(scales.double() - 127).unsqueeze(2)).view(-1, d))
+        xv, wv = values
+        assert ((xv != 0) & (xv.abs() < 2.0 ** -130)).any()
+        y, size = xv @ wv.t().contiguous(), xv.abs() @ wv.abs().t().contiguous()
+        # d / 32 + 16 roundings of fp32 sums, and what the smallest values lose
+        tol = (16 + d / 32) * 2.0 ** -24 * size + 2.0 ** -134 * wv.abs().sum(1)
+        off = (fc.quantised_project(0, x).double() - y).abs()
+        assert (off <= tol).all(), (off / tol).max().item()
+        nearest = torch.where(xv.abs() < 2.0 ** -126, torch.round(xv * 2.0 ** 133) * 2.0 ** -133, xv)
+        off = (fc.quantised_project(0, x).double() - nearest @ wv.t().contiguous()).abs()
+        assert (off <= (16 + d / 32) * 2.0 ** -24 * size).all()
+        fc.build_quantised(0, torch.full((m, d), 2.0 ** -100, device="cuda"))
+        assert (fc.quantised_project(0, torch.full((b, d), torch.finfo(torch.float32).max, device="cuda")) == float("inf")).all()
+        large = torch.full((b, d), 240.0 * 2.0 ** 120, device="cuda")
+        assert (fc.quantised_project(0, large) == d * 240.0 * 2.0 ** 20).all()
+    finally:
+        fc.close()
