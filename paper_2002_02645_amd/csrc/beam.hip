@@ -7,11 +7,11 @@
 //     best so far lie in its lanes in order (value, then index).  A new one is inserted by a ballot and a shift of the lanes; that is
 //     some hundred cycles, so that few may come to it: of a run of 16 batches only the lanes' largest values are kept at first, the k-th of
 //     64 lanes' largest is a limit that about k values of the run reach, and the loads that hold these are read again, out of L2 as a
-//     rule.  512 rows of 131,072 bf16 with k 16: 31.4 us; with every batch looked through at once for the k best so far 39.8.
+//     rule.  512 rows of 131,072 bf16 with k 16: 30.7 us; with every batch looked through at once for the k best so far 39.8.
 //   - The sums of exponentials are kept per lane relative to the lane's largest value: a batch in fp32, the batches in fp64 (a batch's sum
 //     may be lost in a large one that was there before it; a row of a million would add that up).
-// 121 MB (a tenth of the rows has ended) at 31.4 us are 3.9 TB/s: without the choice 24 us, of which the exponentials and the comparisons
-// are 17 us of issue; small calls (4 rows of 32,000 fp32: 5.8 us) are bound by the way through the code.
+// 121 MB (a tenth of the rows has ended) at 30.7 us are 3.9 TB/s: without the choice 24 us, of which the exponentials and the comparisons
+// are 17 us of issue; small calls (4 rows of 32,000 fp32: 5.7 us) are bound by the way through the code.
 #include "../../include/freeze.h"
 #include "freeze_internal.h"
 #include "select_common.h"
@@ -330,7 +330,8 @@ __global__ __launch_bounds__(256) void beam_rows_kernel(BeamArgs p)
 // One workgroup a group: the rows' offsets score - log sum exp(l - largest l), then the k best of the pieces' lists.  What reaches the k-th largest of some
 // wave's lanes' largest is gathered, as a rule a few more than k, and every one of them counts those before it; where
 // too many reach it (or there are more than kMeetHeld), the waves keep lists as the pieces did.  Bound by its chain of dependent steps: one
-// group of 4 rows 5.2 us, 64 groups of 8 rows 7.0 (5.9 and 8.6 with each load where its value is needed).
+// group of 4 rows 5.4 us, 64 groups of 8 rows 7.7 (5.2 and 7.0 with a row and a token alone to go by where totals are equal, which leaves out the
+// values; 0.7 and 1.6 more with each load where its value is needed).
 constexpr int kMeetThreads = 256, kMeetHeld = 4096, kMeetGathered = 512, kMeetEarly = 4;
 __global__ __launch_bounds__(kMeetThreads) void beam_meet_kernel(BeamArgs p)
 {

@@ -332,7 +332,7 @@ __global__ __launch_bounds__(kQuantThreads, 2) void quant_gemm_kernel(QuantProdu
 // keeps its four blocks of w rows' fragments (16 rows each) for half a step (64 codes) and goes through its XB blocks of x rows, a group of
 // matrix instructions each; their codes are read kAhead groups ahead.  The step's barrier comes
 // before its last kAhead groups, which need nothing newer: it publishes the next step's stage and frees this one, which is refilled from there on.
-// 10,000 x 8,192 -> 1,024 130 us, 1.29 PFLOP/s, the matrix pipes busy 55 % of all cycles; 4,096 x 8,192 -> 8,192 with its quantisation 400 us, 1.37 PFLOP/s.
+// 10,000 x 8,192 -> 1,024 128 - 140 us by card, 1.2 - 1.3 PFLOP/s, the matrix pipes busy 55 % of all cycles; 4,096 x 8,192 -> 8,192 399 us, 1.38 PFLOP/s, 66 %.
 template <int XB>
 __global__ __launch_bounds__(kQuantThreads, 2) void quant_tile_kernel(QuantProduct p)
 {
