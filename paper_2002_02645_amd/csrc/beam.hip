@@ -523,7 +523,7 @@ BeamPlan beam_plan(int64_t rows, int64_t vocab, int size)
     pl.parts = (int)((batches + per - 1) / per);
     return pl;
 }
-// Places for the pieces' lists: as many as fewer rows may take too (a plan's own number goes up and down: 3,068 rows are cut in two, 3,072 not
+// Places for the pieces' lists: as many as fewer rows may take too (a plan's own number goes up and down: 767 groups of 4 rows are cut in two, 768 not
 // at all), so that a workspace serves every smaller call.
 size_t beam_units(int64_t rows, int64_t vocab)
 {
