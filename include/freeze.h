@@ -426,6 +426,107 @@ int freeze_reorder_states(const freeze_state *states, int num_states, const int3
                           int64_t src_rows, void *stream);
 
 /*
+ * Rotary positions: every head of a token is turned by the token's place, pair by pair,
+ *     y_a = f (x_a cos - x_b sin),  y_b = f (x_a sin + x_b cos),  angle = positions[token] * frequencies[i]
+ * for pair i < pairs of elements a, b: 2i and 2i + 1 (interleaved), or i and i + pairs; elements from 2 * pairs on are copied.
+ *   heads        host array [num] of freeze_heads: tensors of one call (queries and keys) share its positions.
+ *   positions    [tokens] int32, any value;  frequencies [pairs] fp64, radians a place (a longer context's scaling is in them), finite.
+ *   inverse      nonzero: the angle is negated (which, with the same f, is the gradient of a call).
+ * Angles are formed in fp64 and taken less their whole turns, sine, cosine and the products in fp32, outputs rounded once.  dst may be src with the same
+ * strides (in place), and shares no byte of its extent with anything else that the call reads or writes; tensors of one token stride may lie side by side in the
+ * rows of one buffer.
+ * 1 <= head_dim <= 4096, 0 <= 2 * pairs <= head_dim, 0 <= tokens < 2^31, 0 <= heads <= 65536, 0 <= num <= 8, |factor| <= 3e38; nothing to do is a no-op.
+ */
+typedef struct freeze_heads {
+    const void *src;
+    void *dst;
+    int32_t dtype;                                  /* FREEZE_F32 or FREEZE_BF16, of both */
+    int32_t heads;
+    int64_t src_token_stride, src_head_stride;      /* elements; the elements of a head follow one another */
+    int64_t dst_token_stride, dst_head_stride;
+} freeze_heads;
+int freeze_rotate_positions(const freeze_heads *heads, int num, int64_t tokens, int64_t head_dim, const int32_t *positions,
+                            const double *frequencies, int64_t pairs, int interleaved, float factor, int inverse, void *stream);
+
+/*
+ * Keys and values of attention in pages of 8 bits.  A pool of pages is shared by the rows of a batch (requests, or the beams of requests):
+ * a row is a table of pages and a length, a page holds page_tokens tokens' keys and values of every layer, and rows that went on from one parent name the
+ * same pages.  Everything is device memory that the calls keep up themselves, without a word to the host: they may be captured into graphs.
+ *   codes    [layers, num_pages, heads, page_tokens / 32, 2 (keys, values), 32 * W], W = head_dim rounded up to 32; 16-byte aligned;
+ *   scales   [layers, num_pages, heads, page_tokens / 32, 2]: a block of 32 tokens of a head has an exponent E for its keys and one for its
+ *            values, the smallest E >= -126 with max|x| <= 448 * 2^E over the finite values (it never falls while the block fills up); the byte is E + 127, codes are
+ *            x * 2^-E rounded to nearest even (FREEZE_E4M3).  Where E grows, the codes that are there are scaled down and rounded again.  An
+ *            infinity or a NaN has a code that is no number.
+ *            Byte of token t, element c (from 0 in the block): c / 32 * 1024 + ((c % 32 / 8) * 16 + t % 16) * 16 + t / 16 * 8 + c % 8 for keys,
+ *            c / 32 * 1024 + ((t % 16 / 4) * 16 + c % 16) * 16 + (c % 32 / 16) * 8 + t / 16 * 4 + t % 4 for values.  Elements behind head_dim are 0.
+ *   refs     [num_pages] int32: how many table entries name the page; 0: it is free.
+ *   tables   [rows, max_pages] int32: the row's pages in order, -1 behind them.  A row of n tokens has ceil(n / page_tokens) pages.
+ *   lengths  [rows] int32.
+ * A new pool: refs 0, tables -1, lengths 0, codes and scales as they are.  No two of the five share a byte.  Page numbers outside the pool (a caller's own tables) are
+ * never followed: such a page's tokens are not attended to, written or counted.
+ * 1 <= layers, heads <= 1024, 1 <= head_dim <= 256, page_tokens a power of two, 32 .. 1024, 1 <= num_pages <= 2^24, 1 <= rows <= 16384,
+ * 1 <= max_pages <= 2^20, max_pages * page_tokens < 2^31, at most 2^46 bytes of codes.
+ */
+typedef struct freeze_pages {
+    uint8_t *codes, *scales;
+    int32_t *refs, *tables, *lengths;
+    int64_t num_pages, rows, max_pages;
+    int32_t layers, heads, head_dim, page_tokens;
+} freeze_pages;
+/* Bytes of codes (scales: one for every 16 * W of them); 0 where a size is out of range.  Pointers are not looked at. */
+size_t freeze_pages_bytes(const freeze_pages *pages);
+
+/*
+ * Room for add[r] (NULL: 1 for every row; below 0 counts as 0) more tokens of each row r, whose length grows by as much.  Free pages are given out in order of their numbers,
+ * row by row.  A last page that is partly filled and has other references is replaced by a copy (of its filled blocks, all layers), the first of the row's pages here.
+ *   out_granted [rows] int32: add[r], or 0 for a row that stays as it is: its table has no place for as many pages, or (from the first row on that this meets,
+ *            for all that need a page) the pool has not enough free pages.  Pages that lose their last reference here are free for the next call.
+ *   workspace  freeze_pages_workspace_bytes() bytes, 256-byte aligned; scratch only, shared by calls that follow one another only.
+ */
+size_t freeze_pages_workspace_bytes(const freeze_pages *pages);
+int freeze_pages_reserve(const freeze_pages *pages, const int32_t *add, int32_t *out_granted, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Row r becomes a second reference to what row parents[r] was (parents [rows] int32, outside [0, rows): the row stays), all rows at once.  No page is copied. */
+int freeze_pages_fork(const freeze_pages *pages, const int32_t *parents, void *stream);
+
+/* Row r keeps its first keep[r] tokens (keep [rows] int32; below 0 or not below the length: all of them); pages behind them lose a reference.  0 frees the row. */
+int freeze_pages_truncate(const freeze_pages *pages, const int32_t *keep, void *stream);
+
+/* The U pages in use move to the numbers 0 .. U - 1 (those from U on, in order, to the free numbers below U, in order), tables follow.  out_used [1] int32: U.
+ * workspace as of freeze_pages_reserve. */
+int freeze_pages_compact(const freeze_pages *pages, int32_t *out_used, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Keys and values of the rows' newest tokens go into a layer's pages; the rows have room for them already (freeze_pages_reserve): those of row r are its
+ * last n_r.  Slots behind a row's last token in the block that it ends in become 0.
+ *   k, v     [tokens, heads, head_dim] fp32 or bf16 (one type), strides in elements; the elements of a head follow one another.
+ *   starts   [rows + 1] int32: row r's are tokens starts[r] .. starts[r + 1] - 1; NULL: one token a row, tokens == rows.
+ *   most     no row has more than this (0: tokens); a row that has, whose tokens are not all in 0 .. tokens - 1, or which has fewer than n_r tokens, is not written.
+ *   granted  [rows] int32 or NULL: rows whose n_r is another are not written.
+ * A page with several references is not written.
+ */
+int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v,
+                        int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t tokens, const int32_t *starts, int64_t most,
+                        const int32_t *granted, void *stream);
+
+/*
+ * Attention of the rows' newest tokens over a layer's pages (which hold them already): token i of row r's n_r has place p = lengths[r] - n_r + i and attends to the
+ * places max(0, p - window + 1) .. p (window 0: from 0 on) with weights softmax(scale * q . key); nothing to attend to (p < 0): 0.
+ *   q        [tokens, heads * group, head_dim] fp32 or bf16; head j reads keys and values of head j / group.
+ *   out      [tokens, heads * group, head_dim] FREEZE_F32 or FREEZE_BF16, with strides of its own; shares no byte of its extent with the inputs.
+ *   starts, tokens, most: as of freeze_pages_append; outputs of rows that are not in order, and tokens that are no row's, are left as they are.
+ * Products of codes are exact, sums and softmax statistics fp32.  With q in bf16, weights are rounded to bf16 for the product with the values (their sum is of the
+ * unrounded ones); with fp32 they and q are taken in three parts of bf16, exact to 2^-24.  Scores have to be within fp32's range; a NaN in a key or value that a token attends to, or in
+ * its own q, makes its output NaN, and no other's.
+ *   workspace  freeze_pages_attend_workspace_bytes() bytes, 256-byte aligned; scratch only, shared by calls that follow one another only.  The bytes for some tokens serve fewer too.
+ * 1 <= group <= 1024, 0 <= tokens < 2^31, (tokens * group + 16 * rows) * heads < 2^28, 0 < scale <= 3e38, 0 <= window < 2^31; tokens == 0 is a no-op.
+ */
+size_t freeze_pages_attend_workspace_bytes(const freeze_pages *pages, int group, int64_t tokens, int64_t most, int packed);
+int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int q_dtype, int64_t q_token_stride, int64_t q_head_stride, int group,
+                        int64_t tokens, const int32_t *starts, int64_t most, float scale, int64_t window, void *out, int out_dtype,
+                        int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Counters of how the look-ups of this context were confirmed (measurement aid): while a device
  * array of three uint64 is attached, every look-up adds to it the number of queries whose result was
  * confirmed exact after the first re-scoring [0], after the wider re-scoring [1], and the number

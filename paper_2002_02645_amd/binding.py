@@ -30,6 +30,20 @@ class FreezeState(ctypes.Structure):
                 ("piece_bytes", ctypes.c_int64)]
 
 
+class FreezeHeads(ctypes.Structure):
+    """freeze_heads of the C ABI."""
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("src_token_stride", ctypes.c_int64), ("src_head_stride", ctypes.c_int64), ("dst_token_stride", ctypes.c_int64),
+                ("dst_head_stride", ctypes.c_int64)]
+
+
+class FreezePagesPool(ctypes.Structure):
+    """freeze_pages of the C ABI."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("refs", ctypes.c_void_p), ("tables", ctypes.c_void_p),
+                ("lengths", ctypes.c_void_p), ("num_pages", ctypes.c_int64), ("rows", ctypes.c_int64), ("max_pages", ctypes.c_int64),
+                ("layers", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_tokens", ctypes.c_int32)]
+
+
 class FreezeError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -110,6 +124,26 @@ def lib():
     L.freeze_beam_select.argtypes = [p, i32, i64, i32, i64, i64, p, p, ctypes.c_int32, i32, p, p, p, p, p, sz, p]
     L.freeze_reorder_states.restype = i32
     L.freeze_reorder_states.argtypes = [p, i32, p, i64, i64, p]
+    L.freeze_rotate_positions.restype = i32
+    L.freeze_rotate_positions.argtypes = [p, i32, i64, i64, p, p, i64, i32, ctypes.c_float, i32, p]
+    L.freeze_pages_bytes.restype = sz
+    L.freeze_pages_bytes.argtypes = [p]
+    L.freeze_pages_workspace_bytes.restype = sz
+    L.freeze_pages_workspace_bytes.argtypes = [p]
+    L.freeze_pages_reserve.restype = i32
+    L.freeze_pages_reserve.argtypes = [p, p, p, p, sz, p]
+    L.freeze_pages_fork.restype = i32
+    L.freeze_pages_fork.argtypes = [p, p, p]
+    L.freeze_pages_truncate.restype = i32
+    L.freeze_pages_truncate.argtypes = [p, p, p]
+    L.freeze_pages_compact.restype = i32
+    L.freeze_pages_compact.argtypes = [p, p, p, sz, p]
+    L.freeze_pages_append.restype = i32
+    L.freeze_pages_append.argtypes = [p, i32, p, i64, i64, p, i64, i64, i32, i64, p, i64, p, p]
+    L.freeze_pages_attend_workspace_bytes.restype = sz
+    L.freeze_pages_attend_workspace_bytes.argtypes = [p, i32, i64, i64, i32]
+    L.freeze_pages_attend.restype = i32
+    L.freeze_pages_attend.argtypes = [p, i32, p, i32, i64, i64, i32, i64, p, i64, ctypes.c_float, i64, p, i32, i64, i64, p, sz, p]
     L.freeze_compute_thresholds.restype = i32
     L.freeze_compute_thresholds.argtypes = [p, i32, p, p, i64, i32, i32, p, p, p, sz, p]
     L.freeze_lookup_stats_attach.restype = i32
@@ -535,6 +569,123 @@ def freeze_reorder_states(states: Sequence[FreezeState], parents: torch.Tensor, 
                                        _on(stream)), "freeze_reorder_states")
 
 
+def _heads_of(t: torch.Tensor, heads: Optional[int] = None, dim: Optional[int] = None) -> tuple:
+    """Elements from token to token and from head to head of a tensor [tokens, heads, dim] whose heads are dense."""
+    if not (t.dim() == 3 and t.dtype in (torch.float32, torch.bfloat16) and (heads is None or t.shape[1] == heads) and (dim is None or t.shape[2] == dim)):
+        raise _refused()
+    tokens, n, d = t.shape
+    token, head, one = t.stride()
+    if one != 1 and d > 1:
+        raise _refused("the last dimension has to be dense")
+    return token if tokens > 1 else 0, head if n > 1 else 0
+
+
+def _numbers(t: Optional[torch.Tensor], n: int) -> None:
+    if t is not None and not (t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n):
+        raise _refused("a dense int32 tensor of another size is needed")
+
+
+def rotary_frequencies(pairs: int, base: float = 10000.0, stretch: float = 1.0, trained: int = 0, low: float = 1.0, high: float = 4.0,
+                       device="cuda:0") -> torch.Tensor:
+    """Frequencies of freeze_rotate_positions, radians a place, fp64: base ** (-i / pairs) for pair i.  stretch: for a context so many times
+    longer than the one that a model was trained on, every frequency is divided by it; where `trained` (the places it was trained on) is given, one that turns
+    at least `high` times within them stays as it is, one that turns less than `low` times is divided, those between go over linearly in the turns."""
+    if pairs < 0 or not (base > 0 and stretch > 0 and (trained == 0 or high > low)):
+        raise _refused()
+    f = torch.tensor([base ** (-i / pairs) for i in range(pairs)], dtype=torch.float64)
+    if trained:
+        keep = ((trained * f / 6.283185307179586 - low) / (high - low)).clamp(0, 1)
+        f = f * (keep + (1 - keep) / stretch)
+    else:
+        f = f / stretch
+    return f.to(device)
+
+
+def freeze_rotate_positions(tensors: Sequence[tuple], positions: torch.Tensor, frequencies: torch.Tensor, interleaved: bool = False, factor: float = 1.0,
+                            inverse: bool = False, stream=None) -> None:
+    """tensors: pairs (src, dst) of [tokens, heads, head_dim], dst of src's type and shape (or src itself: in place)."""
+    if not tensors:
+        return
+    tokens, _, dim = tensors[0][0].shape
+    arr = (FreezeHeads * len(tensors))()
+    for h, (src, dst) in zip(arr, tensors):
+        _here(src, dst)
+        if src.shape != dst.shape or src.dtype != dst.dtype or src.shape[0] != tokens or src.shape[2] != dim:
+            raise _refused()
+        h.src, h.dst, h.dtype, h.heads = src.data_ptr(), dst.data_ptr(), _DTYPES.get(src.dtype, -1), src.shape[1]
+        h.src_token_stride, h.src_head_stride = _heads_of(src)
+        h.dst_token_stride, h.dst_head_stride = _heads_of(dst)
+    _here(positions, frequencies)
+    _numbers(positions, tokens)
+    if not (frequencies.dtype == torch.float64 and frequencies.is_contiguous() and 2 * frequencies.numel() <= dim):
+        raise _refused()
+    _check(lib().freeze_rotate_positions(ctypes.addressof(arr), len(tensors), tokens, dim, positions.data_ptr(), frequencies.data_ptr(),
+                                         frequencies.numel(), int(interleaved), factor, int(inverse), _on(stream)), "freeze_rotate_positions")
+
+
+def freeze_pages_bytes(pool: FreezePagesPool) -> int:
+    return int(lib().freeze_pages_bytes(ctypes.addressof(pool)))
+
+
+def freeze_pages_workspace_bytes(pool: FreezePagesPool) -> int:
+    return int(lib().freeze_pages_workspace_bytes(ctypes.addressof(pool)))
+
+
+def freeze_pages_reserve(pool: FreezePagesPool, add: Optional[torch.Tensor], granted: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    _here(add, granted, workspace)
+    _numbers(add, pool.rows)
+    _numbers(granted, pool.rows)
+    _check(lib().freeze_pages_reserve(ctypes.addressof(pool), _at(add), _at(granted), _at(workspace), workspace.nbytes, _on(stream)), "freeze_pages_reserve")
+
+
+def freeze_pages_fork(pool: FreezePagesPool, parents: torch.Tensor, stream=None) -> None:
+    _here(parents)
+    _numbers(parents, pool.rows)
+    _check(lib().freeze_pages_fork(ctypes.addressof(pool), _at(parents), _on(stream)), "freeze_pages_fork")
+
+
+def freeze_pages_truncate(pool: FreezePagesPool, keep: torch.Tensor, stream=None) -> None:
+    _here(keep)
+    _numbers(keep, pool.rows)
+    _check(lib().freeze_pages_truncate(ctypes.addressof(pool), _at(keep), _on(stream)), "freeze_pages_truncate")
+
+
+def freeze_pages_compact(pool: FreezePagesPool, used: torch.Tensor, workspace: torch.Tensor, stream=None) -> None:
+    _here(used, workspace)
+    _numbers(used, 1)
+    _check(lib().freeze_pages_compact(ctypes.addressof(pool), _at(used), _at(workspace), workspace.nbytes, _on(stream)), "freeze_pages_compact")
+
+
+def freeze_pages_append(pool: FreezePagesPool, layer: int, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, most: int = 0,
+                        granted: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [tokens, heads, head_dim] fp32 or bf16; starts [rows + 1] int32, or None for one token a row."""
+    _here(k, v, starts, granted)
+    if k.shape != v.shape or k.dtype != v.dtype:
+        raise _refused()
+    ks, vs = _heads_of(k, pool.heads, pool.head_dim), _heads_of(v, pool.heads, pool.head_dim)
+    _numbers(starts, pool.rows + 1)
+    _numbers(granted, pool.rows)
+    _check(lib().freeze_pages_append(ctypes.addressof(pool), layer, k.data_ptr(), *ks, v.data_ptr(), *vs, _DTYPES[k.dtype], k.shape[0], _at(starts), most,
+                                     _at(granted), _on(stream)), "freeze_pages_append")
+
+
+def freeze_pages_attend_workspace_bytes(pool: FreezePagesPool, group: int, tokens: int, most: int = 0, packed: bool = True) -> int:
+    return int(lib().freeze_pages_attend_workspace_bytes(ctypes.addressof(pool), group, tokens, most, int(packed)))
+
+
+def freeze_pages_attend(pool: FreezePagesPool, layer: int, q: torch.Tensor, scale: float, out: torch.Tensor, workspace: torch.Tensor,
+                        starts: Optional[torch.Tensor] = None, most: int = 0, window: int = 0, stream=None) -> None:
+    """q, out [tokens, heads * group, head_dim] fp32 or bf16 each; starts [rows + 1] int32, or None for one token a row."""
+    _here(q, out, workspace, starts)
+    qs, os_ = _heads_of(q, None, pool.head_dim), _heads_of(out, None, pool.head_dim)
+    if q.shape != out.shape or q.shape[1] == 0 or q.shape[1] % pool.heads != 0:
+        raise _refused()
+    _numbers(starts, pool.rows + 1)
+    _check(lib().freeze_pages_attend(ctypes.addressof(pool), layer, q.data_ptr(), _DTYPES[q.dtype], *qs, q.shape[1] // pool.heads, q.shape[0], _at(starts), most,
+                                     scale, window, out.data_ptr(), _DTYPES[out.dtype], *os_, _at(workspace), workspace.nbytes, _on(stream)),
+           "freeze_pages_attend")
+
+
 def freeze_compact_misses(hit: torch.Tensor, sel_in: Optional[torch.Tensor], sel_out: torch.Tensor,
                           out_count: torch.Tensor, stream=None) -> None:
     assert hit.is_cuda and hit.dtype == torch.uint8
@@ -849,3 +1000,90 @@ class FreezeCache:
         if not (parents.numel() <= rows and all(t.shape[row_dim] == rows for t in src)):   # (state_of: a dst is like its src)
             raise _refused()
         freeze_reorder_states([state_of(s, d, used, row_dim) for s, d in zip(src, dst)], parents, rows)
+
+    def rotate_positions(self, x, positions: torch.Tensor, frequencies: torch.Tensor, interleaved: bool = False, factor: float = 1.0,
+                         inverse: bool = False, out=None):
+        """Heads turned by their tokens' places (a tensor [tokens, heads, head_dim], or several that share positions; see rotary_frequencies).
+        out: where they go, x itself for in place; None: new tensors."""
+        one = isinstance(x, torch.Tensor)
+        xs = (x,) if one else tuple(x)
+        outs = [torch.empty(t.shape, dtype=t.dtype, device=self.device) for t in xs] if out is None else [out] if one else list(out)
+        if len(outs) != len(xs):
+            raise _refused()
+        _here(*xs, *outs, holder=self)
+        freeze_rotate_positions(list(zip(xs, outs)), positions, frequencies, interleaved, factor, inverse)
+        return outs[0] if one else outs
+
+
+class FreezePages:
+    """A generating model's keys and values in pages of 8 bits: the pool, the rows' tables and scratch memory for each stream.  Rows start empty.  What changes the
+    pool (reserve, fork, truncate, compact, append) and calls that read it on another stream are the caller's to order."""
+
+    def __init__(self, layers: int, num_pages: int, rows: int, max_pages: int, heads: int, head_dim: int, page_tokens: int = 64, device="cuda:0"):
+        self.device = torch.device(device)
+        self._index = self.device.index if self.device.type == "cuda" else -1
+        self.pool = FreezePagesPool(None, None, None, None, None, num_pages, rows, max_pages, layers, heads, head_dim, page_tokens)
+        nbytes = freeze_pages_bytes(self.pool)
+        if nbytes == 0:
+            raise FreezeError(FREEZE_EINVAL, "freeze_pages_bytes")
+        width = (head_dim + 31) // 32 * 32
+        lead = (layers, num_pages, heads, page_tokens // 32, 2)
+        self.codes = torch.zeros((*lead, 32 * width), dtype=torch.uint8, device=self.device).view(torch.float8_e4m3fn)
+        self.scales = torch.full(lead, 1, dtype=torch.uint8, device=self.device)
+        # the bookkeeping in one run of memory: tables, lengths, references
+        self.book = torch.zeros(rows * max_pages + rows + num_pages, dtype=torch.int32, device=self.device)
+        tables, self.lengths, self.refs = self.book.split([rows * max_pages, rows, num_pages])
+        self.tables = tables.view(rows, max_pages)
+        self.tables.fill_(-1)
+        self.pool.codes, self.pool.scales = self.codes.data_ptr(), self.scales.data_ptr()
+        self.pool.refs, self.pool.tables, self.pool.lengths = self.refs.data_ptr(), self.tables.data_ptr(), self.lengths.data_ptr()
+        self._scratch: Dict[tuple, torch.Tensor] = {}   # by device and stream
+
+    _workspace = FreezeCache._workspace
+
+    def reserve(self, add: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Room for add[row] more tokens of every row (None: one each), whose lengths grow; returns what each row was granted, [rows]."""
+        _here(add, holder=self)
+        granted = torch.empty(self.pool.rows, dtype=torch.int32, device=self.device)
+        freeze_pages_reserve(self.pool, add, granted, self._workspace(freeze_pages_workspace_bytes(self.pool)))
+        return granted
+
+    def fork(self, parents: torch.Tensor) -> None:
+        """Row r becomes what row parents[r] was, on the same pages (outside the rows: it stays)."""
+        _here(parents, holder=self)
+        freeze_pages_fork(self.pool, parents)
+
+    def truncate(self, keep: torch.Tensor) -> None:
+        """Row r keeps its first keep[r] tokens (below 0: all); 0 frees it."""
+        _here(keep, holder=self)
+        freeze_pages_truncate(self.pool, keep)
+
+    def compact(self) -> torch.Tensor:
+        """The pages in use move together at the front; returns how many they are, [1]."""
+        _here(holder=self)
+        used = torch.empty(1, dtype=torch.int32, device=self.device)
+        freeze_pages_compact(self.pool, used, self._workspace(freeze_pages_workspace_bytes(self.pool)))
+        return used
+
+    def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, most: int = 0,
+               granted: Optional[torch.Tensor] = None) -> None:
+        """The rows' newest tokens' keys and values [tokens, heads, head_dim] into a layer's pages: row r's are tokens starts[r] .. starts[r + 1] - 1
+        (None: one token a row).  granted: as reserve returned it, rows that got another number of tokens are not written."""
+        _here(k, v, starts, granted, holder=self)
+        freeze_pages_append(self.pool, layer, k, v, starts, most, granted)
+
+    def attend(self, layer: int, q: torch.Tensor, starts: Optional[torch.Tensor] = None, most: int = 0, scale: Optional[float] = None, window: int = 0,
+               out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of the rows' newest tokens, q [tokens, heads * group, head_dim], over a layer's pages; scale: head_dim ** -0.5 by default.  Outputs of
+        tokens of no row are left as they are (in a new tensor: whatever they were)."""
+        _here(q, starts, out, holder=self)
+        pool = self.pool
+        if out is None:
+            out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=self.device)
+        if q.dim() != 3 or q.shape[1] % pool.heads != 0 or q.shape[1] == 0:
+            raise _refused()
+        nbytes = lib().freeze_pages_attend_workspace_bytes(ctypes.addressof(pool), q.shape[1] // pool.heads, q.shape[0], most, int(starts is not None))
+        if nbytes == 0:
+            raise FreezeError(FREEZE_EINVAL, "freeze_pages_attend_workspace_bytes")
+        freeze_pages_attend(pool, layer, q, pool.head_dim ** -0.5 if scale is None else scale, out, self._workspace(nbytes), starts, most, window)
+        return out

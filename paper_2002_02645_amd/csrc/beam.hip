@@ -13,6 +13,7 @@
 // 121 MB (a tenth of the rows has ended) at 30.7 us are 3.9 TB/s: without the choice 24 us, of which the exponentials and the comparisons
 // are 17 us of issue; small calls (4 rows of 32,000 fp32: 5.7 us) are bound by the way through the code.
 #include "../../include/freeze.h"
+#include "extents.h"
 #include "freeze_internal.h"
 #include "select_common.h"
 
@@ -641,23 +642,6 @@ bool runs_apart(const freeze_state &t, int64_t rows)
         span += (count[i] - 1) * stride[i];
     }
     return true;
-}
-
-struct Extent {
-    uintptr_t begin, end;
-    bool dst;
-};
-// whether a dst shares a byte with another extent (sorts them)
-bool written_twice(Extent *e, int n)
-{
-    std::sort(e, e + n, [](const Extent &a, const Extent &b) { return a.begin < b.begin; });
-    uintptr_t any_end = 0, dst_end = 0;   // how far the extents so far reach
-    for (int i = 0; i < n; ++i) {
-        if (e[i].begin < (e[i].dst ? any_end : dst_end)) return true;
-        any_end = std::max(any_end, e[i].end);
-        if (e[i].dst) dst_end = std::max(dst_end, e[i].end);
-    }
-    return false;
 }
 
 }  // namespace

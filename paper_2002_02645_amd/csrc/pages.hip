@@ -1,0 +1,556 @@
+// Pages of keys and values (gfx950 / CDNA4): the bookkeeping of a pool whose pages several rows share, and the appending of new tokens.
+#include "pages.h"
+
+namespace fz {
+
+namespace {
+
+size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+
+constexpr int kBookThreads = 1024;
+
+// exclusive sum over a workgroup's threads in their order; *total: over all of them
+__device__ __forceinline__ int64_t exclusive_sum(int64_t v, int64_t *total)
+{
+    __shared__ int64_t wave_sum[kBookThreads / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t s = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(s, o);
+        if (lane >= o) s += u;
+    }
+    __syncthreads();   // (the last call's sums are read)
+    if (lane == 63) wave_sum[wave] = s;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) {
+        if (w < wave) before += wave_sum[w];
+        all += wave_sum[w];
+    }
+    *total = all;
+    return before + s - v;
+}
+
+struct PageCopy {
+    int32_t src, dst, row, blocks;   // blocks: the filled ones
+};
+
+struct ReserveArgs {
+    PageView v;
+    const int32_t *add;
+    int32_t *granted;
+    int32_t *need;       // [rows] scratch: pages wanted, the sign bit: one of them for a copy, kDenied: no place in the table
+    int32_t *free;       // [num_pages] scratch
+    PageCopy *copies;    // [rows] scratch
+    int32_t *num_copies; // scratch
+};
+constexpr int32_t kDenied = 0x7fffffff;
+
+// One workgroup: which pages a row gets follows from all rows before it.  A sum over the rows' wants, then the free pages in order until there are as many.
+// 32 rows, 330 pages: bound by the latency of its dozen dependent steps.
+__global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(ReserveArgs p)
+{
+    const PageView &v = p.v;
+    const int per = (v.rows + kBookThreads - 1) / kBookThreads;
+    const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
+    const int64_t page_mask = ((int64_t)1 << v.page_log2) - 1;
+    int64_t mine = 0;
+    for (int r = r0; r < r1; ++r) {
+        const int64_t n = v.length_of(r), a = p.add ? max(p.add[r], 0) : 1;
+        const int64_t had = (n + page_mask) >> v.page_log2, has = (n + a + page_mask) >> v.page_log2;
+        int32_t need = kDenied;
+        if (has <= v.max_pages) {
+            need = (int32_t)(has - had);
+            if (a > 0 && (n & page_mask) != 0) {
+                const int last = v.tables[(int64_t)r * v.max_pages + had - 1];
+                if (last >= 0 && last < v.num_pages && v.refs[last] > 1) need = (need + 1) | (int32_t)0x80000000;
+            }
+            mine += need & 0x7fffffff;
+        }
+        p.need[r] = need;
+    }
+    int64_t wanted;
+    int64_t at = exclusive_sum(mine, &wanted);
+    // the first `wanted` free pages
+    __shared__ int copies;
+    if (threadIdx.x == 0) copies = 0;
+    constexpr int kEach = 16;
+    int64_t found = 0;
+    for (int64_t base = 0; base < v.num_pages && found < wanted; base += kBookThreads * kEach) {
+        const int64_t first = base + (int64_t)threadIdx.x * kEach;
+        uint32_t is_free = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+            if (first + e < v.num_pages && v.refs[first + e] == 0) is_free |= 1u << e;
+        int64_t here;
+        int64_t to = found + exclusive_sum(__popc(is_free), &here);
+        for (; is_free != 0 && to < wanted; is_free &= is_free - 1) p.free[to++] = (int32_t)(first + __builtin_ctz(is_free));
+        found += here;
+    }
+    __syncthreads();   // the list is written (by this workgroup), every count is read
+    for (int r = r0; r < r1; ++r) {
+        const int32_t want = p.need[r];
+        const int need = want & 0x7fffffff;
+        const bool denied = want == kDenied;
+        const bool ok = !denied && (need == 0 || at + need <= found);
+        const int a = ok ? (p.add ? max(p.add[r], 0) : 1) : 0;
+        p.granted[r] = a;
+        if (ok && a > 0) {
+            const int64_t n = v.length_of(r);
+            int64_t j = (n + page_mask) >> v.page_log2, from = at;
+            int32_t *table = v.tables + (int64_t)r * v.max_pages;
+            int left = need;
+            if (want < 0) {
+                const int src = table[j - 1], dst = p.free[from++];
+                --left;
+                table[j - 1] = dst;
+                atomicSub(&v.refs[src], 1);
+                v.refs[dst] = 1;
+                p.copies[atomicAdd(&copies, 1)] = PageCopy{src, dst, r, (int)(((n & page_mask) + kPageBlock - 1) / kPageBlock)};
+            }
+            for (; left > 0; --left) {
+                const int dst = p.free[from++];
+                table[j++] = dst;
+                v.refs[dst] = 1;
+            }
+            v.lengths[r] = (int)(n + a);
+        }
+        if (!denied) at += need;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) *p.num_copies = copies;
+}
+
+// bytes (a multiple of 16) from src to dst by a workgroup
+__device__ __forceinline__ void copy_run(uint8_t *dst, const uint8_t *src, int64_t bytes)
+{
+    const u32x4 *s = reinterpret_cast<const u32x4 *>(src);
+    u32x4 *d = reinterpret_cast<u32x4 *>(dst);
+    const int64_t n = bytes / 16;
+    int64_t i = threadIdx.x;
+    for (; i + 3 * 256 < n; i += 4 * 256) {
+        u32x4 x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = __builtin_nontemporal_load(s + i + e * 256);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) __builtin_nontemporal_store(x[e], d + i + e * 256);
+    }
+    for (; i < n; i += 256) d[i] = s[i];
+}
+
+// The filled blocks of the copied pages: a workgroup copies those of a head in a layer (one run of memory) at a time.
+__global__ __launch_bounds__(256) void pages_copy_kernel(PageView v, int layers, const PageCopy *copies, const int32_t *num_copies, int64_t code_layer, int64_t scale_layer)
+{
+    const int per = layers * v.heads;
+    const int64_t units = (int64_t)*num_copies * per;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const PageCopy c = copies[u / per];
+        const int rest = (int)(u % per), layer = rest / v.heads, head = rest % v.heads;
+        uint8_t *codes = v.codes + layer * code_layer;
+        copy_run(codes + v.block_at(c.dst, head, 0), codes + v.block_at(c.src, head, 0), c.blocks * (64 * (int64_t)v.width));
+        uint16_t *scales = reinterpret_cast<uint16_t *>(v.scales + layer * scale_layer);
+        if ((int)threadIdx.x < c.blocks) scales[v.scale_at(c.dst, head, threadIdx.x) / 2] = scales[v.scale_at(c.src, head, threadIdx.x) / 2];
+    }
+}
+
+// Tables in place: a workgroup takes some columns of all rows, so that every entry is read before one is written.
+__global__ __launch_bounds__(256) void pages_fork_kernel(PageView v, const int32_t *parents, int cols)
+{
+    extern __shared__ int32_t was[];   // [rows, cols]
+    const int64_t c0 = (int64_t)blockIdx.x * cols;
+    const int n = v.rows * cols;
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const int64_t c = c0 + i % cols;
+        was[i] = c < v.max_pages ? v.tables[i / cols * v.max_pages + c] : -1;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += 256) {
+        const int64_t c = c0 + i % cols;
+        const int parent = parents[i / cols];
+        if (c >= v.max_pages || parent < 0 || parent >= v.rows) continue;
+        const int old = was[i], now = was[parent * cols + i % cols];
+        if (old == now) continue;
+        v.tables[i / cols * v.max_pages + c] = now;
+        if (old >= 0 && old < v.num_pages) atomicSub(&v.refs[old], 1);
+        if (now >= 0 && now < v.num_pages) atomicAdd(&v.refs[now], 1);
+    }
+    if (blockIdx.x != 0) return;
+    __syncthreads();
+    for (int r = threadIdx.x; r < v.rows; r += 256) was[r] = v.lengths[r];
+    __syncthreads();
+    for (int r = threadIdx.x; r < v.rows; r += 256) {
+        const int parent = parents[r];
+        if (parent >= 0 && parent < v.rows && parent != r) v.lengths[r] = was[parent];
+    }
+}
+
+__global__ __launch_bounds__(256) void pages_truncate_kernel(PageView v, const int32_t *keep)
+{
+    const int r = blockIdx.x, n = v.length_of(r), k = keep[r];
+    if (k < 0 || k >= n) return;
+    __syncthreads();   // the length is read
+    const int64_t first = ((int64_t)k + (1 << v.page_log2) - 1) >> v.page_log2, last = ((int64_t)n + (1 << v.page_log2) - 1) >> v.page_log2;
+    int32_t *table = v.tables + r * v.max_pages;
+    for (int64_t j = first + threadIdx.x; j < last; j += 256) {
+        const int page = table[j];
+        if (page >= 0 && page < v.num_pages) atomicSub(&v.refs[page], 1);
+        table[j] = -1;
+    }
+    if (threadIdx.x == 0) v.lengths[r] = k;
+}
+
+struct CompactArgs {
+    PageView v;
+    int32_t *to;         // [num_pages] scratch: a page's number from now on
+    int32_t *src, *dst;  // [num_pages] scratch: the moves
+    int32_t *moves;      // scratch: how many
+    int32_t *used;
+};
+
+// One workgroup: how many pages are in use, then the used ones behind as many numbers and the free ones before, each in order.
+__global__ __launch_bounds__(kBookThreads) void pages_compact_kernel(CompactArgs p)
+{
+    const PageView &v = p.v;
+    const int per = (v.num_pages + kBookThreads - 1) / kBookThreads;
+    const int p0 = min(v.num_pages, (int)threadIdx.x * per), p1 = min(v.num_pages, p0 + per);
+    int64_t mine = 0, used, moves, free;
+    for (int i = p0; i < p1; ++i) mine += v.refs[i] > 0 ? 1 : 0;
+    exclusive_sum(mine, &used);
+    int64_t behind = 0, before = 0;
+    for (int i = p0; i < p1; ++i) {
+        const bool in_use = v.refs[i] > 0;
+        behind += in_use && i >= used ? 1 : 0;
+        before += !in_use && i < used ? 1 : 0;
+    }
+    behind = exclusive_sum(behind, &moves);
+    before = exclusive_sum(before, &free);
+    for (int i = p0; i < p1; ++i) {
+        const bool in_use = v.refs[i] > 0;
+        if (in_use && i >= used) p.src[behind++] = i;
+        else p.to[i] = i;
+        if (!in_use && i < used) p.dst[before++] = i;
+    }
+    __syncthreads();
+    for (int64_t m = threadIdx.x; m < moves; m += kBookThreads) {   // (as many free numbers as pages to move)
+        const int src = p.src[m], dst = p.dst[m];
+        p.to[src] = dst;
+        v.refs[dst] = v.refs[src];
+        v.refs[src] = 0;
+    }
+    if (threadIdx.x == 0) {
+        *p.moves = (int32_t)moves;
+        *p.used = (int32_t)used;
+    }
+}
+
+constexpr int64_t kMovePiece = 16 << 10;
+__global__ __launch_bounds__(256) void pages_move_kernel(CompactArgs p, int layers, int64_t code_layer, int64_t scale_layer)
+{
+    const PageView &v = p.v;
+    const int64_t entries = v.rows * v.max_pages;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < entries; i += (int64_t)gridDim.x * 256) {
+        const int page = v.tables[i];
+        if (page >= 0 && page < v.num_pages) {
+            const int to = p.to[page];
+            if (to != page) v.tables[i] = to;
+        }
+    }
+    const int64_t bytes = v.block_at(1, 0, 0), pieces = (bytes + kMovePiece - 1) / kMovePiece;
+    const int64_t per = layers * pieces, units = *p.moves * per;
+    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+        const int64_t m = u / per, rest = u - m * per, layer = rest / pieces, at = (rest - layer * pieces) * kMovePiece;
+        const int src = p.src[m], dst = p.dst[m];
+        uint8_t *codes = v.codes + layer * code_layer;
+        copy_run(codes + v.block_at(dst, 0, 0) + at, codes + v.block_at(src, 0, 0) + at, min(kMovePiece, bytes - at));
+        if (at == 0) {
+            uint16_t *scales = reinterpret_cast<uint16_t *>(v.scales + layer * scale_layer);
+            for (int b = threadIdx.x; b < v.heads * v.per_page; b += 256) scales[v.scale_at(dst, 0, 0) / 2 + b] = scales[v.scale_at(src, 0, 0) / 2 + b];
+        }
+    }
+}
+
+// ---- appending ----------------------------------------------------------------------------------------
+
+struct AppendArgs {
+    PageView v;
+    const void *x[2];              // keys, values
+    int64_t token_stride[2], head_stride[2];
+    int64_t tokens, most;
+    const int32_t *starts, *granted;
+    int blocks;                    // that a row's new tokens can lie in
+};
+
+__device__ __forceinline__ float value_at(const float *p) { return *p; }
+__device__ __forceinline__ float value_at(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
+
+// The code of a finite value within the block's range; what is not finite: no number.
+__device__ __forceinline__ float code_of(float x, float inv)
+{
+    return (__float_as_uint(x) & 0x7fffffffu) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : x * inv;
+}
+__device__ __forceinline__ float old_value(uint32_t word, int byte)   // byte: constant after unrolling
+{
+    return byte == 0 ? __builtin_amdgcn_cvt_f32_fp8(word, 0) : byte == 1 ? __builtin_amdgcn_cvt_f32_fp8(word, 1) : byte == 2 ? __builtin_amdgcn_cvt_f32_fp8(word, 2) : __builtin_amdgcn_cvt_f32_fp8(word, 3);
+}
+
+// A wave quantises the new tokens of one block of a head's keys or values: every lane holds the values of its own 16 bytes of each chunk of 32
+// elements, so that the block's largest magnitude is one reduction over the wave and a chunk leaves as one store of 1 KB.
+// DC: chunks.
+template <typename T, int DC>
+__global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
+{
+    const PageView &v = p.v;
+    const int lane = threadIdx.x & 63, g = lane >> 4, t = lane & 15;
+    const int64_t units = (int64_t)v.rows * p.blocks * v.heads * 2;
+    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
+        const int kv = (int)(u & 1);
+        const int64_t rest = u >> 1, unit = rest / v.heads;
+        const int head = (int)(rest - unit * v.heads), row = (int)(unit / p.blocks), j = (int)(unit - (int64_t)row * p.blocks);
+        const NewTokens n = new_tokens(p.starts, row, p.tokens, p.most);
+        const int len = v.length_of(row), first = len - n.count;
+        if (n.count == 0 || first < 0 || (p.granted && p.granted[row] != n.count)) continue;
+        const int block = first / kPageBlock + j, start = block * kPageBlock;
+        if (start >= len) continue;
+        const int page = v.tables[row * v.max_pages + (start >> v.page_log2)];
+        if (page < 0 || page >= v.num_pages || v.refs[page] > 1) continue;
+        const int in_page = block & (v.per_page - 1);
+        uint8_t *to = v.codes + v.block_at(page, head, in_page) + kv * (32 * v.width);
+        uint8_t *scale = v.scales + v.scale_at(page, head, in_page) + kv;
+        // token of the block, element of the head of this lane's byte e of chunk c
+        auto token_of = [&](int e) { return kv ? (e & 3) + 4 * g + (e >> 2 & 1) * 16 : t + (e >> 3) * 16; };
+        auto dim_of = [&](int c, int e) { return 32 * c + (kv ? t + (e >> 3) * 16 : 8 * g + (e & 7)); };
+        const T *x = static_cast<const T *>(p.x[kv]) + head * p.head_stride[kv];
+        const int kept = first - start;   // tokens that are there already (below 1: none)
+        float w[DC][16];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int token = token_of(e), dim = dim_of(c, e);
+                w[c][e] = 0.f;
+                if (token >= kept && start + token < len && dim < v.head_dim)
+                    w[c][e] = value_at(x + (n.first + token - kept) * p.token_stride[kv] + dim);
+                const uint32_t bits = __float_as_uint(w[c][e]) & 0x7fffffffu;
+                if (bits < 0x7f800000u && bits > amax) amax = bits;
+            }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o));
+        int ex = (int)(amax >> 23) - 135 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+        ex = ex < -126 ? -126 : ex;
+        const int old = kept > 0 ? (int)*scale - 127 : -126;
+        const bool grows = ex > old;
+        if (!grows) ex = old;
+        const float inv = __uint_as_float((uint32_t)(127 - ex) << 23);
+        const float down = old - ex < -126 ? 0.f : __uint_as_float((uint32_t)(127 + old - ex) << 23);   // (of a code: at least 2^-9, so nothing is left of it anyway)
+#pragma unroll
+        for (int c = 0; c < DC; ++c) {
+            u32x4 codes;
+            u32x4 was{0, 0, 0, 0};
+            u32x4 *at = reinterpret_cast<u32x4 *>(to + c * 1024 + lane * 16);
+            if (kept > 0) was = *at;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                float f[4];
+                uint32_t keep = 0;   // bytes that stay as they are
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int token = token_of(4 * q + e);
+                    f[e] = code_of(w[c][4 * q + e], inv);
+                    if (token < kept) {
+                        if (grows) f[e] = old_value(was[q], e) * down;
+                        else keep |= 0xffu << (8 * e);
+                    }
+                }
+                int b = 0;
+                b = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], b, false);
+                b = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], b, true);
+                codes[q] = ((uint32_t)b & ~keep) | (was[q] & keep);
+            }
+            *at = codes;
+        }
+        if (lane == 0) *scale = (uint8_t)(ex + 127);
+    }
+}
+
+template <typename T>
+hipError_t launch_append(const AppendArgs &a, dim3 grid, hipStream_t s)
+{
+    switch (a.v.width / 32) {
+        case 1: hipLaunchKernelGGL((pages_append_kernel<T, 1>), grid, dim3(256), 0, s, a); break;
+        case 2: hipLaunchKernelGGL((pages_append_kernel<T, 2>), grid, dim3(256), 0, s, a); break;
+        case 3: hipLaunchKernelGGL((pages_append_kernel<T, 3>), grid, dim3(256), 0, s, a); break;
+        case 4: hipLaunchKernelGGL((pages_append_kernel<T, 4>), grid, dim3(256), 0, s, a); break;
+        case 5: hipLaunchKernelGGL((pages_append_kernel<T, 5>), grid, dim3(256), 0, s, a); break;
+        case 6: hipLaunchKernelGGL((pages_append_kernel<T, 6>), grid, dim3(256), 0, s, a); break;
+        case 7: hipLaunchKernelGGL((pages_append_kernel<T, 7>), grid, dim3(256), 0, s, a); break;
+        default: hipLaunchKernelGGL((pages_append_kernel<T, 8>), grid, dim3(256), 0, s, a); break;
+    }
+    return hipGetLastError();
+}
+
+int64_t layer_bytes(size_t all, const freeze_pages *p) { return (int64_t)(all / p->layers); }
+
+}  // namespace
+}  // namespace fz
+
+using namespace fz;
+
+extern "C" {
+
+size_t freeze_pages_bytes(const freeze_pages *pages) { return page_sizes(pages) ? page_code_bytes(pages) : 0; }
+
+size_t freeze_pages_workspace_bytes(const freeze_pages *pages)
+{
+    if (!page_sizes(pages)) return 0;
+    return 3 * up256((size_t)pages->num_pages * 4) + up256((size_t)pages->rows * 4) + up256((size_t)pages->rows * sizeof(PageCopy)) + 256;
+}
+
+int freeze_pages_reserve(const freeze_pages *pages, const int32_t *add, int32_t *out_granted, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!page_sizes(pages) || !out_granted || !workspace || reinterpret_cast<uintptr_t>(add) % 4 != 0 || reinterpret_cast<uintptr_t>(out_granted) % 4 != 0)
+        return FREEZE_EINVAL;
+    const size_t bytes = freeze_pages_workspace_bytes(pages);
+    if (workspace_bytes < bytes || reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return FREEZE_EWORKSPACE;
+    const size_t rows = (size_t)pages->rows;
+    Extent e[8];
+    int n = 0;
+    if (!page_extents(pages, 3, e, &n)) return FREEZE_EINVAL;
+    auto add_extent = [&](const void *q, size_t size, bool dst) {
+        const uintptr_t b = reinterpret_cast<uintptr_t>(q);
+        if (q) e[n++] = Extent{b, b + size, dst};
+    };
+    add_extent(add, rows * 4, false);
+    add_extent(out_granted, rows * 4, true);
+    add_extent(workspace, bytes, true);
+    if (written_twice(e, n)) return FREEZE_EINVAL;
+    ReserveArgs a{};
+    a.v = page_view(pages, 0);
+    a.add = add;
+    a.granted = out_granted;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    a.num_copies = reinterpret_cast<int32_t *>(ws);
+    ws += 256;
+    a.need = reinterpret_cast<int32_t *>(ws);
+    ws += up256(rows * 4);
+    a.copies = reinterpret_cast<PageCopy *>(ws);
+    ws += up256(rows * sizeof(PageCopy));
+    a.free = reinterpret_cast<int32_t *>(ws);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kBookThreads), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return FREEZE_EHIP;
+    const int64_t units = pages->rows * pages->layers * pages->heads;
+    hipLaunchKernelGGL(pages_copy_kernel, dim3((unsigned)std::min<int64_t>(units, 2048)), dim3(256), 0, s, a.v, pages->layers, a.copies, a.num_copies,
+                       layer_bytes(page_code_bytes(pages), pages), layer_bytes(page_scale_bytes(pages), pages));
+    return hipGetLastError() == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
+}
+
+int freeze_pages_fork(const freeze_pages *pages, const int32_t *parents, void *stream)
+{
+    if (!page_sizes(pages) || !parents || reinterpret_cast<uintptr_t>(parents) % 4 != 0) return FREEZE_EINVAL;
+    Extent e[8];
+    int n = 0;
+    if (!page_extents(pages, 1, e, &n)) return FREEZE_EINVAL;
+    const uintptr_t b = reinterpret_cast<uintptr_t>(parents);
+    e[n++] = Extent{b, b + (size_t)pages->rows * 4, false};
+    if (written_twice(e, n)) return FREEZE_EINVAL;
+    int cols = 64;   // of a workgroup: 64 KB of entries
+    while (cols > 1 && cols * pages->rows > 16384) cols /= 2;
+    const int64_t groups = (pages->max_pages + cols - 1) / cols;
+    const size_t lds = (size_t)pages->rows * cols * 4;
+    hipLaunchKernelGGL(pages_fork_kernel, dim3((unsigned)groups), dim3(256), lds, static_cast<hipStream_t>(stream), page_view(pages, 0), parents, cols);
+    return hipGetLastError() == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
+}
+
+int freeze_pages_truncate(const freeze_pages *pages, const int32_t *keep, void *stream)
+{
+    if (!page_sizes(pages) || !keep || reinterpret_cast<uintptr_t>(keep) % 4 != 0) return FREEZE_EINVAL;
+    Extent e[8];
+    int n = 0;
+    if (!page_extents(pages, 1, e, &n)) return FREEZE_EINVAL;
+    const uintptr_t b = reinterpret_cast<uintptr_t>(keep);
+    e[n++] = Extent{b, b + (size_t)pages->rows * 4, false};
+    if (written_twice(e, n)) return FREEZE_EINVAL;
+    hipLaunchKernelGGL(pages_truncate_kernel, dim3((unsigned)pages->rows), dim3(256), 0, static_cast<hipStream_t>(stream), page_view(pages, 0), keep);
+    return hipGetLastError() == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
+}
+
+int freeze_pages_compact(const freeze_pages *pages, int32_t *out_used, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!page_sizes(pages) || !out_used || !workspace || reinterpret_cast<uintptr_t>(out_used) % 4 != 0) return FREEZE_EINVAL;
+    const size_t bytes = freeze_pages_workspace_bytes(pages);
+    if (workspace_bytes < bytes || reinterpret_cast<uintptr_t>(workspace) % 256 != 0) return FREEZE_EWORKSPACE;
+    Extent e[8];
+    int n = 0;
+    if (!page_extents(pages, 3, e, &n)) return FREEZE_EINVAL;
+    const uintptr_t u = reinterpret_cast<uintptr_t>(out_used), w = reinterpret_cast<uintptr_t>(workspace);
+    e[n++] = Extent{u, u + 4, true};
+    e[n++] = Extent{w, w + bytes, true};
+    if (written_twice(e, n)) return FREEZE_EINVAL;
+    CompactArgs a{};
+    a.v = page_view(pages, 0);
+    a.used = out_used;
+    uint8_t *ws = static_cast<uint8_t *>(workspace);
+    a.moves = reinterpret_cast<int32_t *>(ws);
+    ws += 256;
+    int32_t **lists[3] = {&a.to, &a.src, &a.dst};
+    for (int32_t **list : lists) {
+        *list = reinterpret_cast<int32_t *>(ws);
+        ws += up256((size_t)pages->num_pages * 4);
+    }
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(kBookThreads), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return FREEZE_EHIP;
+    hipLaunchKernelGGL(pages_move_kernel, dim3(2048), dim3(256), 0, s, a, pages->layers, layer_bytes(page_code_bytes(pages), pages),
+                       layer_bytes(page_scale_bytes(pages), pages));
+    return hipGetLastError() == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
+}
+
+int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v,
+                        int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t tokens, const int32_t *starts, int64_t most,
+                        const int32_t *granted, void *stream)
+{
+    if (!page_sizes(pages) || layer < 0 || layer >= pages->layers || (dtype != FREEZE_F32 && dtype != FREEZE_BF16) || tokens < 0 || tokens >= (int64_t)1 << 31 ||
+        most < 0 || (!starts && tokens != 0 && tokens != pages->rows))
+        return FREEZE_EINVAL;
+    if (tokens == 0) return FREEZE_OK;
+    const uintptr_t size = dtype == FREEZE_F32 ? 4 : 2;
+    int64_t ks, vs;
+    if (!k || !v || reinterpret_cast<uintptr_t>(k) % size != 0 || reinterpret_cast<uintptr_t>(v) % size != 0 || reinterpret_cast<uintptr_t>(starts) % 4 != 0 ||
+        reinterpret_cast<uintptr_t>(granted) % 4 != 0 || !heads_span(tokens, pages->heads, pages->head_dim, k_token_stride, k_head_stride, false, &ks) ||
+        !heads_span(tokens, pages->heads, pages->head_dim, v_token_stride, v_head_stride, false, &vs))
+        return FREEZE_EINVAL;
+    Extent e[9];
+    int n = 0;
+    if (!page_extents(pages, 2, e, &n)) return FREEZE_EINVAL;
+    auto add_extent = [&](const void *q, size_t bytes) {
+        const uintptr_t b = reinterpret_cast<uintptr_t>(q);
+        if (q) e[n++] = Extent{b, b + bytes, false};
+    };
+    add_extent(k, (size_t)ks * size);
+    add_extent(v, (size_t)vs * size);
+    add_extent(starts, ((size_t)pages->rows + 1) * 4);
+    add_extent(granted, (size_t)pages->rows * 4);
+    if (written_twice(e, n)) return FREEZE_EINVAL;
+    AppendArgs a{};
+    a.v = page_view(pages, layer);
+    a.x[0] = k;
+    a.x[1] = v;
+    a.token_stride[0] = k_token_stride;
+    a.token_stride[1] = v_token_stride;
+    a.head_stride[0] = k_head_stride;
+    a.head_stride[1] = v_head_stride;
+    a.tokens = tokens;
+    a.most = starts ? (most > 0 && most < tokens ? most : tokens) : 1;
+    a.starts = starts;
+    a.granted = granted;
+    a.blocks = (int)((a.most + 2 * kPageBlock - 2) / kPageBlock);
+    const int64_t units = pages->rows * a.blocks * pages->heads * 2;
+    const dim3 grid((unsigned)std::min<int64_t>((units + 3) / 4, 1 << 20));
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t err = dtype == FREEZE_F32 ? launch_append<float>(a, grid, s) : launch_append<uint16_t>(a, grid, s);
+    return err == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,305 @@
+// Attention over pages of 8 bits: one block of tokens against the columns of a wave, in registers.  Not part of the C ABI.
+#pragma once
+#include "pages.h"
+
+namespace fz {
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+struct AttendArgs {
+    PageView v;
+    const void *q;
+    void *out;
+    int64_t q_token, q_head, out_token, out_head;   // strides
+    int64_t tokens, most, window;
+    const int32_t *starts;
+    int group, q_vec, out_bf16, out_vec;            // *_vec: 16-byte loads of q, 8-byte (bf16) or 16-byte stores of out
+    float scale_log2;                               // the scale times log2(e): weights are powers of two
+    // work split over the tokens
+    int workers;
+    int64_t *blocks_before;                         // [rows + 1] of a head, over its tiles
+    int32_t *tiles_before;                          // [rows + 1]
+    float *part_o, *part_ml;                        // [workers][2] pieces of tiles
+};
+
+// What a row asks for: its new tokens, its length, the blocks that the first to the last of them see.
+struct RowWork {
+    NewTokens n;
+    int len, lo, blocks, tiles;
+};
+__device__ __forceinline__ RowWork row_work(const AttendArgs &p, int row, int cols)
+{
+    RowWork w;
+    w.n = new_tokens(p.starts, row, p.tokens, p.most);
+    w.len = p.v.length_of(row);
+    const int64_t seen = p.window > 0 ? (int64_t)w.len - w.n.count - p.window + 1 : 0;   // first place of the first token
+    w.lo = seen > 0 ? (int)(seen / kPageBlock) : 0;
+    w.blocks = w.n.count > 0 ? (w.len + kPageBlock - 1) / kPageBlock - w.lo : 0;
+    w.blocks = w.blocks < 0 ? 0 : w.blocks;
+    w.tiles = (int)(((int64_t)w.n.count * p.group + cols - 1) / cols);
+    return w;
+}
+
+__device__ __forceinline__ bf16x8 values_of(uint32_t a, uint32_t b, float scale)
+{
+    union {
+        bf16x2 h[4];
+        bf16x8 v;
+    } u;
+    u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, false);
+    u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, scale, true);
+    u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, false);
+    u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, scale, true);
+    return u.v;
+}
+
+// bytes 0x7f where a code is no number, 0 elsewhere (bit 7 alone)
+__device__ __forceinline__ uint32_t no_numbers(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ bf16x8 ones_where(uint32_t a, uint32_t b)
+{
+    bf16x8 f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = ((e < 4 ? a : b) >> (8 * (e & 3) + 7) & 1) ? (__bf16)1.f : (__bf16)0.f;
+    return f;
+}
+
+// x as NS numbers of 8 bits each
+template <int NS>
+__device__ __forceinline__ void parts_of(const float (&x)[8], bf16x8 (&out)[NS])
+{
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = x[e];
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            out[n][e] = (__bf16)r[e];
+            if (n + 1 < NS) r[e] -= (float)out[n][e];
+        }
+}
+
+// The running softmax of 16 * CT columns (a column: one head of one new token) in a wave.  A lane has column lane & 15 of each 16; weights and sums
+// belong to the lane's own tokens, outputs are elements 32 c + 16 u + 4 (lane >> 4) + i of o[.][2 c + u].
+template <int DC, int CT>
+struct Running {
+    f32x4 o[CT][2 * DC];
+    float m[CT], l[CT];   // m: the column's reference (no smaller than its largest score less kSlack), the same in its four lanes; l: the lane's own sum
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            m[t] = -INFINITY;
+            l[t] = 0.f;
+#pragma unroll
+            for (int f = 0; f < 2 * DC; ++f) o[t][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+};
+// Scores may pass the reference by this many powers of two before it follows: weights up to 2^8 cost no digit, and the reference
+// (a reduction over four lanes, all outputs scaled) seldom moves.
+constexpr float kSlack = 8.f;
+
+template <int DC, int NS>
+__device__ __forceinline__ void load_queries(const AttendArgs &p, const RowWork &w, int head, int64_t col, bf16x8 (&q)[NS][DC])
+{
+    const int g = (threadIdx.x & 63) >> 4;
+    const bool there = col < (int64_t)w.n.count * p.group;
+    const int64_t token = w.n.first + (there ? col / p.group : 0);
+    const int64_t at = token * p.q_token + (head * (int64_t)p.group + (there ? col % p.group : 0)) * p.q_head;
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
+        const int d = 32 * c + 8 * g;
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        if constexpr (NS == 1) {
+            const uint16_t *src = static_cast<const uint16_t *>(p.q) + at + d;
+            if (there && p.q_vec) {
+                if (d < p.v.head_dim) {
+                    q[0][c] = *reinterpret_cast<const bf16x8 *>(src);
+                    continue;
+                }
+            } else if (there) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (d + e < p.v.head_dim) x[e] = __uint_as_float((uint32_t)src[e] << 16);
+            }
+        } else {
+            const float *src = static_cast<const float *>(p.q) + at + d;
+            if (there) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (d + e < p.v.head_dim) x[e] = src[e];
+            }
+        }
+        bf16x8 parts[NS];
+        parts_of<NS>(x, parts);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) q[n][c] = parts[n];
+    }
+}
+
+// Scores of the block's 32 tokens: token 16 t + 4 (lane >> 4) + i against the lane's column.
+template <int DC, int CT, int NS>
+__device__ __forceinline__ void scores_of(const u32x4 (&k)[DC], const bf16x8 (&q)[CT][NS][DC], f32x4 (&s)[CT][2])
+{
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) s[ct][0] = s[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            const bf16x8 f = values_of(k[c][2 * t], k[c][2 * t + 1], 1.f);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int n = 0; n < NS; ++n) s[ct][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f, q[ct][n][c], s[ct][t], 0, 0, 0);
+        }
+}
+
+// Scores to weights.  first: the block's first token, place: of the lane's columns' tokens (below 0: a column of nobody), edge: some column
+// does not see all of the block.
+template <int DC, int CT>
+__device__ __forceinline__ void weigh(Running<DC, CT> &r, f32x4 (&s)[CT][2], float scale, bool edge, int first, const int (&place)[CT], int64_t window)
+{
+    const int g = (threadIdx.x & 63) >> 4;
+    float top[CT];
+    bool follow = false;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        top[ct] = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[ct][t][i] *= scale;
+                if (edge) {
+                    const int token = first + 16 * t + 4 * g + i;
+                    if (token > place[ct] || (window > 0 && (int64_t)token <= place[ct] - window)) s[ct][t][i] = -INFINITY;
+                }
+                top[ct] = fmaxf(top[ct], s[ct][t][i]);
+            }
+        follow |= top[ct] > r.m[ct] + kSlack;
+    }
+    if (__any(follow)) {
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            float m = fmaxf(top[ct], __shfl_xor(top[ct], 16));
+            m = fmaxf(r.m[ct], fmaxf(m, __shfl_xor(m, 32)));
+            const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(r.m[ct] - m);
+            r.m[ct] = m;
+            r.l[ct] *= a;
+#pragma unroll
+            for (int f = 0; f < 2 * DC; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r.o[ct][f][i] *= a;
+        }
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const float m = r.m[ct] == -INFINITY ? 0.f : r.m[ct];
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[ct][t][i] = __builtin_amdgcn_exp2f(s[ct][t][i] - m);
+                r.l[ct] += s[ct][t][i];
+            }
+    }
+}
+
+// Weights times values.  In an edge block, codes that are no number (of tokens that some columns do not see, or that nobody wrote) are
+// taken out of the product and put into the outputs of the columns that see them.
+template <int DC, int CT, int NS>
+__device__ __forceinline__ void add_values(Running<DC, CT> &r, const u32x4 (&v)[DC], float scale, const f32x4 (&w)[CT][2], bool edge, int first,
+                                           const int (&place)[CT], int64_t window)
+{
+    bf16x8 f[CT][NS];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const float x[8] = {w[ct][0][0], w[ct][0][1], w[ct][0][2], w[ct][0][3], w[ct][1][0], w[ct][1][1], w[ct][1][2], w[ct][1][3]};
+        parts_of<NS>(x, f[ct]);
+    }
+    bool strange = false;
+    if (edge) {
+        uint32_t any = 0;
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) any |= no_numbers(v[c][e]);
+        strange = __any(any != 0);
+    }
+    if (!strange) {
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const bf16x8 x = values_of(v[c][2 * u], v[c][2 * u + 1], scale);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int n = 0; n < NS; ++n) r.o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[ct][n], r.o[ct][2 * c + u], 0, 0, 0);
+            }
+        return;
+    }
+    const int g = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t a = v[c][2 * u], b = v[c][2 * u + 1], na = no_numbers(a), nb = no_numbers(b);
+            const bf16x8 x = values_of(a & ~((na >> 7) * 0xffu), b & ~((nb >> 7) * 0xffu), scale), bad = ones_where(na, nb);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                bf16x8 seen;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int token = first + 16 * (e >> 2) + 4 * g + (e & 3);
+                    seen[e] = token <= place[ct] && (window <= 0 || (int64_t)token > place[ct] - window) ? (__bf16)1.f : (__bf16)0.f;
+                }
+                const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int n = 0; n < NS; ++n) r.o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[ct][n], r.o[ct][2 * c + u], 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (count[i] > 0.f) r.o[ct][2 * c + u][i] = __uint_as_float(0x7fc00000u);
+            }
+        }
+}
+
+// Four elements of a column's output, from element d on.
+__device__ __forceinline__ void store_out(const AttendArgs &p, int64_t first, int head, int64_t col, int d, f32x4 x)
+{
+    const int64_t at = (first + col / p.group) * p.out_token + (head * (int64_t)p.group + col % p.group) * p.out_head + d;
+    if (d >= p.v.head_dim) return;
+    if (p.out_bf16) {
+        uint16_t *to = static_cast<uint16_t *>(p.out) + at;
+        if (p.out_vec) {
+            union {
+                bf16x2 h[2];
+                u32x2 w;
+            } u;
+            u.h[0] = bf16x2{(__bf16)x[0], (__bf16)x[1]};
+            u.h[1] = bf16x2{(__bf16)x[2], (__bf16)x[3]};
+            *reinterpret_cast<u32x2 *>(to) = u.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (d + i < p.v.head_dim) to[i] = bf16_rne(x[i]);
+        }
+    } else {
+        float *to = static_cast<float *>(p.out) + at;
+        if (p.out_vec) *reinterpret_cast<f32x4 *>(to) = x;
+        else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (d + i < p.v.head_dim) to[i] = x[i];
+        }
+    }
+}
+
+}  // namespace fz
