@@ -103,44 +103,93 @@ struct Running {
 // (a reduction over four lanes, all outputs scaled) seldom moves.
 constexpr float kSlack = 8.f;
 
+// The queries of kCols columns from col0 on into LDS, [NS][kCols] rows of 32 DC + 8 bf16 (the 16 bytes more keep a wave's reads off each other's banks), zeros behind
+// the last column and element.
+template <int DC>
+constexpr int kQueryRow = 32 * DC + 8;
 template <int DC, int NS>
-__device__ __forceinline__ void load_queries(const AttendArgs &p, const RowWork &w, int head, int64_t col, bf16x8 (&q)[NS][DC])
+__device__ __forceinline__ void stage_queries(const AttendArgs &p, const RowWork &w, int head, int col0, int cols, uint16_t *to)
 {
-    const int g = (threadIdx.x & 63) >> 4;
-    const bool there = col < (int64_t)w.n.count * p.group;
-    const int64_t token = w.n.first + (there ? col / p.group : 0);
-    const int64_t at = token * p.q_token + (head * (int64_t)p.group + (there ? col % p.group : 0)) * p.q_head;
-#pragma unroll
-    for (int c = 0; c < DC; ++c) {
-        const int d = 32 * c + 8 * g;
+    const int there = w.n.count * p.group;
+    for (int i = threadIdx.x; i < cols * (4 * DC); i += 256) {
+        const int c = i / (4 * DC), d = i % (4 * DC) * 8, col = col0 + c;
+        bf16x8 parts[NS];
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.f;
-        if constexpr (NS == 1) {
-            const uint16_t *src = static_cast<const uint16_t *>(p.q) + at + d;
-            if (there && p.q_vec) {
-                if (d < p.v.head_dim) {
-                    q[0][c] = *reinterpret_cast<const bf16x8 *>(src);
-                    continue;
+        if (col < there) {
+            const int token = col / p.group;
+            const int64_t at = (w.n.first + token) * p.q_token + (head * p.group + col - token * p.group) * p.q_head + d;
+            if (p.q_vec && d < p.v.head_dim) {
+                if constexpr (NS == 1) {
+                    const u32x4 u = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p.q) + at);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e & 1 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const f32x4 u = reinterpret_cast<const f32x4 *>(static_cast<const float *>(p.q) + at)[h];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[4 * h + e] = u[e];
+                    }
                 }
-            } else if (there) {
+            } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if (d + e < p.v.head_dim) x[e] = __uint_as_float((uint32_t)src[e] << 16);
-            }
-        } else {
-            const float *src = static_cast<const float *>(p.q) + at + d;
-            if (there) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (d + e < p.v.head_dim) x[e] = src[e];
+                    if (d + e < p.v.head_dim) {
+                        if constexpr (NS == 1) x[e] = __uint_as_float((uint32_t)static_cast<const uint16_t *>(p.q)[at + e] << 16);
+                        else x[e] = static_cast<const float *>(p.q)[at + e];
+                    }
             }
         }
-        bf16x8 parts[NS];
         parts_of<NS>(x, parts);
 #pragma unroll
-        for (int n = 0; n < NS; ++n) q[n][c] = parts[n];
+        for (int n = 0; n < NS; ++n) *reinterpret_cast<bf16x8 *>(to + (n * cols + c) * kQueryRow<DC> + d) = parts[n];
     }
+}
+// a lane's part of the 16 columns from c0 on
+template <int DC, int NS>
+__device__ __forceinline__ void take_queries(const uint16_t *from, int cols, int c0, bf16x8 (&q)[NS][DC])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int n = 0; n < NS; ++n)
+#pragma unroll
+        for (int c = 0; c < DC; ++c) q[n][c] = *reinterpret_cast<const bf16x8 *>(from + (n * cols + c0 + (lane & 15)) * kQueryRow<DC> + 32 * c + 8 * (lane >> 4));
+}
+
+// Sums over the workgroup's threads before this one, of two numbers, and over all.
+struct TwoSums {
+    int64_t before[2], all[2];
+};
+__device__ __forceinline__ TwoSums two_sums(int64_t a, int64_t b, int64_t *lds /* [8] */)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t x = a, y = b;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t u = __shfl_up(x, o), w = __shfl_up(y, o);
+        if (lane >= o) {
+            x += u;
+            y += w;
+        }
+    }
+    if (lane == 63) {
+        lds[wave] = x;
+        lds[4 + wave] = y;
+    }
+    __syncthreads();
+    TwoSums s{{x - a, y - b}, {0, 0}};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave) {
+            s.before[0] += lds[w];
+            s.before[1] += lds[4 + w];
+        }
+        s.all[0] += lds[w];
+        s.all[1] += lds[4 + w];
+    }
+    return s;
 }
 
 // Scores of the block's 32 tokens: token 16 t + 4 (lane >> 4) + i against the lane's column.
@@ -161,28 +210,69 @@ __device__ __forceinline__ void scores_of(const u32x4 (&k)[DC], const bf16x8 (&q
         }
 }
 
+// Whether the token of weight e (0 .. 7: scores [e / 4][e % 4]) of the block is one that a column of this place sees.
+__device__ __forceinline__ bool sees(int first, int e, int place, int64_t window)
+{
+    const int token = first + 16 * (e >> 2) + 4 * ((threadIdx.x & 63) >> 4) + (e & 3);
+    return token <= place && (window <= 0 || (int64_t)token > place - window);
+}
+template <int CT>
+__device__ __forceinline__ void hide(f32x4 (&s)[CT][2], int first, const int (&place)[CT], int64_t window)
+{
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (!sees(first, e, place[ct], window)) s[ct][e >> 2][e & 3] = -INFINITY;
+}
+
+// Codes that are no number, in a block that some columns do not see all of (or that nobody wrote all of): they are taken out of the values, and the
+// outputs of the columns that see them become NaN.
+template <int DC, int CT>
+__device__ __forceinline__ void take_out_strange(f32x4 (&o)[CT][2 * DC], u32x4 (&v)[DC], int first, const int (&place)[CT], int64_t window)
+{
+    uint32_t any = 0;
+#pragma unroll
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) any |= no_numbers(v[c][e]);
+    if (!__any(any != 0)) return;
+    bf16x8 seen[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) seen[ct][e] = sees(first, e, place[ct], window) ? (__bf16)1.f : (__bf16)0.f;
+#pragma unroll
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t a = no_numbers(v[c][2 * u]), b = no_numbers(v[c][2 * u + 1]);
+            v[c][2 * u] &= ~((a >> 7) * 0xffu);
+            v[c][2 * u + 1] &= ~((b >> 7) * 0xffu);
+            const bf16x8 bad = ones_where(a, b);
+            __builtin_amdgcn_sched_barrier(0);   // (one at a time: seldom run, and not to cost the others registers)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, seen[ct], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (count[i] > 0.f) o[ct][2 * c + u][i] = __uint_as_float(0x7fc00000u);
+            }
+        }
+}
+
 // Scores to weights.  first: the block's first token, place: of the lane's columns' tokens (below 0: a column of nobody), edge: some column
 // does not see all of the block.
 template <int DC, int CT>
 __device__ __forceinline__ void weigh(Running<DC, CT> &r, f32x4 (&s)[CT][2], float scale, bool edge, int first, const int (&place)[CT], int64_t window)
 {
-    const int g = (threadIdx.x & 63) >> 4;
+    if (edge) hide<CT>(s, first, place, window);
     float top[CT];
     bool follow = false;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        top[ct] = -INFINITY;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[ct][t][i] *= scale;
-                if (edge) {
-                    const int token = first + 16 * t + 4 * g + i;
-                    if (token > place[ct] || (window > 0 && (int64_t)token <= place[ct] - window)) s[ct][t][i] = -INFINITY;
-                }
-                top[ct] = fmaxf(top[ct], s[ct][t][i]);
-            }
+        top[ct] = fmaxf(fmaxf(fmaxf(s[ct][0][0], s[ct][0][1]), fmaxf(s[ct][0][2], s[ct][0][3])),
+                        fmaxf(fmaxf(s[ct][1][0], s[ct][1][1]), fmaxf(s[ct][1][2], s[ct][1][3]))) * scale;
         follow |= top[ct] > r.m[ct] + kSlack;
     }
     if (__any(follow)) {
@@ -206,16 +296,15 @@ __device__ __forceinline__ void weigh(Running<DC, CT> &r, f32x4 (&s)[CT][2], flo
         for (int t = 0; t < 2; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s[ct][t][i] = __builtin_amdgcn_exp2f(s[ct][t][i] - m);
+                s[ct][t][i] = __builtin_amdgcn_exp2f(fmaf(s[ct][t][i], scale, -m));
                 r.l[ct] += s[ct][t][i];
             }
     }
 }
 
-// Weights times values.  In an edge block, codes that are no number (of tokens that some columns do not see, or that nobody wrote) are
-// taken out of the product and put into the outputs of the columns that see them.
+// Weights times values.
 template <int DC, int CT, int NS>
-__device__ __forceinline__ void add_values(Running<DC, CT> &r, const u32x4 (&v)[DC], float scale, const f32x4 (&w)[CT][2], bool edge, int first,
+__device__ __forceinline__ void add_values(Running<DC, CT> &r, u32x4 (&v)[DC], float scale, const f32x4 (&w)[CT][2], bool edge, int first,
                                            const int (&place)[CT], int64_t window)
 {
     bf16x8 f[CT][NS];
@@ -224,58 +313,25 @@ __device__ __forceinline__ void add_values(Running<DC, CT> &r, const u32x4 (&v)[
         const float x[8] = {w[ct][0][0], w[ct][0][1], w[ct][0][2], w[ct][0][3], w[ct][1][0], w[ct][1][1], w[ct][1][2], w[ct][1][3]};
         parts_of<NS>(x, f[ct]);
     }
-    bool strange = false;
-    if (edge) {
-        uint32_t any = 0;
-#pragma unroll
-        for (int c = 0; c < DC; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) any |= no_numbers(v[c][e]);
-        strange = __any(any != 0);
-    }
-    if (!strange) {
-#pragma unroll
-        for (int c = 0; c < DC; ++c)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const bf16x8 x = values_of(v[c][2 * u], v[c][2 * u + 1], scale);
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int n = 0; n < NS; ++n) r.o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[ct][n], r.o[ct][2 * c + u], 0, 0, 0);
-            }
-        return;
-    }
-    const int g = (threadIdx.x & 63) >> 4;
+    if (edge) take_out_strange<DC, CT>(r.o, v, first, place, window);
 #pragma unroll
     for (int c = 0; c < DC; ++c)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const uint32_t a = v[c][2 * u], b = v[c][2 * u + 1], na = no_numbers(a), nb = no_numbers(b);
-            const bf16x8 x = values_of(a & ~((na >> 7) * 0xffu), b & ~((nb >> 7) * 0xffu), scale), bad = ones_where(na, nb);
+            const bf16x8 x = values_of(v[c][2 * u], v[c][2 * u + 1], scale);
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                bf16x8 seen;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int token = first + 16 * (e >> 2) + 4 * g + (e & 3);
-                    seen[e] = token <= place[ct] && (window <= 0 || (int64_t)token > place[ct] - window) ? (__bf16)1.f : (__bf16)0.f;
-                }
-                const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int n = 0; n < NS; ++n) r.o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[ct][n], r.o[ct][2 * c + u], 0, 0, 0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (count[i] > 0.f) r.o[ct][2 * c + u][i] = __uint_as_float(0x7fc00000u);
-            }
         }
 }
 
 // Four elements of a column's output, from element d on.
-__device__ __forceinline__ void store_out(const AttendArgs &p, int64_t first, int head, int64_t col, int d, f32x4 x)
+__device__ __forceinline__ void store_out(const AttendArgs &p, int64_t first, int head, int col, int d, f32x4 x)
 {
-    const int64_t at = (first + col / p.group) * p.out_token + (head * (int64_t)p.group + col % p.group) * p.out_head + d;
     if (d >= p.v.head_dim) return;
+    const int token = col / p.group;
+    const int64_t at = (first + token) * p.out_token + (head * p.group + col - token * p.group) * p.out_head + d;
     if (p.out_bf16) {
         uint16_t *to = static_cast<uint16_t *>(p.out) + at;
         if (p.out_vec) {

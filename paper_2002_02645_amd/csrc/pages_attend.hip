@@ -24,7 +24,7 @@ __host__ __device__ inline int64_t share_of(int64_t blocks, int workers)
 // cut into equal shares, one a workgroup, wherever that falls; a tile that several workgroups meet in goes through `part` and pages_join_kernel.  A share's
 // blocks go round the workgroup's four waves, whose results meet in LDS at the tile's end.
 template <int DC, int CT, int NS>
-__global__ __launch_bounds__(256) void pages_attend_kernel(AttendArgs p)
+__global__ __launch_bounds__(256, CT <= 2 && NS == 1 && DC <= 4 ? 2 : 1) void pages_attend_kernel(AttendArgs p)
 {
     constexpr int kCols = 16 * CT, kFrags = CT * 2 * DC;
     extern __shared__ float lds[];
@@ -41,19 +41,10 @@ __global__ __launch_bounds__(256) void pages_attend_kernel(AttendArgs p)
         mine += (int64_t)w.blocks * w.tiles;
         tiles += w.tiles;
     }
-    sums[threadIdx.x] = mine;
-    sums[256 + threadIdx.x] = tiles;
-    __syncthreads();
-    int64_t before = 0, total = 0, tiles_before = 0;
-    for (int t = 0; t < 256; ++t) {
-        if (t < (int)threadIdx.x) {
-            before += sums[t];
-            tiles_before += sums[256 + t];
-        }
-        total += sums[t];
-    }
+    const TwoSums so_far = two_sums(mine, tiles, sums);
+    const int64_t before = so_far.before[0], total = so_far.all[0];
     if (blockIdx.x == 0) {   // for pages_join_kernel
-        int64_t b = before, n = tiles_before;
+        int64_t b = before, n = so_far.before[1];
         for (int r = r0; r < r1; ++r) {
             p.blocks_before[r] = b;
             p.tiles_before[r] = (int32_t)n;
@@ -69,8 +60,8 @@ __global__ __launch_bounds__(256) void pages_attend_kernel(AttendArgs p)
     const int64_t share = share_of(total * v.heads, p.workers);
     const int64_t begin = blockIdx.x * share, end = min(total * v.heads, begin + share);
     if (begin >= end) return;
-    int *found = reinterpret_cast<int *>(sums + 512);
-    int64_t *found_before = sums + 513;
+    int *found = reinterpret_cast<int *>(sums + 8);
+    int64_t *found_before = sums + 9;
     if (before * v.heads <= begin && begin < (before + mine) * v.heads) {
         int64_t b = before;
         int r = r0;
@@ -99,20 +90,21 @@ __global__ __launch_bounds__(256) void pages_attend_kernel(AttendArgs p)
         const int64_t item = (at - base) / w.blocks;
         const int b0 = (int)(at - base - item * w.blocks), tile = (int)(item / v.heads), head = (int)(item - (int64_t)tile * v.heads);
         const int count = (int)min((int64_t)w.blocks - b0, end - at);
-        const int64_t col0 = (int64_t)tile * kCols;
+        const int col0 = tile * kCols, cols = w.n.count * p.group;
 
+        uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
+        stage_queries<DC, NS>(p, w, head, col0, kCols, staged);
+        __syncthreads();
         bf16x8 q[CT][NS][DC];
         int place[CT];
-        int lowest = INT32_MAX, highest = -1;   // places of the tile's tokens
-        const int64_t cols = (int64_t)w.n.count * p.group;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            const int64_t c = col0 + 16 * ct + col;
-            load_queries<DC, NS>(p, w, head, c, q[ct]);
-            place[ct] = c < cols ? w.len - w.n.count + (int)(c / p.group) : -1;
+            take_queries<DC, NS>(staged, kCols, 16 * ct, q[ct]);
+            const int c = col0 + 16 * ct + col;
+            place[ct] = c < cols ? w.len - w.n.count + c / p.group : -1;
         }
-        lowest = w.len - w.n.count + (int)(col0 / p.group);
-        highest = w.len - w.n.count + (int)((min(cols, col0 + kCols) - 1) / p.group);
+        // places of the tile's tokens
+        const int lowest = w.len - w.n.count + col0 / p.group, highest = w.len - w.n.count + (min(cols, col0 + kCols) - 1) / p.group;
 
         Running<DC, CT> run;
         run.clear();
@@ -163,20 +155,23 @@ __global__ __launch_bounds__(256) void pages_attend_kernel(AttendArgs p)
             next = after;
         }
 
-        // the four waves' results into the first one's
+        // the four waves' results under one reference
+        __syncthreads();   // (the queries are read)
         float *ml = lds;   // [4][2][kCols]
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             float l = run.l[ct];
             l += __shfl_xor(l, 16);
             l += __shfl_xor(l, 32);
-            run.l[ct] = l;
             if (lane < 16) {
                 ml[(wave * 2) * kCols + 16 * ct + lane] = run.m[ct];
                 ml[(wave * 2 + 1) * kCols + 16 * ct + lane] = l;
             }
         }
         __syncthreads();
+        const bool whole = b0 == 0 && count == w.blocks;
+        const int64_t slot = blockIdx.x * 2 + (at == begin ? 0 : 1);
+        f32x4 *frags = reinterpret_cast<f32x4 *>(lds + 8 * kCols);   // [4][2 DC][64]
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             float m = -INFINITY, l = 0.f;
@@ -186,58 +181,24 @@ __global__ __launch_bounds__(256) void pages_attend_kernel(AttendArgs p)
 #pragma unroll
             for (int u = 0; u < 4; ++u) l += ml[(u * 2 + 1) * kCols + 16 * ct + col] * __builtin_amdgcn_exp2f(ml[u * 2 * kCols + 16 * ct + col] - ref);
             const float a = __builtin_amdgcn_exp2f(run.m[ct] - ref);
-            run.m[ct] = m;
-            run.l[ct] = l;
 #pragma unroll
-            for (int f = 0; f < 2 * DC; ++f)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) run.o[ct][f][e] *= a;
-        }
-        __syncthreads();
-        f32x4 *frags = reinterpret_cast<f32x4 *>(lds);   // [2][kFrags][64]
-#pragma unroll
-        for (int half = 2; half > 0; half >>= 1) {
-            if (wave >= half && wave < 2 * half)
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int f = 0; f < 2 * DC; ++f) frags[((wave - half) * kFrags + ct * 2 * DC + f) * 64 + lane] = run.o[ct][f];
-            __syncthreads();
-            if (wave < half)
-#pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                    for (int f = 0; f < 2 * DC; ++f) {
-                        const f32x4 o = frags[(wave * kFrags + ct * 2 * DC + f) * 64 + lane];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) run.o[ct][f][e] += o[e];
-                    }
-            __syncthreads();
-        }
-        if (wave == 0) {
-            const bool whole = b0 == 0 && count == w.blocks;
-            const int64_t slot = blockIdx.x * 2 + (at == begin ? 0 : 1);
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const int64_t c = col0 + 16 * ct + col;
-                if (c >= cols) continue;
-                const float inv = run.l[ct] == 0.f ? 0.f : 1.f / run.l[ct];
-                if (!whole && lane < 16) {
-                    p.part_ml[(slot * 2) * kCols + 16 * ct + col] = run.m[ct];
-                    p.part_ml[(slot * 2 + 1) * kCols + 16 * ct + col] = run.l[ct];
-                }
-#pragma unroll
-                for (int f = 0; f < 2 * DC; ++f) {
-                    f32x4 o = run.o[ct][f];
-                    if (!whole) {
-                        reinterpret_cast<f32x4 *>(p.part_o)[(slot * kFrags + ct * 2 * DC + f) * 64 + lane] = o;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] *= inv;
-                        store_out(p, w.n.first, head, c, 16 * f + 4 * (lane >> 4), o);
-                    }
-                }
+            for (int f = 0; f < 2 * DC; ++f) frags[(wave * 2 * DC + f) * 64 + lane] = run.o[ct][f] * a;
+            if (!whole && threadIdx.x < 16) {
+                p.part_ml[(slot * 2) * kCols + 16 * ct + lane] = m;
+                p.part_ml[(slot * 2 + 1) * kCols + 16 * ct + lane] = l;
             }
+            __syncthreads();
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            const int c = col0 + 16 * ct + col;   // (of thread and of lane alike)
+            if (c < cols)
+                for (int f = wave; f < 2 * DC; f += 4) {
+                    f32x4 o = frags[f * 64 + lane];
+#pragma unroll
+                    for (int u = 1; u < 4; ++u) o += frags[(u * 2 * DC + f) * 64 + lane];
+                    if (whole) store_out(p, w.n.first, head, c, 16 * f + 4 * (lane >> 4), o * inv);
+                    else reinterpret_cast<f32x4 *>(p.part_o)[(slot * kFrags + ct * 2 * DC + f) * 64 + lane] = o;
+                }
+            __syncthreads();
         }
         at += count;
     }
@@ -263,8 +224,8 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
     const int lane = e & 63, frag = e >> 6;
     if (frag >= kFrags || (w.blocks > 0 && w0 == w1)) return;
     const int ct = frag / (2 * DC), in = 16 * ct + (lane & 15);
-    const int64_t c = (int64_t)in_row * kCols + in;
-    if (c >= (int64_t)w.n.count * p.group) return;
+    const int c = in_row * kCols + in;
+    if (c >= w.n.count * p.group) return;
     f32x4 o{0.f, 0.f, 0.f, 0.f};
     if (w.blocks > 0) {
         auto slot_of = [&](int64_t u) { return u * 2 + (u == w0 && begin != u * share ? 1 : 0); };
@@ -287,20 +248,162 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
     store_out(p, w.n.first, head, c, 16 * (frag - ct * 2 * DC) + 4 * (lane >> 4), o);
 }
 
+// Prompts: a workgroup's waves have 16 * CT columns each, one after another, and walk over the blocks that these see, each by itself: the codes of a
+// block come from memory once and from the caches for the other waves.  Nothing is split: there are tiles enough.  Later tiles of a row see more and go first.
+template <int DC, int CT>
+__global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(AttendArgs p)
+{
+    constexpr int kWave = 16 * CT, kCols = 4 * kWave;
+    const PageView &v = p.v;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15;
+    extern __shared__ float lds[];
+    // the tile: row and number within it
+    int64_t *sums = reinterpret_cast<int64_t *>(lds);
+    int *found = reinterpret_cast<int *>(sums + 8);
+    const int per = (v.rows + 255) / 256;
+    const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
+    int mine = 0;
+    for (int r = r0; r < r1; ++r) mine += row_work(p, r, kCols).tiles;
+    const TwoSums so_far = two_sums(mine, 0, sums);
+    const int before = (int)so_far.before[0], total = (int)so_far.all[0];
+    const int head = blockIdx.x % v.heads, tile = total - 1 - (int)(blockIdx.x / v.heads);
+    if (tile < 0) return;
+    if (before <= tile && tile < before + mine)
+        for (int r = r0, b = before; r < r1; ++r) {
+            const int n = row_work(p, r, kCols).tiles;
+            if (tile < b + n) {
+                found[0] = r;
+                found[1] = tile - b;
+                break;
+            }
+            b += n;
+        }
+    __syncthreads();
+    const int row = __builtin_amdgcn_readfirstlane(found[0]);
+    const RowWork w = row_work(p, row, kCols);
+    const int cols = w.n.count * p.group, tile0 = __builtin_amdgcn_readfirstlane(found[1]) * kCols, col0 = tile0 + wave * kWave;
+    __syncthreads();
+    uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
+    stage_queries<DC, 1>(p, w, head, tile0, kCols, staged);
+    __syncthreads();
+    if (col0 >= cols) return;
+    bf16x8 q[CT][1][DC];
+    int place[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        take_queries<DC, 1>(staged, kCols, wave * kWave + 16 * ct, q[ct]);
+        const int c = col0 + 16 * ct + col;
+        place[ct] = c < cols ? w.len - w.n.count + c / p.group : -1;
+    }
+    const int lowest = w.len - w.n.count + col0 / p.group, highest = w.len - w.n.count + (min(cols, col0 + kWave) - 1) / p.group;
+    const int seen = p.window > 0 ? (int)max((int64_t)0, lowest - p.window + 1) : 0;
+    const int lo = seen / kPageBlock, hi = highest < 0 ? 0 : highest / kPageBlock + 1;
+
+    f32x4 o[CT][2 * DC], sum[CT];
+    float m[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        m[ct] = -INFINITY;
+        sum[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < 2 * DC; ++f) o[ct][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int32_t *table = v.tables + row * v.max_pages;
+    bf16x8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
+    for (int b = lo; b < hi; ++b) {
+        const int page = table[b >> (v.page_log2 - 5)];
+        if (page < 0 || page >= v.num_pages) continue;
+        const uint8_t *from = v.codes + v.block_at(page, head, b & (v.per_page - 1)) + lane * 16;
+        const uint32_t scales = *reinterpret_cast<const uint16_t *>(v.scales + v.scale_at(page, head, b & (v.per_page - 1)));
+        u32x4 k[DC], x[DC];
+#pragma unroll
+        for (int c = 0; c < DC; ++c) k[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
+#pragma unroll
+        for (int c = 0; c < DC; ++c) x[c] = *reinterpret_cast<const u32x4 *>(from + 32 * v.width + c * 1024);
+        const int first = b * kPageBlock;
+        const bool edge = first + kPageBlock - 1 > lowest || (p.window > 0 && (int64_t)first <= highest - p.window);
+        const float ks = p.scale_log2 * __uint_as_float((scales & 0xffu) << 23), vs = __uint_as_float((scales >> 8) << 23);
+        f32x4 s[CT][2];
+        scores_of<DC, CT, 1>(k, q, s);
+        if (edge) hide(s, first, place, p.window);
+        bool follow = false;
+        float top[CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            top[ct] = fmaxf(fmaxf(fmaxf(s[ct][0][0], s[ct][0][1]), fmaxf(s[ct][0][2], s[ct][0][3])), fmaxf(fmaxf(s[ct][1][0], s[ct][1][1]), fmaxf(s[ct][1][2], s[ct][1][3]))) * ks;
+            follow |= top[ct] > m[ct] + kSlack;
+        }
+        if (__any(follow)) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                float t = fmaxf(top[ct], __shfl_xor(top[ct], 16));
+                t = fmaxf(m[ct], fmaxf(t, __shfl_xor(t, 32)));
+                const float a = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - t);
+                m[ct] = t;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum[ct][i] *= a;
+#pragma unroll
+                for (int f = 0; f < 2 * DC; ++f)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[ct][f][i] *= a;
+            }
+        }
+        bf16x8 f[CT];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            const float ref = m[ct] == -INFINITY ? 0.f : m[ct];
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) f[ct][4 * t + i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[ct][t][i], ks, -ref));
+            sum[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, f[ct], sum[ct], 0, 0, 0);
+        }
+        if (edge) take_out_strange<DC, CT>(o, x, first, place, p.window);
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const bf16x8 y = values_of(x[c][2 * u], x[c][2 * u + 1], vs);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, f[ct], o[ct][2 * c + u], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const int c = col0 + 16 * ct + col;
+        if (c >= cols) continue;
+        const float inv = sum[ct][0] == 0.f ? 0.f : 1.f / sum[ct][0];
+#pragma unroll
+        for (int f = 0; f < 2 * DC; ++f) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[ct][f][e] *= inv;
+            store_out(p, w.n.first, head, c, 16 * f + 4 * (lane >> 4), o[ct][f]);
+        }
+    }
+}
+
 // ---- host -------------------------------------------------------------------------------------------
 
+#ifndef PROMPT_CT
+#define PROMPT_CT 2
+#endif
+constexpr int kPromptCT = PROMPT_CT;
 struct AttendPlan {
     int ct, parts;
+    bool prompt;
     size_t o_bytes, ml_bytes, rows_bytes;
     size_t bytes() const { return o_bytes + ml_bytes + 2 * rows_bytes; }
 };
-AttendPlan attend_plan(const freeze_pages *p, int group, int64_t most, int parts)
+AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t most, int parts)
 {
     AttendPlan pl;
     const int dc = page_width(p->head_dim) / 32;
     const int64_t cols = (most > 0 ? most : 1) * group;
     pl.parts = parts;
     pl.ct = parts > 1 || cols <= 16 ? 1 : cols <= 32 || dc > 4 ? 2 : 4;
+    pl.prompt = parts == 1 && cols > 64 && tokens * group * p->heads >= (int64_t)256 * 128;
     const size_t slots = 2 * kWorkers, kCols = 16 * pl.ct;
     pl.o_bytes = slots * kCols * page_width(p->head_dim) * 4;
     pl.ml_bytes = slots * 2 * kCols * 4;
@@ -312,7 +415,8 @@ template <int DC, int CT, int NS>
 hipError_t launch_attend(const AttendArgs &a, int64_t tiles, hipStream_t s)
 {
     constexpr int kFrags = CT * 2 * DC;
-    constexpr size_t lds = std::max<size_t>({2 * (size_t)kFrags * 1024, 8 * 16 * CT * 4, 515 * 8});
+    constexpr size_t lds = std::max((size_t)NS * 16 * CT * kQueryRow<DC> * 2, (size_t)8 * 16 * CT * 4 + 4 * 2 * DC * 1024);
+    static_assert(lds <= 65536 + 2048, "LDS");
     hipLaunchKernelGGL((pages_attend_kernel<DC, CT, NS>), dim3(a.workers), dim3(256), lds, s, a);
     if (hipGetLastError() != hipSuccess) return hipErrorLaunchFailure;
     hipLaunchKernelGGL((pages_join_kernel<DC, CT>), dim3((unsigned)(tiles * a.v.heads), (kFrags * 64 + 255) / 256), dim3(256), 0, s, a);
@@ -321,6 +425,12 @@ hipError_t launch_attend(const AttendArgs &a, int64_t tiles, hipStream_t s)
 template <int DC>
 hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, int64_t tiles, hipStream_t s)
 {
+    if (pl.prompt) {
+        constexpr int CT = DC <= 4 ? kPromptCT : 1;
+        const int64_t n = std::min(a.tokens * a.group / (64 * CT) + a.v.rows, a.tokens * ((a.group + 64 * CT - 1) / (64 * CT)));
+        hipLaunchKernelGGL((pages_prompt_kernel<DC, CT>), dim3((unsigned)(n * a.v.heads)), dim3(256), (size_t)64 * CT * kQueryRow<DC> * 2, s, a);
+        return hipGetLastError();
+    }
     if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, tiles, s);
     if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, tiles, s);
     if (pl.ct == 2) return launch_attend<DC, 2, 1>(a, tiles, s);
@@ -345,7 +455,7 @@ extern "C" {
 size_t freeze_pages_attend_workspace_bytes(const freeze_pages *pages, int group, int64_t tokens, int64_t most, int packed)
 {
     if (!attend_sizes(pages, group, tokens, most)) return 0;
-    const AttendPlan pl = attend_plan(pages, group, most_of(tokens, most, packed), 1);
+    const AttendPlan pl = attend_plan(pages, group, tokens, most_of(tokens, most, packed), 1);
     return pl.bytes();
 }
 
@@ -367,7 +477,7 @@ int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int
         !heads_span(tokens, heads, pages->head_dim, out_token_stride, out_head_stride, true, &out_span))
         return FREEZE_EINVAL;
     const int64_t each = most_of(tokens, most, starts != nullptr);
-    const AttendPlan pl = attend_plan(pages, group, each, q_dtype == FREEZE_F32 ? 3 : 1);
+    const AttendPlan pl = attend_plan(pages, group, tokens, each, q_dtype == FREEZE_F32 ? 3 : 1);
     if (workspace_bytes < freeze_pages_attend_workspace_bytes(pages, group, tokens, most, starts != nullptr) || wb % 256 != 0) return FREEZE_EWORKSPACE;
     Extent e[10];
     int n = 0;
@@ -393,7 +503,7 @@ int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int
     a.window = window;
     a.starts = starts;
     a.group = group;
-    a.q_vec = q_dtype == FREEZE_BF16 && qb % 16 == 0 && pages->head_dim % 8 == 0 && a.q_token % 8 == 0 && a.q_head % 8 == 0;
+    a.q_vec = qb % 16 == 0 && pages->head_dim % 8 == 0 && a.q_token % 8 == 0 && a.q_head % 8 == 0;
     a.out_bf16 = out_dtype == FREEZE_BF16;
     a.out_vec = ob % (4 * os) == 0 && pages->head_dim % 4 == 0 && a.out_token % 4 == 0 && a.out_head % 4 == 0;
     a.scale_log2 = scale * 1.4426950408889634f;
