@@ -435,7 +435,7 @@ int freeze_reorder_states(const freeze_state *states, int num_states, const int3
  * Angles are formed in fp64 and taken less their whole turns, sine, cosine and the products in fp32, outputs rounded once.  dst may be src with the same
  * strides (in place), and shares no byte of its extent with anything else that the call reads or writes; tensors of one token stride may lie side by side in the
  * rows of one buffer.
- * 1 <= head_dim <= 4096, 0 <= 2 * pairs <= head_dim, 0 <= tokens < 2^31, 0 <= heads <= 65536, 0 <= num <= 8, |factor| <= 3e38; nothing to do is a no-op.
+ * 1 <= head_dim <= 4096, 0 <= 2 * pairs <= head_dim, 0 <= tokens < 2^31, 0 <= heads <= 8192, 0 <= num <= 8, |factor| <= 3e38; nothing to do is a no-op.
  */
 typedef struct freeze_heads {
     const void *src;
@@ -503,7 +503,7 @@ int freeze_pages_compact(const freeze_pages *pages, int32_t *out_used, void *wor
  *   starts   [rows + 1] int32: row r's are tokens starts[r] .. starts[r + 1] - 1; NULL: one token a row, tokens == rows.
  *   most     no row has more than this (0: tokens); a row that has, whose tokens are not all in 0 .. tokens - 1, or which has fewer than n_r tokens, is not written.
  *   granted  [rows] int32 or NULL: rows whose n_r is another are not written.
- * A page with several references is not written.
+ * A page with several references is not written.  0 <= tokens < 2^31, (tokens + 64 * rows) * (heads + 2) < 2^30.
  */
 int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int64_t k_token_stride, int64_t k_head_stride, const void *v,
                         int64_t v_token_stride, int64_t v_head_stride, int dtype, int64_t tokens, const int32_t *starts, int64_t most,

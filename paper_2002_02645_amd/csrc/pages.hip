@@ -278,100 +278,217 @@ struct AppendArgs {
     int64_t token_stride[2], head_stride[2];
     int64_t tokens, most;
     const int32_t *starts, *granted;
-    int blocks;                    // that a row's new tokens can lie in
+    int vec;                       // eight elements from a multiple of eight on are 16-byte loads
 };
 
-__device__ __forceinline__ float value_at(const float *p) { return *p; }
-__device__ __forceinline__ float value_at(const uint16_t *p) { return __uint_as_float((uint32_t)*p << 16); }
+// The new tokens of a row and the blocks that they lie in.
+struct AppendRow {
+    NewTokens n;
+    int len, first, blocks;
+};
+__device__ __forceinline__ AppendRow append_row(const AppendArgs &p, int row)
+{
+    AppendRow w;
+    w.n = new_tokens(p.starts, row, p.tokens, p.most);
+    w.len = p.v.length_of(row);
+    w.first = w.len - w.n.count;
+    const bool as_it_should = w.n.count > 0 && w.first >= 0 && (!p.granted || p.granted[row] == w.n.count);
+    w.blocks = as_it_should ? (w.len + kPageBlock - 1) / kPageBlock - w.first / kPageBlock : 0;
+    return w;
+}
 
 // The code of a finite value within the block's range; what is not finite: no number.
 __device__ __forceinline__ float code_of(float x, float inv)
 {
     return (__float_as_uint(x) & 0x7fffffffu) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : x * inv;
 }
-__device__ __forceinline__ float old_value(uint32_t word, int byte)   // byte: constant after unrolling
+__device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d)
 {
-    return byte == 0 ? __builtin_amdgcn_cvt_f32_fp8(word, 0) : byte == 1 ? __builtin_amdgcn_cvt_f32_fp8(word, 1) : byte == 2 ? __builtin_amdgcn_cvt_f32_fp8(word, 2) : __builtin_amdgcn_cvt_f32_fp8(word, 3);
+    int w = 0;
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, w, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+// codes scaled down by a power of two
+__device__ __forceinline__ uint32_t scaled_codes(uint32_t w, float down)
+{
+    return four_codes(__builtin_amdgcn_cvt_f32_fp8(w, 0) * down, __builtin_amdgcn_cvt_f32_fp8(w, 1) * down, __builtin_amdgcn_cvt_f32_fp8(w, 2) * down,
+                      __builtin_amdgcn_cvt_f32_fp8(w, 3) * down);
 }
 
-// A wave quantises the new tokens of one block of a head's keys or values: every lane holds the values of its own 16 bytes of each chunk of 32
-// elements, so that the block's largest magnitude is one reduction over the wave and a chunk leaves as one store of 1 KB.
-// DC: chunks.
+// Byte b of lane i of each four lanes becomes byte i of lane b: rows of four tokens to columns.
+__device__ __forceinline__ uint32_t across_four(uint32_t w)
+{
+    const uint32_t i = threadIdx.x & 3;
+    // what lies one, two and three lanes on
+    const uint32_t w1 = (uint32_t)__builtin_amdgcn_mov_dpp((int)w, 0x39, 0xf, 0xf, true), w2 = (uint32_t)__builtin_amdgcn_mov_dpp((int)w, 0x4e, 0xf, 0xf, true),
+                   w3 = (uint32_t)__builtin_amdgcn_mov_dpp((int)w, 0x93, 0xf, 0xf, true);
+    // byte i of each, in the order of the lanes that they are from: i, i + 1, i + 2, i + 3
+    const uint32_t lo = __builtin_amdgcn_perm(w1, w, i | (4 + i) << 8), hi = __builtin_amdgcn_perm(w3, w2, i | (4 + i) << 8);
+    const uint32_t all = (lo & 0xffffu) | hi << 16;
+    const uint32_t turn = 8 * i;                        // from lane i on: turned to begin with lane 0's
+    return turn ? all << turn | all >> (32 - turn) : all;
+}
+
+// A wave quantises the new tokens of one block of a head's keys or values.  A lane reads eight elements of two tokens of each chunk of 32 elements
+// (keys' own 16 bytes of the chunk), so that the block's largest magnitude is one reduction over the wave; values' codes change places among four lanes with four
+// tokens each.  DC: chunks.
 template <typename T, int DC>
 __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
 {
     const PageView &v = p.v;
-    const int lane = threadIdx.x & 63, g = lane >> 4, t = lane & 15;
-    const int64_t units = (int64_t)v.rows * p.blocks * v.heads * 2;
-    for (int64_t u = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); u < units; u += (int64_t)gridDim.x * 4) {
-        const int kv = (int)(u & 1);
-        const int64_t rest = u >> 1, unit = rest / v.heads;
-        const int head = (int)(rest - unit * v.heads), row = (int)(unit / p.blocks), j = (int)(unit - (int64_t)row * p.blocks);
-        const NewTokens n = new_tokens(p.starts, row, p.tokens, p.most);
-        const int len = v.length_of(row), first = len - n.count;
-        if (n.count == 0 || first < 0 || (p.granted && p.granted[row] != n.count)) continue;
-        const int block = first / kPageBlock + j, start = block * kPageBlock;
-        if (start >= len) continue;
-        const int page = v.tables[row * v.max_pages + (start >> v.page_log2)];
-        if (page < 0 || page >= v.num_pages || v.refs[page] > 1) continue;
-        const int in_page = block & (v.per_page - 1);
-        uint8_t *to = v.codes + v.block_at(page, head, in_page) + kv * (32 * v.width);
-        uint8_t *scale = v.scales + v.scale_at(page, head, in_page) + kv;
-        // token of the block, element of the head of this lane's byte e of chunk c
-        auto token_of = [&](int e) { return kv ? (e & 3) + 4 * g + (e >> 2 & 1) * 16 : t + (e >> 3) * 16; };
-        auto dim_of = [&](int c, int e) { return 32 * c + (kv ? t + (e >> 3) * 16 : 8 * g + (e & 7)); };
-        const T *x = static_cast<const T *>(p.x[kv]) + head * p.head_stride[kv];
-        const int kept = first - start;   // tokens that are there already (below 1: none)
-        float w[DC][16];
-        uint32_t amax = 0;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, t = lane & 15;
+    __shared__ int wave_sum[4], found[2];
+    // the row of this workgroup's block
+    const int groups = (2 * v.heads + 3) / 4;
+    const int which = (int)(blockIdx.x / groups), unit = (int)(blockIdx.x - (unsigned)which * groups) * 4 + wave;
+    {
+        const int per = (v.rows + 255) / 256;
+        const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
+        int mine = 0;
+        for (int r = r0; r < r1; ++r) mine += append_row(p, r).blocks;
+        int before = mine;
 #pragma unroll
-        for (int c = 0; c < DC; ++c)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int token = token_of(e), dim = dim_of(c, e);
-                w[c][e] = 0.f;
-                if (token >= kept && start + token < len && dim < v.head_dim)
-                    w[c][e] = value_at(x + (n.first + token - kept) * p.token_stride[kv] + dim);
-                const uint32_t bits = __float_as_uint(w[c][e]) & 0x7fffffffu;
-                if (bits < 0x7f800000u && bits > amax) amax = bits;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int u = __shfl_up(before, o);
+            if (lane >= o) before += u;
+        }
+        if (lane == 63) wave_sum[wave] = before;
+        __syncthreads();
+        before -= mine;
+        int total = 0;
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) before += wave_sum[w];
+            total += wave_sum[w];
+        }
+        if (which >= total) return;
+        if (before <= which && which < before + mine)
+            for (int r = r0, b = before; r < r1; ++r) {
+                const int n = append_row(p, r).blocks;
+                if (which < b + n) {
+                    found[0] = r;
+                    found[1] = which - b;
+                    break;
+                }
+                b += n;
             }
+        __syncthreads();
+    }
+    if (unit >= 2 * v.heads) return;
+    const int row = __builtin_amdgcn_readfirstlane(found[0]);
+    const AppendRow w = append_row(p, row);
+    const int block = w.first / kPageBlock + __builtin_amdgcn_readfirstlane(found[1]), start = block * kPageBlock;
+    const int kv = unit & 1, head = unit >> 1;
+    const int page = v.tables[row * v.max_pages + (start >> v.page_log2)];
+    const int kept = w.first - start, end = w.len - start;   // tokens of the block: those below `kept` are there already, those below `end` are new
+
+    const T *x = static_cast<const T *>(p.x[kv]) + head * p.head_stride[kv];
+    float y[DC][2][8];
+    uint32_t amax = 0;
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o));
-        int ex = (int)(amax >> 23) - 135 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
-        ex = ex < -126 ? -126 : ex;
-        const int old = kept > 0 ? (int)*scale - 127 : -126;
-        const bool grows = ex > old;
-        if (!grows) ex = old;
-        const float inv = __uint_as_float((uint32_t)(127 - ex) << 23);
-        const float down = old - ex < -126 ? 0.f : __uint_as_float((uint32_t)(127 + old - ex) << 23);   // (of a code: at least 2^-9, so nothing is left of it anyway)
+    for (int h = 0; h < 2; ++h) {
+        const int token = 16 * h + t;
+        const T *src = x + (w.n.first + token - kept) * p.token_stride[kv] + 8 * g;
+        const bool there = token >= kept && token < end;
 #pragma unroll
         for (int c = 0; c < DC; ++c) {
-            u32x4 codes;
-            u32x4 was{0, 0, 0, 0};
-            u32x4 *at = reinterpret_cast<u32x4 *>(to + c * 1024 + lane * 16);
-            if (kept > 0) was = *at;
+            const int d = 32 * c + 8 * g;
+            if (p.vec) {
+                const bool in = there && d < v.head_dim;
+                if constexpr (sizeof(T) == 2) {
+                    u32x4 u{0, 0, 0, 0};
+                    if (in) u = *reinterpret_cast<const u32x4 *>(src + 32 * c);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                float f[4];
-                uint32_t keep = 0;   // bytes that stay as they are
+                    for (int e = 0; e < 8; ++e) y[c][h][e] = __uint_as_float(e & 1 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
+                } else {
+                    u32x4 u{0, 0, 0, 0}, u2{0, 0, 0, 0};
+                    if (in) {
+                        u = reinterpret_cast<const u32x4 *>(src + 32 * c)[0];
+                        u2 = reinterpret_cast<const u32x4 *>(src + 32 * c)[1];
+                    }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int token = token_of(4 * q + e);
-                    f[e] = code_of(w[c][4 * q + e], inv);
-                    if (token < kept) {
-                        if (grows) f[e] = old_value(was[q], e) * down;
-                        else keep |= 0xffu << (8 * e);
+                    for (int e = 0; e < 8; ++e) y[c][h][e] = __uint_as_float(e < 4 ? u[e & 3] : u2[e & 3]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    y[c][h][e] = 0.f;
+                    if (there && d + e < v.head_dim) {
+                        if constexpr (sizeof(T) == 2) y[c][h][e] = __uint_as_float((uint32_t)src[32 * c + e] << 16);
+                        else y[c][h][e] = src[32 * c + e];
                     }
                 }
-                int b = 0;
-                b = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], b, false);
-                b = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], b, true);
-                codes[q] = ((uint32_t)b & ~keep) | (was[q] & keep);
             }
-            *at = codes;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t bits = __float_as_uint(y[c][h][e]) & 0x7fffffffu;
+                if (bits < 0x7f800000u && bits > amax) amax = bits;
+            }
         }
-        if (lane == 0) *scale = (uint8_t)(ex + 127);
     }
+    if (page < 0 || page >= v.num_pages || v.refs[page] > 1) return;
+    const int in_page = block & (v.per_page - 1);
+    uint8_t *to = v.codes + v.block_at(page, head, in_page) + kv * (32 * v.width);
+    uint8_t *scale = v.scales + v.scale_at(page, head, in_page) + kv;
+    const int old = kept > 0 ? (int)*scale - 127 : -126;
+    // where this lane's four words of a chunk go: two times eight bytes
+    const int at0 = kv ? (t >> 2) * 256 + ((8 * g + (t & 3)) & 15) * 16 + (g >> 1) * 8 : lane * 16, at1 = at0 + (kv ? 64 : 8);
+    u32x2 was[DC][2];
+    if (kept > 0) {
+#pragma unroll
+        for (int c = 0; c < DC; ++c) {
+            was[c][0] = *reinterpret_cast<const u32x2 *>(to + c * 1024 + at0);
+            was[c][1] = *reinterpret_cast<const u32x2 *>(to + c * 1024 + at1);
+        }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o));
+    int ex = (int)(amax >> 23) - 135 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
+    ex = ex < -126 ? -126 : ex;
+    const bool grows = ex > old;
+    if (!grows) ex = old;
+    const float inv = __uint_as_float((uint32_t)(127 - ex) << 23);
+    const float down = old - ex < -126 ? 0.f : __uint_as_float((uint32_t)(127 + old - ex) << 23);   // (of a code: at least 2^-9, so nothing is left of it anyway)
+    // bytes of this lane's words that stay: of word q of a piece
+    uint32_t stay[2][2];
+#pragma unroll
+    for (int piece = 0; piece < 2; ++piece)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            stay[piece][q] = 0;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int token = kv ? 16 * q + (t & 12) + b : 16 * piece + t;
+                if (token < kept) stay[piece][q] |= 0xffu << (8 * b);
+            }
+        }
+#pragma unroll
+    for (int c = 0; c < DC; ++c) {
+        uint32_t code[2][2];   // [token half][four elements]
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float f[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) f[e] = code_of(y[c][h][4 * q + e], inv);
+                code[h][q] = four_codes(f[0], f[1], f[2], f[3]);
+                if (kv) code[h][q] = across_four(code[h][q]);
+            }
+#pragma unroll
+        for (int piece = 0; piece < 2; ++piece) {
+            u32x2 out;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                out[q] = kv ? code[q][piece] : code[piece][q];
+                if (kept > 0) {
+                    const uint32_t before = grows ? scaled_codes(was[c][piece][q], down) : was[c][piece][q];
+                    out[q] = (out[q] & ~stay[piece][q]) | (before & stay[piece][q]);
+                }
+            }
+            *reinterpret_cast<u32x2 *>(to + c * 1024 + (piece ? at1 : at0)) = out;
+        }
+    }
+    if (lane == 0) *scale = (uint8_t)(ex + 127);
 }
 
 template <typename T>
@@ -512,7 +629,7 @@ int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int
                         const int32_t *granted, void *stream)
 {
     if (!page_sizes(pages) || layer < 0 || layer >= pages->layers || (dtype != FREEZE_F32 && dtype != FREEZE_BF16) || tokens < 0 || tokens >= (int64_t)1 << 31 ||
-        most < 0 || (!starts && tokens != 0 && tokens != pages->rows))
+        most < 0 || (!starts && tokens != 0 && tokens != pages->rows) || (double)(tokens + 64 * pages->rows) * (pages->heads + 2) >= 1073741824.0)
         return FREEZE_EINVAL;
     if (tokens == 0) return FREEZE_OK;
     const uintptr_t size = dtype == FREEZE_F32 ? 4 : 2;
@@ -545,9 +662,16 @@ int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int
     a.most = starts ? (most > 0 && most < tokens ? most : tokens) : 1;
     a.starts = starts;
     a.granted = granted;
-    a.blocks = (int)((a.most + 2 * kPageBlock - 2) / kPageBlock);
-    const int64_t units = pages->rows * a.blocks * pages->heads * 2;
-    const dim3 grid((unsigned)std::min<int64_t>((units + 3) / 4, 1 << 20));
+    a.vec = pages->head_dim % 8 == 0;
+    const void *both[2] = {k, v};
+    for (int i = 0; i < 2; ++i) {
+        if (tokens == 1) a.token_stride[i] = 0;
+        if (pages->heads == 1) a.head_stride[i] = 0;
+        a.vec &= reinterpret_cast<uintptr_t>(both[i]) % 16 == 0 && a.token_stride[i] % 8 == 0 && a.head_stride[i] % 8 == 0;
+    }
+    // a row's tokens lie in one block more than they fill, or two
+    const int64_t blocks = std::min(tokens / kPageBlock + 2 * pages->rows, tokens);
+    const dim3 grid((unsigned)(blocks * ((2 * pages->heads + 3) / 4)));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t err = dtype == FREEZE_F32 ? launch_append<float>(a, grid, s) : launch_append<uint16_t>(a, grid, s);
     return err == hipSuccess ? FREEZE_OK : FREEZE_EHIP;

@@ -12,10 +12,13 @@ struct RotateTensor {
     void *dst;
     int64_t src_token, src_head, dst_token, dst_head;
     int heads, bf16;
+    int per_head;        // items of a head: of 16 bytes or two times as many (vec), or of a pair or an element that is copied
+    int vec;
 };
 struct RotateArgs {
     RotateTensor t[kMostTensors];
     int num, pairs, dim, interleaved;
+    int each;            // tokens of a workgroup
     int64_t tokens;
     const int32_t *positions;
     const double *frequencies;
@@ -32,37 +35,106 @@ __device__ __forceinline__ void store_value(void *p, int64_t i, int bf16, float 
     else static_cast<float *>(p)[i] = x;
 }
 
-// Sine and cosine of 2 pi x for |x| <= 1/2 turns, sign and factor applied by the caller.
-__device__ __forceinline__ void turn(const RotateArgs &p, int64_t token, int i, float *c, float *s)
+// Factor times sine and cosine of a token's angle.
+__device__ __forceinline__ float2 turn(const RotateArgs &p, int64_t token, int i)
 {
     constexpr double kTurn = 0.15915494309189533577;   // 1 / (2 pi)
     const double x = (double)p.positions[token] * p.frequencies[i] * kTurn;
     const float r = (float)(x - rint(x));              // whole turns taken off in fp64: what is left is as exact as the angle itself
-    sincospif(2.f * r, s, c);
-    *c *= p.factor;
-    *s *= p.factor * p.sign;
+    float s, c;
+    sincospif(2.f * r, &s, &c);
+    return float2{c * p.factor, s * p.factor * p.sign};
 }
 
-// A workgroup takes a token: its sines and cosines once, for the heads of every tensor.
+// a and b turned by w (cosine, sine): one rounding of a product and of a sum each, the same in every form of the kernel
+__device__ __forceinline__ float turned_a(float a, float b, float2 w) { return fmaf(a, w.x, -(b * w.y)); }
+__device__ __forceinline__ float turned_b(float a, float b, float2 w) { return fmaf(b, w.x, a * w.y); }
+
+// 16 bytes as their values and back
+template <int V>
+__device__ __forceinline__ void open_up(u32x4 w, float (&x)[V])
+{
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = __uint_as_float(V == 4 ? w[e] : e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+}
+template <int V>
+__device__ __forceinline__ u32x4 close_up(const float (&x)[V])
+{
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if constexpr (V == 4) w[e] = __float_as_uint(x[e]);
+        else w[e] = (uint32_t)bf16_rne(x[2 * e]) | (uint32_t)bf16_rne(x[2 * e + 1]) << 16;
+    }
+    return w;
+}
+
+// An item of a head in 16-byte pieces: V / 2 pairs side by side; V pairs, half a turned part apart; or a piece that is copied.
+template <int V>
+__device__ __forceinline__ void rotate_pieces(const RotateArgs &p, const RotateTensor &t, const uint8_t *src, uint8_t *dst, const float2 *table, int i)
+{
+    const int pieces = p.pairs / V;   // of one half of the turned part
+    if (p.interleaved) {
+        u32x4 w = reinterpret_cast<const u32x4 *>(src)[i];
+        if (i < 2 * pieces) {
+            float x[V], y[V];
+            open_up<V>(w, x);
+#pragma unroll
+            for (int e = 0; e < V / 2; ++e) {
+                const float2 a = table[i * (V / 2) + e];
+                y[2 * e] = turned_a(x[2 * e], x[2 * e + 1], a);
+                y[2 * e + 1] = turned_b(x[2 * e], x[2 * e + 1], a);
+            }
+            w = close_up<V>(y);
+        }
+        reinterpret_cast<u32x4 *>(dst)[i] = w;
+        return;
+    }
+    if (i >= pieces) {
+        reinterpret_cast<u32x4 *>(dst)[i + pieces] = reinterpret_cast<const u32x4 *>(src)[i + pieces];
+        return;
+    }
+    float a[V], b[V], x[V], y[V];
+    open_up<V>(reinterpret_cast<const u32x4 *>(src)[i], a);
+    open_up<V>(reinterpret_cast<const u32x4 *>(src)[i + pieces], b);
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+        const float2 w = table[i * V + e];
+        x[e] = turned_a(a[e], b[e], w);
+        y[e] = turned_b(a[e], b[e], w);
+    }
+    reinterpret_cast<u32x4 *>(dst)[i] = close_up<V>(x);
+    reinterpret_cast<u32x4 *>(dst)[i + pieces] = close_up<V>(y);
+}
+
+// A workgroup takes some tokens (and, of few tokens, a part of their heads: blockIdx.y): their sines and cosines once, for the heads of every tensor.
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p)
 {
-    extern __shared__ float table[];   // [pairs] cosines, [pairs] sines
-    for (int64_t token = blockIdx.x; token < p.tokens; token += gridDim.x) {
+    extern __shared__ float2 table[];   // [each][pairs]
+    for (int64_t first = (int64_t)blockIdx.x * p.each; first < p.tokens; first += (int64_t)gridDim.x * p.each) {
+        const int here = (int)min((int64_t)p.each, p.tokens - first);
         __syncthreads();
-        for (int i = threadIdx.x; i < p.pairs; i += 256) turn(p, token, i, &table[i], &table[p.pairs + i]);
+        for (int j = threadIdx.x; j < here * p.pairs; j += 256) {
+            const int token = j / p.pairs;
+            table[j] = turn(p, first + token, j - token * p.pairs);
+        }
         __syncthreads();
         for (int k = 0; k < p.num; ++k) {
             const RotateTensor &t = p.t[k];
-            const int items = p.dim - p.pairs;   // of a head: pairs, then elements that are copied
-            for (int j = threadIdx.x; j < t.heads * items; j += 256) {
-                const int head = j / items, i = j - head * items;
-                const int64_t src = token * t.src_token + head * t.src_head, dst = token * t.dst_token + head * t.dst_head;
-                if (i < p.pairs) {
+            const int per_token = t.heads * t.per_head;
+            for (int j = blockIdx.y * 256 + threadIdx.x; j < here * per_token; j += 256 * gridDim.y) {
+                const int token = j / per_token, rest = j - token * per_token, head = rest / t.per_head, i = rest - head * t.per_head;
+                const int64_t src = (first + token) * t.src_token + head * t.src_head, dst = (first + token) * t.dst_token + head * t.dst_head;
+                const float2 *w = table + token * p.pairs;
+                if (t.vec) {
+                    if (t.bf16) rotate_pieces<8>(p, t, static_cast<const uint8_t *>(t.src) + src * 2, static_cast<uint8_t *>(t.dst) + dst * 2, w, i);
+                    else rotate_pieces<4>(p, t, static_cast<const uint8_t *>(t.src) + src * 4, static_cast<uint8_t *>(t.dst) + dst * 4, w, i);
+                } else if (i < p.pairs) {
                     const int a = p.interleaved ? 2 * i : i, b = p.interleaved ? a + 1 : i + p.pairs;
-                    const float x = load_value(t.src, src + a, t.bf16), y = load_value(t.src, src + b, t.bf16), c = table[i], s = table[p.pairs + i];
-                    store_value(t.dst, dst + a, t.bf16, x * c - y * s);
-                    store_value(t.dst, dst + b, t.bf16, x * s + y * c);
-                } else if (t.src != t.dst) {
+                    const float x = load_value(t.src, src + a, t.bf16), y = load_value(t.src, src + b, t.bf16);
+                    store_value(t.dst, dst + a, t.bf16, turned_a(x, y, w[i]));
+                    store_value(t.dst, dst + b, t.bf16, turned_b(x, y, w[i]));
+                } else {
                     const int e = i + p.pairs;
                     if (t.bf16) static_cast<uint16_t *>(t.dst)[dst + e] = static_cast<const uint16_t *>(t.src)[src + e];
                     else static_cast<uint32_t *>(t.dst)[dst + e] = static_cast<const uint32_t *>(t.src)[src + e];
@@ -102,9 +174,10 @@ int freeze_rotate_positions(const freeze_heads *heads, int num, int64_t tokens, 
     RotateArgs a{};
     Region e[2 * kMostTensors + 2];
     int n = 0;
+    double items = 0;
     for (int i = 0; i < num; ++i) {
         const freeze_heads &h = heads[i];
-        if ((h.dtype != FREEZE_F32 && h.dtype != FREEZE_BF16) || h.heads < 0 || h.heads > 65536) return FREEZE_EINVAL;
+        if ((h.dtype != FREEZE_F32 && h.dtype != FREEZE_BF16) || h.heads < 0 || h.heads > 8192) return FREEZE_EINVAL;
         if (tokens == 0 || h.heads == 0) continue;
         const uintptr_t size = h.dtype == FREEZE_F32 ? 4 : 2, src = reinterpret_cast<uintptr_t>(h.src), dst = reinterpret_cast<uintptr_t>(h.dst);
         int64_t ss, ds;
@@ -120,7 +193,12 @@ int freeze_rotate_positions(const freeze_heads *heads, int num, int64_t tokens, 
         add(dst, ds, h.dst_token_stride, h.dst_head_stride, true);
         RotateTensor &t = a.t[a.num++];
         t = RotateTensor{h.src, h.dst, tokens > 1 ? h.src_token_stride : 0, h.heads > 1 ? h.src_head_stride : 0, tokens > 1 ? h.dst_token_stride : 0,
-                         h.heads > 1 ? h.dst_head_stride : 0, h.heads, h.dtype == FREEZE_BF16};
+                         h.heads > 1 ? h.dst_head_stride : 0, h.heads, h.dtype == FREEZE_BF16, 0, 0};
+        // whole pieces of 16 bytes: of the turned part (of either half), of what is copied, from head to head and token to token
+        const int64_t piece = 16 / (int64_t)size, turned = interleaved ? 2 * pairs : pairs;
+        t.vec = src % 16 == 0 && dst % 16 == 0 && (t.src_token | t.src_head | t.dst_token | t.dst_head | turned | head_dim) % piece == 0;
+        t.per_head = (int)(t.vec ? (head_dim - (interleaved ? 0 : pairs)) / piece : head_dim - pairs);
+        items += (double)tokens * t.heads * t.per_head;
     }
     if (a.num == 0) return FREEZE_OK;
     const uintptr_t pb = reinterpret_cast<uintptr_t>(positions), fb = reinterpret_cast<uintptr_t>(frequencies);
@@ -138,8 +216,12 @@ int freeze_rotate_positions(const freeze_heads *heads, int num, int64_t tokens, 
     a.frequencies = frequencies;
     a.factor = factor;
     a.sign = inverse ? -1.f : 1.f;
-    const unsigned grid = (unsigned)std::min<int64_t>(tokens, 1 << 16);
-    hipLaunchKernelGGL(rotate_kernel, dim3(grid), dim3(256), (size_t)pairs * 8, static_cast<hipStream_t>(stream), a);
+    // Eight tokens a workgroup where that leaves 2,048 of them, and their sines fit; few tokens' heads over several.
+    a.each = (int)std::max<int64_t>(1, std::min<int64_t>({8, tokens / 2048, pairs > 0 ? 4096 / pairs : 8}));
+    const int64_t groups = (tokens + a.each - 1) / a.each;
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>({512 / groups, (int64_t)(items / (double)groups / 256), 64}));
+    hipLaunchKernelGGL(rotate_kernel, dim3((unsigned)std::min<int64_t>(groups, 1 << 16), (unsigned)parts), dim3(256), (size_t)pairs * a.each * 8,
+                       static_cast<hipStream_t>(stream), a);
     return hipGetLastError() == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
 }
 

@@ -89,7 +89,7 @@ def test_append_refusals():
     assert call(tokens=0) == 0 and call(tokens=0, k=None, v=None, starts=None) == 0
     for kw in SIZES + POINTERS:
         assert call(pool(**kw)) == EINVAL, kw
-    for kw in (dict(layer=-1), dict(layer=2), dict(k=None), dict(v=None), dict(dtype=2), dict(dtype=-1), dict(tokens=-1), dict(tokens=1 << 31), dict(most=-1), dict(starts=None),
+    for kw in (dict(layer=-1), dict(layer=2), dict(k=None), dict(v=None), dict(dtype=2), dict(dtype=-1), dict(tokens=-1), dict(tokens=1 << 31), dict(tokens=1 << 28, kt=0, vt=0), dict(most=-1), dict(starts=None),
                dict(starts=None, tokens=3), dict(k=P(6 * GB + 1)), dict(v=P(7 * GB + 2), dtype=0), dict(starts=P(8 * GB + 2)), dict(granted=P(9 * GB + 1)), dict(kt=-1), dict(vh=-1),
                dict(kt=1 << 45), dict(k=P(GB)), dict(v=P(2 * GB)), dict(starts=P(GB + 64)), dict(granted=P(2 * GB))):
         assert call(**kw) == EINVAL, kw
@@ -134,7 +134,7 @@ def test_rotate_refusals():
     for kw in (dict(tokens=-1), dict(tokens=1 << 31), dict(dim=0), dict(dim=4097, pairs=4), dict(pairs=-1), dict(pairs=5), dict(positions=None), dict(frequencies=None),
                dict(positions=P(8 * GB + 2)), dict(frequencies=P(9 * GB + 4)), dict(factor=float("nan")), dict(factor=float("inf"))):
         assert call([good], **kw) == EINVAL, kw
-    for h in (H(None, 2 * GB, 1, 3, 24, 8, 24, 8), H(GB, None, 1, 3, 24, 8, 24, 8), H(GB, 2 * GB, 2, 3, 24, 8, 24, 8), H(GB, 2 * GB, 1, -1, 24, 8, 24, 8), H(GB, 2 * GB, 1, 65537, 24, 8, 24, 8),
+    for h in (H(None, 2 * GB, 1, 3, 24, 8, 24, 8), H(GB, None, 1, 3, 24, 8, 24, 8), H(GB, 2 * GB, 2, 3, 24, 8, 24, 8), H(GB, 2 * GB, 1, -1, 24, 8, 24, 8), H(GB, 2 * GB, 1, 8193, 24, 8, 24, 8),
               H(GB + 1, 2 * GB, 1, 3, 24, 8, 24, 8), H(GB, 2 * GB + 2, 0, 3, 24, 8, 24, 8), H(GB, 2 * GB, 1, 3, -1, 8, 24, 8), H(GB, 2 * GB, 1, 3, 24, 8, 23, 8), H(GB, 2 * GB, 1, 3, 24, 8, 24, 7),
               H(GB, 2 * GB, 1, 3, 24, 8, 0, 8), H(GB, GB, 1, 3, 24, 8, 48, 8), H(GB, GB + 16, 1, 3, 24, 8, 24, 8), H(GB, 8 * GB, 1, 3, 24, 8, 24, 8), H(GB, 9 * GB, 1, 3, 24, 8, 24, 8)):
         assert call([h]) == EINVAL
