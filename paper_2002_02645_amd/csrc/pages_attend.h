@@ -19,9 +19,13 @@ struct AttendArgs {
     float scale_log2;                               // the scale times log2(e): weights are powers of two
     // work split over the tokens
     int workers;
-    int64_t *blocks_before;                         // [rows + 1] of a head, over its tiles
-    int32_t *tiles_before;                          // [rows + 1]
+    struct SplitTile *split;                        // [workers]: the tile that a worker has the first piece of and others go on with
     float *part_o, *part_ml;                        // [workers][2] pieces of tiles
+};
+struct SplitTile {
+    int64_t first;                                  // of the row's new tokens
+    int32_t columns;                                // of the row
+    int32_t col0, head, pieces, slot;               // pieces 0: none; slot: of the first one, the others' are their workers' first
 };
 
 // What a row asks for: its new tokens, its length, the blocks that the first to the last of them see.
@@ -42,6 +46,17 @@ __device__ __forceinline__ RowWork row_work(const AttendArgs &p, int row, int co
     return w;
 }
 
+// What is the same in every lane, in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)(((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32) | (uint32_t)uniform((int)x));
+}
+__device__ __forceinline__ RowWork uniform(const RowWork &w)
+{
+    return RowWork{{uniform(w.n.count), uniform(w.n.first)}, uniform(w.len), uniform(w.lo), uniform(w.blocks), uniform(w.tiles)};
+}
+
 __device__ __forceinline__ bf16x8 values_of(uint32_t a, uint32_t b, float scale)
 {
     union {
@@ -57,12 +72,19 @@ __device__ __forceinline__ bf16x8 values_of(uint32_t a, uint32_t b, float scale)
 
 // bytes 0x7f where a code is no number, 0 elsewhere (bit 7 alone)
 __device__ __forceinline__ uint32_t no_numbers(uint32_t codes) { return ((codes & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// 1 where no_numbers() has a bit
 __device__ __forceinline__ bf16x8 ones_where(uint32_t a, uint32_t b)
 {
-    bf16x8 f;
+    union {
+        uint32_t w[4];
+        bf16x8 v;
+    } u;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = ((e < 4 ? a : b) >> (8 * (e & 3) + 7) & 1) ? (__bf16)1.f : (__bf16)0.f;
-    return f;
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t pair = __builtin_amdgcn_perm(0, e < 2 ? a : b, e & 1 ? 0x0c030c02u : 0x0c010c00u);   // two bytes to two halves
+        u.w[e] = (pair >> 7) * 0x3f80u;
+    }
+    return u.v;
 }
 
 // x as NS numbers of 8 bits each

@@ -11,86 +11,113 @@ namespace {
 
 size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 
-constexpr int kWorkers = 512;         // workgroups that share the work
-constexpr int64_t kLeastShare = 4;    // blocks of a workgroup: one a wave
+// 64 rows of 4,000 .. 16,000 tokens (1.21 GB) and one of 131,072: 512 workgroups 193 and 50 us, 640: 192 and 48, 768 (three a CU): 189 and 47, 1,024: 225 and 57.
+// A tile costs about what eight blocks do: 32 rows of up to 2,000 tokens 16.6 us at 2, 14.1 at 4, 12.7 at 8, 15.6 at 12.
+constexpr int kWorkers = 768;         // workgroups that share the work
+constexpr int64_t kTileCost = 8;      // of a tile beside its blocks', in blocks: queries, joining the waves
+constexpr int64_t kLeastShare = 8;    // of a workgroup
 
-__host__ __device__ inline int64_t share_of(int64_t blocks, int workers)
-{
-    const int64_t share = (blocks + workers - 1) / workers;
-    return share < kLeastShare ? kLeastShare : share;
-}
+// Codes are read once (or by rows that share pages, at about the same time) and leave the caches to others: 189 us instead of 215.
+__device__ __forceinline__ u32x4 load_codes(const uint8_t *p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
 
-// Rows of a few columns each (a token or some of a row): all blocks of all (row, tile of columns, head) lie in one line, which is
-// cut into equal shares, one a workgroup, wherever that falls; a tile that several workgroups meet in goes through `part` and pages_join_kernel.  A share's
+template <int DC, int CT, int NS>
+constexpr int kAttendPerCu = NS == 1 && CT == 1 && DC <= 4 ? 3 : NS == 1 && ((CT == 2 && DC <= 4) || CT == 1) ? 2 : 1;
+
+// Rows of a few columns each (a token or some of a row): all blocks of all (row, tile of columns, head) lie in one line, kTileCost places before each tile's, which
+// is cut into equal shares, one a workgroup, wherever that falls; a tile that several workgroups meet in goes through `part` and pages_join_kernel.  A share's
 // blocks go round the workgroup's four waves, whose results meet in LDS at the tile's end.
 template <int DC, int CT, int NS>
-__global__ __launch_bounds__(256, CT <= 2 && NS == 1 && DC <= 4 ? 2 : 1) void pages_attend_kernel(AttendArgs p)
+__global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_kernel(AttendArgs p)
 {
     constexpr int kCols = 16 * CT, kFrags = CT * 2 * DC;
     extern __shared__ float lds[];
     const PageView &v = p.v;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15;
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 15;
 
     // where this workgroup's share begins
-    int64_t *sums = reinterpret_cast<int64_t *>(lds);
+    struct Found {
+        int64_t sums[8], base;
+        RowWork w;
+        int row;
+    };
+    Found *found = reinterpret_cast<Found *>(lds);
     const int per = (v.rows + 255) / 256;
     const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
-    int64_t mine = 0, tiles = 0;
+    auto cost_of = [&](const RowWork &w) { return (w.blocks + kTileCost) * w.tiles * v.heads; };
+    RowWork last;
+    int64_t mine = 0;
     for (int r = r0; r < r1; ++r) {
-        const RowWork w = row_work(p, r, kCols);
-        mine += (int64_t)w.blocks * w.tiles;
-        tiles += w.tiles;
+        last = row_work(p, r, kCols);
+        mine += cost_of(last);
     }
-    const TwoSums so_far = two_sums(mine, tiles, sums);
-    const int64_t before = so_far.before[0], total = so_far.all[0];
-    if (blockIdx.x == 0) {   // for pages_join_kernel
-        int64_t b = before, n = so_far.before[1];
-        for (int r = r0; r < r1; ++r) {
-            p.blocks_before[r] = b;
-            p.tiles_before[r] = (int32_t)n;
-            const RowWork w = row_work(p, r, kCols);
-            b += (int64_t)w.blocks * w.tiles;
-            n += w.tiles;
-            if (r + 1 == v.rows) {
-                p.blocks_before[v.rows] = b;
-                p.tiles_before[v.rows] = (int32_t)n;
-            }
-        }
-    }
-    const int64_t share = share_of(total * v.heads, p.workers);
-    const int64_t begin = blockIdx.x * share, end = min(total * v.heads, begin + share);
+    const TwoSums so_far = two_sums(mine, 0, found->sums);
+    const int64_t before = so_far.before[0], total = uniform(so_far.all[0]);
+    int64_t share = (total + p.workers - 1) / p.workers;
+    share = share < kLeastShare ? kLeastShare : share;
+    const int64_t begin = blockIdx.x * share, end = min(total, begin + share);
+    if (threadIdx.x == 0) p.split[blockIdx.x].pieces = 0;
     if (begin >= end) return;
-    int *found = reinterpret_cast<int *>(sums + 8);
-    int64_t *found_before = sums + 9;
-    if (before * v.heads <= begin && begin < (before + mine) * v.heads) {
+    if (before <= begin && begin < before + mine) {
         int64_t b = before;
         int r = r0;
-        for (; r < r1; ++r) {
-            const RowWork w = row_work(p, r, kCols);
-            const int64_t n = (int64_t)w.blocks * w.tiles;
-            if (begin < (b + n) * v.heads) break;
-            b += n;
-        }
-        *found = r;
-        *found_before = b;
+        if (per > 1)
+            for (;; ++r) {
+                last = row_work(p, r, kCols);
+                if (begin < b + cost_of(last)) break;
+                b += cost_of(last);
+            }
+        found->row = r;
+        found->base = b;
+        found->w = last;
     }
     __syncthreads();
-    int row = __builtin_amdgcn_readfirstlane(*found);
-    int64_t base = *found_before * v.heads;
+    int row = uniform(found->row);
+    int64_t base = uniform(found->base);
+    RowWork w = uniform(found->w);
     __syncthreads();
 
     for (int64_t at = begin; at < end;) {
-        const RowWork w = row_work(p, row, kCols);
-        const int64_t row_blocks = (int64_t)w.blocks * w.tiles * v.heads;
-        if (at >= base + row_blocks) {
-            base += row_blocks;
+        const int64_t row_cost = cost_of(w);
+        if (at >= base + row_cost) {
+            base += row_cost;
             ++row;
+            w = uniform(row_work(p, row, kCols));
             continue;
         }
-        const int64_t item = (at - base) / w.blocks;
-        const int b0 = (int)(at - base - item * w.blocks), tile = (int)(item / v.heads), head = (int)(item - (int64_t)tile * v.heads);
-        const int count = (int)min((int64_t)w.blocks - b0, end - at);
+        const int tile_cost = w.blocks + (int)kTileCost, item = (int)((at - base) / tile_cost);
+        const int from = (int)(at - base - (int64_t)item * tile_cost), upto = (int)min((int64_t)tile_cost, from + end - at);   // places of the tile's
+        const int tile = item / v.heads, head = item - tile * v.heads;
         const int col0 = tile * kCols, cols = w.n.count * p.group;
+        const int b0 = max(0, from - (int)kTileCost), count = max(0, upto - (int)kTileCost) - b0;
+        const int64_t slot = blockIdx.x * 2 + (at == begin ? 0 : 1);
+        at += upto - from;
+        if (count == 0 && (w.blocks > 0 || from > 0)) continue;   // (a tile with nothing to attend to: zeros, by whoever has its first place)
+
+        const int32_t *table = v.tables + row * v.max_pages;
+        const int block0 = w.lo + b0;
+        auto page_of = [&](int i) { return uniform(table[(block0 + i) >> (v.page_log2 - 5)]); };
+        u32x4 k[DC], x[DC];
+        uint32_t scales = 0;
+        auto base_of = [&](int page, int i) { return v.codes + v.block_at(page, head, (block0 + i) & (v.per_page - 1)); };
+        auto load_keys = [&](int page, int i) {
+            const uint8_t *from = base_of(page, i);
+#pragma unroll
+            for (int c = 0; c < DC; ++c) k[c] = load_codes(from + c * 1024 + lane * 16);
+        };
+        auto load_values = [&](int page, int i) {
+            const uint8_t *from = base_of(page, i) + 32 * v.width;
+#pragma unroll
+            for (int c = 0; c < DC; ++c) x[c] = load_codes(from + c * 1024 + lane * 16);
+        };
+        auto load_scales = [&](int page, int i) { return (uint32_t)*reinterpret_cast<const uint16_t *>(v.scales + v.scale_at(page, head, (block0 + i) & (v.per_page - 1))); };
+        auto there = [&](int page) { return page >= 0 && page < v.num_pages; };
+        int i = wave;
+        int page = i < count ? page_of(i) : -1, next = i + 4 < count ? page_of(i + 4) : -1;
+        if (there(page)) {
+            scales = load_scales(page, i);
+            load_keys(page, i);
+            load_values(page, i);
+        }
 
         uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
         stage_queries<DC, NS>(p, w, head, col0, kCols, staged);
@@ -108,32 +135,6 @@ __global__ __launch_bounds__(256, CT <= 2 && NS == 1 && DC <= 4 ? 2 : 1) void pa
 
         Running<DC, CT> run;
         run.clear();
-        const int32_t *table = v.tables + row * v.max_pages;
-        const int block0 = w.lo + b0;
-        auto page_of = [&](int i) { return table[(block0 + i) >> (v.page_log2 - 5)]; };
-        u32x4 k[DC], x[DC];
-        uint32_t scales = 0;
-        auto base_of = [&](int page, int i) { return v.codes + v.block_at(page, head, (block0 + i) & (v.per_page - 1)) + lane * 16; };
-        auto load_keys = [&](int page, int i) {
-            const uint8_t *from = base_of(page, i);
-#pragma unroll
-            for (int c = 0; c < DC; ++c) k[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
-        };
-        auto load_values = [&](int page, int i) {
-            const uint8_t *from = base_of(page, i) + 32 * v.width;
-#pragma unroll
-            for (int c = 0; c < DC; ++c) x[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
-        };
-        auto load_scales = [&](int page, int i) { return (uint32_t)*reinterpret_cast<const uint16_t *>(v.scales + v.scale_at(page, head, (block0 + i) & (v.per_page - 1))); };
-        auto there = [&](int page) { return page >= 0 && page < v.num_pages; };
-
-        int i = wave;
-        int page = i < count ? page_of(i) : -1, next = i + 4 < count ? page_of(i + 4) : -1;
-        if (there(page)) {
-            load_keys(page, i);
-            scales = load_scales(page, i);
-            load_values(page, i);
-        }
         for (; i < count; i += 4) {
             const int after = i + 8 < count ? page_of(i + 8) : -1;
             f32x4 s[CT][2];
@@ -169,8 +170,12 @@ __global__ __launch_bounds__(256, CT <= 2 && NS == 1 && DC <= 4 ? 2 : 1) void pa
             }
         }
         __syncthreads();
-        const bool whole = b0 == 0 && count == w.blocks;
-        const int64_t slot = blockIdx.x * 2 + (at == begin ? 0 : 1);
+        const bool whole = count == w.blocks;
+        if (threadIdx.x == 0 && !whole && b0 == 0) {
+            // the others: up to the share that the tile's last place lies in
+            const int64_t last_place = at - upto + tile_cost - 1;
+            p.split[blockIdx.x] = SplitTile{w.n.first, cols, col0, head, (int)(last_place / share - blockIdx.x) + 1, (int)slot};
+        }
         f32x4 *frags = reinterpret_cast<f32x4 *>(lds + 8 * kCols);   // [4][2 DC][64]
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
@@ -200,52 +205,74 @@ __global__ __launch_bounds__(256, CT <= 2 && NS == 1 && DC <= 4 ? 2 : 1) void pa
                 }
             __syncthreads();
         }
-        at += count;
     }
 }
 
-// A tile that several workgroups had a piece of: their sums under one reference.  Tiles of nobody's blocks get their zeros.
+// A tile that several workgroups had a piece of: their sums under one reference, the pieces over a workgroup's waves.  blockIdx.x: the worker of the first
+// piece, blockIdx.y: a fragment (16 columns x 16 elements).
 template <int DC, int CT>
 __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 {
     constexpr int kCols = 16 * CT, kFrags = CT * 2 * DC;
-    const PageView &v = p.v;
-    const int tile = blockIdx.x / v.heads, head = blockIdx.x - tile * v.heads;
-    if (tile >= p.tiles_before[v.rows]) return;
-    int row = 0;
-    for (int step = 1 << 14; step > 0; step >>= 1)
-        if (row + step < v.rows && p.tiles_before[row + step] <= tile) row += step;
-    const RowWork w = row_work(p, row, kCols);
-    const int in_row = tile - p.tiles_before[row];
-    const int64_t share = share_of(p.blocks_before[v.rows] * v.heads, p.workers);
-    const int64_t begin = p.blocks_before[row] * v.heads + ((int64_t)in_row * v.heads + head) * w.blocks;
-    const int64_t w0 = begin / share, w1 = (begin + w.blocks - 1) / share;
-    const int e = blockIdx.y * 256 + threadIdx.x;   // a fragment of a lane
-    const int lane = e & 63, frag = e >> 6;
-    if (frag >= kFrags || (w.blocks > 0 && w0 == w1)) return;
-    const int ct = frag / (2 * DC), in = 16 * ct + (lane & 15);
-    const int c = in_row * kCols + in;
-    if (c >= w.n.count * p.group) return;
+    const SplitTile t = p.split[blockIdx.x];
+    if (t.pieces == 0) return;
+    __shared__ f32x4 os[4][64];
+    __shared__ float ms[4][16], ls[4][16];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, frag = blockIdx.y, ct = frag / (2 * DC), in = 16 * ct + (lane & 15);
+    const bool there = t.col0 + in < t.columns;
     f32x4 o{0.f, 0.f, 0.f, 0.f};
-    if (w.blocks > 0) {
-        auto slot_of = [&](int64_t u) { return u * 2 + (u == w0 && begin != u * share ? 1 : 0); };
-        float m = -INFINITY, l = 0.f;
-        for (int64_t u = w0; u <= w1; ++u) m = fmaxf(m, p.part_ml[slot_of(u) * 2 * kCols + in]);
-        const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll 4
-        for (int64_t u = w0; u <= w1; ++u) {
-            const int64_t slot = slot_of(u);
-            const float a = __builtin_amdgcn_exp2f(p.part_ml[slot * 2 * kCols + in] - ref);
-            l += a * p.part_ml[(slot * 2 + 1) * kCols + in];
-            const f32x4 x = reinterpret_cast<const f32x4 *>(p.part_o)[(slot * kFrags + frag) * 64 + lane];
+    float m = -INFINITY, l = 0.f;
+    if (there) {
+        constexpr int kAhead = 4;
+        for (int u = wave; u < t.pieces; u += 4 * kAhead) {
+            f32x4 x[kAhead];
+            float pm[kAhead], pl[kAhead];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] += a * x[i];
+            for (int e = 0; e < kAhead; ++e) {
+                const int piece = u + 4 * e;
+                pm[e] = -INFINITY;
+                pl[e] = 0.f;
+                x[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (piece < t.pieces) {
+                    const int64_t slot = piece == 0 ? t.slot : 2 * ((int64_t)blockIdx.x + piece);
+                    pm[e] = p.part_ml[slot * 2 * kCols + in];
+                    pl[e] = p.part_ml[(slot * 2 + 1) * kCols + in];
+                    x[e] = reinterpret_cast<const f32x4 *>(p.part_o)[(slot * kFrags + frag) * 64 + lane];
+                }
+            }
+            float top = m;
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) top = fmaxf(top, pm[e]);
+            const float ref = top == -INFINITY ? 0.f : top, a = __builtin_amdgcn_exp2f(m - ref);
+            m = top;
+            l *= a;
+            o *= a;
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) {
+                const float b = __builtin_amdgcn_exp2f(pm[e] - ref);
+                l += b * pl[e];
+                o += x[e] * b;
+            }
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] *= inv;
     }
-    store_out(p, w.n.first, head, c, 16 * (frag - ct * 2 * DC) + 4 * (lane >> 4), o);
+    os[wave][lane] = o;
+    if (lane < 16) {
+        ms[wave][lane] = m;
+        ls[wave][lane] = l;
+    }
+    __syncthreads();
+    if (wave != 0 || !there) return;
+    const int c = lane & 15;
+    const float top = fmaxf(fmaxf(ms[0][c], ms[1][c]), fmaxf(ms[2][c], ms[3][c])), ref = top == -INFINITY ? 0.f : top;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+    l = 0.f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const float a = __builtin_amdgcn_exp2f(ms[u][c] - ref);
+        l += a * ls[u][c];
+        o += os[u][lane] * a;
+    }
+    store_out(p, t.first, t.head, t.col0 + in, 16 * (frag - ct * 2 * DC) + 4 * (lane >> 4), o * (l == 0.f ? 0.f : 1.f / l));
 }
 
 // Prompts: a workgroup's waves have 16 * CT columns each, one after another, and walk over the blocks that these see, each by itself: the codes of a
@@ -255,7 +282,7 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
 {
     constexpr int kWave = 16 * CT, kCols = 4 * kWave;
     const PageView &v = p.v;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15;
+    const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), col = lane & 15;
     extern __shared__ float lds[];
     // the tile: row and number within it
     int64_t *sums = reinterpret_cast<int64_t *>(lds);
@@ -279,9 +306,9 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
             b += n;
         }
     __syncthreads();
-    const int row = __builtin_amdgcn_readfirstlane(found[0]);
+    const int row = uniform((int)found[0]);
     const RowWork w = row_work(p, row, kCols);
-    const int cols = w.n.count * p.group, tile0 = __builtin_amdgcn_readfirstlane(found[1]) * kCols, col0 = tile0 + wave * kWave;
+    const int cols = w.n.count * p.group, tile0 = uniform((int)found[1]) * kCols, col0 = tile0 + wave * kWave;
     __syncthreads();
     uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
     stage_queries<DC, 1>(p, w, head, tile0, kCols, staged);
@@ -393,8 +420,8 @@ constexpr int kPromptCT = PROMPT_CT;
 struct AttendPlan {
     int ct, parts;
     bool prompt;
-    size_t o_bytes, ml_bytes, rows_bytes;
-    size_t bytes() const { return o_bytes + ml_bytes + 2 * rows_bytes; }
+    size_t o_bytes, ml_bytes, split_bytes;
+    size_t bytes() const { return o_bytes + ml_bytes + split_bytes; }
 };
 AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t most, int parts)
 {
@@ -407,23 +434,23 @@ AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t
     const size_t slots = 2 * kWorkers, kCols = 16 * pl.ct;
     pl.o_bytes = slots * kCols * page_width(p->head_dim) * 4;
     pl.ml_bytes = slots * 2 * kCols * 4;
-    pl.rows_bytes = up256(((size_t)p->rows + 1) * 8);
+    pl.split_bytes = up256(kWorkers * sizeof(SplitTile));
     return pl;
 }
 
 template <int DC, int CT, int NS>
-hipError_t launch_attend(const AttendArgs &a, int64_t tiles, hipStream_t s)
+hipError_t launch_attend(const AttendArgs &a, hipStream_t s)
 {
     constexpr int kFrags = CT * 2 * DC;
     constexpr size_t lds = std::max((size_t)NS * 16 * CT * kQueryRow<DC> * 2, (size_t)8 * 16 * CT * 4 + 4 * 2 * DC * 1024);
     static_assert(lds <= 65536 + 2048, "LDS");
     hipLaunchKernelGGL((pages_attend_kernel<DC, CT, NS>), dim3(a.workers), dim3(256), lds, s, a);
     if (hipGetLastError() != hipSuccess) return hipErrorLaunchFailure;
-    hipLaunchKernelGGL((pages_join_kernel<DC, CT>), dim3((unsigned)(tiles * a.v.heads), (kFrags * 64 + 255) / 256), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((pages_join_kernel<DC, CT>), dim3(a.workers, kFrags), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 template <int DC>
-hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, int64_t tiles, hipStream_t s)
+hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s)
 {
     if (pl.prompt) {
         constexpr int CT = DC <= 4 ? kPromptCT : 1;
@@ -431,10 +458,10 @@ hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, int64_t tiles
         hipLaunchKernelGGL((pages_prompt_kernel<DC, CT>), dim3((unsigned)(n * a.v.heads)), dim3(256), (size_t)64 * CT * kQueryRow<DC> * 2, s, a);
         return hipGetLastError();
     }
-    if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, tiles, s);
-    if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, tiles, s);
-    if (pl.ct == 2) return launch_attend<DC, 2, 1>(a, tiles, s);
-    if constexpr (DC <= 4) return launch_attend<DC, 4, 1>(a, tiles, s);
+    if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, s);
+    if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, s);
+    if (pl.ct == 2) return launch_attend<DC, 2, 1>(a, s);
+    if constexpr (DC <= 4) return launch_attend<DC, 4, 1>(a, s);
     return hipErrorInvalidValue;
 }
 
@@ -509,26 +536,22 @@ int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int
     a.scale_log2 = scale * 1.4426950408889634f;
     a.workers = kWorkers;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
-    a.blocks_before = reinterpret_cast<int64_t *>(ws);
-    ws += pl.rows_bytes;
-    a.tiles_before = reinterpret_cast<int32_t *>(ws);
-    ws += pl.rows_bytes;
+    a.split = reinterpret_cast<SplitTile *>(ws);
+    ws += pl.split_bytes;
     a.part_ml = reinterpret_cast<float *>(ws);
     ws += pl.ml_bytes;
     a.part_o = reinterpret_cast<float *>(ws);
-    const int64_t cols = 16 * pl.ct;
-    const int64_t tiles = std::min(tokens * group / cols + pages->rows, tokens * ((group + cols - 1) / cols));
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t err = hipErrorInvalidValue;
     switch (a.v.width / 32) {
-        case 1: err = launch_width<1>(a, pl, tiles, s); break;
-        case 2: err = launch_width<2>(a, pl, tiles, s); break;
-        case 3: err = launch_width<3>(a, pl, tiles, s); break;
-        case 4: err = launch_width<4>(a, pl, tiles, s); break;
-        case 5: err = launch_width<5>(a, pl, tiles, s); break;
-        case 6: err = launch_width<6>(a, pl, tiles, s); break;
-        case 7: err = launch_width<7>(a, pl, tiles, s); break;
-        case 8: err = launch_width<8>(a, pl, tiles, s); break;
+        case 1: err = launch_width<1>(a, pl, s); break;
+        case 2: err = launch_width<2>(a, pl, s); break;
+        case 3: err = launch_width<3>(a, pl, s); break;
+        case 4: err = launch_width<4>(a, pl, s); break;
+        case 5: err = launch_width<5>(a, pl, s); break;
+        case 6: err = launch_width<6>(a, pl, s); break;
+        case 7: err = launch_width<7>(a, pl, s); break;
+        case 8: err = launch_width<8>(a, pl, s); break;
     }
     return err == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
 }
