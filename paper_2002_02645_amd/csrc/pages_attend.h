@@ -105,6 +105,17 @@ __device__ __forceinline__ void parts_of(const float (&x)[8], bf16x8 (&out)[NS])
 
 // The running softmax of 16 * CT columns (a column: one head of one new token) in a wave.  A lane has column lane & 15 of each 16; weights and sums
 // belong to the lane's own tokens, outputs are elements 32 c + 16 u + 4 (lane >> 4) + i of o[.][2 c + u].
+__device__ __forceinline__ float largest(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));   // (fmaxf quiets its operands first)
+    return r;
+}
+template <int CT>
+__device__ __forceinline__ float largest_of(const f32x4 (&s)[CT][2], int ct)
+{
+    return largest(largest(s[ct][0][0], s[ct][0][1], s[ct][0][2]), largest(s[ct][0][3], s[ct][1][0], s[ct][1][1]), fmaxf(s[ct][1][2], s[ct][1][3]));
+}
 template <int DC, int CT>
 struct Running {
     f32x4 o[CT][2 * DC];
@@ -214,6 +225,31 @@ __device__ __forceinline__ TwoSums two_sums(int64_t a, int64_t b, int64_t *lds /
     return s;
 }
 
+// The blocks of a row for one head, by their number in the row.
+struct Blocks {
+    const int32_t *table;
+    const uint8_t *codes, *scales;          // of the head in page 0
+    uint32_t page_bytes, page_scales;       // from page to page
+    uint32_t block_bytes;
+    int log2, mask, num_pages;
+    __device__ __forceinline__ Blocks(const PageView &v, int row, int head)
+        : table(v.tables + row * v.max_pages), codes(v.codes + v.block_at(0, head, 0)), scales(v.scales + v.scale_at(0, head, 0)),
+          page_bytes((uint32_t)v.block_at(1, 0, 0)), page_scales((uint32_t)v.scale_at(1, 0, 0)), block_bytes(64 * v.width), log2(v.page_log2 - 5),
+          mask(v.per_page - 1), num_pages(v.num_pages)
+    {
+    }
+    __device__ __forceinline__ int page(int b) const { return uniform(table[b >> log2]); }
+    __device__ __forceinline__ bool there(int page) const { return (unsigned)page < (unsigned)num_pages; }
+    __device__ __forceinline__ const uint8_t *at(int page, int b) const
+    {
+        return codes + ((uint64_t)(uint32_t)page * page_bytes + (uint32_t)(b & mask) * block_bytes);
+    }
+    __device__ __forceinline__ uint32_t scale_bytes(int page, int b) const
+    {
+        return *reinterpret_cast<const uint16_t *>(scales + ((uint64_t)(uint32_t)page * page_scales + (uint32_t)(b & mask) * 2));
+    }
+};
+
 // Scores of the block's 32 tokens: token 16 t + 4 (lane >> 4) + i against the lane's column.
 template <int DC, int CT, int NS>
 __device__ __forceinline__ void scores_of(const u32x4 (&k)[DC], const bf16x8 (&q)[CT][NS][DC], f32x4 (&s)[CT][2])
@@ -232,26 +268,36 @@ __device__ __forceinline__ void scores_of(const u32x4 (&k)[DC], const bf16x8 (&q
         }
 }
 
-// Whether the token of weight e (0 .. 7: scores [e / 4][e % 4]) of the block is one that a column of this place sees.
-__device__ __forceinline__ bool sees(int first, int e, int place, int64_t window)
-{
-    const int token = first + 16 * (e >> 2) + 4 * ((threadIdx.x & 63) >> 4) + (e & 3);
-    return token <= place && (window <= 0 || (int64_t)token > place - window);
-}
+// What a lane's columns see: the places behind `before` up to `place` (below 0: a column of nobody).
 template <int CT>
-__device__ __forceinline__ void hide(f32x4 (&s)[CT][2], int first, const int (&place)[CT], int64_t window)
+struct Sight {
+    int place[CT], before[CT];
+    __device__ __forceinline__ void set(int ct, int at, int64_t window)
+    {
+        place[ct] = at;
+        before[ct] = window > 0 ? (int)(at - window) : -1;   // (a window has less than 2^31 places)
+    }
+    // the token of weight e (0 .. 7: scores [e / 4][e % 4]) of the block that begins with `first`
+    __device__ __forceinline__ bool sees(int ct, int first, int e) const
+    {
+        const int token = first + 16 * (e >> 2) + 4 * ((threadIdx.x & 63) >> 4) + (e & 3);
+        return token <= place[ct] && token > before[ct];
+    }
+};
+template <int CT>
+__device__ __forceinline__ void hide(f32x4 (&s)[CT][2], int first, const Sight<CT> &sight)
 {
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (!sees(first, e, place[ct], window)) s[ct][e >> 2][e & 3] = -INFINITY;
+            if (!sight.sees(ct, first, e)) s[ct][e >> 2][e & 3] = -INFINITY;
 }
 
 // Codes that are no number, in a block that some columns do not see all of (or that nobody wrote all of): they are taken out of the values, and the
 // outputs of the columns that see them become NaN.
 template <int DC, int CT>
-__device__ __forceinline__ void take_out_strange(f32x4 (&o)[CT][2 * DC], u32x4 (&v)[DC], int first, const int (&place)[CT], int64_t window)
+__device__ __forceinline__ void take_out_strange(f32x4 (&o)[CT][2 * DC], u32x4 (&v)[DC], int first, const Sight<CT> &sight)
 {
     uint32_t any = 0;
 #pragma unroll
@@ -263,7 +309,7 @@ __device__ __forceinline__ void take_out_strange(f32x4 (&o)[CT][2 * DC], u32x4 (
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) seen[ct][e] = sees(first, e, place[ct], window) ? (__bf16)1.f : (__bf16)0.f;
+        for (int e = 0; e < 8; ++e) seen[ct][e] = sight.sees(ct, first, e) ? (__bf16)1.f : (__bf16)0.f;
 #pragma unroll
     for (int c = 0; c < DC; ++c)
 #pragma unroll
@@ -283,18 +329,16 @@ __device__ __forceinline__ void take_out_strange(f32x4 (&o)[CT][2 * DC], u32x4 (
         }
 }
 
-// Scores to weights.  first: the block's first token, place: of the lane's columns' tokens (below 0: a column of nobody), edge: some column
-// does not see all of the block.
+// Scores to weights.  first: the block's first token, edge: some column does not see all of the block.
 template <int DC, int CT>
-__device__ __forceinline__ void weigh(Running<DC, CT> &r, f32x4 (&s)[CT][2], float scale, bool edge, int first, const int (&place)[CT], int64_t window)
+__device__ __forceinline__ void weigh(Running<DC, CT> &r, f32x4 (&s)[CT][2], float scale, bool edge, int first, const Sight<CT> &sight)
 {
-    if (edge) hide<CT>(s, first, place, window);
+    if (edge) hide<CT>(s, first, sight);
     float top[CT];
     bool follow = false;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        top[ct] = fmaxf(fmaxf(fmaxf(s[ct][0][0], s[ct][0][1]), fmaxf(s[ct][0][2], s[ct][0][3])),
-                        fmaxf(fmaxf(s[ct][1][0], s[ct][1][1]), fmaxf(s[ct][1][2], s[ct][1][3]))) * scale;
+        top[ct] = largest_of(s, ct) * scale;
         follow |= top[ct] > r.m[ct] + kSlack;
     }
     if (__any(follow)) {
@@ -327,7 +371,7 @@ __device__ __forceinline__ void weigh(Running<DC, CT> &r, f32x4 (&s)[CT][2], flo
 // Weights times values.
 template <int DC, int CT, int NS>
 __device__ __forceinline__ void add_values(Running<DC, CT> &r, u32x4 (&v)[DC], float scale, const f32x4 (&w)[CT][2], bool edge, int first,
-                                           const int (&place)[CT], int64_t window)
+                                           const Sight<CT> &sight)
 {
     bf16x8 f[CT][NS];
 #pragma unroll
@@ -335,7 +379,7 @@ __device__ __forceinline__ void add_values(Running<DC, CT> &r, u32x4 (&v)[DC], f
         const float x[8] = {w[ct][0][0], w[ct][0][1], w[ct][0][2], w[ct][0][3], w[ct][1][0], w[ct][1][1], w[ct][1][2], w[ct][1][3]};
         parts_of<NS>(x, f[ct]);
     }
-    if (edge) take_out_strange<DC, CT>(r.o, v, first, place, window);
+    if (edge) take_out_strange<DC, CT>(r.o, v, first, sight);
 #pragma unroll
     for (int c = 0; c < DC; ++c)
 #pragma unroll

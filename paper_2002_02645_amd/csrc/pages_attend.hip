@@ -93,28 +93,24 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
         at += upto - from;
         if (count == 0 && (w.blocks > 0 || from > 0)) continue;   // (a tile with nothing to attend to: zeros, by whoever has its first place)
 
-        const int32_t *table = v.tables + row * v.max_pages;
+        const Blocks blocks(v, row, head);
         const int block0 = w.lo + b0;
-        auto page_of = [&](int i) { return uniform(table[(block0 + i) >> (v.page_log2 - 5)]); };
         u32x4 k[DC], x[DC];
         uint32_t scales = 0;
-        auto base_of = [&](int page, int i) { return v.codes + v.block_at(page, head, (block0 + i) & (v.per_page - 1)); };
         auto load_keys = [&](int page, int i) {
-            const uint8_t *from = base_of(page, i);
+            const uint8_t *from = blocks.at(page, block0 + i);
 #pragma unroll
             for (int c = 0; c < DC; ++c) k[c] = load_codes(from + c * 1024 + lane * 16);
+            scales = blocks.scale_bytes(page, block0 + i);
         };
         auto load_values = [&](int page, int i) {
-            const uint8_t *from = base_of(page, i) + 32 * v.width;
+            const uint8_t *from = blocks.at(page, block0 + i) + blocks.block_bytes / 2;
 #pragma unroll
             for (int c = 0; c < DC; ++c) x[c] = load_codes(from + c * 1024 + lane * 16);
         };
-        auto load_scales = [&](int page, int i) { return (uint32_t)*reinterpret_cast<const uint16_t *>(v.scales + v.scale_at(page, head, (block0 + i) & (v.per_page - 1))); };
-        auto there = [&](int page) { return page >= 0 && page < v.num_pages; };
         int i = wave;
-        int page = i < count ? page_of(i) : -1, next = i + 4 < count ? page_of(i + 4) : -1;
-        if (there(page)) {
-            scales = load_scales(page, i);
+        int page = i < count ? blocks.page(block0 + i) : -1, next = i + 4 < count ? blocks.page(block0 + i + 4) : -1;
+        if (blocks.there(page)) {
             load_keys(page, i);
             load_values(page, i);
         }
@@ -123,33 +119,31 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
         stage_queries<DC, NS>(p, w, head, col0, kCols, staged);
         __syncthreads();
         bf16x8 q[CT][NS][DC];
-        int place[CT];
+        Sight<CT> sight;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             take_queries<DC, NS>(staged, kCols, 16 * ct, q[ct]);
             const int c = col0 + 16 * ct + col;
-            place[ct] = c < cols ? w.len - w.n.count + c / p.group : -1;
+            sight.set(ct, c < cols ? w.len - w.n.count + c / p.group : -1, p.window);
         }
         // places of the tile's tokens
         const int lowest = w.len - w.n.count + col0 / p.group, highest = w.len - w.n.count + (min(cols, col0 + kCols) - 1) / p.group;
 
         Running<DC, CT> run;
         run.clear();
+        const int unseen = p.window > 0 ? (int)(highest - p.window) : -1;   // the last place that some column does not see any more
         for (; i < count; i += 4) {
-            const int after = i + 8 < count ? page_of(i + 8) : -1;
+            const int after = i + 8 < count ? blocks.page(block0 + i + 8) : -1;
             f32x4 s[CT][2];
-            const bool here = there(page), more = there(next);
+            const bool here = blocks.there(page), more = blocks.there(next);
             const int first = (block0 + i) * kPageBlock;
-            const bool edge = first + kPageBlock - 1 > lowest || (p.window > 0 && (int64_t)first <= highest - p.window);
+            const bool edge = first + kPageBlock - 1 > lowest || first <= unseen;
             const float ks = p.scale_log2 * __uint_as_float((scales & 0xffu) << 23), vs = __uint_as_float((scales >> 8) << 23);
             if (here) scores_of<DC, CT, NS>(k, q, s);
-            if (more) {
-                load_keys(next, i + 4);
-                scales = load_scales(next, i + 4);
-            }
+            if (more) load_keys(next, i + 4);
             if (here) {
-                weigh<DC, CT>(run, s, ks, edge, first, place, p.window);
-                add_values<DC, CT, NS>(run, x, vs, s, edge, first, place, p.window);
+                weigh<DC, CT>(run, s, ks, edge, first, sight);
+                add_values<DC, CT, NS>(run, x, vs, s, edge, first, sight);
             }
             if (more) load_values(next, i + 4);
             page = next;
@@ -313,15 +307,16 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
     uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
     stage_queries<DC, 1>(p, w, head, tile0, kCols, staged);
     __syncthreads();
-    if (col0 >= cols) return;
     bf16x8 q[CT][1][DC];
-    int place[CT];
+    Sight<CT> sight;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         take_queries<DC, 1>(staged, kCols, wave * kWave + 16 * ct, q[ct]);
         const int c = col0 + 16 * ct + col;
-        place[ct] = c < cols ? w.len - w.n.count + c / p.group : -1;
+        sight.set(ct, c < cols ? w.len - w.n.count + c / p.group : -1, p.window);
     }
+    __syncthreads();   // (the queries are read)
+    if (col0 >= cols) return;
     const int lowest = w.len - w.n.count + col0 / p.group, highest = w.len - w.n.count + (min(cols, col0 + kWave) - 1) / p.group;
     const int seen = p.window > 0 ? (int)max((int64_t)0, lowest - p.window + 1) : 0;
     const int lo = seen / kPageBlock, hi = highest < 0 ? 0 : highest / kPageBlock + 1;
@@ -335,31 +330,51 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
 #pragma unroll
         for (int f = 0; f < 2 * DC; ++f) o[ct][f] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int32_t *table = v.tables + row * v.max_pages;
     bf16x8 ones;
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
+    const Blocks blocks(v, row, head);
+    const int unseen = p.window > 0 ? (int)(highest - p.window) : -1;   // the last place that some column does not see any more
+    const float scale_log2 = p.scale_log2;
+    u32x4 k[DC], x[DC];
+    uint32_t scales = 0;
+    // (a page that is not there is not looked at: block b of page 0 in its place)
+    auto load_keys = [&](int page, int b) {
+        page = blocks.there(page) ? page : 0;
+        const uint8_t *from = blocks.at(page, b);
+#pragma unroll
+        for (int c = 0; c < DC; ++c) k[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024 + lane * 16);
+        scales = blocks.scale_bytes(page, b);
+    };
+    auto load_values = [&](int page, int b) {
+        const uint8_t *from = blocks.at(blocks.there(page) ? page : 0, b) + blocks.block_bytes / 2;
+#pragma unroll
+        for (int c = 0; c < DC; ++c) x[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024 + lane * 16);
+    };
+    int page = lo < hi ? blocks.page(lo) : -1, next = lo + 1 < hi ? blocks.page(lo + 1) : -1;
+    load_keys(page, lo);
+    load_values(page, lo);
     for (int b = lo; b < hi; ++b) {
-        const int page = table[b >> (v.page_log2 - 5)];
-        if (page < 0 || page >= v.num_pages) continue;
-        const uint8_t *from = v.codes + v.block_at(page, head, b & (v.per_page - 1)) + lane * 16;
-        const uint32_t scales = *reinterpret_cast<const uint16_t *>(v.scales + v.scale_at(page, head, b & (v.per_page - 1)));
-        u32x4 k[DC], x[DC];
-#pragma unroll
-        for (int c = 0; c < DC; ++c) k[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024);
-#pragma unroll
-        for (int c = 0; c < DC; ++c) x[c] = *reinterpret_cast<const u32x4 *>(from + 32 * v.width + c * 1024);
+        const int now = page;
+        page = next;
+        next = b + 2 < hi ? blocks.page(b + 2) : -1;
         const int first = b * kPageBlock;
-        const bool edge = first + kPageBlock - 1 > lowest || (p.window > 0 && (int64_t)first <= highest - p.window);
-        const float ks = p.scale_log2 * __uint_as_float((scales & 0xffu) << 23), vs = __uint_as_float((scales >> 8) << 23);
+        const bool edge = first + kPageBlock - 1 > lowest || first <= unseen;
+        const float ks = scale_log2 * __uint_as_float((scales & 0xffu) << 23), vs = __uint_as_float((scales >> 8) << 23);
+        if (!blocks.there(now)) {
+            load_keys(page, b + 1);
+            load_values(page, b + 1);
+            continue;
+        }
         f32x4 s[CT][2];
         scores_of<DC, CT, 1>(k, q, s);
-        if (edge) hide(s, first, place, p.window);
+        load_keys(page, b + 1);
+        if (edge) hide(s, first, sight);
         bool follow = false;
         float top[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            top[ct] = fmaxf(fmaxf(fmaxf(s[ct][0][0], s[ct][0][1]), fmaxf(s[ct][0][2], s[ct][0][3])), fmaxf(fmaxf(s[ct][1][0], s[ct][1][1]), fmaxf(s[ct][1][2], s[ct][1][3]))) * ks;
+            top[ct] = largest_of(s, ct) * ks;
             follow |= top[ct] > m[ct] + kSlack;
         }
         if (__any(follow)) {
@@ -387,7 +402,7 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
                 for (int i = 0; i < 4; ++i) f[ct][4 * t + i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[ct][t][i], ks, -ref));
             sum[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, f[ct], sum[ct], 0, 0, 0);
         }
-        if (edge) take_out_strange<DC, CT>(o, x, first, place, p.window);
+        if (edge) take_out_strange<DC, CT>(o, x, first, sight);
 #pragma unroll
         for (int c = 0; c < DC; ++c)
 #pragma unroll
@@ -396,18 +411,22 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, f[ct], o[ct][2 * c + u], 0, 0, 0);
             }
+        load_values(page, b + 1);
     }
+    // outputs go through LDS, 16 columns of a wave at a time, to leave as whole rows
+    f32x4 *mine_out = reinterpret_cast<f32x4 *>(lds) + wave * (16 * (8 * DC + 1));   // [16][8 DC + 1]
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        const int c = col0 + 16 * ct + col;
-        if (c >= cols) continue;
         const float inv = sum[ct][0] == 0.f ? 0.f : 1.f / sum[ct][0];
 #pragma unroll
-        for (int f = 0; f < 2 * DC; ++f) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[ct][f][e] *= inv;
-            store_out(p, w.n.first, head, c, 16 * f + 4 * (lane >> 4), o[ct][f]);
+        for (int f = 0; f < 2 * DC; ++f) mine_out[col * (8 * DC + 1) + 4 * f + (lane >> 4)] = o[ct][f] * inv;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+        for (int e = lane; e < 16 * 8 * DC; e += 64) {
+            const int in = e / (8 * DC), d = e % (8 * DC), c = col0 + 16 * ct + in;
+            if (c < cols) store_out(p, w.n.first, head, c, 4 * d, mine_out[in * (8 * DC + 1) + d]);
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -455,7 +474,7 @@ hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s
     if (pl.prompt) {
         constexpr int CT = DC <= 4 ? kPromptCT : 1;
         const int64_t n = std::min(a.tokens * a.group / (64 * CT) + a.v.rows, a.tokens * ((a.group + 64 * CT - 1) / (64 * CT)));
-        hipLaunchKernelGGL((pages_prompt_kernel<DC, CT>), dim3((unsigned)(n * a.v.heads)), dim3(256), (size_t)64 * CT * kQueryRow<DC> * 2, s, a);
+        hipLaunchKernelGGL((pages_prompt_kernel<DC, CT>), dim3((unsigned)(n * a.v.heads)), dim3(256), std::max((size_t)64 * CT * kQueryRow<DC> * 2, (size_t)4 * 16 * (8 * DC + 1) * 16), s, a);
         return hipGetLastError();
     }
     if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, s);
