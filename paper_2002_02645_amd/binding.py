@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Dict, List, Optional, Sequence
 
 import torch
@@ -569,11 +570,16 @@ def freeze_reorder_states(states: Sequence[FreezeState], parents: torch.Tensor, 
                                        _on(stream)), "freeze_reorder_states")
 
 
+_HEADS = struct.Struct("QQiiqqqq")   # freeze_heads
+
+
 def _heads_of(t: torch.Tensor, heads: Optional[int] = None, dim: Optional[int] = None) -> tuple:
     """Elements from token to token and from head to head of a tensor [tokens, heads, dim] whose heads are dense."""
-    if not (t.dim() == 3 and t.dtype in (torch.float32, torch.bfloat16) and (heads is None or t.shape[1] == heads) and (dim is None or t.shape[2] == dim)):
+    if not (t.dim() == 3 and t.dtype in (torch.float32, torch.bfloat16)):
         raise _refused()
     tokens, n, d = t.shape
+    if not ((heads is None or n == heads) and (dim is None or d == dim)):
+        raise _refused()
     token, head, one = t.stride()
     if one != 1 and d > 1:
         raise _refused("the last dimension has to be dense")
@@ -607,20 +613,20 @@ def freeze_rotate_positions(tensors: Sequence[tuple], positions: torch.Tensor, f
     if not tensors:
         return
     tokens, _, dim = tensors[0][0].shape
-    arr = (FreezeHeads * len(tensors))()
-    for h, (src, dst) in zip(arr, tensors):
+    arr = b""   # freeze_heads, one after another
+    for src, dst in tensors:
         _here(src, dst)
-        if src.shape != dst.shape or src.dtype != dst.dtype or src.shape[0] != tokens or src.shape[2] != dim:
+        shape = src.shape
+        if shape != dst.shape or src.dtype != dst.dtype or shape[0] != tokens or shape[2] != dim:
             raise _refused()
-        h.src, h.dst, h.dtype, h.heads = src.data_ptr(), dst.data_ptr(), _DTYPES.get(src.dtype, -1), src.shape[1]
-        h.src_token_stride, h.src_head_stride = _heads_of(src)
-        h.dst_token_stride, h.dst_head_stride = _heads_of(dst)
+        arr += _HEADS.pack(src.data_ptr(), dst.data_ptr(), _DTYPES[src.dtype], shape[1], *_heads_of(src), *_heads_of(dst))
     _here(positions, frequencies)
     _numbers(positions, tokens)
-    if not (frequencies.dtype == torch.float64 and frequencies.is_contiguous() and 2 * frequencies.numel() <= dim):
+    pairs = frequencies.numel()
+    if not (frequencies.dtype == torch.float64 and frequencies.is_contiguous() and 2 * pairs <= dim):
         raise _refused()
-    _check(lib().freeze_rotate_positions(ctypes.addressof(arr), len(tensors), tokens, dim, positions.data_ptr(), frequencies.data_ptr(),
-                                         frequencies.numel(), int(interleaved), factor, int(inverse), _on(stream)), "freeze_rotate_positions")
+    _check(lib().freeze_rotate_positions(arr, len(tensors), tokens, dim, positions.data_ptr(), frequencies.data_ptr(), pairs, int(interleaved), factor,
+                                         int(inverse), _on(stream)), "freeze_rotate_positions")
 
 
 def freeze_pages_bytes(pool: FreezePagesPool) -> int:
@@ -1010,8 +1016,22 @@ class FreezeCache:
         outs = [torch.empty(t.shape, dtype=t.dtype, device=self.device) for t in xs] if out is None else [out] if one else list(out)
         if len(outs) != len(xs):
             raise _refused()
-        _here(*xs, *outs, holder=self)
-        freeze_rotate_positions(list(zip(xs, outs)), positions, frequencies, interleaved, factor, inverse)
+        dev = _here(*xs, *outs, positions, frequencies, holder=self)
+        if not xs:
+            return outs
+        tokens, _, dim = xs[0].shape
+        pairs, arr = frequencies.numel(), b""
+        for src, dst in zip(xs, outs):
+            shape = src.shape
+            if dst.shape != shape or src.dtype != dst.dtype or shape[0] != tokens or shape[2] != dim:
+                raise _refused()
+            strides = _heads_of(src)
+            arr += _HEADS.pack(src.data_ptr(), dst.data_ptr(), _DTYPES[src.dtype], shape[1], *strides, *(strides if dst is src else _heads_of(dst)))
+        _numbers(positions, tokens)
+        if not (frequencies.dtype == torch.float64 and frequencies.is_contiguous() and 2 * pairs <= dim):
+            raise _refused()
+        _check(lib().freeze_rotate_positions(arr, len(xs), tokens, dim, positions.data_ptr(), frequencies.data_ptr(), pairs, interleaved, factor, inverse,
+                                             torch._C._cuda_getCurrentRawStream(dev)), "freeze_rotate_positions")
         return outs[0] if one else outs
 
 
@@ -1038,14 +1058,19 @@ class FreezePages:
         self.pool.codes, self.pool.scales = self.codes.data_ptr(), self.scales.data_ptr()
         self.pool.refs, self.pool.tables, self.pool.lengths = self.refs.data_ptr(), self.tables.data_ptr(), self.lengths.data_ptr()
         self._scratch: Dict[tuple, torch.Tensor] = {}   # by device and stream
+        self._at = ctypes.addressof(self.pool)
+        self._book_bytes = freeze_pages_workspace_bytes(self.pool)
 
     _workspace = FreezeCache._workspace
 
     def reserve(self, add: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Room for add[row] more tokens of every row (None: one each), whose lengths grow; returns what each row was granted, [rows]."""
-        _here(add, holder=self)
-        granted = torch.empty(self.pool.rows, dtype=torch.int32, device=self.device)
-        freeze_pages_reserve(self.pool, add, granted, self._workspace(freeze_pages_workspace_bytes(self.pool)))
+        dev, pool = _here(add, holder=self), self.pool
+        _numbers(add, pool.rows)
+        granted = torch.empty(pool.rows, dtype=torch.int32, device=self.device)
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+        ws = self._workspace(self._book_bytes, (dev, stream))
+        _check(lib().freeze_pages_reserve(self._at, _at(add), granted.data_ptr(), ws.data_ptr(), ws.numel(), stream), "freeze_pages_reserve")
         return granted
 
     def fork(self, parents: torch.Tensor) -> None:
@@ -1062,28 +1087,41 @@ class FreezePages:
         """The pages in use move together at the front; returns how many they are, [1]."""
         _here(holder=self)
         used = torch.empty(1, dtype=torch.int32, device=self.device)
-        freeze_pages_compact(self.pool, used, self._workspace(freeze_pages_workspace_bytes(self.pool)))
+        freeze_pages_compact(self.pool, used, self._workspace(self._book_bytes))
         return used
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, starts: Optional[torch.Tensor] = None, most: int = 0,
                granted: Optional[torch.Tensor] = None) -> None:
         """The rows' newest tokens' keys and values [tokens, heads, head_dim] into a layer's pages: row r's are tokens starts[r] .. starts[r + 1] - 1
         (None: one token a row).  granted: as reserve returned it, rows that got another number of tokens are not written."""
-        _here(k, v, starts, granted, holder=self)
-        freeze_pages_append(self.pool, layer, k, v, starts, most, granted)
+        dev, pool = _here(k, v, starts, granted, holder=self), self.pool
+        if k.shape != v.shape or k.dtype != v.dtype:
+            raise _refused()
+        ks, vs = _heads_of(k, pool.heads, pool.head_dim), _heads_of(v, pool.heads, pool.head_dim)
+        _numbers(starts, pool.rows + 1)
+        _numbers(granted, pool.rows)
+        _check(lib().freeze_pages_append(self._at, layer, k.data_ptr(), *ks, v.data_ptr(), *vs, _DTYPES[k.dtype], k.shape[0], _at(starts), most, _at(granted),
+                                         torch._C._cuda_getCurrentRawStream(dev)), "freeze_pages_append")
 
     def attend(self, layer: int, q: torch.Tensor, starts: Optional[torch.Tensor] = None, most: int = 0, scale: Optional[float] = None, window: int = 0,
                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of the rows' newest tokens, q [tokens, heads * group, head_dim], over a layer's pages; scale: head_dim ** -0.5 by default.  Outputs of
         tokens of no row are left as they are (in a new tensor: whatever they were)."""
-        _here(q, starts, out, holder=self)
-        pool = self.pool
+        dev, pool = _here(q, starts, out, holder=self), self.pool
         if out is None:
             out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=self.device)
-        if q.dim() != 3 or q.shape[1] % pool.heads != 0 or q.shape[1] == 0:
+        dim = pool.head_dim
+        qs, os_ = _heads_of(q, None, dim), _heads_of(out, None, dim)
+        tokens, heads, _ = shape = q.shape
+        if shape != out.shape or heads == 0 or heads % pool.heads != 0:
             raise _refused()
-        nbytes = lib().freeze_pages_attend_workspace_bytes(ctypes.addressof(pool), q.shape[1] // pool.heads, q.shape[0], most, int(starts is not None))
+        _numbers(starts, pool.rows + 1)
+        L, group = lib(), heads // pool.heads
+        nbytes = L.freeze_pages_attend_workspace_bytes(self._at, group, tokens, most, starts is not None)
         if nbytes == 0:
             raise FreezeError(FREEZE_EINVAL, "freeze_pages_attend_workspace_bytes")
-        freeze_pages_attend(pool, layer, q, pool.head_dim ** -0.5 if scale is None else scale, out, self._workspace(nbytes), starts, most, window)
+        stream = torch._C._cuda_getCurrentRawStream(dev)
+        ws = self._workspace(nbytes, (dev, stream))
+        _check(L.freeze_pages_attend(self._at, layer, q.data_ptr(), _DTYPES[q.dtype], *qs, group, tokens, _at(starts), most, dim ** -0.5 if scale is None else scale,
+                                     window, out.data_ptr(), _DTYPES[out.dtype], *os_, ws.data_ptr(), ws.numel(), stream), "freeze_pages_attend")
         return out

@@ -35,6 +35,9 @@ __device__ __forceinline__ int64_t exclusive_sum(int64_t v, int64_t *total)
 struct PageCopy {
     int32_t src, dst, row, blocks;   // blocks: the filled ones
 };
+struct PageFill {
+    int32_t row, place, from, count; // places of a row's table, entries of the list of free pages
+};
 
 struct ReserveArgs {
     PageView v;
@@ -43,18 +46,28 @@ struct ReserveArgs {
     int32_t *need;       // [rows] scratch: pages wanted, the sign bit: one of them for a copy, kDenied: no place in the table
     int32_t *free;       // [num_pages] scratch
     PageCopy *copies;    // [rows] scratch
+    PageFill *fills;     // [rows] scratch
     int32_t *num_copies; // scratch
 };
 constexpr int32_t kDenied = 0x7fffffff;
 
-// One workgroup: which pages a row gets follows from all rows before it.  A sum over the rows' wants, then the free pages in order until there are as many.
-// 32 rows, 330 pages: bound by the latency of its dozen dependent steps.
+// One workgroup: which pages a row gets follows from all rows before it.  A sum over the rows' wants, then the free pages in order until there are as many, then a
+// wave for each row that gets several.  Bound by the latency of its dependent steps: RESERVE_FIGURES.
 __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(ReserveArgs p)
 {
     const PageView &v = p.v;
     const int per = (v.rows + kBookThreads - 1) / kBookThreads;
     const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
     const int64_t page_mask = ((int64_t)1 << v.page_log2) - 1;
+    constexpr int kEach = 16;
+    auto free_from = [&](int64_t first) {   // which of kEach pages are free
+        uint32_t is_free = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+            if (first + e < v.num_pages && v.refs[first + e] == 0) is_free |= 1u << e;
+        return is_free;
+    };
+    uint32_t is_free = free_from((int64_t)threadIdx.x * kEach);   // (on its way while the rows are looked at)
     int64_t mine = 0;
     for (int r = r0; r < r1; ++r) {
         const int64_t n = v.length_of(r), a = p.add ? max(p.add[r], 0) : 1;
@@ -73,16 +86,12 @@ __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(ReserveArgs
     int64_t wanted;
     int64_t at = exclusive_sum(mine, &wanted);
     // the first `wanted` free pages
-    __shared__ int copies;
-    if (threadIdx.x == 0) copies = 0;
-    constexpr int kEach = 16;
+    __shared__ int copies, fills;
+    if (threadIdx.x == 0) copies = fills = 0;
     int64_t found = 0;
     for (int64_t base = 0; base < v.num_pages && found < wanted; base += kBookThreads * kEach) {
         const int64_t first = base + (int64_t)threadIdx.x * kEach;
-        uint32_t is_free = 0;
-#pragma unroll
-        for (int e = 0; e < kEach; ++e)
-            if (first + e < v.num_pages && v.refs[first + e] == 0) is_free |= 1u << e;
+        if (base > 0) is_free = free_from(first);
         int64_t here;
         int64_t to = found + exclusive_sum(__popc(is_free), &here);
         for (; is_free != 0 && to < wanted; is_free &= is_free - 1) p.free[to++] = (int32_t)(first + __builtin_ctz(is_free));
@@ -109,9 +118,10 @@ __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(ReserveArgs
                 v.refs[dst] = 1;
                 p.copies[atomicAdd(&copies, 1)] = PageCopy{src, dst, r, (int)(((n & page_mask) + kPageBlock - 1) / kPageBlock)};
             }
-            for (; left > 0; --left) {
-                const int dst = p.free[from++];
-                table[j++] = dst;
+            if (left > 1) p.fills[atomicAdd(&fills, 1)] = PageFill{r, (int32_t)j, (int32_t)from, left};
+            if (left == 1) {
+                const int dst = p.free[from];
+                table[j] = dst;
                 v.refs[dst] = 1;
             }
             v.lengths[r] = (int)(n + a);
@@ -120,6 +130,15 @@ __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(ReserveArgs
     }
     __syncthreads();
     if (threadIdx.x == 0) *p.num_copies = copies;
+    for (int i = threadIdx.x >> 6; i < fills; i += kBookThreads / 64) {
+        const PageFill f = p.fills[i];
+        int32_t *table = v.tables + (int64_t)f.row * v.max_pages + f.place;
+        for (int e = threadIdx.x & 63; e < f.count; e += 64) {
+            const int dst = p.free[f.from + e];
+            table[e] = dst;
+            v.refs[dst] = 1;
+        }
+    }
 }
 
 // bytes (a multiple of 16) from src to dst by a workgroup
@@ -521,7 +540,7 @@ size_t freeze_pages_bytes(const freeze_pages *pages) { return page_sizes(pages) 
 size_t freeze_pages_workspace_bytes(const freeze_pages *pages)
 {
     if (!page_sizes(pages)) return 0;
-    return 3 * up256((size_t)pages->num_pages * 4) + up256((size_t)pages->rows * 4) + up256((size_t)pages->rows * sizeof(PageCopy)) + 256;
+    return 3 * up256((size_t)pages->num_pages * 4) + up256((size_t)pages->rows * 4) + 2 * up256((size_t)pages->rows * sizeof(PageCopy)) + 256;
 }
 
 int freeze_pages_reserve(const freeze_pages *pages, const int32_t *add, int32_t *out_granted, void *workspace, size_t workspace_bytes, void *stream)
@@ -553,6 +572,8 @@ int freeze_pages_reserve(const freeze_pages *pages, const int32_t *add, int32_t 
     ws += up256(rows * 4);
     a.copies = reinterpret_cast<PageCopy *>(ws);
     ws += up256(rows * sizeof(PageCopy));
+    a.fills = reinterpret_cast<PageFill *>(ws);
+    ws += up256(rows * sizeof(PageFill));
     a.free = reinterpret_cast<int32_t *>(ws);
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kBookThreads), 0, s, a);

@@ -31,7 +31,7 @@ def test_sizes():
     L = binding.lib()
     p = pool()
     assert binding.freeze_pages_bytes(p) == 2 * 100 * 3 * 2 * 2 * 32 * 64
-    assert binding.freeze_pages_workspace_bytes(p) == 3 * 512 + 256 + 256 + 256
+    assert binding.freeze_pages_workspace_bytes(p) == 3 * 512 + 256 + 2 * 256 + 256
     assert L.freeze_pages_bytes(None) == 0 and L.freeze_pages_workspace_bytes(None) == 0
     for kw in SIZES:
         assert binding.freeze_pages_bytes(pool(**kw)) == 0 and binding.freeze_pages_workspace_bytes(pool(**kw)) == 0, kw
