@@ -140,11 +140,11 @@ constexpr float kSlack = 8.f;
 // the last column and element.
 template <int DC>
 constexpr int kQueryRow = 32 * DC + 8;
-template <int DC, int NS>
+template <int DC, int NS, int THREADS>
 __device__ __forceinline__ void stage_queries(const AttendArgs &p, const RowWork &w, int head, int col0, int cols, uint16_t *to)
 {
     const int there = w.n.count * p.group;
-    for (int i = threadIdx.x; i < cols * (4 * DC); i += 256) {
+    for (int i = threadIdx.x; i < cols * (4 * DC); i += THREADS) {
         const int c = i / (4 * DC), d = i % (4 * DC) * 8, col = col0 + c;
         bf16x8 parts[NS];
         float x[8];
@@ -191,11 +191,13 @@ __device__ __forceinline__ void take_queries(const uint16_t *from, int cols, int
         for (int c = 0; c < DC; ++c) q[n][c] = *reinterpret_cast<const bf16x8 *>(from + (n * cols + c0 + (lane & 15)) * kQueryRow<DC> + 32 * c + 8 * (lane >> 4));
 }
 
-// Sums over the workgroup's threads before this one, of two numbers, and over all.
+// Sums over the workgroup's threads before this one, of two numbers, and over all.  WAVES: of the workgroup
+template <int WAVES>
 struct TwoSums {
     int64_t before[2], all[2];
 };
-__device__ __forceinline__ TwoSums two_sums(int64_t a, int64_t b, int64_t *lds /* [8] */)
+template <int WAVES>
+__device__ __forceinline__ TwoSums<WAVES> two_sums(int64_t a, int64_t b, int64_t *lds /* [2 WAVES] */)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int64_t x = a, y = b;
@@ -209,18 +211,18 @@ __device__ __forceinline__ TwoSums two_sums(int64_t a, int64_t b, int64_t *lds /
     }
     if (lane == 63) {
         lds[wave] = x;
-        lds[4 + wave] = y;
+        lds[WAVES + wave] = y;
     }
     __syncthreads();
-    TwoSums s{{x - a, y - b}, {0, 0}};
+    TwoSums<WAVES> s{{x - a, y - b}, {0, 0}};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         if (w < wave) {
             s.before[0] += lds[w];
-            s.before[1] += lds[4 + w];
+            s.before[1] += lds[WAVES + w];
         }
         s.all[0] += lds[w];
-        s.all[1] += lds[4 + w];
+        s.all[1] += lds[WAVES + w];
     }
     return s;
 }
@@ -238,7 +240,7 @@ struct Blocks {
           mask(v.per_page - 1), num_pages(v.num_pages)
     {
     }
-    __device__ __forceinline__ int page(int b) const { return uniform(table[b >> log2]); }
+    __device__ __forceinline__ int page(int b) const { return table[b >> log2]; }   // (a load: uniform() of it a step later, not to wait for it here)
     __device__ __forceinline__ bool there(int page) const { return (unsigned)page < (unsigned)num_pages; }
     __device__ __forceinline__ const uint8_t *at(int page, int b) const
     {
@@ -290,8 +292,10 @@ __device__ __forceinline__ void hide(f32x4 (&s)[CT][2], int first, const Sight<C
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
+        for (int e = 0; e < 8; ++e) {
             if (!sight.sees(ct, first, e)) s[ct][e >> 2][e & 3] = -INFINITY;
+            __builtin_amdgcn_sched_barrier(0);   // (one at a time: their masks together would push the loop's own scalars out of their registers)
+        }
 }
 
 // Codes that are no number, in a block that some columns do not see all of (or that nobody wrote all of): they are taken out of the values, and the
@@ -309,7 +313,10 @@ __device__ __forceinline__ void take_out_strange(f32x4 (&o)[CT][2 * DC], u32x4 (
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) seen[ct][e] = sight.sees(ct, first, e) ? (__bf16)1.f : (__bf16)0.f;
+        for (int e = 0; e < 8; ++e) {
+            seen[ct][e] = sight.sees(ct, first, e) ? (__bf16)1.f : (__bf16)0.f;
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
     for (int c = 0; c < DC; ++c)
 #pragma unroll
@@ -325,6 +332,7 @@ __device__ __forceinline__ void take_out_strange(f32x4 (&o)[CT][2 * DC], u32x4 (
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (count[i] > 0.f) o[ct][2 * c + u][i] = __uint_as_float(0x7fc00000u);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
 }

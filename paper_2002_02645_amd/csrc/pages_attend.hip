@@ -50,7 +50,7 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
         last = row_work(p, r, kCols);
         mine += cost_of(last);
     }
-    const TwoSums so_far = two_sums(mine, 0, found->sums);
+    const TwoSums<4> so_far = two_sums<4>(mine, 0, found->sums);
     const int64_t before = so_far.before[0], total = uniform(so_far.all[0]);
     int64_t share = (total + p.workers - 1) / p.workers;
     share = share < kLeastShare ? kLeastShare : share;
@@ -109,14 +109,14 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
             for (int c = 0; c < DC; ++c) x[c] = load_codes(from + c * 1024 + lane * 16);
         };
         int i = wave;
-        int page = i < count ? blocks.page(block0 + i) : -1, next = i + 4 < count ? blocks.page(block0 + i + 4) : -1;
+        int page = i < count ? uniform(blocks.page(block0 + i)) : -1, coming = i + 4 < count ? blocks.page(block0 + i + 4) : -1;
         if (blocks.there(page)) {
             load_keys(page, i);
             load_values(page, i);
         }
 
         uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
-        stage_queries<DC, NS>(p, w, head, col0, kCols, staged);
+        stage_queries<DC, NS, 256>(p, w, head, col0, kCols, staged);
         __syncthreads();
         bf16x8 q[CT][NS][DC];
         Sight<CT> sight;
@@ -133,7 +133,8 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
         run.clear();
         const int unseen = p.window > 0 ? (int)(highest - p.window) : -1;   // the last place that some column does not see any more
         for (; i < count; i += 4) {
-            const int after = i + 8 < count ? blocks.page(block0 + i + 8) : -1;
+            const int next = uniform(coming);   // (asked for a block ago)
+            coming = i + 8 < count ? blocks.page(block0 + i + 8) : -1;
             f32x4 s[CT][2];
             const bool here = blocks.there(page), more = blocks.there(next);
             const int first = (block0 + i) * kPageBlock;
@@ -147,7 +148,6 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
             }
             if (more) load_values(next, i + 4);
             page = next;
-            next = after;
         }
 
         // the four waves' results under one reference
@@ -271,6 +271,9 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 
 // Prompts: a workgroup's waves have 16 * CT columns each, one after another, and walk over the blocks that these see, each by itself: the codes of a
 // block come from memory once and from the caches for the other waves.  Nothing is split: there are tiles enough.  Later tiles of a row see more and go first.
+// Bound by what a SIMD issues: a block's 34 matrix instructions (544 cycles) come with 64 conversions and 70 other vector instructions, and two waves overlap them
+// in part only: PROMPT_FIGURES  Four columns of 16 a wave need 512 registers and copy half of them (643 us where two need 307); codes turned into bf16 once for a
+// workgroup of eight waves, in LDS, wait for what LDS hands out (283 us against 250).
 template <int DC, int CT>
 __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(AttendArgs p)
 {
@@ -285,7 +288,7 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
     const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
     int mine = 0;
     for (int r = r0; r < r1; ++r) mine += row_work(p, r, kCols).tiles;
-    const TwoSums so_far = two_sums(mine, 0, sums);
+    const TwoSums<4> so_far = two_sums<4>(mine, 0, sums);
     const int before = (int)so_far.before[0], total = (int)so_far.all[0];
     const int head = blockIdx.x % v.heads, tile = total - 1 - (int)(blockIdx.x / v.heads);
     if (tile < 0) return;
@@ -305,7 +308,7 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
     const int cols = w.n.count * p.group, tile0 = uniform((int)found[1]) * kCols, col0 = tile0 + wave * kWave;
     __syncthreads();
     uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
-    stage_queries<DC, 1>(p, w, head, tile0, kCols, staged);
+    stage_queries<DC, 1, 256>(p, w, head, tile0, kCols, staged);
     __syncthreads();
     bf16x8 q[CT][1][DC];
     Sight<CT> sight;
@@ -337,39 +340,42 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
     const int unseen = p.window > 0 ? (int)(highest - p.window) : -1;   // the last place that some column does not see any more
     const float scale_log2 = p.scale_log2;
     u32x4 k[DC], x[DC];
-    uint32_t scales = 0;
-    // (a page that is not there is not looked at: block b of page 0 in its place)
+    // a page that is not there: block b of page 0 in its place, none of whose tokens count
     auto load_keys = [&](int page, int b) {
-        page = blocks.there(page) ? page : 0;
-        const uint8_t *from = blocks.at(page, b);
+        const uint8_t *from = blocks.at(blocks.there(page) ? page : 0, b);
 #pragma unroll
         for (int c = 0; c < DC; ++c) k[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024 + lane * 16);
-        scales = blocks.scale_bytes(page, b);
     };
     auto load_values = [&](int page, int b) {
         const uint8_t *from = blocks.at(blocks.there(page) ? page : 0, b) + blocks.block_bytes / 2;
 #pragma unroll
         for (int c = 0; c < DC; ++c) x[c] = *reinterpret_cast<const u32x4 *>(from + c * 1024 + lane * 16);
     };
-    int page = lo < hi ? blocks.page(lo) : -1, next = lo + 1 < hi ? blocks.page(lo + 1) : -1;
+    auto scale_of = [&](int page, int b) { return blocks.scale_bytes(blocks.there(page) ? page : 0, b); };
+    // Block b's weights and its values' product, beside the scores of block b + 1 (`then`): matrix and vector instructions that do not wait for each other.
+    int page = lo < hi ? uniform(blocks.page(lo)) : -1, next = lo + 1 < hi ? uniform(blocks.page(lo + 1)) : -1, coming = lo + 2 < hi ? blocks.page(lo + 2) : -1;
+    uint32_t scales = scale_of(page, lo), scales_next = scale_of(next, lo + 1);
+    f32x4 s0[CT][2], s1[CT][2];
     load_keys(page, lo);
     load_values(page, lo);
-    for (int b = lo; b < hi; ++b) {
-        const int now = page;
-        page = next;
-        next = b + 2 < hi ? blocks.page(b + 2) : -1;
+    scores_of<DC, CT, 1>(k, q, s0);
+    load_keys(next, lo + 1);
+    auto step = [&](int b, f32x4 (&s)[CT][2], f32x4 (&then)[CT][2]) {
         const int first = b * kPageBlock;
-        const bool edge = first + kPageBlock - 1 > lowest || first <= unseen;
         const float ks = scale_log2 * __uint_as_float((scales & 0xffu) << 23), vs = __uint_as_float((scales >> 8) << 23);
-        if (!blocks.there(now)) {
-            load_keys(page, b + 1);
-            load_values(page, b + 1);
-            continue;
+        if (first + kPageBlock - 1 > lowest || first <= unseen) {
+            hide(s, first, sight);
+            take_out_strange<DC, CT>(o, x, first, sight);
         }
-        f32x4 s[CT][2];
-        scores_of<DC, CT, 1>(k, q, s);
-        load_keys(page, b + 1);
-        if (edge) hide(s, first, sight);
+        if (!blocks.there(page)) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) s[ct][0] = s[ct][1] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < DC; ++c) x[c] = u32x4{0, 0, 0, 0};
+        }
+        page = next;
+        next = uniform(coming);   // (asked for a block ago)
+        coming = b + 3 < hi ? blocks.page(b + 3) : -1;
         bool follow = false;
         float top[CT];
 #pragma unroll
@@ -384,14 +390,12 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
                 t = fmaxf(m[ct], fmaxf(t, __shfl_xor(t, 32)));
                 const float a = t == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - t);
                 m[ct] = t;
+                sum[ct] *= a;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) sum[ct][i] *= a;
-#pragma unroll
-                for (int f = 0; f < 2 * DC; ++f)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[ct][f][i] *= a;
+                for (int f = 0; f < 2 * DC; ++f) o[ct][f] *= a;
             }
         }
+        scores_of<DC, CT, 1>(k, q, then);
         bf16x8 f[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
@@ -400,9 +404,10 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) f[ct][4 * t + i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[ct][t][i], ks, -ref));
-            sum[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, f[ct], sum[ct], 0, 0, 0);
         }
-        if (edge) take_out_strange<DC, CT>(o, x, first, sight);
+        load_keys(next, b + 2);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) sum[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, f[ct], sum[ct], 0, 0, 0);   // (of the rounded weights)
 #pragma unroll
         for (int c = 0; c < DC; ++c)
 #pragma unroll
@@ -411,7 +416,13 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, f[ct], o[ct][2 * c + u], 0, 0, 0);
             }
+        scales = scales_next;
+        scales_next = scale_of(next, b + 2);
         load_values(page, b + 1);
+    };
+    for (int b = lo; b < hi; b += 2) {
+        step(b, s0, s1);
+        if (b + 1 < hi) step(b + 1, s1, s0);
     }
     // outputs go through LDS, 16 columns of a wave at a time, to leave as whole rows
     f32x4 *mine_out = reinterpret_cast<f32x4 *>(lds) + wave * (16 * (8 * DC + 1));   // [16][8 DC + 1]
@@ -432,10 +443,6 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
 
 // ---- host -------------------------------------------------------------------------------------------
 
-#ifndef PROMPT_CT
-#define PROMPT_CT 2
-#endif
-constexpr int kPromptCT = PROMPT_CT;
 struct AttendPlan {
     int ct, parts;
     bool prompt;
@@ -472,7 +479,7 @@ template <int DC>
 hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s)
 {
     if (pl.prompt) {
-        constexpr int CT = DC <= 4 ? kPromptCT : 1;
+        constexpr int CT = DC <= 4 ? 2 : 1;
         const int64_t n = std::min(a.tokens * a.group / (64 * CT) + a.v.rows, a.tokens * ((a.group + 64 * CT - 1) / (64 * CT)));
         hipLaunchKernelGGL((pages_prompt_kernel<DC, CT>), dim3((unsigned)(n * a.v.heads)), dim3(256), std::max((size_t)64 * CT * kQueryRow<DC> * 2, (size_t)4 * 16 * (8 * DC + 1) * 16), s, a);
         return hipGetLastError();
