@@ -452,11 +452,16 @@ struct AttendPlan {
 AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t most, int parts)
 {
     AttendPlan pl;
-    const int dc = page_width(p->head_dim) / 32;
     const int64_t cols = (most > 0 ? most : 1) * group;
     pl.parts = parts;
-    pl.ct = parts > 1 || cols <= 16 ? 1 : cols <= 32 || dc > 4 ? 2 : 4;
-    pl.prompt = parts == 1 && cols > 64 && tokens * group * p->heads >= (int64_t)256 * 128;
+    // Eight heads, groups of four, dim 128; new tokens a row behind 500 / 4,000 / 16,000 places, us:
+    //   16 columns a wave against 32: 16 rows of 5: 16 18 / 49 47 / 161 112; of 16: 24 32 / 98 70 / 337 192; 4 rows of 8: 15 16 / 21 27 / 50 45
+    //   (twice as much is read, but smaller tiles come and go faster: 4,096 columns and heads are where it turns);
+    //   the better of those against the prompts' kernel: 1 row of 256: 24 26 / 48 91 / 130 341; of 512: 39 32 / 125 96 / 357 354; 4 rows of 64: 24 23 / 53 97 / 136 357;
+    //   of 128: 34 25 / 121 98 / 383 355; 16 rows of 32: 36 23 / 123 101 / 393 464; of 64: 61 26 / 196 104 / 670 459 (16,384).
+    const int64_t all = tokens * group * p->heads;
+    pl.ct = parts > 1 || cols <= 16 || all < 4096 ? 1 : 2;
+    pl.prompt = parts == 1 && cols > 64 && all >= 16384;
     const size_t slots = 2 * kWorkers, kCols = 16 * pl.ct;
     pl.o_bytes = slots * kCols * page_width(p->head_dim) * 4;
     pl.ml_bytes = slots * 2 * kCols * 4;
@@ -486,9 +491,7 @@ hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s
     }
     if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, s);
     if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, s);
-    if (pl.ct == 2) return launch_attend<DC, 2, 1>(a, s);
-    if constexpr (DC <= 4) return launch_attend<DC, 4, 1>(a, s);
-    return hipErrorInvalidValue;
+    return launch_attend<DC, 2, 1>(a, s);
 }
 
 bool attend_sizes(const freeze_pages *p, int group, int64_t tokens, int64_t most)
