@@ -1012,25 +1012,27 @@ class FreezeCache:
         """Heads turned by their tokens' places (a tensor [tokens, heads, head_dim], or several that share positions; see rotary_frequencies).
         out: where they go, x itself for in place; None: new tensors."""
         one = isinstance(x, torch.Tensor)
-        xs = (x,) if one else tuple(x)
-        outs = [torch.empty(t.shape, dtype=t.dtype, device=self.device) for t in xs] if out is None else [out] if one else list(out)
+        xs = (x,) if one else x
+        outs = list(map(torch.empty_like, xs)) if out is None else [out] if one else list(out)
         if len(outs) != len(xs):
             raise _refused()
         dev = _here(*xs, *outs, positions, frequencies, holder=self)
-        if not xs:
+        if not outs:
             return outs
         tokens, _, dim = xs[0].shape
         pairs, arr = frequencies.numel(), b""
         for src, dst in zip(xs, outs):
-            shape = src.shape
-            if dst.shape != shape or src.dtype != dst.dtype or shape[0] != tokens or shape[2] != dim:
+            if out is not None and not (dst.shape == src.shape and dst.dtype == src.dtype):
                 raise _refused()
-            strides = _heads_of(src)
-            arr += _HEADS.pack(src.data_ptr(), dst.data_ptr(), _DTYPES[src.dtype], shape[1], *strides, *(strides if dst is src else _heads_of(dst)))
+            strides = _heads_of(src, None, dim)
+            if src.shape[0] != tokens:
+                raise _refused()
+            same = dst is src or (out is None and src.is_contiguous())
+            arr += _HEADS.pack(src.data_ptr(), dst.data_ptr(), _DTYPES[src.dtype], src.shape[1], *strides, *(strides if same else _heads_of(dst)))
         _numbers(positions, tokens)
         if not (frequencies.dtype == torch.float64 and frequencies.is_contiguous() and 2 * pairs <= dim):
             raise _refused()
-        _check(lib().freeze_rotate_positions(arr, len(xs), tokens, dim, positions.data_ptr(), frequencies.data_ptr(), pairs, interleaved, factor, inverse,
+        _check(lib().freeze_rotate_positions(arr, len(outs), tokens, dim, positions.data_ptr(), frequencies.data_ptr(), pairs, interleaved, factor, inverse,
                                              torch._C._cuda_getCurrentRawStream(dev)), "freeze_rotate_positions")
         return outs[0] if one else outs
 
@@ -1108,11 +1110,12 @@ class FreezePages:
         """Attention of the rows' newest tokens, q [tokens, heads * group, head_dim], over a layer's pages; scale: head_dim ** -0.5 by default.  Outputs of
         tokens of no row are left as they are (in a new tensor: whatever they were)."""
         dev, pool = _here(q, starts, out, holder=self), self.pool
-        if out is None:
-            out = torch.empty(q.shape, dtype=out_dtype or q.dtype, device=self.device)
         dim = pool.head_dim
-        qs, os_ = _heads_of(q, None, dim), _heads_of(out, None, dim)
+        qs = _heads_of(q, None, dim)
         tokens, heads, _ = shape = q.shape
+        if out is None:
+            out = torch.empty_like(q, dtype=out_dtype) if out_dtype else torch.empty_like(q)
+        os_ = _heads_of(out, None, dim)
         if shape != out.shape or heads == 0 or heads % pool.heads != 0:
             raise _refused()
         _numbers(starts, pool.rows + 1)

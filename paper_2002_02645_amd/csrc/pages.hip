@@ -69,6 +69,7 @@ __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(ReserveArgs
     };
     uint32_t is_free = free_from((int64_t)threadIdx.x * kEach);   // (on its way while the rows are looked at)
     int64_t mine = 0;
+    int32_t only = 0;   // of the one row of a thread
     for (int r = r0; r < r1; ++r) {
         const int64_t n = v.length_of(r), a = p.add ? max(p.add[r], 0) : 1;
         const int64_t had = (n + page_mask) >> v.page_log2, has = (n + a + page_mask) >> v.page_log2;
@@ -81,7 +82,8 @@ __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(ReserveArgs
             }
             mine += need & 0x7fffffff;
         }
-        p.need[r] = need;
+        if (per > 1) p.need[r] = need;
+        else only = need;
     }
     int64_t wanted;
     int64_t at = exclusive_sum(mine, &wanted);
@@ -99,7 +101,7 @@ __global__ __launch_bounds__(kBookThreads) void pages_reserve_kernel(ReserveArgs
     }
     __syncthreads();   // the list is written (by this workgroup), every count is read
     for (int r = r0; r < r1; ++r) {
-        const int32_t want = p.need[r];
+        const int32_t want = per > 1 ? p.need[r] : only;
         const int need = want & 0x7fffffff;
         const bool denied = want == kDenied;
         const bool ok = !denied && (need == 0 || at + need <= found);
@@ -174,23 +176,23 @@ __global__ __launch_bounds__(256) void pages_copy_kernel(PageView v, int layers,
 }
 
 // Tables in place: a workgroup takes some columns of all rows, so that every entry is read before one is written.
-__global__ __launch_bounds__(256) void pages_fork_kernel(PageView v, const int32_t *parents, int cols)
+__global__ __launch_bounds__(256) void pages_fork_kernel(PageView v, const int32_t *parents, int cols_log2)
 {
     extern __shared__ int32_t was[];   // [rows, cols]
-    const int64_t c0 = (int64_t)blockIdx.x * cols;
-    const int n = v.rows * cols;
+    const int cols = 1 << cols_log2, n = v.rows << cols_log2;
+    const int64_t c0 = (int64_t)blockIdx.x << cols_log2;
     for (int i = threadIdx.x; i < n; i += 256) {
-        const int64_t c = c0 + i % cols;
-        was[i] = c < v.max_pages ? v.tables[i / cols * v.max_pages + c] : -1;
+        const int64_t c = c0 + (i & (cols - 1));
+        was[i] = c < v.max_pages ? v.tables[(i >> cols_log2) * v.max_pages + c] : -1;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += 256) {
-        const int64_t c = c0 + i % cols;
-        const int parent = parents[i / cols];
+        const int row = i >> cols_log2, parent = parents[row];
+        const int64_t c = c0 + (i & (cols - 1));
         if (c >= v.max_pages || parent < 0 || parent >= v.rows) continue;
-        const int old = was[i], now = was[parent * cols + i % cols];
+        const int old = was[i], now = was[(parent << cols_log2) + (i & (cols - 1))];
         if (old == now) continue;
-        v.tables[i / cols * v.max_pages + c] = now;
+        v.tables[row * v.max_pages + c] = now;
         if (old >= 0 && old < v.num_pages) atomicSub(&v.refs[old], 1);
         if (now >= 0 && now < v.num_pages) atomicAdd(&v.refs[now], 1);
     }
@@ -360,7 +362,9 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
     // the row of this workgroup's block
     const int groups = (2 * v.heads + 3) / 4;
     const int which = (int)(blockIdx.x / groups), unit = (int)(blockIdx.x - (unsigned)which * groups) * 4 + wave;
-    {
+    if (!p.starts) {   // one token a row: a block each
+        if (append_row(p, which).blocks == 0) return;
+    } else {
         const int per = (v.rows + 255) / 256;
         const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
         int mine = 0;
@@ -393,9 +397,9 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
         __syncthreads();
     }
     if (unit >= 2 * v.heads) return;
-    const int row = __builtin_amdgcn_readfirstlane(found[0]);
+    const int row = p.starts ? __builtin_amdgcn_readfirstlane(found[0]) : which;
     const AppendRow w = append_row(p, row);
-    const int block = w.first / kPageBlock + __builtin_amdgcn_readfirstlane(found[1]), start = block * kPageBlock;
+    const int block = w.first / kPageBlock + (p.starts ? __builtin_amdgcn_readfirstlane(found[1]) : 0), start = block * kPageBlock;
     const int kv = unit & 1, head = unit >> 1;
     const int page = v.tables[row * v.max_pages + (start >> v.page_log2)];
     const int kept = w.first - start, end = w.len - start;   // tokens of the block: those below `kept` are there already, those below `end` are new
@@ -444,11 +448,11 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
             }
         }
     }
-    if (page < 0 || page >= v.num_pages || v.refs[page] > 1) return;
-    const int in_page = block & (v.per_page - 1);
+    if (page < 0 || page >= v.num_pages) return;
+    const int in_page = block & (v.per_page - 1), holders = v.refs[page];
     uint8_t *to = v.codes + v.block_at(page, head, in_page) + kv * (32 * v.width);
     uint8_t *scale = v.scales + v.scale_at(page, head, in_page) + kv;
-    const int old = kept > 0 ? (int)*scale - 127 : -126;
+    int old = (int)*scale - 127;
     // where this lane's four words of a chunk go: two times eight bytes
     const int at0 = kv ? (t >> 2) * 256 + ((8 * g + (t & 3)) & 15) * 16 + (g >> 1) * 8 : lane * 16, at1 = at0 + (kv ? 64 : 8);
     u32x2 was[DC][2];
@@ -459,6 +463,9 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
             was[c][1] = *reinterpret_cast<const u32x2 *>(to + c * 1024 + at1);
         }
     }
+    asm volatile("" : "+v"(old));   // (all on their way before the first is waited for)
+    if (holders > 1) return;
+    if (kept <= 0) old = -126;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) amax = max(amax, (uint32_t)__shfl_xor((int)amax, o));
     int ex = (int)(amax >> 23) - 135 + ((amax & 0x7fffffu) > 0x600000u ? 1 : 0);
@@ -593,11 +600,11 @@ int freeze_pages_fork(const freeze_pages *pages, const int32_t *parents, void *s
     const uintptr_t b = reinterpret_cast<uintptr_t>(parents);
     e[n++] = Extent{b, b + (size_t)pages->rows * 4, false};
     if (written_twice(e, n)) return FREEZE_EINVAL;
-    int cols = 64;   // of a workgroup: 64 KB of entries
-    while (cols > 1 && cols * pages->rows > 16384) cols /= 2;
-    const int64_t groups = (pages->max_pages + cols - 1) / cols;
-    const size_t lds = (size_t)pages->rows * cols * 4;
-    hipLaunchKernelGGL(pages_fork_kernel, dim3((unsigned)groups), dim3(256), lds, static_cast<hipStream_t>(stream), page_view(pages, 0), parents, cols);
+    int log2 = 6;   // of a workgroup's columns: an entry or some a thread, several columns as long as 64 KB hold them
+    while (log2 > 0 && pages->rows << log2 > (log2 > 2 ? 512 : 16384)) --log2;
+    const int64_t groups = (pages->max_pages + (1 << log2) - 1) >> log2;
+    const size_t lds = (size_t)pages->rows << (log2 + 2);
+    hipLaunchKernelGGL(pages_fork_kernel, dim3((unsigned)groups), dim3(256), lds, static_cast<hipStream_t>(stream), page_view(pages, 0), parents, log2);
     return hipGetLastError() == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
 }
 
@@ -640,7 +647,7 @@ int freeze_pages_compact(const freeze_pages *pages, int32_t *out_used, void *wor
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(kBookThreads), 0, s, a);
     if (hipGetLastError() != hipSuccess) return FREEZE_EHIP;
-    hipLaunchKernelGGL(pages_move_kernel, dim3(2048), dim3(256), 0, s, a, pages->layers, layer_bytes(page_code_bytes(pages), pages),
+    hipLaunchKernelGGL(pages_move_kernel, dim3(8192), dim3(256), 0, s, a, pages->layers, layer_bytes(page_code_bytes(pages), pages),
                        layer_bytes(page_scale_bytes(pages), pages));
     return hipGetLastError() == hipSuccess ? FREEZE_OK : FREEZE_EHIP;
 }
@@ -691,7 +698,7 @@ int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int
         a.vec &= reinterpret_cast<uintptr_t>(both[i]) % 16 == 0 && a.token_stride[i] % 8 == 0 && a.head_stride[i] % 8 == 0;
     }
     // a row's tokens lie in one block more than they fill, or two
-    const int64_t blocks = std::min(tokens / kPageBlock + 2 * pages->rows, tokens);
+    const int64_t blocks = starts ? std::min(tokens / kPageBlock + 2 * pages->rows, tokens) : tokens;
     const dim3 grid((unsigned)(blocks * ((2 * pages->heads + 3) / 4)));
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t err = dtype == FREEZE_F32 ? launch_append<float>(a, grid, s) : launch_append<uint16_t>(a, grid, s);

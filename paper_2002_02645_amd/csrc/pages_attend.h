@@ -376,16 +376,16 @@ __device__ __forceinline__ void weigh(Running<DC, CT> &r, f32x4 (&s)[CT][2], flo
     }
 }
 
-// Weights times values.
-template <int DC, int CT, int NS>
+// Weights times values, the weights in NP parts.
+template <int DC, int CT, int NP>
 __device__ __forceinline__ void add_values(Running<DC, CT> &r, u32x4 (&v)[DC], float scale, const f32x4 (&w)[CT][2], bool edge, int first,
                                            const Sight<CT> &sight)
 {
-    bf16x8 f[CT][NS];
+    bf16x8 f[CT][NP];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         const float x[8] = {w[ct][0][0], w[ct][0][1], w[ct][0][2], w[ct][0][3], w[ct][1][0], w[ct][1][1], w[ct][1][2], w[ct][1][3]};
-        parts_of<NS>(x, f[ct]);
+        parts_of<NP>(x, f[ct]);
     }
     if (edge) take_out_strange<DC, CT>(r.o, v, first, sight);
 #pragma unroll
@@ -396,7 +396,7 @@ __device__ __forceinline__ void add_values(Running<DC, CT> &r, u32x4 (&v)[DC], f
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int n = 0; n < NS; ++n) r.o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[ct][n], r.o[ct][2 * c + u], 0, 0, 0);
+                for (int n = 0; n < NP; ++n) r.o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, f[ct][n], r.o[ct][2 * c + u], 0, 0, 0);
         }
 }
 
