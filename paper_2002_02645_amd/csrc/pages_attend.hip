@@ -367,15 +367,15 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
     auto step = [&](int b, f32x4 (&s)[CT][2], f32x4 (&then)[CT][2]) {
         const int first = b * kPageBlock;
         const float ks = scale_log2 * __uint_as_float((scales & 0xffu) << 23), vs = __uint_as_float((scales >> 8) << 23);
-        if (first + kPageBlock - 1 > lowest || first <= unseen) {
-            hide(s, first, sight);
-            take_out_strange<DC, CT>(o, x, first, sight);
-        }
         if (!blocks.there(page)) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) s[ct][0] = s[ct][1] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
             for (int c = 0; c < DC; ++c) x[c] = u32x4{0, 0, 0, 0};
+        }
+        if (first + kPageBlock - 1 > lowest || first <= unseen) {
+            hide(s, first, sight);
+            take_out_strange<DC, CT>(o, x, first, sight);
         }
         page = next;
         next = uniform(coming);   // (asked for a block ago)
