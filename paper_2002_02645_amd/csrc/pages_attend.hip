@@ -143,7 +143,7 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
             const bool here = blocks.there(page), more = blocks.there(next);
             const int first = (block0 + i) * kPageBlock;
             const bool edge = first + kPageBlock - 1 > lowest || first <= unseen;
-            const float ks = p.scale_log2 * __uint_as_float((scales & 0xffu) << 23), vs = __uint_as_float((scales >> 8) << 23);
+            const float ks = score_factor(p.scale_log2, scales), vs = value_factor(scales);
             if (here) scores_of<DC, CT, NS>(k, q, s);
             if (more) load_keys(next, i + 4);
             if (here) {
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
     load_keys(next, lo + 1);
     auto step = [&](int b, f32x4 (&s)[CT][2], f32x4 (&then)[CT][2]) {
         const int first = b * kPageBlock;
-        const float ks = scale_log2 * __uint_as_float((scales & 0xffu) << 23), vs = __uint_as_float((scales >> 8) << 23);
+        const float ks = score_factor(scale_log2, scales), vs = value_factor(scales);
         if (!blocks.there(page)) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) s[ct][0] = s[ct][1] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};

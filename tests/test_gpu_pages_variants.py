@@ -160,6 +160,27 @@ def test_rising_scores():
     check(p, pool, [64], torch.bfloat16, 1)
 
 
+@pytest.mark.parametrize("new", [WIDE, PROMPTS, [1] * 8], ids=["wide", "prompts", "one"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_keys_of_zeros_and_tiny_scales(new, dtype):
+    """Scores that are all as good as 0: every visible token has the same weight, hidden ones none."""
+    lengths = [n + 40 for n in new]
+    p, pool = pair(1, 120, len(new), 12, HEADS, 64, 32)
+    p.reserve(ints(lengths))
+    pool.reserve(lengths)
+    g = torch.Generator("cuda").manual_seed(4)
+    v = torch.randn(sum(lengths), HEADS, 64, device="cuda", generator=g)
+    first = ints([sum(lengths[:r]) for r in range(len(new) + 1)])
+    q = torch.randn(sum(new), HEADS * GROUP, 64, device="cuda", generator=g).to(dtype)
+    starts = ints([sum(new[:r]) for r in range(len(new) + 1)])
+    for k, scale in ((torch.zeros_like(v), 0.125), (torch.zeros_like(v), 1e-30), (torch.full_like(v, 1e-38), 1.0), (v, 1e-37), (v * 1e-30, 1e-20)):
+        p.append(0, k, v, first)
+        pool.append(0, k.cpu(), v.cpu(), lengths)
+        want, size = exact(pool, q.cpu(), new, 1e-200, 0)   # (0 times a hidden token's -inf would be no number)
+        off = (p.attend(0, q, starts, scale=scale, out_dtype=torch.float32).double().cpu() - want).abs()
+        assert bool((off <= size * (2.0 ** -8 if dtype == torch.bfloat16 else 2.0 ** -18)).all()), scale
+
+
 def test_same_results_every_time():
     p, pool = pair(1, 300, 6, 45, HEADS, 128, 64)
     p.reserve(ints([2000, 300, 64, 0, 900, 1200]))
