@@ -405,8 +405,13 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
     const int kept = w.first - start, end = w.len - start;   // tokens of the block: those below `kept` are there already, those below `end` are new
 
     const T *x = static_cast<const T *>(p.x[kv]) + head * p.head_stride[kv];
-    float y[DC][2][8];
-    uint32_t amax = 0;
+    // a lane's values as they came: bf16 in pairs, fp32
+    constexpr int kWords = sizeof(T) == 2 ? 1 : 2;
+    u32x4 y[DC][2][kWords];
+    auto value = [&](int c, int h, int e) {   // (constants after unrolling)
+        if constexpr (sizeof(T) == 2) return __uint_as_float(e & 1 ? y[c][h][0][e / 2] & 0xffff0000u : y[c][h][0][e / 2] << 16);
+        else return __uint_as_float(y[c][h][e / 4][e & 3]);
+    };
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int token = 16 * h + t;
@@ -415,38 +420,41 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
 #pragma unroll
         for (int c = 0; c < DC; ++c) {
             const int d = 32 * c + 8 * g;
+#pragma unroll
+            for (int u = 0; u < kWords; ++u) y[c][h][u] = u32x4{0, 0, 0, 0};
             if (p.vec) {
-                const bool in = there && d < v.head_dim;
-                if constexpr (sizeof(T) == 2) {
-                    u32x4 u{0, 0, 0, 0};
-                    if (in) u = *reinterpret_cast<const u32x4 *>(src + 32 * c);
+                if (there && d < v.head_dim)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[c][h][e] = __uint_as_float(e & 1 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
-                } else {
-                    u32x4 u{0, 0, 0, 0}, u2{0, 0, 0, 0};
-                    if (in) {
-                        u = reinterpret_cast<const u32x4 *>(src + 32 * c)[0];
-                        u2 = reinterpret_cast<const u32x4 *>(src + 32 * c)[1];
-                    }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) y[c][h][e] = __uint_as_float(e < 4 ? u[e & 3] : u2[e & 3]);
-                }
+                    for (int u = 0; u < kWords; ++u) y[c][h][u] = reinterpret_cast<const u32x4 *>(src + 32 * c)[u];
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    y[c][h][e] = 0.f;
+                for (int e = 0; e < 8; ++e)
                     if (there && d + e < v.head_dim) {
-                        if constexpr (sizeof(T) == 2) y[c][h][e] = __uint_as_float((uint32_t)src[32 * c + e] << 16);
-                        else y[c][h][e] = src[32 * c + e];
+                        if constexpr (sizeof(T) == 2) y[c][h][0][e / 2] |= (uint32_t)src[32 * c + e] << (16 * (e & 1));
+                        else y[c][h][e / 4][e & 3] = __float_as_uint(src[32 * c + e]);
                     }
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t bits = __float_as_uint(y[c][h][e]) & 0x7fffffffu;
-                if (bits < 0x7f800000u && bits > amax) amax = bits;
             }
         }
+    }
+    // the largest magnitude, of the finite ones where some are not
+    uint32_t amax = 0;
+#pragma unroll
+    for (int c = 0; c < DC; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(value(c, h, e)) & 0x7fffffffu);
+    if (__any(amax >= 0x7f800000u)) {
+        amax = 0;
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t bits = __float_as_uint(value(c, h, e)) & 0x7fffffffu;
+                    if (bits < 0x7f800000u && bits > amax) amax = bits;
+                }
     }
     if (page < 0 || page >= v.num_pages) return;
     const int in_page = block & (v.per_page - 1), holders = v.refs[page];
@@ -496,7 +504,7 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
             for (int q = 0; q < 2; ++q) {
                 float f[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = code_of(y[c][h][4 * q + e], inv);
+                for (int e = 0; e < 4; ++e) f[e] = code_of(value(c, h, 4 * q + e), inv);
                 code[h][q] = four_codes(f[0], f[1], f[2], f[3]);
                 if (kv) code[h][q] = across_four(code[h][q]);
             }
