@@ -318,10 +318,10 @@ __device__ __forceinline__ AppendRow append_row(const AppendArgs &p, int row)
     return w;
 }
 
-// The code of a finite value within the block's range; what is not finite: no number.
-__device__ __forceinline__ float code_of(float x, float inv)
+// A value in units of its block's power of two, and no number for one that is not finite.
+__device__ __forceinline__ float code_of(float x)
 {
-    return (__float_as_uint(x) & 0x7fffffffu) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : x * inv;
+    return (__float_as_uint(x) & 0x7fffffffu) >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : x;
 }
 __device__ __forceinline__ uint32_t four_codes(float a, float b, float c, float d)
 {
@@ -335,6 +335,8 @@ __device__ __forceinline__ uint32_t scaled_codes(uint32_t w, float down)
     return four_codes(__builtin_amdgcn_cvt_f32_fp8(w, 0) * down, __builtin_amdgcn_cvt_f32_fp8(w, 1) * down, __builtin_amdgcn_cvt_f32_fp8(w, 2) * down,
                       __builtin_amdgcn_cvt_f32_fp8(w, 3) * down);
 }
+
+typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
 
 // Byte b of lane i of each four lanes becomes byte i of lane b: rows of four tokens to columns.
 __device__ __forceinline__ uint32_t across_four(uint32_t w)
@@ -438,13 +440,25 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
     }
     // the largest magnitude, of the finite ones where some are not
     uint32_t amax = 0;
+    if constexpr (sizeof(T) == 2) {
+        u16x2 most{0, 0};   // two values at a time
 #pragma unroll
-    for (int c = 0; c < DC; ++c)
+        for (int c = 0; c < DC; ++c)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(value(c, h, e)) & 0x7fffffffu);
-    if (__any(amax >= 0x7f800000u)) {
+                for (int e = 0; e < 4; ++e) most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, y[c][h][0][e] & 0x7fff7fffu));
+        amax = (uint32_t)max(most[0], most[1]) << 16;
+    } else {
+#pragma unroll
+        for (int c = 0; c < DC; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(value(c, h, e)) & 0x7fffffffu);
+    }
+    const bool strange = __any(amax >= 0x7f800000u);
+    if (strange) {
         amax = 0;
 #pragma unroll
         for (int c = 0; c < DC; ++c)
@@ -504,7 +518,11 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
             for (int q = 0; q < 2; ++q) {
                 float f[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) f[e] = code_of(value(c, h, 4 * q + e), inv);
+                for (int e = 0; e < 4; ++e) f[e] = value(c, h, 4 * q + e) * inv;
+                if (strange) {   // (the product is no number either, or infinite)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) f[e] = code_of(f[e]);
+                }
                 code[h][q] = four_codes(f[0], f[1], f[2], f[3]);
                 if (kv) code[h][q] = across_four(code[h][q]);
             }
