@@ -453,7 +453,7 @@ int freeze_rotate_positions(const freeze_heads *heads, int num, int64_t tokens, 
  * a row is a table of pages and a length, a page holds page_tokens tokens' keys and values of every layer, and rows that went on from one parent name the
  * same pages.  Everything is device memory that the calls keep up themselves, without a word to the host: they may be captured into graphs.
  *   codes    [layers, num_pages, heads, page_tokens / 32, 2 (keys, values), 32 * W], W = head_dim rounded up to 32; 16-byte aligned;
- *   scales   [layers, num_pages, heads, page_tokens / 32, 2]: a block of 32 tokens of a head has an exponent E for its keys and one for its
+ *   scales   [layers, num_pages, heads, page_tokens / 32, 2]; 2-byte aligned: a block of 32 tokens of a head has an exponent E for its keys and one for its
  *            values, the smallest E >= -126 with max|x| <= 448 * 2^E over the finite values (it never falls while the block fills up); the byte is E + 127, codes are
  *            x * 2^-E rounded to nearest even (FREEZE_E4M3).  Where E grows, the codes that are there are scaled down and rounded again.  An
  *            infinity or a NaN has a code that is no number.
@@ -473,7 +473,7 @@ typedef struct freeze_pages {
     int64_t num_pages, rows, max_pages;
     int32_t layers, heads, head_dim, page_tokens;
 } freeze_pages;
-/* Bytes of codes (scales: one for every 16 * W of them); 0 where a size is out of range.  Pointers are not looked at. */
+/* Bytes of codes (scales: one byte for every 32 * W of them); 0 where a size is out of range.  Pointers are not looked at. */
 size_t freeze_pages_bytes(const freeze_pages *pages);
 
 /*

@@ -191,3 +191,35 @@ def test_refused_by_the_holder():
         with pytest.raises(binding.FreezeError):
             call()
     cache.close()
+
+
+def test_far_pages():
+    """A layer of more than 4 GiB whose last pages are in use: the same codes and outputs as in a small pool, through appending, copies, attention of each kind and a
+    compaction that brings the pages to the front."""
+    sizes = dict(rows=3, max_pages=8, heads=8, head_dim=128, page_tokens=64)
+    far, near = binding.FreezePages(1, 40000, **sizes), binding.FreezePages(1, 40, **sizes)
+    assert far.codes.numel() > 4 << 30
+    far.refs[:39970] = 1                                  # somebody else's
+    g = torch.Generator("cuda").manual_seed(3)
+    k, v = (torch.randn(600, 8, 128, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(600, 64, 128, device="cuda", generator=g).to(torch.bfloat16)
+    starts = ints([0, 300, 410, 600])
+
+    def outputs(p):
+        return [p.attend(0, q[:3]), p.attend(0, q[:36], ints([0, 12, 24, 36])), p.attend(0, q, starts), p.attend(0, q[:36].float(), ints([0, 12, 24, 36]))]
+
+    for p in (far, near):
+        assert p.reserve(ints([300, 110, 190])).tolist() == [300, 110, 190]
+        p.append(0, k, v, starts)
+    assert int(far.tables.max()) > 39975 and torch.equal(far.tables - 39970, torch.where(near.tables >= 0, near.tables, -1 - 39970))
+    for step in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(outputs(far), outputs(near)))
+        assert torch.equal(far.codes.view(torch.uint8)[:, 39970:39990], near.codes.view(torch.uint8)[:, :20])
+        for p in (far, near):                             # shared last pages are copied
+            p.fork(ints([0, 0, 1]))
+            assert p.reserve().tolist() == [1] * 3
+            p.append(0, k[step * 3:step * 3 + 3], v[step * 3:step * 3 + 3])
+    want = outputs(far)
+    far.refs[:39970] = 0
+    assert far.compact().tolist() == near.compact().tolist()
+    assert int(far.tables.max()) < 40 and all(torch.equal(a, b) for a, b in zip(outputs(far), want))
