@@ -19,6 +19,7 @@ struct AttendArgs {
     float scale_log2;                               // the scale times log2(e): weights are powers of two
     // work split over the tokens
     int workers;
+    int whole;                                      // no tile is split
     struct SplitTile *split;                        // [workers]: the tile that a worker has the first piece of and others go on with
     float *part_o, *part_ml;                        // [workers][2] pieces of tiles
 };

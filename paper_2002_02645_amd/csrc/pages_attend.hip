@@ -16,6 +16,12 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int kWorkers = 768;         // workgroups that share the work
 constexpr int64_t kTileCost = 8;      // of a tile beside its blocks', in blocks: queries, joining the waves
 constexpr int64_t kLeastShare = 8;    // of a workgroup
+// From so many tiles on there are as many workgroups as divide them, at most kWorkers, so that none of equal ones is split: 64 rows of 3,900 tokens 98 -> 88 us, 128 rows
+// 174 -> 161; of ragged ones 21.9 -> 22.7 and 35.9 -> 36.3.
+constexpr int kEvenTiles = 512;
+// Where no row can have more blocks (by its table or the window) and there are no more tiles than workgroups, no tile is split and nothing joined. One row of 250 tokens 10.0
+// -> 7.3 us, of 500 11.1 -> 9.5, of 900 11.3 against 12.7; 64 rows of 500 20.3 -> 15.8, of 900 33 -> 26.
+constexpr int64_t kWholeBlocks = 24;
 
 // Weights are taken in two parts of bf16 (2^-17 in all): the outputs are as exact as fp32 sums rounded once, and reading the codes hides the second product (64 rows of
 // 10,000 tokens 192 us either way; 32 columns a wave 2 % more).
@@ -47,19 +53,24 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
     Found *found = reinterpret_cast<Found *>(lds);
     const int per = (v.rows + 255) / 256;
     const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
-    auto cost_of = [&](const RowWork &w) { return (w.blocks + kTileCost) * w.tiles * v.heads; };
+    auto places_of = [&](const RowWork &w) { return p.whole ? 1 : w.blocks + (int)kTileCost; };
+    auto cost_of = [&](const RowWork &w) { return (int64_t)places_of(w) * w.tiles * v.heads; };
     RowWork last;
-    int64_t mine = 0;
+    int64_t mine = 0, tiles = 0;
     for (int r = r0; r < r1; ++r) {
         last = row_work(p, r, kCols);
         mine += cost_of(last);
+        tiles += last.tiles;
     }
-    const TwoSums<4> so_far = two_sums<4>(mine, 0, found->sums);
+    const TwoSums<4> so_far = two_sums<4>(mine, tiles, found->sums);
     const int64_t before = so_far.before[0], total = uniform(so_far.all[0]);
-    int64_t share = (total + p.workers - 1) / p.workers;
-    share = share < kLeastShare ? kLeastShare : share;
+    int workers = p.workers;
+    const int all = (int)uniform(so_far.all[1]) * v.heads;
+    if (!p.whole && all >= kEvenTiles) workers = (all + (all + kWorkers - 1) / kWorkers - 1) / ((all + kWorkers - 1) / kWorkers);
+    int64_t share = (total + workers - 1) / workers;
+    share = share < kLeastShare && !p.whole ? kLeastShare : share;
     const int64_t begin = blockIdx.x * share, end = min(total, begin + share);
-    if (threadIdx.x == 0) p.split[blockIdx.x].pieces = 0;
+    if (threadIdx.x == 0 && !p.whole) p.split[blockIdx.x].pieces = 0;
     if (begin >= end) return;
     if (before <= begin && begin < before + mine) {
         int64_t b = before;
@@ -88,11 +99,11 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
             w = uniform(row_work(p, row, kCols));
             continue;
         }
-        const int tile_cost = w.blocks + (int)kTileCost, item = (int)((at - base) / tile_cost);
+        const int tile_cost = places_of(w), item = (int)((at - base) / tile_cost);
         const int from = (int)(at - base - (int64_t)item * tile_cost), upto = (int)min((int64_t)tile_cost, from + end - at);   // places of the tile's
         const int tile = item / v.heads, head = item - tile * v.heads;
         const int col0 = tile * kCols, cols = w.n.count * p.group;
-        const int b0 = max(0, from - (int)kTileCost), count = max(0, upto - (int)kTileCost) - b0;
+        const int b0 = p.whole ? 0 : max(0, from - (int)kTileCost), count = p.whole ? w.blocks : max(0, upto - (int)kTileCost) - b0;
         const int64_t slot = blockIdx.x * 2 + (at == begin ? 0 : 1);
         at += upto - from;
         if (count == 0 && (w.blocks > 0 || from > 0)) continue;   // (a tile with nothing to attend to: zeros, by whoever has its first place)
@@ -482,6 +493,7 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t s)
     static_assert(lds <= 65536 + 2048, "LDS");
     hipLaunchKernelGGL((pages_attend_kernel<DC, CT, NS>), dim3(a.workers), dim3(256), lds, s, a);
     if (hipGetLastError() != hipSuccess) return hipErrorLaunchFailure;
+    if (a.whole) return hipSuccess;
     hipLaunchKernelGGL((pages_join_kernel<DC, CT>), dim3(a.workers, kFrags), dim3(256), 0, s, a);
     return hipGetLastError();
 }
@@ -568,7 +580,10 @@ int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int
     a.out_bf16 = out_dtype == FREEZE_BF16;
     a.out_vec = ob % (4 * os) == 0 && pages->head_dim % 4 == 0 && a.out_token % 4 == 0 && a.out_head % 4 == 0;
     a.scale_log2 = scale * 1.4426950408889634f;
-    a.workers = kWorkers;
+    const int64_t cols = 16 * pl.ct, tiles = std::min(tokens * group / cols + pages->rows, tokens * ((group + cols - 1) / cols)) * pages->heads;
+    const int64_t most_blocks = std::min(pages->max_pages * a.v.per_page, window > 0 ? (window + each) / kPageBlock + 2 : (int64_t)1 << 31);
+    a.whole = most_blocks <= kWholeBlocks && tiles <= kWorkers;
+    a.workers = a.whole ? (int)std::min<int64_t>(tiles, kWorkers) : kWorkers;
     uint8_t *ws = static_cast<uint8_t *>(workspace);
     a.split = reinterpret_cast<SplitTile *>(ws);
     ws += pl.split_bytes;
