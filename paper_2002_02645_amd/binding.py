@@ -571,15 +571,19 @@ def freeze_reorder_states(states: Sequence[FreezeState], parents: torch.Tensor, 
 
 
 _HEADS = struct.Struct("QQiiqqqq")   # freeze_heads
+_HEAD_TYPES = {torch.float32: FREEZE_F32, torch.bfloat16: FREEZE_BF16}
 
 
 def _heads_of(t: torch.Tensor, heads: Optional[int] = None, dim: Optional[int] = None) -> tuple:
     """Elements from token to token and from head to head of a tensor [tokens, heads, dim] whose heads are dense."""
-    if not (t.dim() == 3 and t.dtype in (torch.float32, torch.bfloat16)):
+    shape = t.shape
+    if len(shape) != 3 or t.dtype not in _HEAD_TYPES:
         raise _refused()
-    tokens, n, d = t.shape
-    if not ((heads is None or n == heads) and (dim is None or d == dim)):
+    tokens, n, d = shape
+    if (heads is not None and n != heads) or (dim is not None and d != dim):
         raise _refused()
+    if t.is_contiguous():
+        return n * d, d
     token, head, one = t.stride()
     if one != 1 and d > 1:
         raise _refused("the last dimension has to be dense")
@@ -1022,13 +1026,16 @@ class FreezeCache:
         tokens, _, dim = xs[0].shape
         pairs, arr = frequencies.numel(), b""
         for src, dst in zip(xs, outs):
-            if out is not None and not (dst.shape == src.shape and dst.dtype == src.dtype):
+            strides, shape, dtype = _heads_of(src, None, dim), src.shape, src.dtype
+            if shape[0] != tokens:
                 raise _refused()
-            strides = _heads_of(src, None, dim)
-            if src.shape[0] != tokens:
-                raise _refused()
-            same = dst is src or (out is None and src.is_contiguous())
-            arr += _HEADS.pack(src.data_ptr(), dst.data_ptr(), _DTYPES[src.dtype], src.shape[1], *strides, *(strides if same else _heads_of(dst)))
+            if out is None and src.is_contiguous():
+                to = strides
+            else:
+                if dst.shape != shape or dst.dtype != dtype:
+                    raise _refused()
+                to = _heads_of(dst)
+            arr += _HEADS.pack(src.data_ptr(), dst.data_ptr(), _HEAD_TYPES[dtype], shape[1], *strides, *to)
         _numbers(positions, tokens)
         if not (frequencies.dtype == torch.float64 and frequencies.is_contiguous() and 2 * pairs <= dim):
             raise _refused()
@@ -1062,6 +1069,7 @@ class FreezePages:
         self._scratch: Dict[tuple, torch.Tensor] = {}   # by device and stream
         self._at = ctypes.addressof(self.pool)
         self._book_bytes = freeze_pages_workspace_bytes(self.pool)
+        self._attend_bytes: Dict[tuple, int] = {}       # by what the size goes by
 
     _workspace = FreezeCache._workspace
 
@@ -1120,9 +1128,15 @@ class FreezePages:
             raise _refused()
         _numbers(starts, pool.rows + 1)
         L, group = lib(), heads // pool.heads
-        nbytes = L.freeze_pages_attend_workspace_bytes(self._at, group, tokens, most, starts is not None)
-        if nbytes == 0:
-            raise FreezeError(FREEZE_EINVAL, "freeze_pages_attend_workspace_bytes")
+        sizes = (group, tokens, most, starts is not None)
+        nbytes = self._attend_bytes.get(sizes)
+        if nbytes is None:
+            nbytes = L.freeze_pages_attend_workspace_bytes(self._at, *sizes)
+            if nbytes == 0:
+                raise FreezeError(FREEZE_EINVAL, "freeze_pages_attend_workspace_bytes")
+            if len(self._attend_bytes) >= 256:
+                self._attend_bytes.clear()
+            self._attend_bytes[sizes] = nbytes
         stream = torch._C._cuda_getCurrentRawStream(dev)
         ws = self._workspace(nbytes, (dev, stream))
         _check(L.freeze_pages_attend(self._at, layer, q.data_ptr(), _DTYPES[q.dtype], *qs, group, tokens, _at(starts), most, dim ** -0.5 if scale is None else scale,
