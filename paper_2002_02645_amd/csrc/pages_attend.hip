@@ -291,7 +291,7 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 // the same card: 1.10).  Four columns of 16 a wave need 512 registers and copy half of them (643 us where two needed 307), three spill (406); codes turned into bf16
 // once for a workgroup of eight waves, in LDS, 283 us; codes shared by four waves through LDS 275; codes two blocks ahead 241 against 245, at registers that wide heads lack.
 template <int DC, int CT>
-__global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(AttendArgs p)
+__global__ __launch_bounds__(256, CT == 1 && DC <= 4 ? 3 : 2) void pages_prompt_kernel(AttendArgs p)
 {
     constexpr int kWave = 16 * CT, kCols = 4 * kWave;
     const PageView &v = p.v;
@@ -461,11 +461,12 @@ __global__ __launch_bounds__(256, CT <= 2 ? 2 : 1) void pages_prompt_kernel(Atte
 
 struct AttendPlan {
     int ct, parts;
-    bool prompt;
+    int prompt;   // 0: not the prompts' kernel; 1, 2: with 16, 32 columns a wave (16 where heads are wider than 128)
     size_t o_bytes, ml_bytes, split_bytes;
     size_t bytes() const { return o_bytes + ml_bytes + split_bytes; }
 };
-AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t most, int parts)
+// most_blocks: that a row can have
+AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t most, int parts, int64_t most_blocks)
 {
     AttendPlan pl;
     const int64_t cols = (most > 0 ? most : 1) * group;
@@ -473,11 +474,14 @@ AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t
     // Eight heads, groups of four, dim 128; new tokens a row behind 500 / 4,000 / 16,000 places, us:
     //   16 columns a wave against 32: 16 rows of 5: 16 18 / 49 47 / 161 112; of 16: 24 32 / 98 70 / 337 192; 4 rows of 8: 15 16 / 21 27 / 50 45
     //   (twice as much is read, but smaller tiles come and go faster: 4,096 columns and heads are where it turns);
-    //   the better of those against the prompts' kernel: 1 row of 256: 24 26 / 48 91 / 130 341; of 512: 39 32 / 125 96 / 357 354; 4 rows of 64: 24 23 / 53 97 / 136 357;
-    //   of 128: 34 25 / 121 98 / 383 355; 16 rows of 32: 36 23 / 123 101 / 393 464; of 64: 61 26 / 196 104 / 670 459 (16,384).
+    //   the better of those, the prompts' kernel with 16 and with 32 columns a wave: 1 row of 256 (8,192): 41 19 26 / 57 70 93 / 150 265 343; of 512 (16,384): 30 24 32 /
+    //   75 75 98 / 232 285 360; of 1,024 (32,768): 66 39 43 / 157 117 111 / 491 374 378; 4 rows of 64: 15 17 23 / 59 75 98 / 154 281 363; of 128: 20 18 25 / 73 79 100 /
+    //   242 282 359; of 256: 42 28 29 / 142 110 107 / 485 379 360; 16 rows of 32: 18 16 23 / 77 78 101 / 270 399 466; of 64: 39 24 26 / 146 106 102 / 544 438 468;
+    //   of 128 (65,536): 86 42 38 / 340 194 153 / 1229 844 591.
+    //   (A prompt's tile walks its blocks one after another, about 0.5 us each: few tiles of long rows wait for that, so sizes between take it where no row can be long.)
     const int64_t all = tokens * group * p->heads;
     pl.ct = parts > 1 || cols <= 16 || all < 4096 ? 1 : 2;
-    pl.prompt = parts == 1 && cols > 64 && all >= 16384;
+    pl.prompt = parts > 1 || cols <= 64 ? 0 : all >= 32768 ? 2 : all >= 8192 && most_blocks <= 64 ? 1 : 0;
     const size_t slots = 2 * kWorkers, kCols = 16 * pl.ct;
     pl.o_bytes = slots * kCols * page_width(p->head_dim) * 4;
     pl.ml_bytes = slots * 2 * kCols * 4;
@@ -497,14 +501,22 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t s)
     hipLaunchKernelGGL((pages_join_kernel<DC, CT>), dim3(a.workers, kFrags), dim3(256), 0, s, a);
     return hipGetLastError();
 }
+template <int DC, int CT>
+hipError_t launch_prompt(const AttendArgs &a, hipStream_t s)
+{
+    constexpr int64_t cols = 64 * CT;
+    constexpr size_t lds = std::max((size_t)cols * kQueryRow<DC> * 2, (size_t)4 * 16 * (8 * DC + 1) * 16);
+    const int64_t n = std::min(a.tokens * a.group / cols + a.v.rows, a.tokens * ((a.group + cols - 1) / cols));
+    hipLaunchKernelGGL((pages_prompt_kernel<DC, CT>), dim3((unsigned)(n * a.v.heads)), dim3(256), lds, s, a);
+    return hipGetLastError();
+}
 template <int DC>
 hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s)
 {
     if (pl.prompt) {
-        constexpr int CT = DC <= 4 ? 2 : 1;
-        const int64_t n = std::min(a.tokens * a.group / (64 * CT) + a.v.rows, a.tokens * ((a.group + 64 * CT - 1) / (64 * CT)));
-        hipLaunchKernelGGL((pages_prompt_kernel<DC, CT>), dim3((unsigned)(n * a.v.heads)), dim3(256), std::max((size_t)64 * CT * kQueryRow<DC> * 2, (size_t)4 * 16 * (8 * DC + 1) * 16), s, a);
-        return hipGetLastError();
+        if constexpr (DC <= 4)
+            if (pl.prompt == 2) return launch_prompt<DC, 2>(a, s);
+        return launch_prompt<DC, 1>(a, s);
     }
     if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, s);
     if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, s);
@@ -528,7 +540,7 @@ extern "C" {
 size_t freeze_pages_attend_workspace_bytes(const freeze_pages *pages, int group, int64_t tokens, int64_t most, int packed)
 {
     if (!attend_sizes(pages, group, tokens, most)) return 0;
-    const AttendPlan pl = attend_plan(pages, group, tokens, most_of(tokens, most, packed), 1);
+    const AttendPlan pl = attend_plan(pages, group, tokens, most_of(tokens, most, packed), 1, 0);
     return pl.bytes();
 }
 
@@ -550,7 +562,8 @@ int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int
         !heads_span(tokens, heads, pages->head_dim, out_token_stride, out_head_stride, true, &out_span))
         return FREEZE_EINVAL;
     const int64_t each = most_of(tokens, most, starts != nullptr);
-    const AttendPlan pl = attend_plan(pages, group, tokens, each, q_dtype == FREEZE_F32 ? 3 : 1);
+    const int64_t most_blocks = std::min(pages->max_pages * (pages->page_tokens / kPageBlock), window > 0 ? (window + each) / kPageBlock + 2 : (int64_t)1 << 31);
+    const AttendPlan pl = attend_plan(pages, group, tokens, each, q_dtype == FREEZE_F32 ? 3 : 1, most_blocks);
     if (workspace_bytes < freeze_pages_attend_workspace_bytes(pages, group, tokens, most, starts != nullptr) || wb % 256 != 0) return FREEZE_EWORKSPACE;
     Extent e[10];
     int n = 0;
@@ -581,7 +594,6 @@ int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int
     a.out_vec = ob % (4 * os) == 0 && pages->head_dim % 4 == 0 && a.out_token % 4 == 0 && a.out_head % 4 == 0;
     a.scale_log2 = scale * 1.4426950408889634f;
     const int64_t cols = 16 * pl.ct, tiles = std::min(tokens * group / cols + pages->rows, tokens * ((group + cols - 1) / cols)) * pages->heads;
-    const int64_t most_blocks = std::min(pages->max_pages * a.v.per_page, window > 0 ? (window + each) / kPageBlock + 2 : (int64_t)1 << 31);
     a.whole = most_blocks <= kWholeBlocks && tiles <= kWorkers;
     a.workers = a.whole ? (int)std::min<int64_t>(tiles, kWorkers) : kWorkers;
     uint8_t *ws = static_cast<uint8_t *>(workspace);

@@ -193,3 +193,27 @@ def test_same_results_every_time():
         first = p.attend(0, q, starts)
         for _ in range(4):
             assert torch.equal(first, p.attend(0, q, starts))
+
+
+@pytest.mark.parametrize("dim", [17, 64, 96, 128, 160, 200, 256])
+def test_longer_prompts(dim):
+    """632 new tokens of 64 heads are 40,448 columns: 32 columns a wave in the prompts' kernel where the heads allow it."""
+    new = [130, 5, 64, 0, 33, 400]
+    lengths = [n + m for n, m in zip(new, [140, 0, 33, 70, 96, 1])]
+    p, pool = pair(1, 120, len(new), 14, HEADS, dim, 32)
+    assert p.reserve(ints(lengths)).tolist() == pool.reserve(lengths) == lengths
+    fill(p, pool, lengths, dim, 0, torch.bfloat16)
+    check(p, pool, new, torch.bfloat16, 1)
+    check(p, pool, new, torch.bfloat16, 2, window=45, out_dtype=torch.float32, most=max(new))
+    check(p, pool, new, torch.bfloat16, 3, window=1, strided=True)
+
+
+@pytest.mark.parametrize("new", [[130, 5, 64, 0, 33, 40], PROMPTS, [130, 5, 64, 0, 33, 400]], ids=["17408", "27648", "40448"])
+def test_prompts_in_long_tables(new):
+    """Tables that could hold more than 64 blocks a row: sizes between go to the kernel that splits rows over workgroups."""
+    lengths = [n + m for n, m in zip(new, [140, 0, 33, 70, 96, 1])]
+    p, pool = pair(1, 120, len(new), 100, HEADS, 128, 32)
+    assert p.reserve(ints(lengths)).tolist() == pool.reserve(lengths) == lengths
+    fill(p, pool, lengths, 7, 0, torch.bfloat16)
+    check(p, pool, new, torch.bfloat16, 4)
+    check(p, pool, new, torch.bfloat16, 5, window=45, most=max(new))
