@@ -290,8 +290,10 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 // other vector instructions, about 850 cycles, and two waves take 1,300 for it: five rows of up to 4,096 new tokens 247 us, 0.82 - 0.86 PFLOP/s (a library product of 8,192^3 on
 // the same card: 1.10).  Four columns of 16 a wave need 512 registers and copy half of them (643 us where two needed 307), three spill (406); codes turned into bf16
 // once for a workgroup of eight waves, in LDS, 283 us; codes shared by four waves through LDS 275; codes two blocks ahead 241 against 245, at registers that wide heads lack.
-template <int DC, int CT>
-__global__ __launch_bounds__(256, CT == 1 && DC <= 4 ? 3 : 2) void pages_prompt_kernel(AttendArgs p)
+// NS = 3: queries of fp32 and the weights in three parts of bf16 each, three times the products: 4 rows of 2,048 new tokens behind 500 places 577 us, where the kernel
+// above needs 1,600 (it knows the end of a row's blocks, not of a tile's).
+template <int DC, int CT, int NS>
+__global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : 2) void pages_prompt_kernel(AttendArgs p)
 {
     constexpr int kWave = 16 * CT, kCols = 4 * kWave;
     const PageView &v = p.v;
@@ -324,13 +326,13 @@ __global__ __launch_bounds__(256, CT == 1 && DC <= 4 ? 3 : 2) void pages_prompt_
     const int cols = w.n.count * p.group, tile0 = uniform((int)found[1]) * kCols, col0 = tile0 + wave * kWave;
     __syncthreads();
     uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
-    stage_queries<DC, 1, 256>(p, w, head, tile0, kCols, staged);
+    stage_queries<DC, NS, 256>(p, w, head, tile0, kCols, staged);
     __syncthreads();
-    bf16x8 q[CT][1][DC];
+    bf16x8 q[CT][NS][DC];
     Sight<CT> sight;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        take_queries<DC, 1>(staged, kCols, wave * kWave + 16 * ct, q[ct]);
+        take_queries<DC, NS>(staged, kCols, wave * kWave + 16 * ct, q[ct]);
         const int c = col0 + 16 * ct + col;
         sight.set(ct, c < cols ? w.len - w.n.count + c / p.group : -1, p.window);
     }
@@ -374,7 +376,7 @@ __global__ __launch_bounds__(256, CT == 1 && DC <= 4 ? 3 : 2) void pages_prompt_
     f32x4 s0[CT][2], s1[CT][2];
     load_keys(page, lo);
     load_values(page, lo);
-    scores_of<DC, CT, 1>(k, q, s0);
+    scores_of<DC, CT, NS>(k, q, s0);
     load_keys(next, lo + 1);
     auto step = [&](int b, f32x4 (&s)[CT][2], f32x4 (&then)[CT][2]) {
         const int first = b * kPageBlock;
@@ -411,26 +413,32 @@ __global__ __launch_bounds__(256, CT == 1 && DC <= 4 ? 3 : 2) void pages_prompt_
                 for (int f = 0; f < 2 * DC; ++f) o[ct][f] *= a;
             }
         }
-        scores_of<DC, CT, 1>(k, q, then);
-        bf16x8 f[CT];
+        scores_of<DC, CT, NS>(k, q, then);
+        bf16x8 f[CT][NS];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             const float ref = m[ct] == -INFINITY ? 0.f : m[ct];
+            float e[8];
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) f[ct][4 * t + i] = (__bf16)__builtin_amdgcn_exp2f(fmaf(s[ct][t][i], ks, -ref));
+                for (int i = 0; i < 4; ++i) e[4 * t + i] = __builtin_amdgcn_exp2f(fmaf(s[ct][t][i], ks, -ref));
+            parts_of<NS>(e, f[ct]);
         }
         load_keys(next, b + 2);
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) sum[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, f[ct], sum[ct], 0, 0, 0);   // (of the rounded weights)
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int n = 0; n < NS; ++n) sum[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, f[ct][n], sum[ct], 0, 0, 0);   // (of the rounded weights)
 #pragma unroll
         for (int c = 0; c < DC; ++c)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const bf16x8 y = values_of(x[c][2 * u], x[c][2 * u + 1], vs);
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, f[ct], o[ct][2 * c + u], 0, 0, 0);
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int n = 0; n < NS; ++n) o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, f[ct][n], o[ct][2 * c + u], 0, 0, 0);
             }
         scales = scales_next;
         scales_next = scale_of(next, b + 2);
@@ -459,6 +467,7 @@ __global__ __launch_bounds__(256, CT == 1 && DC <= 4 ? 3 : 2) void pages_prompt_
 
 // ---- host -------------------------------------------------------------------------------------------
 
+constexpr int kWidestExact = 6;   // queries of fp32 in the prompts' kernel: wider heads' parts do not fit in registers (head_dim / 32)
 struct AttendPlan {
     int ct, parts;
     int prompt;   // 0: not the prompts' kernel; 1, 2: with 16, 32 columns a wave (16 where heads are wider than 128)
@@ -479,9 +488,11 @@ AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t
     //   242 282 359; of 256: 42 28 29 / 142 110 107 / 485 379 360; 16 rows of 32: 18 16 23 / 77 78 101 / 270 399 466; of 64: 39 24 26 / 146 106 102 / 544 438 468;
     //   of 128 (65,536): 86 42 38 / 340 194 153 / 1229 844 591.
     //   (A prompt's tile walks its blocks one after another, about 0.5 us each: few tiles of long rows wait for that, so sizes between take it where no row can be long.)
+    //   With fp32, that kernel and this: 1 row of 256: 12 15 without a past, 21 26 / - / -; of 512: 42 32 / - / -; of 1,024: 132 62 / 370 207 / 1166 697; 4 rows of 64: 17 22;
+    //   of 128: 31 25; of 256: 80 42 / 318 190 / 1113 699; 16 rows of 64: 73 35 / 311 186 / 1151 772; heads of 192: 1 row of 512: 79 43; of 1,024: 241 85 / 667 287 / 2082 982.
     const int64_t all = tokens * group * p->heads;
     pl.ct = parts > 1 || cols <= 16 || all < 4096 ? 1 : 2;
-    pl.prompt = parts > 1 || cols <= 64 ? 0 : all >= 32768 ? 2 : all >= 8192 && most_blocks <= 64 ? 1 : 0;
+    pl.prompt = (parts > 1 && p->head_dim > 32 * kWidestExact) || cols <= 64 ? 0 : all >= 32768 ? 2 : all >= (parts > 1 ? 16384 : 8192) && most_blocks <= 64 ? 1 : 0;
     const size_t slots = 2 * kWorkers, kCols = 16 * pl.ct;
     pl.o_bytes = slots * kCols * page_width(p->head_dim) * 4;
     pl.ml_bytes = slots * 2 * kCols * 4;
@@ -501,22 +512,26 @@ hipError_t launch_attend(const AttendArgs &a, hipStream_t s)
     hipLaunchKernelGGL((pages_join_kernel<DC, CT>), dim3(a.workers, kFrags), dim3(256), 0, s, a);
     return hipGetLastError();
 }
-template <int DC, int CT>
+template <int DC, int CT, int NS>
 hipError_t launch_prompt(const AttendArgs &a, hipStream_t s)
 {
     constexpr int64_t cols = 64 * CT;
-    constexpr size_t lds = std::max((size_t)cols * kQueryRow<DC> * 2, (size_t)4 * 16 * (8 * DC + 1) * 16);
+    constexpr size_t lds = std::max((size_t)NS * cols * kQueryRow<DC> * 2, (size_t)4 * 16 * (8 * DC + 1) * 16);
     const int64_t n = std::min(a.tokens * a.group / cols + a.v.rows, a.tokens * ((a.group + cols - 1) / cols));
-    hipLaunchKernelGGL((pages_prompt_kernel<DC, CT>), dim3((unsigned)(n * a.v.heads)), dim3(256), lds, s, a);
+    hipLaunchKernelGGL((pages_prompt_kernel<DC, CT, NS>), dim3((unsigned)(n * a.v.heads)), dim3(256), lds, s, a);
     return hipGetLastError();
 }
 template <int DC>
 hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s)
 {
     if (pl.prompt) {
-        if constexpr (DC <= 4)
-            if (pl.prompt == 2) return launch_prompt<DC, 2>(a, s);
-        return launch_prompt<DC, 1>(a, s);
+        if (pl.parts > 1) {
+            if constexpr (DC <= kWidestExact) return launch_prompt<DC, 1, 3>(a, s);
+        } else {
+            if constexpr (DC <= 4)
+                if (pl.prompt == 2) return launch_prompt<DC, 2, 1>(a, s);
+            return launch_prompt<DC, 1, 1>(a, s);
+        }
     }
     if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, s);
     if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, s);

@@ -208,12 +208,13 @@ def test_longer_prompts(dim):
     check(p, pool, new, torch.bfloat16, 3, window=1, strided=True)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("new", [[130, 5, 64, 0, 33, 40], PROMPTS, [130, 5, 64, 0, 33, 400]], ids=["17408", "27648", "40448"])
-def test_prompts_in_long_tables(new):
+def test_prompts_in_long_tables(new, dtype):
     """Tables that could hold more than 64 blocks a row: sizes between go to the kernel that splits rows over workgroups."""
     lengths = [n + m for n, m in zip(new, [140, 0, 33, 70, 96, 1])]
     p, pool = pair(1, 120, len(new), 100, HEADS, 128, 32)
     assert p.reserve(ints(lengths)).tolist() == pool.reserve(lengths) == lengths
-    fill(p, pool, lengths, 7, 0, torch.bfloat16)
-    check(p, pool, new, torch.bfloat16, 4)
-    check(p, pool, new, torch.bfloat16, 5, window=45, most=max(new))
+    fill(p, pool, lengths, 7, 0, dtype)
+    check(p, pool, new, dtype, 4)
+    check(p, pool, new, dtype, 5, window=45, most=max(new))
