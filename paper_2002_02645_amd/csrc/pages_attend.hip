@@ -291,9 +291,10 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 // the same card: 1.10).  Four columns of 16 a wave need 512 registers and copy half of them (643 us where two needed 307), three spill (406); codes turned into bf16
 // once for a workgroup of eight waves, in LDS, 283 us; codes shared by four waves through LDS 275; codes two blocks ahead 241 against 245, at registers that wide heads lack.
 // NS = 3: queries of fp32 and the weights in three parts of bf16 each, three times the products: 4 rows of 2,048 new tokens behind 500 places 577 us, where the kernel
-// above needs 1,600 (it knows the end of a row's blocks, not of a tile's).
+// above needs 1,600 (it knows the end of a row's blocks, not of a tile's). Heads above
+// 192 then have a SIMD's registers to one wave: 16 rows of 256 behind 4,000, heads of 256, 1,597 us against 2,449.
 template <int DC, int CT, int NS>
-__global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : 2) void pages_prompt_kernel(AttendArgs p)
+__global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && DC > 6 ? 1 : 2) void pages_prompt_kernel(AttendArgs p)
 {
     constexpr int kWave = 16 * CT, kCols = 4 * kWave;
     const PageView &v = p.v;
@@ -467,7 +468,6 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : 2) void pa
 
 // ---- host -------------------------------------------------------------------------------------------
 
-constexpr int kWidestExact = 6;   // queries of fp32 in the prompts' kernel: wider heads' parts do not fit in registers (head_dim / 32)
 struct AttendPlan {
     int ct, parts;
     int prompt;   // 0: not the prompts' kernel; 1, 2: with 16, 32 columns a wave (16 where heads are wider than 128)
@@ -492,7 +492,7 @@ AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t
     //   of 128: 31 25; of 256: 80 42 / 318 190 / 1113 699; 16 rows of 64: 73 35 / 311 186 / 1151 772; heads of 192: 1 row of 512: 79 43; of 1,024: 241 85 / 667 287 / 2082 982.
     const int64_t all = tokens * group * p->heads;
     pl.ct = parts > 1 || cols <= 16 || all < 4096 ? 1 : 2;
-    pl.prompt = (parts > 1 && p->head_dim > 32 * kWidestExact) || cols <= 64 ? 0 : all >= 32768 ? 2 : all >= (parts > 1 ? 16384 : 8192) && most_blocks <= 64 ? 1 : 0;
+    pl.prompt = cols <= 64 ? 0 : all >= 32768 ? 2 : all >= (parts > 1 ? 16384 : 8192) && most_blocks <= 64 ? 1 : 0;
     const size_t slots = 2 * kWorkers, kCols = 16 * pl.ct;
     pl.o_bytes = slots * kCols * page_width(p->head_dim) * 4;
     pl.ml_bytes = slots * 2 * kCols * 4;
@@ -525,13 +525,10 @@ template <int DC>
 hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s)
 {
     if (pl.prompt) {
-        if (pl.parts > 1) {
-            if constexpr (DC <= kWidestExact) return launch_prompt<DC, 1, 3>(a, s);
-        } else {
-            if constexpr (DC <= 4)
-                if (pl.prompt == 2) return launch_prompt<DC, 2, 1>(a, s);
-            return launch_prompt<DC, 1, 1>(a, s);
-        }
+        if (pl.parts > 1) return launch_prompt<DC, 1, 3>(a, s);
+        if constexpr (DC <= 4)
+            if (pl.prompt == 2) return launch_prompt<DC, 2, 1>(a, s);
+        return launch_prompt<DC, 1, 1>(a, s);
     }
     if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, s);
     if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, s);
