@@ -290,6 +290,8 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 // other vector instructions, about 850 cycles, and two waves take 1,300 for it: five rows of up to 4,096 new tokens 247 us, 0.82 - 0.86 PFLOP/s (a library product of 8,192^3 on
 // the same card: 1.10).  Four columns of 16 a wave need 512 registers and copy half of them (643 us where two needed 307), three spill (406); codes turned into bf16
 // once for a workgroup of eight waves, in LDS, 283 us; codes shared by four waves through LDS 275; codes two blocks ahead 241 against 245, at registers that wide heads lack.
+// Heads above 160 have one column of 16 a wave and two waves a SIMD; with two columns and one wave 16 rows of 256 behind 4,000 need 714 us against 597 (heads of 192) and 918
+// against 769 (256); heads of 160, two waves either way, 367 against 470.
 // NS = 3: queries of fp32 and the weights in three parts of bf16 each, three times the products: 4 rows of 2,048 new tokens behind 500 places 577 us, where the kernel
 // above needs 1,600 (it knows the end of a row's blocks, not of a tile's). Heads above
 // 192 then have a SIMD's registers to one wave: 16 rows of 256 behind 4,000, heads of 256, 1,597 us against 2,449.
@@ -470,7 +472,7 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
 
 struct AttendPlan {
     int ct, parts;
-    int prompt;   // 0: not the prompts' kernel; 1, 2: with 16, 32 columns a wave (16 where heads are wider than 128)
+    int prompt;   // 0: not the prompts' kernel; 1, 2: with 16, 32 columns a wave (16 where heads are wider than 160)
     size_t o_bytes, ml_bytes, split_bytes;
     size_t bytes() const { return o_bytes + ml_bytes + split_bytes; }
 };
@@ -526,7 +528,7 @@ hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s
 {
     if (pl.prompt) {
         if (pl.parts > 1) return launch_prompt<DC, 1, 3>(a, s);
-        if constexpr (DC <= 4)
+        if constexpr (DC <= 5)
             if (pl.prompt == 2) return launch_prompt<DC, 2, 1>(a, s);
         return launch_prompt<DC, 1, 1>(a, s);
     }
