@@ -12,8 +12,8 @@ struct RotateTensor {
     void *dst;
     int64_t src_token, src_head, dst_token, dst_head;
     int heads, bf16;
-    int per_head;        // items of a head: of 16 bytes or two times as many (vec), or of a pair or an element that is copied
-    int vec;
+    int per_head;        // items of a head: of a piece or two of them, or of a pair or an element that is copied
+    int piece;           // bytes: 16, 8, 4; 0: by elements
 };
 struct RotateArgs {
     RotateTensor t[kMostTensors];
@@ -50,65 +50,71 @@ __device__ __forceinline__ float2 turn(const RotateArgs &p, int64_t token, int i
 __device__ __forceinline__ float turned_a(float a, float b, float2 w) { return fmaf(a, w.x, -(b * w.y)); }
 __device__ __forceinline__ float turned_b(float a, float b, float2 w) { return fmaf(b, w.x, a * w.y); }
 
-// 16 bytes as their values and back
-template <int V>
-__device__ __forceinline__ void open_up(u32x4 w, float (&x)[V])
+// A piece of W words as its V values and back
+template <int W>
+using Words = __attribute__((ext_vector_type(W))) uint32_t;
+template <int V, int W>
+__device__ __forceinline__ void open_up(Words<W> w, float (&x)[V])
 {
 #pragma unroll
-    for (int e = 0; e < V; ++e) x[e] = __uint_as_float(V == 4 ? w[e] : e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+    for (int e = 0; e < V; ++e) x[e] = __uint_as_float(V == W ? w[e] : e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
 }
-template <int V>
-__device__ __forceinline__ u32x4 close_up(const float (&x)[V])
+template <int V, int W>
+__device__ __forceinline__ Words<W> close_up(const float (&x)[V])
 {
-    u32x4 w;
+    Words<W> w;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if constexpr (V == 4) w[e] = __float_as_uint(x[e]);
+    for (int e = 0; e < W; ++e) {
+        if constexpr (V == W) w[e] = __float_as_uint(x[e]);
         else w[e] = (uint32_t)bf16_rne(x[2 * e]) | (uint32_t)bf16_rne(x[2 * e + 1]) << 16;
     }
     return w;
 }
 
-// An item of a head in 16-byte pieces: V / 2 pairs side by side; V pairs, half a turned part apart; or a piece that is copied.
-template <int V>
-__device__ __forceinline__ void rotate_pieces(const RotateArgs &p, const RotateTensor &t, const uint8_t *src, uint8_t *dst, const float2 *table, int i)
+// An item of a head in pieces of V values, W words: V / 2 pairs side by side; V pairs, half a turned part apart; or a piece that is copied.
+template <int V, int W>
+__device__ __forceinline__ void rotate_pieces(const RotateArgs &p, const void *from, int64_t src_at, void *to, int64_t dst_at, const float2 *table, int i)
 {
+    const Words<W> *src = reinterpret_cast<const Words<W> *>(static_cast<const uint8_t *>(from) + src_at * (4 * W / V));
+    Words<W> *dst = reinterpret_cast<Words<W> *>(static_cast<uint8_t *>(to) + dst_at * (4 * W / V));
     const int pieces = p.pairs / V;   // of one half of the turned part
     if (p.interleaved) {
-        u32x4 w = reinterpret_cast<const u32x4 *>(src)[i];
-        if (i < 2 * pieces) {
+        Words<W> w = src[i];
+        if (i * V < 2 * p.pairs) {
             float x[V], y[V];
-            open_up<V>(w, x);
+            open_up<V, W>(w, x);
 #pragma unroll
             for (int e = 0; e < V / 2; ++e) {
                 const float2 a = table[i * (V / 2) + e];
                 y[2 * e] = turned_a(x[2 * e], x[2 * e + 1], a);
                 y[2 * e + 1] = turned_b(x[2 * e], x[2 * e + 1], a);
             }
-            w = close_up<V>(y);
+            w = close_up<V, W>(y);
         }
-        reinterpret_cast<u32x4 *>(dst)[i] = w;
+        dst[i] = w;
         return;
     }
     if (i >= pieces) {
-        reinterpret_cast<u32x4 *>(dst)[i + pieces] = reinterpret_cast<const u32x4 *>(src)[i + pieces];
+        dst[i + pieces] = src[i + pieces];
         return;
     }
     float a[V], b[V], x[V], y[V];
-    open_up<V>(reinterpret_cast<const u32x4 *>(src)[i], a);
-    open_up<V>(reinterpret_cast<const u32x4 *>(src)[i + pieces], b);
+    open_up<V, W>(src[i], a);
+    open_up<V, W>(src[i + pieces], b);
 #pragma unroll
     for (int e = 0; e < V; ++e) {
         const float2 w = table[i * V + e];
         x[e] = turned_a(a[e], b[e], w);
         y[e] = turned_b(a[e], b[e], w);
     }
-    reinterpret_cast<u32x4 *>(dst)[i] = close_up<V>(x);
-    reinterpret_cast<u32x4 *>(dst)[i + pieces] = close_up<V>(y);
+    dst[i] = close_up<V, W>(x);
+    dst[i + pieces] = close_up<V, W>(y);
 }
 
 // A workgroup takes some tokens (and, of few tokens, a part of their heads: blockIdx.y): their sines and cosines once, for the heads of every tensor.
 // Bound by memory: 32,768 tokens of 40 heads of 128 bf16 (671 MB read and written) 128 us, 5.2 TB/s (400 by pairs); 16 tokens 5.0 us.
+// Heads that are no whole pieces of 16 bytes go by the widest that fit: 40 M elements of bf16 (160 MB), halves apart, 28 us in pieces of 16 (heads of 128), 32 in 8 (of 72;
+// 79 by elements), 47 in 4 (of 100; 77), 81 by elements (of 66, whose halves are odd), which what an item costs to find bounds.
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p)
 {
     extern __shared__ float2 table[];   // [each][pairs]
@@ -127,9 +133,14 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs p)
                 const int token = j / per_token, rest = j - token * per_token, head = rest / t.per_head, i = rest - head * t.per_head;
                 const int64_t src = (first + token) * t.src_token + head * t.src_head, dst = (first + token) * t.dst_token + head * t.dst_head;
                 const float2 *w = table + token * p.pairs;
-                if (t.vec) {
-                    if (t.bf16) rotate_pieces<8>(p, t, static_cast<const uint8_t *>(t.src) + src * 2, static_cast<uint8_t *>(t.dst) + dst * 2, w, i);
-                    else rotate_pieces<4>(p, t, static_cast<const uint8_t *>(t.src) + src * 4, static_cast<uint8_t *>(t.dst) + dst * 4, w, i);
+                if (t.piece == 16) {
+                    if (t.bf16) rotate_pieces<8, 4>(p, t.src, src, t.dst, dst, w, i);
+                    else rotate_pieces<4, 4>(p, t.src, src, t.dst, dst, w, i);
+                } else if (t.piece == 8) {
+                    if (t.bf16) rotate_pieces<4, 2>(p, t.src, src, t.dst, dst, w, i);
+                    else rotate_pieces<2, 2>(p, t.src, src, t.dst, dst, w, i);
+                } else if (t.piece == 4) {
+                    rotate_pieces<2, 1>(p, t.src, src, t.dst, dst, w, i);
                 } else if (i < p.pairs) {
                     const int a = p.interleaved ? 2 * i : i, b = p.interleaved ? a + 1 : i + p.pairs;
                     const float x = load_value(t.src, src + a, t.bf16), y = load_value(t.src, src + b, t.bf16);
@@ -195,10 +206,11 @@ int freeze_rotate_positions(const freeze_heads *heads, int num, int64_t tokens, 
         RotateTensor &t = a.t[a.num++];
         t = RotateTensor{h.src, h.dst, tokens > 1 ? h.src_token_stride : 0, h.heads > 1 ? h.src_head_stride : 0, tokens > 1 ? h.dst_token_stride : 0,
                          h.heads > 1 ? h.dst_head_stride : 0, h.heads, h.dtype == FREEZE_BF16, 0, 0};
-        // whole pieces of 16 bytes: of the turned part (of either half), of what is copied, from head to head and token to token
-        const int64_t piece = 16 / (int64_t)size, turned = interleaved ? 2 * pairs : pairs;
-        t.vec = src % 16 == 0 && dst % 16 == 0 && (t.src_token | t.src_head | t.dst_token | t.dst_head | turned | head_dim) % piece == 0;
-        t.per_head = (int)(t.vec ? (head_dim - (interleaved ? 0 : pairs)) / piece : head_dim - pairs);
+        // the widest pieces that are whole: of the turned part (of either half), of what is copied, from head to head and token to token
+        const int64_t turned = interleaved ? 2 * pairs : pairs;
+        for (int bytes = 16; bytes > (int)size && t.piece == 0; bytes /= 2)
+            if (src % bytes == 0 && dst % bytes == 0 && (t.src_token | t.src_head | t.dst_token | t.dst_head | turned | head_dim) % (bytes / (int64_t)size) == 0) t.piece = bytes;
+        t.per_head = (int)(t.piece ? (head_dim - (interleaved ? 0 : pairs)) * (int64_t)size / t.piece : head_dim - pairs);
         items += (double)tokens * t.heads * t.per_head;
     }
     if (a.num == 0) return FREEZE_OK;

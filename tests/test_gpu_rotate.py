@@ -101,3 +101,27 @@ def test_nothing_to_do(cache):
     assert cache.rotate_positions(torch.empty(0, 3, 8, device="cuda"), none, f).shape == (0, 3, 8)
     assert cache.rotate_positions(torch.empty(2, 0, 8, device="cuda"), none.new_zeros(2), f).shape == (2, 0, 8)
     assert cache.rotate_positions((), none, f) == []
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,pairs", [(128, 64), (72, 36), (100, 50), (66, 33), (80, 36), (68, 18), (34, 14), (22, 0), (33, 16)])
+def test_every_piece(cache, dim, pairs, interleaved, dtype):
+    """Heads that come in pieces of 16, 8 or 4 bytes or by elements, from addresses of every alignment, into others: the same bytes."""
+    tokens, heads = 21, 3
+    x = torch.randn(tokens, heads, dim, device="cuda").to(dtype)
+    positions, f = torch.arange(tokens, device="cuda", dtype=torch.int32) * 5, binding.rotary_frequencies(pairs)
+    want = None
+    for row in (dim, dim + 1, dim + 2, dim + 4):
+        for shift in (0, 1, 2, 4):
+            src = torch.zeros(tokens * heads * row + 8, device="cuda", dtype=dtype)
+            dst = torch.full_like(src, 7.0)
+            view = lambda t: t[shift:shift + tokens * heads * row].view(tokens, heads, row)[:, :, :dim]
+            view(src).copy_(x)
+            cache.rotate_positions(view(src), positions, f, interleaved, out=view(dst))
+            if want is None:
+                want = view(dst).clone()
+                _close(want, ref.rotate(x.double().cpu(), positions.cpu(), f.cpu(), interleaved), x, 1.0, dtype)
+            assert torch.equal(view(dst), want), (row, shift)
+            view(dst).fill_(7.0)
+            assert bool((dst == 7).all())
