@@ -515,8 +515,8 @@ int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int
  *   q        [tokens, heads * group, head_dim] fp32 or bf16; head j reads keys and values of head j / group.
  *   out      [tokens, heads * group, head_dim] FREEZE_F32 or FREEZE_BF16, with strides of its own; shares no byte of its extent with the inputs.
  *   starts, tokens, most: as of freeze_pages_append; outputs of rows that are not in order, and tokens that are no row's, are left as they are.
- * Products of codes are exact, sums and softmax statistics fp32.  With q in bf16, weights are taken in two parts of bf16 (2^-17), prompts' (many new tokens) are
- * rounded to bf16 and their sum is of the rounded ones; with fp32 they and q are taken in three parts, exact to 2^-24.  Scores have to be within fp32's range; a NaN in a key or value that a token attends to, or in
+ * Products of codes are exact, sums and softmax statistics fp32.  With q in bf16, weights are taken in two parts of bf16 (2^-17); with fp32 they and q are taken in
+ * three parts, exact to 2^-24.  Scores have to be within fp32's range; a NaN in a key or value that a token attends to, or in
  * its own q, makes its output NaN, and no other's.  Values below 2^-126 may count as 0.
  *   workspace  freeze_pages_attend_workspace_bytes() bytes, 256-byte aligned; scratch only, shared by calls that follow one another only.  The bytes for some tokens serve fewer too.
  * 1 <= group <= 1024, 0 <= tokens < 2^31, (tokens * group + 16 * rows) * heads < 2^28, 0 < scale <= 3e38, 0 <= window < 2^31; tokens == 0 is a no-op.

@@ -23,8 +23,9 @@ constexpr int kEvenTiles = 512;
 // -> 7.3 us, of 500 11.1 -> 9.5, of 900 11.3 against 12.7; 64 rows of 500 20.3 -> 15.8, of 900 33 -> 26.
 constexpr int64_t kWholeBlocks = 24;
 
-// Weights are taken in two parts of bf16 (2^-17 in all): the outputs are as exact as fp32 sums rounded once, and reading the codes hides the second product (64 rows of
-// 10,000 tokens 192 us either way; 32 columns a wave 2 % more).
+// With bf16 queries, weights are taken in two parts of bf16 (2^-17 in all) by both kernels, so that an output does not depend on how many others the call has, and is as exact
+// as fp32 sums rounded once. Reading the codes hides the second product in the first kernel (64 rows of 10,000 tokens 192 us either way; 32 columns a wave 2 % more);
+// prompts pay for it: five rows of up to 4,096 new tokens 302 us instead of 227 with weights rounded once (2^-8).
 constexpr int kWeightParts = 2;
 
 // Codes are read once (or by rows that share pages, at about the same time) and leave the caches to others: 189 us instead of 215.
@@ -286,15 +287,16 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 
 // Prompts: a workgroup's waves have 16 * CT columns each, one after another, and walk over the blocks that these see, each by itself: the codes of a
 // block come from memory once and from the caches for the other waves.  Nothing is split: there are tiles enough.  Later tiles of a row see more and go first.
-// Bound by what a SIMD issues: a block's 34 matrix instructions (544 cycles of the matrix cores, two issue places each) come with 64 conversions, 16 exponentials and 50
-// other vector instructions, about 850 cycles, and two waves take 1,300 for it: five rows of up to 4,096 new tokens 247 us, 0.82 - 0.86 PFLOP/s (a library product of 8,192^3 on
-// the same card: 1.10).  Four columns of 16 a wave need 512 registers and copy half of them (643 us where two needed 307), three spill (406); codes turned into bf16
+// Bound by what a SIMD issues: a block's 48 matrix instructions (16 for scores, 32 for values with the weights in two parts: 768 cycles of the matrix cores, two issue places
+// each) come with 64 conversions, 16 exponentials and 160 other vector instructions, which together take 108 % of the SIMDs' cycles: five rows of up to 4,096 new tokens
+// 302 us, 0.62 PFLOP/s of the products asked for, 0.94 of those done (a library product of 8,192^3 on the same card: 1.10).  Measured with weights in one part (243 us):
+// four columns of 16 a wave need 512 registers and copy half of them (643 us where two needed 307), three spill (406); codes turned into bf16
 // once for a workgroup of eight waves, in LDS, 283 us; codes shared by four waves through LDS 275; codes two blocks ahead 241 against 245, at registers that wide heads lack.
-// Heads above 160 have one column of 16 a wave and two waves a SIMD; with two columns and one wave 16 rows of 256 behind 4,000 need 714 us against 597 (heads of 192) and 918
-// against 769 (256); heads of 160, two waves either way, 367 against 470.
-// NS = 3: queries of fp32 and the weights in three parts of bf16 each, three times the products: 4 rows of 2,048 new tokens behind 500 places 577 us, where the kernel
-// above needs 1,600 (it knows the end of a row's blocks, not of a tile's). Heads above
-// 192 then have a SIMD's registers to one wave: 16 rows of 256 behind 4,000, heads of 256, 1,597 us against 2,449.
+// Heads above 160 have one column of 16 a wave and two waves a SIMD; with two columns and one wave 16 rows of 256 behind 4,000 need 857 us against 694 (heads of 192) and 1,039
+// against 869 (256); heads of 160, two waves either way, 450 against 556.
+// NS = 3: queries of fp32 and the weights in three parts of bf16 each, three times the products: 4 rows of 2,048 new tokens behind 500 places 529 us, where the kernel
+// above needs 1,565 (it knows the end of a row's blocks, not of a tile's). Heads above
+// 192 then have a SIMD's registers to one wave: 16 rows of 256 behind 4,000, heads of 256, 1,650 us against 2,436.
 template <int DC, int CT, int NS>
 __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && DC > 6 ? 1 : 2) void pages_prompt_kernel(AttendArgs p)
 {
@@ -345,18 +347,16 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
     const int seen = p.window > 0 ? (int)max((int64_t)0, lowest - p.window + 1) : 0;
     const int lo = seen / kPageBlock, hi = highest < 0 ? 0 : highest / kPageBlock + 1;
 
-    f32x4 o[CT][2 * DC], sum[CT];
-    float m[CT];
+    constexpr int kParts = NS > 1 ? NS : kWeightParts;
+    f32x4 o[CT][2 * DC];
+    float m[CT], sum[CT];   // sum: of the lane's own tokens
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         m[ct] = -INFINITY;
-        sum[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+        sum[ct] = 0.f;
 #pragma unroll
         for (int f = 0; f < 2 * DC; ++f) o[ct][f] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    bf16x8 ones;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ones[e] = (__bf16)1.f;
     const Blocks blocks(v, row, head);
     const int unseen = p.window > 0 ? (int)(highest - p.window) : -1;   // the last place that some column does not see any more
     const float scale_log2 = p.scale_log2;
@@ -417,7 +417,7 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
             }
         }
         scores_of<DC, CT, NS>(k, q, then);
-        bf16x8 f[CT][NS];
+        bf16x8 f[CT][kParts];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
             const float ref = m[ct] == -INFINITY ? 0.f : m[ct];
@@ -425,23 +425,22 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[4 * t + i] = __builtin_amdgcn_exp2f(fmaf(s[ct][t][i], ks, -ref));
-            parts_of<NS>(e, f[ct]);
+                for (int i = 0; i < 4; ++i) {
+                    e[4 * t + i] = __builtin_amdgcn_exp2f(fmaf(s[ct][t][i], ks, -ref));
+                    sum[ct] += e[4 * t + i];
+                }
+            parts_of<kParts>(e, f[ct]);
         }
         load_keys(next, b + 2);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int n = 0; n < NS; ++n) sum[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, f[ct][n], sum[ct], 0, 0, 0);   // (of the rounded weights)
 #pragma unroll
         for (int c = 0; c < DC; ++c)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const bf16x8 y = values_of(x[c][2 * u], x[c][2 * u + 1], vs);
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct)
+                for (int n = 0; n < kParts; ++n)
 #pragma unroll
-                    for (int n = 0; n < NS; ++n) o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, f[ct][n], o[ct][2 * c + u], 0, 0, 0);
+                    for (int ct = 0; ct < CT; ++ct) o[ct][2 * c + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, f[ct][n], o[ct][2 * c + u], 0, 0, 0);
             }
         scales = scales_next;
         scales_next = scale_of(next, b + 2);
@@ -455,7 +454,10 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
     f32x4 *mine_out = reinterpret_cast<f32x4 *>(lds) + wave * (16 * (8 * DC + 1));   // [16][8 DC + 1]
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-        const float inv = sum[ct][0] == 0.f ? 0.f : 1.f / sum[ct][0];
+        float l = sum[ct];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
         for (int f = 0; f < 2 * DC; ++f) mine_out[col * (8 * DC + 1) + 4 * f + (lane >> 4)] = o[ct][f] * inv;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -485,10 +487,10 @@ AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t
     // Eight heads, groups of four, dim 128; new tokens a row behind 500 / 4,000 / 16,000 places, us:
     //   16 columns a wave against 32: 16 rows of 5: 16 18 / 49 47 / 161 112; of 16: 24 32 / 98 70 / 337 192; 4 rows of 8: 15 16 / 21 27 / 50 45
     //   (twice as much is read, but smaller tiles come and go faster: 4,096 columns and heads are where it turns);
-    //   the better of those, the prompts' kernel with 16 and with 32 columns a wave: 1 row of 256 (8,192): 41 19 26 / 57 70 93 / 150 265 343; of 512 (16,384): 30 24 32 /
-    //   75 75 98 / 232 285 360; of 1,024 (32,768): 66 39 43 / 157 117 111 / 491 374 378; 4 rows of 64: 15 17 23 / 59 75 98 / 154 281 363; of 128: 20 18 25 / 73 79 100 /
-    //   242 282 359; of 256: 42 28 29 / 142 110 107 / 485 379 360; 16 rows of 32: 18 16 23 / 77 78 101 / 270 399 466; of 64: 39 24 26 / 146 106 102 / 544 438 468;
-    //   of 128 (65,536): 86 42 38 / 340 194 153 / 1229 844 591.
+    //   the better of those, the prompts' kernel with 16 and with 32 columns a wave: 1 row of 256 (8,192): 40 19 29 / 56 73 114 / 151 307 416; of 512 (16,384): 27 23 35 /
+    //   72 78 120 / 233 322 424; of 1,024 (32,768): 60 40 48 / 153 133 133 / 485 473 438; 4 rows of 64: 14 16 24 / 60 84 114 / 154 311 418; of 128: 19 18 26 / 70 86 115 /
+    //   242 311 415; of 256: 39 28 30 / 138 128 118 / 474 472 417; 16 rows of 32: 17 16 24 / 75 86 116 / 260 425 512; of 64: 38 24 26 / 145 127 116 / 522 508 511;
+    //   of 128 (65,536): 85 45 41 / 334 232 192 / 1189 962 771.
     //   (A prompt's tile walks its blocks one after another, about 0.5 us each: few tiles of long rows wait for that, so sizes between take it where no row can be long.)
     //   With fp32, that kernel and this: 1 row of 256: 12 15 without a past, 21 26 / - / -; of 512: 42 32 / - / -; of 1,024: 132 62 / 370 207 / 1166 697; 4 rows of 64: 17 22;
     //   of 128: 31 25; of 256: 80 42 / 318 190 / 1113 699; 16 rows of 64: 73 35 / 311 186 / 1151 772; heads of 192: 1 row of 512: 79 43; of 1,024: 241 85 / 667 287 / 2082 982.
