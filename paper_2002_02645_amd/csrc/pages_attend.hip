@@ -383,8 +383,9 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
     load_keys(next, lo + 1);
     auto step = [&](int b, f32x4 (&s)[CT][2], f32x4 (&then)[CT][2]) {
         const int first = b * kPageBlock;
-        const float ks = score_factor(scale_log2, scales), vs = value_factor(scales);
+        float ks = score_factor(scale_log2, scales), vs = value_factor(scales);
         if (!blocks.there(page)) {
+            ks = vs = 1.f;   // (page 0's bytes may be anything: an infinite factor would make its zeros no numbers)
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) s[ct][0] = s[ct][1] = f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
