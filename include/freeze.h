@@ -501,7 +501,8 @@ int freeze_pages_compact(const freeze_pages *pages, int32_t *out_used, void *wor
  * last n_r.  Slots behind a row's last token in the block that it ends in become 0.
  *   k, v     [tokens, heads, head_dim] fp32 or bf16 (one type), strides in elements; the elements of a head follow one another.
  *   starts   [rows + 1] int32: row r's are tokens starts[r] .. starts[r + 1] - 1; NULL: one token a row, tokens == rows.
- *   most     no row has more than this (0: tokens); a row that has, whose tokens are not all in 0 .. tokens - 1, or which has fewer than n_r tokens, is not written.
+ *   most     no row has more than this (0: tokens); a row that has, whose tokens are not all in 0 .. tokens - 1, or which has fewer than n_r tokens, is not written,
+ *            nor one that begins before the end of an earlier row's tokens (that lie in 0 .. tokens - 1 and are no more than `most`): no token is two rows'.
  *   granted  [rows] int32 or NULL: rows whose n_r is another are not written.
  * A page with several references is not written.  0 <= tokens < 2^31, (tokens + 64 * rows) * (heads + 2) < 2^30.
  */
@@ -514,7 +515,7 @@ int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int
  * places max(0, p - window + 1) .. p (window 0: from 0 on) with weights softmax(scale * q . key); nothing to attend to (p < 0): 0.
  *   q        [tokens, heads * group, head_dim] fp32 or bf16; head j reads keys and values of head j / group.
  *   out      [tokens, heads * group, head_dim] FREEZE_F32 or FREEZE_BF16, with strides of its own; shares no byte of its extent with the inputs.
- *   starts, tokens, most: as of freeze_pages_append; outputs of rows that are not in order, and tokens that are no row's, are left as they are.
+ *   starts, tokens, most: as of freeze_pages_append; outputs of rows that are not as they should be there, and tokens that are no row's, are left as they are.
  * Products of codes are exact, sums and softmax statistics fp32.  With q in bf16, weights are taken in two parts of bf16 (2^-17); with fp32 they and q are taken in
  * three parts, exact to 2^-24.  Scores have to be within fp32's range; a NaN in a key or value that a token attends to, or in
  * its own q, makes its output NaN, and no other's.  Values below 2^-126 may count as 0.

@@ -105,12 +105,39 @@ struct NewTokens {
     int count;
     int64_t first;
 };
-__device__ __forceinline__ NewTokens new_tokens(const int32_t *starts, int row, int64_t tokens, int64_t most)
+// floor: no smaller than the ends of the rows before that are in order by themselves; the row's own becomes part of it.  A row that begins below it counts for nothing, so that
+// no token is two rows' (the grids have room for `tokens` tokens, and outputs one writer).
+__device__ __forceinline__ NewTokens new_tokens(const int32_t *starts, int row, int64_t tokens, int64_t most, int *floor)
 {
     if (!starts) return NewTokens{row < tokens ? 1 : 0, row};
     const int64_t a = starts[row], b = starts[row + 1];
     if (a < 0 || b <= a || b > tokens || b - a > most) return NewTokens{0, 0};
-    return NewTokens{(int)(b - a), a};
+    const bool apart = a >= *floor;
+    *floor = max(*floor, (int)b);
+    return apart ? NewTokens{(int)(b - a), a} : NewTokens{0, 0};
+}
+// Whether a row ends before it begins.  Where none does, no two rows overlap, and floors of 0 serve all.
+__device__ __forceinline__ bool falls(const int32_t *starts, int row) { return starts && starts[row + 1] < starts[row]; }
+// The floor of a thread's first row, r0, in a workgroup of WAVES waves whose threads have the rows one after another.
+template <int WAVES>
+__device__ __forceinline__ int floor_of(const int32_t *starts, int r0, int r1, int64_t tokens, int64_t most, int *lds /* [WAVES] */)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int end = 0;
+    for (int r = r0; r < r1; ++r) new_tokens(starts, r, tokens, most, &end);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(end, o);
+        if (lane >= o) end = max(end, u);
+    }
+    __syncthreads();   // (what is there is read)
+    if (lane == 63) lds[wave] = end;
+    int before = __shfl_up(end, 1);
+    if (lane == 0) before = 0;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) before = max(before, lds[w]);
+    __syncthreads();   // (it is the caller's again)
+    return before;
 }
 
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;

@@ -310,10 +310,10 @@ struct AppendRow {
     NewTokens n;
     int len, first, blocks;
 };
-__device__ __forceinline__ AppendRow append_row(const AppendArgs &p, int row)
+__device__ __forceinline__ AppendRow append_row(const AppendArgs &p, int row, int *floor)
 {
     AppendRow w;
-    w.n = new_tokens(p.starts, row, p.tokens, p.most);
+    w.n = new_tokens(p.starts, row, p.tokens, p.most, floor);
     w.len = p.v.length_of(row);
     w.first = w.len - w.n.count;
     const bool as_it_should = w.n.count > 0 && w.first >= 0 && (!p.granted || p.granted[row] == w.n.count);
@@ -364,35 +364,56 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
 {
     const PageView &v = p.v;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, t = lane & 15;
-    __shared__ int wave_sum[4], found[2];
+    __shared__ uint32_t wave_sum[4];
+    __shared__ int wave_falls[4], found[2];
+    int floor = 0;
     // the row of this workgroup's block
     const int groups = (2 * v.heads + 3) / 4;
     const int which = (int)(blockIdx.x / groups), unit = (int)(blockIdx.x - (unsigned)which * groups) * 4 + wave;
     if (!p.starts) {   // one token a row: a block each
-        if (append_row(p, which).blocks == 0) return;
+        if (append_row(p, which, &floor).blocks == 0) return;
     } else {
         const int per = (v.rows + 255) / 256;
         const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
-        int mine = 0;
-        for (int r = r0; r < r1; ++r) mine += append_row(p, r).blocks;
-        int before = mine;
+        uint32_t mine, before, total;   // (of rows that overlap, the first time, not what they say)
+        auto sums = [&] {
+            bool fall = false;
+            int f = floor;
+            mine = 0;
+            for (int r = r0; r < r1; ++r) {
+                mine += append_row(p, r, &f).blocks;
+                fall |= falls(p.starts, r);
+            }
+            fall = __any(fall);
+            before = mine;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int u = __shfl_up(before, o);
-            if (lane >= o) before += u;
+            for (int o = 1; o < 64; o <<= 1) {
+                const uint32_t u = __shfl_up(before, o);
+                if (lane >= o) before += u;
+            }
+            if (lane == 63) {
+                wave_sum[wave] = before;
+                wave_falls[wave] = fall;
+            }
+            __syncthreads();
+            before -= mine;
+            total = 0;
+            fall = false;
+            for (int w = 0; w < 4; ++w) {
+                if (w < wave) before += wave_sum[w];
+                total += wave_sum[w];
+                fall |= wave_falls[w] != 0;
+            }
+            return fall;
+        };
+        if (sums()) {
+            floor = floor_of<4>(p.starts, r0, r1, p.tokens, p.most, wave_falls);
+            sums();
         }
-        if (lane == 63) wave_sum[wave] = before;
-        __syncthreads();
-        before -= mine;
-        int total = 0;
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) before += wave_sum[w];
-            total += wave_sum[w];
-        }
-        if (which >= total) return;
-        if (before <= which && which < before + mine)
-            for (int r = r0, b = before; r < r1; ++r) {
-                const int n = append_row(p, r).blocks;
+        if ((uint32_t)which >= total) return;
+        if (before <= (uint32_t)which && (uint32_t)which < before + mine)
+            for (int r = r0, b = (int)before; r < r1; ++r) {
+                const int n = append_row(p, r, &floor).blocks;
                 if (which < b + n) {
                     found[0] = r;
                     found[1] = which - b;
@@ -404,7 +425,8 @@ __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
     }
     if (unit >= 2 * v.heads) return;
     const int row = p.starts ? __builtin_amdgcn_readfirstlane(found[0]) : which;
-    const AppendRow w = append_row(p, row);
+    floor = 0;
+    const AppendRow w = append_row(p, row, &floor);
     const int block = w.first / kPageBlock + (p.starts ? __builtin_amdgcn_readfirstlane(found[1]) : 0), start = block * kPageBlock;
     const int kv = unit & 1, head = unit >> 1;
     const int page = v.tables[row * v.max_pages + (start >> v.page_log2)];

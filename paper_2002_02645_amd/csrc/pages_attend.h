@@ -34,10 +34,10 @@ struct RowWork {
     NewTokens n;
     int len, lo, blocks, tiles;
 };
-__device__ __forceinline__ RowWork row_work(const AttendArgs &p, int row, int cols)
+__device__ __forceinline__ RowWork row_work(const AttendArgs &p, int row, int cols, int *floor)
 {
     RowWork w;
-    w.n = new_tokens(p.starts, row, p.tokens, p.most);
+    w.n = new_tokens(p.starts, row, p.tokens, p.most, floor);
     w.len = p.v.length_of(row);
     const int64_t seen = p.window > 0 ? (int64_t)w.len - w.n.count - p.window + 1 : 0;   // first place of the first token
     w.lo = seen > 0 ? (int)(seen / kPageBlock) : 0;
@@ -192,7 +192,8 @@ __device__ __forceinline__ void take_queries(const uint16_t *from, int cols, int
         for (int c = 0; c < DC; ++c) q[n][c] = *reinterpret_cast<const bf16x8 *>(from + (n * cols + c0 + (lane & 15)) * kQueryRow<DC> + 32 * c + 8 * (lane >> 4));
 }
 
-// Sums over the workgroup's threads before this one, of two numbers, and over all.  WAVES: of the workgroup
+// Sums over the workgroup's threads before this one, of two numbers, and over all.  WAVES: of the workgroup.
+constexpr int64_t kFalls = (int64_t)1 << 48;   // beside a sum below it: how many rows end before they begin
 template <int WAVES>
 struct TwoSums {
     int64_t before[2], all[2];

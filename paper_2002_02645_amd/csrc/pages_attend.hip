@@ -57,16 +57,26 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
     auto places_of = [&](const RowWork &w) { return p.whole ? 1 : w.blocks + (int)kTileCost; };
     auto cost_of = [&](const RowWork &w) { return (int64_t)places_of(w) * w.tiles * v.heads; };
     RowWork last;
-    int64_t mine = 0, tiles = 0;
-    for (int r = r0; r < r1; ++r) {
-        last = row_work(p, r, kCols);
-        mine += cost_of(last);
-        tiles += last.tiles;
+    int64_t mine, tiles;
+    int floor = 0;
+    auto sums = [&] {
+        int f = floor;
+        mine = tiles = 0;
+        for (int r = r0; r < r1; ++r) {
+            last = row_work(p, r, kCols, &f);
+            mine += cost_of(last);
+            tiles += last.tiles + (falls(p.starts, r) ? kFalls : 0);
+        }
+        return two_sums<4>(mine, tiles, found->sums);
+    };
+    TwoSums<4> so_far = sums();
+    if (so_far.all[1] >= kFalls) {
+        floor = floor_of<4>(p.starts, r0, r1, p.tokens, p.most, reinterpret_cast<int *>(&found->base));
+        so_far = sums();
     }
-    const TwoSums<4> so_far = two_sums<4>(mine, tiles, found->sums);
     const int64_t before = so_far.before[0], total = uniform(so_far.all[0]);
     int workers = p.workers;
-    const int all = (int)uniform(so_far.all[1]) * v.heads;
+    const int all = (int)uniform(so_far.all[1] & (kFalls - 1)) * v.heads;
     if (!p.whole && all >= kEvenTiles) workers = (all + (all + kWorkers - 1) / kWorkers - 1) / ((all + kWorkers - 1) / kWorkers);
     int64_t share = (total + workers - 1) / workers;
     share = share < kLeastShare && !p.whole ? kLeastShare : share;
@@ -78,7 +88,7 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
         int r = r0;
         if (per > 1)
             for (;; ++r) {
-                last = row_work(p, r, kCols);
+                last = row_work(p, r, kCols, &floor);
                 if (begin < b + cost_of(last)) break;
                 b += cost_of(last);
             }
@@ -90,6 +100,7 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
     int row = uniform(found->row);
     int64_t base = uniform(found->base);
     RowWork w = uniform(found->w);
+    floor = (int)w.n.first + w.n.count;
     __syncthreads();
 
     for (int64_t at = begin; at < end;) {
@@ -97,7 +108,7 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
         if (at >= base + row_cost) {
             base += row_cost;
             ++row;
-            w = uniform(row_work(p, row, kCols));
+            w = uniform(row_work(p, row, kCols, &floor));
             continue;
         }
         const int tile_cost = places_of(w), item = (int)((at - base) / tile_cost);
@@ -309,15 +320,29 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
     int *found = reinterpret_cast<int *>(sums + 8);
     const int per = (v.rows + 255) / 256;
     const int r0 = min(v.rows, (int)threadIdx.x * per), r1 = min(v.rows, r0 + per);
-    int mine = 0;
-    for (int r = r0; r < r1; ++r) mine += row_work(p, r, kCols).tiles;
-    const TwoSums<4> so_far = two_sums<4>(mine, 0, sums);
+    int64_t mine;
+    int floor = 0;
+    auto tiles_of = [&] {
+        int f = floor;
+        int64_t fall = 0;
+        mine = 0;
+        for (int r = r0; r < r1; ++r) {
+            mine += row_work(p, r, kCols, &f).tiles;
+            fall += falls(p.starts, r);
+        }
+        return two_sums<4>(mine, fall, sums);
+    };
+    TwoSums<4> so_far = tiles_of();
+    if (so_far.all[1] > 0) {
+        floor = floor_of<4>(p.starts, r0, r1, p.tokens, p.most, found);
+        so_far = tiles_of();
+    }
     const int before = (int)so_far.before[0], total = (int)so_far.all[0];
     const int head = blockIdx.x % v.heads, tile = total - 1 - (int)(blockIdx.x / v.heads);
     if (tile < 0) return;
     if (before <= tile && tile < before + mine)
         for (int r = r0, b = before; r < r1; ++r) {
-            const int n = row_work(p, r, kCols).tiles;
+            const int n = row_work(p, r, kCols, &floor).tiles;
             if (tile < b + n) {
                 found[0] = r;
                 found[1] = tile - b;
@@ -327,7 +352,8 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
         }
     __syncthreads();
     const int row = uniform((int)found[0]);
-    const RowWork w = row_work(p, row, kCols);
+    floor = 0;   // (this row is in order)
+    const RowWork w = row_work(p, row, kCols, &floor);
     const int cols = w.n.count * p.group, tile0 = uniform((int)found[1]) * kCols, col0 = tile0 + wave * kWave;
     __syncthreads();
     uint16_t *staged = reinterpret_cast<uint16_t *>(lds);
