@@ -15,6 +15,7 @@ struct AttendArgs {
     int64_t q_token, q_head, out_token, out_head;   // strides
     int64_t tokens, most, window;
     const int32_t *starts;
+    int64_t least_cols, most_cols;                  // of a row that the kernel takes: others are another launch's
     int group, q_vec, out_bf16, out_vec;            // *_vec: 16-byte loads of q, 8-byte (bf16) or 16-byte stores of out
     float scale_log2;                               // the scale times log2(e): weights are powers of two
     // work split over the tokens
@@ -43,7 +44,8 @@ __device__ __forceinline__ RowWork row_work(const AttendArgs &p, int row, int co
     w.lo = seen > 0 ? (int)(seen / kPageBlock) : 0;
     w.blocks = w.n.count > 0 ? (w.len + kPageBlock - 1) / kPageBlock - w.lo : 0;
     w.blocks = w.blocks < 0 ? 0 : w.blocks;
-    w.tiles = (int)(((int64_t)w.n.count * p.group + cols - 1) / cols);
+    const int64_t own = (int64_t)w.n.count * p.group;
+    w.tiles = own >= p.least_cols && own <= p.most_cols ? (int)((own + cols - 1) / cols) : 0;
     return w;
 }
 

@@ -499,9 +499,12 @@ __global__ __launch_bounds__(256, CT == 1 && NS == 1 && DC <= 4 ? 3 : NS > 1 && 
 
 // ---- host -------------------------------------------------------------------------------------------
 
+constexpr int64_t kFewColumns = 64;   // of a row: the prompts' kernel has as many a workgroup with 16 a wave
+
 struct AttendPlan {
     int ct, parts;
     int prompt;   // 0: not the prompts' kernel; 1, 2: with 16, 32 columns a wave (16 where heads are wider than 160)
+    bool both;    // rows of few columns beside prompts: those go to the kernel that splits them
     size_t o_bytes, ml_bytes, split_bytes;
     size_t bytes() const { return o_bytes + ml_bytes + split_bytes; }
 };
@@ -523,11 +526,20 @@ AttendPlan attend_plan(const freeze_pages *p, int group, int64_t tokens, int64_t
     //   of 128: 31 25; of 256: 80 42 / 318 190 / 1113 699; 16 rows of 64: 73 35 / 311 186 / 1151 772; heads of 192: 1 row of 512: 79 43; of 1,024: 241 85 / 667 287 / 2082 982.
     const int64_t all = tokens * group * p->heads;
     pl.ct = parts > 1 || cols <= 16 || all < 4096 ? 1 : 2;
-    pl.prompt = cols <= 64 ? 0 : all >= 32768 ? 2 : all >= (parts > 1 ? 16384 : 8192) && most_blocks <= 64 ? 1 : 0;
+    pl.prompt = cols <= kFewColumns ? 0 : all >= 32768 ? 2 : all >= (parts > 1 ? 16384 : 8192) && most_blocks <= 64 ? 1 : 0;
     const size_t slots = 2 * kWorkers, kCols = 16 * pl.ct;
     pl.o_bytes = slots * kCols * page_width(p->head_dim) * 4;
     pl.ml_bytes = slots * 2 * kCols * 4;
     pl.split_bytes = up256(kWorkers * sizeof(SplitTile));
+    // Rows of few columns beside prompts would each walk their blocks with one wave of four.  So where there may be such (the shortest row, where the others have as many tokens
+    // as they may), and rows may be long or are short on the average, both kernels are launched, each for its rows.  A prompt of 1,024 tokens beside a row of one token
+    // behind 1,000 / 2,000 / 4,000 / 16,000 / 131,071 places: 36 / 56 / 103 / 418 / 3,761 us with the prompts' kernel alone, 49 / 49 / 50 / 56 / 103 with both; of 2,048 beside 32 rows
+    // of one behind 1,000 / 2,000 / 4,000 / 16,000: 95 114 153 518 and 106 118 140 268, beside 64 rows of 8 behind 10,000: 362 and 286 (472 with 16 columns a wave);
+    // prompts of 4,096, 300, 200, 180 and 7 tokens, none of them long: 208 and 219.  1,024 rows of one token behind 1,000 in the packed form, `most` not given: 452 and 358 (429
+    // with 32 columns a wave).
+    const bool ones = tokens * group <= 16 * p->rows;
+    pl.both = pl.prompt && (tokens - (p->rows - 1) * most) * group <= kFewColumns && (most_blocks > 64 || ones);
+    if (pl.both && ones) pl.ct = 1;   // (the workspace's size is the one for 32 columns a wave)
     return pl;
 }
 
@@ -548,22 +560,35 @@ hipError_t launch_prompt(const AttendArgs &a, hipStream_t s)
 {
     constexpr int64_t cols = 64 * CT;
     constexpr size_t lds = std::max((size_t)NS * cols * kQueryRow<DC> * 2, (size_t)4 * 16 * (8 * DC + 1) * 16);
-    const int64_t n = std::min(a.tokens * a.group / cols + a.v.rows, a.tokens * ((a.group + cols - 1) / cols));
+    const int64_t all = a.tokens * a.group, rows = std::min<int64_t>(a.v.rows, all / a.least_cols);   // (rows that it takes)
+    const int64_t n = std::min(all / cols + rows, a.tokens * ((a.group + cols - 1) / cols));
     hipLaunchKernelGGL((pages_prompt_kernel<DC, CT, NS>), dim3((unsigned)(n * a.v.heads)), dim3(256), lds, s, a);
     return hipGetLastError();
 }
 template <int DC>
-hipError_t launch_width(const AttendArgs &a, const AttendPlan &pl, hipStream_t s)
+hipError_t launch_split(const AttendArgs &a, const AttendPlan &pl, hipStream_t s)
 {
+    if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, s);
+    if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, s);
+    return launch_attend<DC, 2, 1>(a, s);
+}
+template <int DC>
+hipError_t launch_width(AttendArgs a, const AttendPlan &pl, hipStream_t s)
+{
+    if (pl.both) {
+        a.most_cols = kFewColumns;
+        const hipError_t err = launch_split<DC>(a, pl, s);
+        if (err != hipSuccess) return err;
+        a.least_cols = kFewColumns + 1;
+        a.most_cols = (int64_t)1 << 31;
+    }
     if (pl.prompt) {
         if (pl.parts > 1) return launch_prompt<DC, 1, 3>(a, s);
         if constexpr (DC <= 5)
             if (pl.prompt == 2) return launch_prompt<DC, 2, 1>(a, s);
         return launch_prompt<DC, 1, 1>(a, s);
     }
-    if (pl.parts > 1) return launch_attend<DC, 1, 3>(a, s);
-    if (pl.ct == 1) return launch_attend<DC, 1, 1>(a, s);
-    return launch_attend<DC, 2, 1>(a, s);
+    return launch_split<DC>(a, pl, s);
 }
 
 bool attend_sizes(const freeze_pages *p, int group, int64_t tokens, int64_t most)
@@ -631,6 +656,8 @@ int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int
     a.most = each;
     a.window = window;
     a.starts = starts;
+    a.least_cols = 1;
+    a.most_cols = (int64_t)1 << 31;
     a.group = group;
     a.q_vec = qb % 16 == 0 && pages->head_dim % 8 == 0 && a.q_token % 8 == 0 && a.q_head % 8 == 0;
     a.out_bf16 = out_dtype == FREEZE_BF16;
