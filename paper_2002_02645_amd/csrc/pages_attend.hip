@@ -16,9 +16,11 @@ size_t up256(size_t n) { return (n + 255) / 256 * 256; }
 constexpr int kWorkers = 768;         // workgroups that share the work
 constexpr int64_t kTileCost = 8;      // of a tile beside its blocks', in blocks: queries, joining the waves
 constexpr int64_t kLeastShare = 8;    // of a workgroup
-// From so many tiles on there are as many workgroups as divide them, at most kWorkers, so that none of equal ones is split: 64 rows of 3,900 tokens 98 -> 88 us, 128 rows
-// 174 -> 161; of ragged ones 21.9 -> 22.7 and 35.9 -> 36.3.
-constexpr int kEvenTiles = 512;
+// From kEvenTiles to kMostEven tiles there are as many workgroups as divide them, at most kWorkers, so that none of equal ones is split. Rows of 8 heads and 3,900 tokens each (and of
+// 975 .. 6,825): 64 rows 105 -> 83 us (88 -> 86), 80 112 -> 107 (108 -> 111), 97, where 388 workgroups are left, 134 -> 123 (124 -> 122), 112 154 -> 138 (161 -> 155), 128
+// 188 -> 157 (173 -> 169). Beyond, ragged ones lose: 144 rows 190 -> 198 (191 -> 209), 160 215 -> 207 (217 -> 223), 193 257 -> 279 (267 -> 305), 256 334 -> 316 (329 -> 331),
+// 300 387 -> 397 (381 -> 407).
+constexpr int kEvenTiles = 512, kMostEven = 1024;
 // Where no row can have more blocks (by its table or the window) and there are no more tiles than workgroups, no tile is split and nothing joined. One row of 250 tokens 10.0
 // -> 7.3 us, of 500 11.1 -> 9.5, of 900 11.3 against 12.7; 64 rows of 500 20.3 -> 15.8, of 900 33 -> 26.
 constexpr int64_t kWholeBlocks = 24;
@@ -77,7 +79,7 @@ __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_
     const int64_t before = so_far.before[0], total = uniform(so_far.all[0]);
     int workers = p.workers;
     const int all = (int)uniform(so_far.all[1] & (kFalls - 1)) * v.heads;
-    if (!p.whole && all >= kEvenTiles) workers = (all + (all + kWorkers - 1) / kWorkers - 1) / ((all + kWorkers - 1) / kWorkers);
+    if (!p.whole && all >= kEvenTiles && all <= kMostEven) workers = (all + (all + kWorkers - 1) / kWorkers - 1) / ((all + kWorkers - 1) / kWorkers);
     int64_t share = (total + workers - 1) / workers;
     share = share < kLeastShare && !p.whole ? kLeastShare : share;
     const int64_t begin = blockIdx.x * share, end = min(total, begin + share);
