@@ -520,7 +520,7 @@ int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int
  * three parts, exact to 2^-24.  Scores have to be within fp32's range; a NaN in a key or value that a token attends to, or in
  * its own q, makes its output NaN, and no other's.  Values below 2^-126 may count as 0.
  *   workspace  freeze_pages_attend_workspace_bytes() bytes, 256-byte aligned; scratch only, shared by calls that follow one another only.  The bytes for some tokens serve fewer too.
- * 1 <= group <= 1024, 0 <= tokens < 2^31, (tokens * group + 16 * rows) * heads < 2^28, 0 < scale <= 3e38, 0 <= window < 2^31; tokens == 0 is a no-op.
+ * 1 <= group <= 1024, 0 <= tokens < 2^31, (tokens * group + 16 * rows) * heads < 2^28, 0 < scale <= 2e38, 0 <= window < 2^31; tokens == 0 is a no-op.
  */
 size_t freeze_pages_attend_workspace_bytes(const freeze_pages *pages, int group, int64_t tokens, int64_t most, int packed);
 int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int q_dtype, int64_t q_token_stride, int64_t q_head_stride, int group,

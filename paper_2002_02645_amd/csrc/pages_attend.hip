@@ -619,7 +619,7 @@ int freeze_pages_attend(const freeze_pages *pages, int layer, const void *q, int
                         int64_t out_token_stride, int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *stream)
 {
     if (!attend_sizes(pages, group, tokens, most) || layer < 0 || layer >= pages->layers || (q_dtype != FREEZE_F32 && q_dtype != FREEZE_BF16) ||
-        (out_dtype != FREEZE_F32 && out_dtype != FREEZE_BF16) || !(scale > 0.f && scale < 3.0e38f) || window < 0 || window >= (int64_t)1 << 31 ||
+        (out_dtype != FREEZE_F32 && out_dtype != FREEZE_BF16) || !(scale > 0.f && scale <= 2.0e38f) || window < 0 || window >= (int64_t)1 << 31 ||
         (!starts && tokens != 0 && tokens != pages->rows))
         return FREEZE_EINVAL;
     if (tokens == 0) return FREEZE_OK;

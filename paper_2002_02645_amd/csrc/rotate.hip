@@ -17,7 +17,7 @@ struct RotateTensor {
 };
 struct RotateArgs {
     RotateTensor t[kMostTensors];
-    int num, pairs, dim, interleaved;
+    int num, pairs, interleaved;
     int each;            // tokens of a workgroup
     int64_t tokens;
     const int32_t *positions;
@@ -181,7 +181,7 @@ int freeze_rotate_positions(const freeze_heads *heads, int num, int64_t tokens, 
                             const double *frequencies, int64_t pairs, int interleaved, float factor, int inverse, void *stream)
 {
     if (num < 0 || num > kMostTensors || tokens < 0 || tokens >= (int64_t)1 << 31 || head_dim < 1 || head_dim > 4096 || pairs < 0 || 2 * pairs > head_dim ||
-        (num > 0 && !heads) || !(factor > -3.0e38f && factor < 3.0e38f))
+        (num > 0 && !heads) || !(factor >= -3.0e38f && factor <= 3.0e38f))
         return FREEZE_EINVAL;
     RotateArgs a{};
     Region e[2 * kMostTensors + 2];
@@ -222,7 +222,6 @@ int freeze_rotate_positions(const freeze_heads *heads, int num, int64_t tokens, 
         for (int j = 0; j < i; ++j)
             if ((e[i].dst || e[j].dst) && share_a_byte(e[i], e[j])) return FREEZE_EINVAL;
     a.pairs = (int)pairs;
-    a.dim = (int)head_dim;
     a.interleaved = interleaved != 0;
     a.tokens = tokens;
     a.positions = positions;
