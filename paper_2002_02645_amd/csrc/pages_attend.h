@@ -274,8 +274,12 @@ __device__ __forceinline__ void scores_of(const u32x4 (&k)[DC], const bf16x8 (&q
         }
 }
 
-// The factor of a block's scores, from its scale bytes: not below the smallest normal number, where scores are as good as 0, so that hidden ones stay -inf.
-__device__ __forceinline__ float score_factor(float scale_log2, uint32_t bytes) { return fmaxf(scale_log2 * __uint_as_float((bytes & 0xffu) << 23), 1.17549435e-38f); }
+// The factor of a block's scores, from its scale bytes: not below the smallest normal number, where scores are as good as 0, so that hidden ones stay -inf; nor infinite, so that
+// scores of 0 stay 0.
+__device__ __forceinline__ float score_factor(float scale_log2, uint32_t bytes)
+{
+    return __builtin_amdgcn_fmed3f(scale_log2 * __uint_as_float((bytes & 0xffu) << 23), 1.17549435e-38f, 3.40282347e38f);
+}
 __device__ __forceinline__ float value_factor(uint32_t bytes) { return __uint_as_float((bytes >> 8) << 23); }
 
 // What a lane's columns see: the places behind `before` up to `place` (below 0: a column of nobody).
