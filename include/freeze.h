@@ -515,6 +515,8 @@ int freeze_pages_append(const freeze_pages *pages, int layer, const void *k, int
  * places max(0, p - window + 1) .. p (window 0: from 0 on) with weights softmax(scale * q . key); nothing to attend to (p < 0): 0.
  *   q        [tokens, heads * group, head_dim] fp32 or bf16; head j reads keys and values of head j / group.
  *   out      [tokens, heads * group, head_dim] FREEZE_F32 or FREEZE_BF16, with strides of its own; shares no byte of its extent with the inputs.
+ *            A row that freeze_pages_reserve granted nothing has no newer token than before: its n_r tokens have the places of its last n_r old ones here, and what comes
+ *            out is no answer to a new one.  The caller passes over such rows by what they were granted.
  *   starts, tokens, most: as of freeze_pages_append; outputs of rows that are not as they should be there, and tokens that are no row's, are left as they are.
  * Products of codes are exact, sums and softmax statistics fp32.  With q in bf16, weights are taken in two parts of bf16 (2^-17); with fp32 they and q are taken in
  * three parts, exact to 2^-24.  Scores have to be within fp32's range; a NaN in a key or value that a token attends to, or in

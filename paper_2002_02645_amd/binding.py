@@ -1116,7 +1116,8 @@ class FreezePages:
     def attend(self, layer: int, q: torch.Tensor, starts: Optional[torch.Tensor] = None, most: int = 0, scale: Optional[float] = None, window: int = 0,
                out_dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of the rows' newest tokens, q [tokens, heads * group, head_dim], over a layer's pages; scale: head_dim ** -0.5 by default.  Outputs of
-        tokens of no row are left as they are (in a new tensor: whatever they were)."""
+        tokens of no row are left as they are (in a new tensor: whatever they were).  A row that reserve granted nothing attends from its last old places: its
+        outputs are no answer to a new token."""
         dev, pool = _here(q, starts, out, holder=self), self.pool
         dim = pool.head_dim
         qs = _heads_of(q, None, dim)

@@ -48,3 +48,45 @@ def test_mixed(dim, new, dtype):
     out = torch.full_like(q, 7.0)
     p.attend(0, q, ints(starts[:1] + [-1] + starts[2:]), out=out)
     assert bool((out[:starts[2]] == 7).all()) and bool((out[starts[2]:] != 7).any(2).any(1).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_captured(dtype):
+    """Both kernels of a mixed call in a graph, replayed beside eager calls and over other lengths and starts."""
+    new = [600, 1, 3, 8, 0, 9, 1]
+    lengths = [n + 700 for n in new]
+    p, _ = pair(1, 200, 7, 80, HEADS, 64, 32)
+    assert p.reserve(ints(lengths)).tolist() == lengths
+    g = torch.Generator("cuda").manual_seed(1)
+    k, v = (torch.randn(sum(lengths), HEADS, 64, device="cuda", generator=g).to(dtype) for _ in range(2))
+    p.append(0, k, v, ints([sum(lengths[:r]) for r in range(8)]))
+    q = torch.randn(sum(new), HEADS * GROUP, 64, device="cuda", generator=g).to(dtype)
+    starts = ints([sum(new[:r]) for r in range(8)])
+    p.attend(0, q, starts)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = p.attend(0, q, starts)
+    for turn, order in enumerate((new, [1, 600, 8, 3, 9, 0, 1], [0, 0, 622, 0, 0, 0, 0], new)):
+        starts.copy_(ints([sum(order[:r]) for r in range(8)]))
+        q.copy_(torch.randn(q.shape, device="cuda", generator=g))
+        out.fill_(9.0)
+        want = p.attend(0, q, starts)
+        graph.replay()
+        assert torch.equal(out, want), turn
+        torch.cuda.synchronize()
+        graph.replay()
+        assert torch.equal(out, want), turn
+
+
+def test_rows_without_room():
+    """A row that got no place for its new token attends from its last old place, as the header says: `granted` tells whose outputs count."""
+    p, pool = pair(1, 5, 3, 3, HEADS, 64, 32)
+    lengths = [64, 32, 40]
+    assert p.reserve(ints(lengths)).tolist() == pool.reserve(lengths) == lengths      # all five pages
+    fill(p, pool, lengths, 1)
+    granted = p.reserve()
+    assert granted.tolist() == pool.reserve([1, 1, 1]) == [0, 0, 1]
+    k, v = (torch.randn(3, HEADS, 64, device="cuda").to(torch.bfloat16) for _ in range(2))
+    p.append(0, k, v, granted=granted)
+    pool.append(0, k.cpu(), v.cpu(), [1, 1, 1], [0, 0, 1])
+    check(p, pool, [1, 1, 1], torch.bfloat16, 1)
