@@ -357,8 +357,11 @@ __device__ __forceinline__ uint32_t across_four(uint32_t w)
 
 // A wave quantises the new tokens of one block of a head's keys or values.  A lane reads eight elements of two tokens of each chunk of 32 elements
 // (keys' own 16 bytes of the chunk), so that the block's largest magnitude is one reduction over the wave; values' codes change places among four lanes with four
-// tokens each.  16.7 k tokens of 8 heads of 128 (103 MB read and written) 22.8 us, 4.5 TB/s (160 with single loads, 30 with a magnitude at a time); one token for each of
-// 64 rows 6.9: lengths, tables, counts and codes wait for one another.  DC: chunks.
+// tokens each.  16.7 k tokens of 8 heads of 128 (103 MB read and written) 23.5 us, 4.4 TB/s (30 with a magnitude at a time); one token for each of
+// 64 rows 7.0: lengths, tables, counts and codes wait for one another.  18.6 k tokens with bf16 and fp32: heads of 128 24 and 38 us (114 and 190 MB), of 96 20 and 30, of 64 17 and 22;
+// by single loads, where a head is no multiple of 8 elements or lies off 16 bytes, of 100 83 and 83, of 68 61 and 56, of 37 34 and 34.
+// In the packed form every workgroup looks through all rows for its own: 256 rows of one token 10 us (9 in the other form), 1,024 32 (20), 4,096 312 (79), 16,384 9,900 (335).
+// DC: chunks.
 template <typename T, int DC>
 __global__ __launch_bounds__(256) void pages_append_kernel(AppendArgs p)
 {

@@ -30,7 +30,7 @@ constexpr int64_t kWholeBlocks = 24;
 // prompts pay for it: five rows of up to 4,096 new tokens 302 us instead of 227 with weights rounded once (2^-8).
 constexpr int kWeightParts = 2;
 
-// Codes are read once (or by rows that share pages, at about the same time) and leave the caches to others: 189 us instead of 215.
+// Codes are read once (or by rows that share pages, at about the same time) and leave the caches to others: 189 us instead of 215 (64 rows of 4,000 .. 16,000).
 __device__ __forceinline__ u32x4 load_codes(const uint8_t *p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p)); }
 
 template <int DC, int CT, int NS>
@@ -38,7 +38,8 @@ constexpr int kAttendPerCu = NS == 1 && CT == 1 && DC <= 4 ? 3 : NS == 1 && ((CT
 
 // Rows of a few columns each (a token or some of a row): all blocks of all (row, tile of columns, head) lie in one line, kTileCost places before each tile's, which
 // is cut into equal shares, one a workgroup, wherever that falls; a tile that several workgroups meet in goes through `part` and pages_join_kernel.  A share's
-// blocks go round the workgroup's four waves, whose results meet in LDS at the tile's end.
+// blocks go round the workgroup's four waves, whose results meet in LDS at the tile's end.  64 rows of 4,000 .. 16,000 tokens (1.37 GB with 8 heads of 128) 217 us, 6.3 TB/s, with
+// fp32 queries, at one workgroup a CU, 220; heads of 100 and 98, whose queries (and outputs) come by elements, the same; heads of 37 120 and 131 (5.7 and 5.2 TB/s).
 template <int DC, int CT, int NS>
 __global__ __launch_bounds__(256, (kAttendPerCu<DC, CT, NS>)) void pages_attend_kernel(AttendArgs p)
 {
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(256) void pages_join_kernel(AttendArgs p)
 // block come from memory once and from the caches for the other waves.  Nothing is split: there are tiles enough.  Later tiles of a row see more and go first.
 // Bound by what a SIMD issues: a block's 48 matrix instructions (16 for scores, 32 for values with the weights in two parts: 768 cycles of the matrix cores, two issue places
 // each) come with 64 conversions, 16 exponentials and 160 other vector instructions, which together take 108 % of the SIMDs' cycles: five rows of up to 4,096 new tokens
-// 302 us, 0.62 PFLOP/s of the products asked for, 0.94 of those done (a library product of 8,192^3 on the same card: 1.10).  Measured with weights in one part (243 us):
+// 302 us, 0.65 PFLOP/s of the products asked for, 1.0 of those done (a library product of 8,192^3 on the same card: 1.10).  Measured with weights in one part (243 us):
 // four columns of 16 a wave need 512 registers and copy half of them (643 us where two needed 307), three spill (406); codes turned into bf16
 // once for a workgroup of eight waves, in LDS, 283 us; codes shared by four waves through LDS 275; codes two blocks ahead 241 against 245, at registers that wide heads lack.
 // Heads above 160 have one column of 16 a wave and two waves a SIMD; with two columns and one wave 16 rows of 256 behind 4,000 need 857 us against 694 (heads of 192) and 1,039
